@@ -60,7 +60,7 @@ typedef enum {
 } nld_status;
 
 /* Device status bits (sticky, OR-ed together). */
-#define NLD_DEV_BAD_TOKEN 0x1u     /* a token id outside [0, vocab) was replaced by 0 */
+#define NLD_DEV_BAD_TOKEN 0x1u     /* a token id outside [0, vocab) was replaced by 0, or left out by a loss */
 #define NLD_DEV_CAPACITY 0x2u      /* P_b + k > max_len: the block's K/V rows at or past max_len were not
                                       written, and a commit that would pass max_len stops the length there */
 #define NLD_DEV_BAD_LENGTH 0x4u    /* a negative committed length was read */
@@ -335,6 +335,111 @@ nld_status nld_refresh_block(const nld_model* m, const nld_kv_cache* kv, const i
 nld_status nld_commit_from_logits(const float* logits, int32_t* block, int32_t batch, int32_t k, int32_t vocab,
                                   int32_t mask_token_id, float threshold, int32_t* argmax, int32_t* n_committed,
                                   int32_t* n_masked, float* confidence, void* stream);
+
+/* ---- operators on rows of logits -------------------------------------------------
+ * What training on the passes above needs of their logits: a teacher's largest
+ * logits, the drafter's distillation loss (the LoRA-enhanced drafter of Sec. 3.3
+ * learns from the verify pass's distributions), and a clipped policy loss for the
+ * AR pathway on decoded tokens.  Each loss gives its gradient in the same call.
+ *
+ * Logits are rows of `vocab` adjacent columns, [batch][rows], of any strides
+ * (in elements), so that a slice of a pass's logits or a trainer's tensor is
+ * taken as it is.  q_j = exp(z_j / temperature) / sum, sums in f32, everything
+ * per row in f64.  -inf is a column of probability 0. */
+#define NLD_F32 0
+#define NLD_BF16 1
+typedef struct {
+    void* data;          /* element (0, 0, 0); aligned to its type */
+    int32_t dtype;       /* NLD_F32 or NLD_BF16 */
+    int32_t batch, rows, vocab;
+    int64_t seq_stride;  /* elements from a sequence to the next, >= 0 (0: one for all) */
+    int64_t row_stride;  /* elements from a row to the next, >= 0 */
+} nld_logits;
+
+#define NLD_TOP_MAX 512          /* entries per row */
+#define NLD_LOGITS_MAX_VOCAB (1 << 24)
+
+/* Workspace of the three calls below for logits of these sizes and up to n_top
+ * entries per row (nld_policy_from_logits: 1), on the current device; to be
+ * initialized with nld_workspace_init once.  It holds the status word and, where
+ * several workgroups share a row, their partial results.  It also serves calls of
+ * fewer rows, columns or entries.  0 for sizes that the calls refuse. */
+size_t nld_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab, int32_t n_top);
+
+/* The n_top largest logits of every row, largest first and the lower column first
+ * among equal ones (-0.0 equals +0.0, and comes back as +0.0; a NaN stands above
+ * +inf): values f32 and ids int32 [batch][rows][n_top]; lse (optional) f32
+ * [batch][rows] = log sum_j exp(z_j / temperature) over the whole row (-inf for a
+ * row of -inf, +inf or NaN where one takes part).
+ * Errors: INVALID_ARG (NULL pointer, sizes < 1, n_top > vocab, a stride outside
+ * [0, 2^40), a temperature outside [1e-3, 1e3], misaligned data, unknown dtype),
+ * SHAPE (n_top > NLD_TOP_MAX, vocab > NLD_LOGITS_MAX_VOCAB, more than 2^20 rows, or
+ * rows so many and so long that one launch cannot hold them), CAPACITY (workspace). */
+nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float temperature, float* values, int32_t* ids,
+                          float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* A teacher's distributions by their largest logits, as nld_top_logits gives them
+ * (any order).  The entries of row (b, j) start at ((b * seq_rows) + j) * n_top, its
+ * log-sum-exp is lse[b * seq_rows + j]: seq_rows > rows takes a leading slice of a
+ * longer array's rows (the verify row j - 1 teaches the draft row j). */
+typedef struct {
+    const float* values;
+    const int32_t* ids;    /* -1: no entry */
+    const float* lse;      /* optional: at the same temperature, over the teacher's whole row */
+    int32_t n_top;
+    int32_t seq_rows;      /* >= rows */
+} nld_teacher;
+
+/* Distillation from a teacher's top logits, the hybrid of KL divergence and total
+ * variation that the drafter is trained with (Sec. 3.3).  With S the teacher's
+ * entries and R every other column taken as one event,
+ *   p_i = exp(t_i / temperature - lse), p_R = max(0, 1 - sum p_i)  (lse NULL: over S
+ *         alone, p_R = 0),    q_i as above, q_R = sum of q over R,
+ *   KL = sum p log(p / q), TV = 1/2 sum |p - q|, alpha = sum min(p, q), each over S and R,
+ *   lambda = kl_share * exp(-eta * alpha), held constant in the gradient,
+ *   loss = weight * (lambda * KL + (1 - lambda) * TV).
+ * kl_share 1, eta 0: KL alone (and with one entry and lse NULL the cross-entropy of
+ * that token); kl_share 0: TV alone; kl_share 1, eta 0.5: the drafter's.
+ * weight (optional, 1) f32 [batch][rows]; last_row (optional) int32 [batch]: rows past
+ * last_row[b] take no part (accept_len of nld_verify_accept: the accepted drafts and
+ * the first rejected one).  A row of weight 0 or past last_row is not read; it, and a
+ * row whose teacher or student has no token at all, has loss 0 and gradient 0.
+ * loss f32 [batch][rows]; accept (optional) f32 [batch][rows] = alpha, the chance that
+ * speculative sampling would accept the student's token.  grad (optional): the
+ * gradient of the sum of loss by the logits, in the logits' dtype and sizes; it may be
+ * the logits' own buffer with the same strides, else it must not overlap it, and its
+ * rows must not overlap each other.
+ * An id outside [-1, vocab), or one that an earlier entry of the row has, is left out
+ * and sets NLD_DEV_BAD_TOKEN.  A NaN or +inf that takes part makes loss, accept and
+ * gradient of its row NaN.
+ * Errors: as nld_top_logits, INVALID_ARG for kl_share outside [0, 1], eta < 0 or not
+ * finite, seq_rows < rows, a grad of other sizes or dtype, or one that overlaps. */
+nld_status nld_distill_from_logits(const nld_logits* student, const nld_teacher* teacher, float temperature,
+                                   float kl_share, float eta, const float* weight, const int32_t* last_row,
+                                   float* loss, float* accept, const nld_logits* grad, void* workspace,
+                                   size_t ws_bytes, void* stream);
+
+/* Decoded tokens and what a policy loss weighs them with, [batch][rows] each. */
+typedef struct {
+    const int32_t* actions;   /* -1: the row takes no part */
+    const float* advantage;
+    const float* old_logp;    /* optional: of the policy that decoded them (NULL: this one, the ratio is 1) */
+    const float* ref_logp;    /* optional: of the reference policy */
+} nld_rollout;
+
+/* Clipped policy loss with a KL term.  With logp = log q_action and rho =
+ * exp(logp - old_logp),
+ *   loss = weight * (-min(rho * A, clip(rho, 1 - clip_low, 1 + clip_high) * A)
+ *                    + kl_coef * (exp(d) - d - 1)),   d = ref_logp - logp
+ * (the KL term only with ref_logp).  weight, last_row, loss and grad as above;
+ * logp (optional) f32 [batch][rows], 0 for rows that take no part.  An action outside
+ * [-1, vocab) takes no part and sets NLD_DEV_BAD_TOKEN.
+ * Errors: as nld_top_logits, INVALID_ARG for a clip_low outside [0, 1], a clip_high or kl_coef < 0
+ * or not finite, and grad as above. */
+nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* rollout, float temperature,
+                                  float clip_low, float clip_high, float kl_coef, const float* weight,
+                                  const int32_t* last_row, float* loss, float* logp, const nld_logits* grad,
+                                  void* workspace, size_t ws_bytes, void* stream);
 
 /* ---- tracing aid -------------------------------------------------------------
  * While enabled, every kernel launch made by the block-decode calls records a

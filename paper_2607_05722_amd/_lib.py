@@ -35,8 +35,13 @@ EXPORTED = [
     "nld_accept_from_logits", "nld_denoise_step", "nld_refresh_block", "nld_commit_from_logits",
     "nld_decode_steps", "nld_choose_block", "nld_quad_workspace_bytes", "nld_quad_step",
     "nld_read_device_status", "nld_trace_enable", "nld_trace_read", "nld_verify_accept_noalloc",
-    "nld_hbm_read_probe",
+    "nld_hbm_read_probe", "nld_logits_workspace_bytes", "nld_top_logits", "nld_distill_from_logits",
+    "nld_policy_from_logits",
 ]
+
+NLD_F32 = 0
+NLD_BF16 = 1
+NLD_TOP_MAX = 512
 
 NLD_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -60,6 +65,19 @@ class Weights(ctypes.Structure):
 
 class KVCache(ctypes.Structure):
     _fields_ = [("k", c_vp), ("v", c_vp), ("lengths", c_vp), ("batch", c_i32), ("max_len", c_i32)]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("dtype", c_i32), ("batch", c_i32), ("rows", c_i32), ("vocab", c_i32),
+                ("seq_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class Teacher(ctypes.Structure):
+    _fields_ = [("values", c_vp), ("ids", c_vp), ("lse", c_vp), ("n_top", c_i32), ("seq_rows", c_i32)]
+
+
+class Rollout(ctypes.Structure):
+    _fields_ = [("actions", c_vp), ("advantage", c_vp), ("old_logp", c_vp), ("ref_logp", c_vp)]
 
 
 class NLDError(RuntimeError):
@@ -150,6 +168,16 @@ def load(path: str = None):
     L.nld_verify_accept_noalloc.restype = c_i32
     L.nld_verify_accept_noalloc.argtypes = [c_vp, P(KVCache), c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp,
                                             c_vp]
+    L.nld_logits_workspace_bytes.restype = c_sz
+    L.nld_logits_workspace_bytes.argtypes = [c_i32, c_i32, c_i32, c_i32]
+    L.nld_top_logits.restype = c_i32
+    L.nld_top_logits.argtypes = [P(Logits), c_i32, c_f32, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.nld_distill_from_logits.restype = c_i32
+    L.nld_distill_from_logits.argtypes = [P(Logits), P(Teacher), c_f32, c_f32, c_f32, c_vp, c_vp, c_vp, c_vp,
+                                          P(Logits), c_vp, c_sz, c_vp]
+    L.nld_policy_from_logits.restype = c_i32
+    L.nld_policy_from_logits.argtypes = [P(Logits), P(Rollout), c_f32, c_f32, c_f32, c_f32, c_vp, c_vp, c_vp, c_vp,
+                                         P(Logits), c_vp, c_sz, c_vp]
     _lib = L
     return L
 

@@ -3,6 +3,7 @@
 #include "../../include/nld.h"
 #include "nld_internal.h"
 
+#include <limits.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -708,6 +709,113 @@ nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int
     return NLD_OK;
 }
 
+// ---------------------------------------------------------------- rows of logits
+constexpr double LOG2E = 1.44269504088896340736;
+constexpr int MAX_LOGIT_ROWS = 1 << 20;
+static_assert(TOP_MAX == NLD_TOP_MAX, "entries per row");
+
+// The workspace of an operator on rows of logits: the status word, the partial statistics of rows that several
+// workgroups share, and their largest keys (the top selection) or the entries' logits (the losses).  Few rows are
+// shared by up to SHARED_WGS workgroups per CU in all, and there is room for those whatever the rows, so that a
+// workspace also serves calls of fewer rows, columns and entries; very long rows are shared by as many as they need.
+struct LogitsLayout {
+    RowPlan top, loss;
+    size_t part, entries, total;
+};
+
+LogitsLayout make_logits_layout(int bf16, int n_rows, int vocab, int n_top) {
+    LogitsLayout L{};
+    const int cus = device_cus();
+    L.top = plan_top(bf16, n_rows, vocab, n_top, cus);
+    L.loss = plan_loss(bf16, n_rows, vocab, cus);
+    size_t shared = (size_t)SHARED_WGS * cus;
+    for (int chunks : {L.top.chunks, L.loss.chunks})
+        if (chunks > 1) shared = std::max(shared, (size_t)n_rows * chunks);
+    L.part = 256;
+    L.entries = align256(L.part + 8 * shared);
+    L.total = align256(L.entries + 8 * shared * n_top);
+    return L;
+}
+
+nld_status check_logits(const nld_logits* z, const char* what) {
+    if (!z || !z->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
+    if (z->dtype != NLD_F32 && z->dtype != NLD_BF16) return fail(NLD_ERR_INVALID_ARG, "%s: dtype must be NLD_F32 or NLD_BF16", what);
+    if (z->batch < 1 || z->rows < 1 || z->vocab < 1) return fail(NLD_ERR_INVALID_ARG, "%s: sizes must be positive", what);
+    if (z->seq_stride < 0 || z->row_stride < 0 || z->seq_stride >> 40 || z->row_stride >> 40)
+        return fail(NLD_ERR_INVALID_ARG, "%s: strides must be in [0, 2^40)", what);
+    if ((uintptr_t)z->data % (z->dtype == NLD_BF16 ? 2 : 4)) return fail(NLD_ERR_INVALID_ARG, "%s: data is not aligned to its type", what);
+    if (z->vocab > NLD_LOGITS_MAX_VOCAB) return fail(NLD_ERR_SHAPE, "%s: vocab (%d) exceeds %d", what, z->vocab, NLD_LOGITS_MAX_VOCAB);
+    if ((long long)z->batch * z->rows > MAX_LOGIT_ROWS)
+        return fail(NLD_ERR_SHAPE, "%s: %lld rows exceed %d", what, (long long)z->batch * z->rows, MAX_LOGIT_ROWS);
+    return NLD_OK;
+}
+
+nld_status validate_logits(const nld_logits* z, int n_top, float temperature, void* ws, size_t ws_bytes, LogitsLayout* out) {
+    nld_status st = check_logits(z, "logits");
+    if (st != NLD_OK) return st;
+    if (n_top < 1 || n_top > z->vocab) return fail(NLD_ERR_INVALID_ARG, "n_top must be in [1, vocab] (got %d)", n_top);
+    if (n_top > NLD_TOP_MAX) return fail(NLD_ERR_SHAPE, "n_top (%d) exceeds %d", n_top, NLD_TOP_MAX);
+    if (!(temperature >= 1e-3f && temperature <= 1e3f)) return fail(NLD_ERR_INVALID_ARG, "temperature must be in [1e-3, 1e3]");
+    if (!ws) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
+    *out = make_logits_layout(z->dtype == NLD_BF16, z->batch * z->rows, z->vocab, n_top);
+    // a launch holds less than 2^32 threads
+    if ((long long)z->batch * z->rows * std::max(out->top.chunks, out->loss.chunks) > (1 << 21))
+        return fail(NLD_ERR_SHAPE, "%d rows of %d columns are too many for one call", z->batch * z->rows, z->vocab);
+    if (ws_bytes < out->total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, out->total);
+    return NLD_OK;
+}
+
+LogitRows logit_rows(const nld_logits* z) {
+    return LogitRows{z->data, z->dtype == NLD_BF16, z->batch, z->rows, z->vocab, z->seq_stride, z->row_stride};
+}
+
+// elements from the first one to past the last one
+long long logits_extent(const nld_logits* z) {
+    return (z->batch - 1) * z->seq_stride + (z->rows - 1) * z->row_stride + z->vocab;
+}
+
+// what both losses share; grad: of the logits' dtype and sizes, its rows apart from each other, and either the logits
+// themselves or apart from them
+nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperature, const float* weight, const int32_t* last_row,
+                     float* loss, float* aux, void* ws, const LogitsLayout& L, LossArgs* out) {
+    LossArgs a{};
+    if (grad) {
+        nld_status st = check_logits(grad, "grad");
+        if (st != NLD_OK) return st;
+        if (grad->dtype != z->dtype || grad->batch != z->batch || grad->rows != z->rows || grad->vocab != z->vocab)
+            return fail(NLD_ERR_INVALID_ARG, "grad must have the logits' dtype and sizes");
+        const long long rs = grad->rows > 1 ? grad->row_stride : LLONG_MAX, ss = grad->batch > 1 ? grad->seq_stride : LLONG_MAX;
+        const long long inner = std::min(rs, ss), outer = std::max(rs, ss);
+        const long long n_inner = rs <= ss ? grad->rows : grad->batch;
+        if (inner < grad->vocab || (outer != LLONG_MAX && outer < (n_inner - 1) * inner + grad->vocab))
+            return fail(NLD_ERR_INVALID_ARG, "rows of grad overlap each other");
+        const size_t es = z->dtype == NLD_BF16 ? 2 : 4;
+        const char *z0 = (const char*)z->data, *z1 = z0 + logits_extent(z) * es;
+        const char *g0 = (const char*)grad->data, *g1 = g0 + logits_extent(grad) * es;
+        const bool same = g0 == z0 && (grad->batch == 1 || grad->seq_stride == z->seq_stride) &&
+                          (grad->rows == 1 || grad->row_stride == z->row_stride);
+        if (!same && g0 < z1 && z0 < g1)
+            return fail(NLD_ERR_INVALID_ARG, "grad overlaps the logits without being the same buffer with the same strides");
+        a.grad = grad->data;
+        a.grad_seq_stride = grad->seq_stride;
+        a.grad_row_stride = grad->row_stride;
+    }
+    a.in = logit_rows(z);
+    a.c_exact = LOG2E / (double)temperature;
+    a.c = (float)a.c_exact;
+    a.inv_tau = 1.0 / (double)temperature;
+    a.weight = weight;
+    a.last_row = last_row;
+    a.loss = loss;
+    a.aux = aux;
+    a.status = at<uint32_t>(ws, 0);
+    a.plan = L.loss;
+    a.part = at<float2>(ws, L.part);
+    a.saved = at<uint2>(ws, L.entries);
+    *out = a;
+    return NLD_OK;
+}
+
 }  // namespace
 
 // =====================================================================================
@@ -1069,6 +1177,87 @@ nld_status nld_accept_from_logits(const float* logits, const int32_t* draft, int
     fa.committed = committed;
     fa.next_anchor = next_anchor;
     HIP_TRY(launch_finish(fa, (hipStream_t)stream));
+    return NLD_OK;
+}
+
+size_t nld_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab, int32_t n_top) {
+    if (batch < 1 || rows < 1 || vocab < 1 || n_top < 1 || n_top > NLD_TOP_MAX || n_top > vocab ||
+        vocab > NLD_LOGITS_MAX_VOCAB || (long long)batch * rows > MAX_LOGIT_ROWS)
+        return 0;
+    return std::max(make_logits_layout(0, batch * rows, vocab, n_top).total, make_logits_layout(1, batch * rows, vocab, n_top).total);
+}
+
+nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float temperature, float* values, int32_t* ids,
+                          float* lse, void* workspace, size_t ws_bytes, void* stream) {
+    LogitsLayout L;
+    nld_status st = validate_logits(logits, n_top, temperature, workspace, ws_bytes, &L);
+    if (st != NLD_OK) return st;
+    if (!values || !ids) return fail(NLD_ERR_INVALID_ARG, "values or ids is NULL");
+    TopArgs a{};
+    a.in = logit_rows(logits);
+    a.n_top = n_top;
+    a.c_exact = LOG2E / (double)temperature;
+    a.c = (float)a.c_exact;
+    a.values = values;
+    a.ids = ids;
+    a.lse = lse;
+    a.plan = L.top;
+    a.part = at<float2>(workspace, L.part);
+    a.keys = at<unsigned long long>(workspace, L.entries);
+    HIP_TRY(launch_top(a, (hipStream_t)stream));
+    return NLD_OK;
+}
+
+nld_status nld_distill_from_logits(const nld_logits* student, const nld_teacher* teacher, float temperature,
+                                   float kl_share, float eta, const float* weight, const int32_t* last_row,
+                                   float* loss, float* accept, const nld_logits* grad, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+    if (!teacher || !teacher->values || !teacher->ids) return fail(NLD_ERR_INVALID_ARG, "teacher, its values or its ids is NULL");
+    LogitsLayout L;
+    nld_status st = validate_logits(student, teacher->n_top, temperature, workspace, ws_bytes, &L);
+    if (st != NLD_OK) return st;
+    if (teacher->seq_rows < student->rows) return fail(NLD_ERR_INVALID_ARG, "teacher->seq_rows (%d) < rows (%d)", teacher->seq_rows, student->rows);
+    if (!loss) return fail(NLD_ERR_INVALID_ARG, "loss is NULL");
+    if (!(kl_share >= 0.f && kl_share <= 1.f)) return fail(NLD_ERR_INVALID_ARG, "kl_share must be in [0, 1]");
+    if (!(eta >= 0.f && eta < INFINITY)) return fail(NLD_ERR_INVALID_ARG, "eta must be >= 0 and finite");
+    LossArgs a{};
+    st = loss_args(student, grad, temperature, weight, last_row, loss, accept, workspace, L, &a);
+    if (st != NLD_OK) return st;
+    a.ids = teacher->ids;
+    a.values = teacher->values;
+    a.lse = teacher->lse;
+    a.n_top = teacher->n_top;
+    a.t_seq_rows = teacher->seq_rows;
+    a.kl_share = kl_share;
+    a.eta = eta;
+    HIP_TRY(launch_loss(LOSS_DISTILL, a, (hipStream_t)stream));
+    return NLD_OK;
+}
+
+nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* rollout, float temperature,
+                                  float clip_low, float clip_high, float kl_coef, const float* weight,
+                                  const int32_t* last_row, float* loss, float* logp, const nld_logits* grad,
+                                  void* workspace, size_t ws_bytes, void* stream) {
+    LogitsLayout L;
+    nld_status st = validate_logits(policy, 1, temperature, workspace, ws_bytes, &L);
+    if (st != NLD_OK) return st;
+    if (!rollout || !rollout->actions || !rollout->advantage)
+        return fail(NLD_ERR_INVALID_ARG, "rollout, its actions or its advantage is NULL");
+    if (!loss) return fail(NLD_ERR_INVALID_ARG, "loss is NULL");
+    if (!(clip_low >= 0.f && clip_low <= 1.f)) return fail(NLD_ERR_INVALID_ARG, "clip_low must be in [0, 1]");
+    if (!(clip_high >= 0.f && clip_high < INFINITY)) return fail(NLD_ERR_INVALID_ARG, "clip_high must be >= 0 and finite");
+    if (!(kl_coef >= 0.f && kl_coef < INFINITY)) return fail(NLD_ERR_INVALID_ARG, "kl_coef must be >= 0 and finite");
+    LossArgs a{};
+    st = loss_args(policy, grad, temperature, weight, last_row, loss, logp, workspace, L, &a);
+    if (st != NLD_OK) return st;
+    a.actions = rollout->actions;
+    a.advantage = rollout->advantage;
+    a.old_logp = rollout->old_logp;
+    a.ref_logp = rollout->ref_logp;
+    a.clip_low = clip_low;
+    a.clip_high = clip_high;
+    a.kl_coef = kl_coef;
+    HIP_TRY(launch_loss(LOSS_POLICY, a, (hipStream_t)stream));
     return NLD_OK;
 }
 

@@ -287,6 +287,66 @@ struct PackArgs {
     uint4* dst;
 };
 
+// ---------------------------------------------------------------- rows of logits (logits.hip)
+// Logits [batch][rows][vocab] in f32 or bf16, strides in elements, columns adjacent.
+struct LogitRows {
+    const void* z;
+    int bf16;
+    int batch, rows, vocab;
+    long long seq_stride, row_stride;
+};
+constexpr int TOP_MAX = 512;    // entries per row of the top selection and of a teacher
+constexpr int SHARED_WGS = 2;   // few rows: at most this many workgroups per CU share them
+
+// How a call's rows are spread: `chunks` workgroups share a row, each taking cv 16-byte vectors of it.
+struct RowPlan {
+    int chunks, cv;
+};
+
+struct TopArgs {
+    LogitRows in;
+    int n_top;
+    float c;                     // log2(e) / temperature
+    double c_exact;              // the same, unrounded
+    float* values;               // [batch * rows][n_top]
+    int32_t* ids;                // [batch * rows][n_top]
+    float* lse;                  // optional [batch * rows]
+    RowPlan plan;
+    float2* part;                // chunks > 1: softmax statistics [batch * rows][chunks]
+    unsigned long long* keys;    // chunks > 1: the chunks' largest keys [batch * rows][chunks][n_top] (0: none)
+};
+
+enum LossKind { LOSS_DISTILL = 0, LOSS_POLICY = 1 };
+
+struct LossArgs {
+    LogitRows in;
+    void* grad;                  // optional, the logits' type; may be the logits themselves
+    long long grad_seq_stride, grad_row_stride;
+    float c;                     // log2(e) / temperature
+    double c_exact;
+    double inv_tau;
+    const float* weight;         // optional [batch * rows]
+    const int32_t* last_row;     // optional [batch]: rows past it take no part
+    float* loss;                 // [batch * rows]
+    float* aux;                  // optional [batch * rows]: sum of min(p, q); log-probability of the action
+    // LOSS_DISTILL: the teacher's entries, row (b, j) at index b * t_seq_rows + j
+    const int32_t* ids;
+    const float* values;
+    const float* lse;            // NULL: the entries are the whole distribution
+    int n_top, t_seq_rows;
+    float kl_share, eta;
+    // LOSS_POLICY, [batch * rows] each
+    const int32_t* actions;
+    const float* advantage;
+    const float* old_logp;       // NULL: on policy
+    const float* ref_logp;       // NULL: no KL term
+    float clip_low, clip_high, kl_coef;
+    uint32_t* status;
+    RowPlan plan;
+    float2* part;                // chunks > 1: softmax statistics of the columns outside the entries [rows][chunks]
+    uint2* saved;                // chunks > 1: the entries' logits (bits, 1: it counts) [rows][n_top]
+};
+
 // ---------------------------------------------------------------- launch tracing (api.hip)
 // While tracing is on, returns true with a fresh pair of events for the next launch, which
 // then records them on its own dispatch (start and end of the kernel itself).
@@ -331,5 +391,13 @@ hipError_t launch_finish(const FinishArgs& a, hipStream_t s);
 constexpr int ENS_CHUNKS = 32;
 hipError_t launch_quad_ensemble(const FinishArgs& a, hipStream_t s);
 hipError_t launch_quad_finish(const FinishArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- launchers (logits.hip)
+// Most 16-byte vectors a row of this type and length covers, whatever its alignment.
+int row_vectors(int bf16, int vocab);
+RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus);
+RowPlan plan_loss(int bf16, int n_rows, int vocab, int cus);
+hipError_t launch_top(const TopArgs& a, hipStream_t s);
+hipError_t launch_loss(LossKind kind, const LossArgs& a, hipStream_t s);
 
 }  // namespace nld

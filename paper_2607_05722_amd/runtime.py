@@ -15,7 +15,8 @@ from . import _lib as C
 
 __all__ = ["DeviceModel", "DeviceCache", "Workspace", "block_forward", "draft", "verify_accept",
            "accept_from_logits", "verify_accept_noalloc", "denoise_step", "refresh_block", "commit_from_logits", "read_device_status",
-           "stream_handle", "VERIFY", "DRAFT"]
+           "stream_handle", "VERIFY", "DRAFT", "LogitsWorkspace", "top_logits", "distill_from_logits",
+           "policy_from_logits", "drafter_loss"]
 
 VERIFY = C.NLD_MODE_VERIFY
 DRAFT = C.NLD_MODE_DRAFT
@@ -390,6 +391,184 @@ def quad_step(model, cache, ws, anchor: torch.Tensor, spec: torch.Tensor, k: int
                                    _ptr(o["next_spec"]), _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
     o["logits"] = logits
     return o
+
+
+class LogitsWorkspace:
+    """Workspace of the operators on rows of logits (top_logits, distill_from_logits, policy_from_logits) for up to
+    batch x rows rows of vocab columns and n_top entries per row."""
+
+    def __init__(self, batch: int, rows: int, vocab: int, n_top: int = 1, device="cuda"):
+        lib = C.load()
+        dev = torch.device(device)
+        with torch.cuda.device(dev):
+            self.nbytes = lib.nld_logits_workspace_bytes(batch, rows, vocab, n_top)
+            if self.nbytes == 0:
+                raise ValueError("no logits workspace for batch %d, rows %d, vocab %d, n_top %d" % (batch, rows, vocab, n_top))
+            self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=dev)
+            C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
+
+    @property
+    def ptr(self) -> int:
+        return _ptr(self.buf)
+
+
+def _logits(t: torch.Tensor, name: str) -> C.Logits:
+    """Descriptor of logits [batch][rows][vocab], f32 or bf16, columns adjacent, other strides free."""
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda:
+        raise ValueError("%s must be a float32 or bfloat16 device tensor [batch][rows][vocab]" % name)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("%s: the columns of a row must be adjacent" % name)
+    return C.Logits(_ptr(t), C.NLD_BF16 if t.dtype == torch.bfloat16 else C.NLD_F32, *t.shape, t.stride(0), t.stride(1))
+
+
+def _rows_of(t, name: str, shape, dtype, like):
+    """A contiguous per-row argument on the logits' device (or None)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
+        raise ValueError("%s must be a contiguous %s tensor %s on %s" % (name, dtype, list(shape), like.device))
+    return t
+
+
+def _entries(values, ids, lse, logits, name) -> C.Teacher:
+    """Descriptor of a teacher's entries [batch][rows][n_top]; a leading slice [:, :rows] of longer arrays will do."""
+    B, T = logits.shape[:2]
+    for t, dt, nd in ((values, torch.float32, 3), (ids, torch.int32, 3), (lse, torch.float32, 2)):
+        if t is None:
+            continue
+        if t.dim() != nd or tuple(t.shape[:2]) != (B, T) or t.dtype != dt or t.device != logits.device:
+            raise ValueError("%s: values f32 and ids int32 [batch][rows][n_top] and lse f32 [batch][rows] on %s" % (name, logits.device))
+    n = values.shape[2]
+    if ids.shape[2] != n or n < 1:
+        raise ValueError("%s: values and ids must have the same entries, at least one" % name)
+
+    def seq_rows(t, width):
+        # rows from a sequence to the next, where the rows of one lie one behind the other
+        ok = (width == 1 or t.dim() == 2 or t.stride(2) == 1) and (T == 1 or t.stride(1) == width)
+        if B == 1:
+            return T if ok else None
+        return t.stride(0) // width if ok and t.stride(0) % width == 0 and t.stride(0) >= T * width else None
+
+    found = {seq_rows(values, n), seq_rows(ids, n)} | ({seq_rows(lse, 1)} if lse is not None else set())
+    if len(found) != 1 or None in found:
+        raise ValueError("%s: values, ids and lse must be whole arrays or the same leading rows of such" % name)
+    return C.Teacher(_ptr(values), _ptr(ids), _ptr(lse), n, found.pop())
+
+
+def _grad_for(logits, want_grad, grad, o):
+    if grad is None and want_grad:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if grad is not None:
+        if grad.device != logits.device:
+            raise ValueError("grad must be on %s" % logits.device)
+        o["grad"] = grad
+        return _logits(grad, "grad")
+    return None
+
+
+def _check_ws(ws, like):
+    if ws.buf.device != like.device:
+        raise ValueError("the workspace is on %s, the logits on %s" % (ws.buf.device, like.device))
+
+
+def top_logits(logits: torch.Tensor, n_top: int, ws: LogitsWorkspace, temperature: float = 1.0, outs=None):
+    """The n_top largest logits of every row of logits [batch][rows][vocab] (f32 or bf16), largest first, the lower
+    column first among equal ones.  Returns dict: values f32 and ids int32 [batch][rows][n_top], lse f32
+    [batch][rows] (log-sum-exp of logits / temperature over the whole row)."""
+    desc = _logits(logits, "logits")
+    _check_ws(ws, logits)
+    B, T = logits.shape[:2]
+    dev = logits.device
+    o = dict(outs or {})
+    o.setdefault("values", torch.empty((B, T, n_top), dtype=torch.float32, device=dev))
+    o.setdefault("ids", torch.empty((B, T, n_top), dtype=torch.int32, device=dev))
+    o.setdefault("lse", torch.empty((B, T), dtype=torch.float32, device=dev))
+    _rows_of(o["values"], "values", (B, T, n_top), torch.float32, logits)
+    _rows_of(o["ids"], "ids", (B, T, n_top), torch.int32, logits)
+    _rows_of(o["lse"], "lse", (B, T), torch.float32, logits)
+    with torch.cuda.device(dev):
+        C.check(C.load().nld_top_logits(ctypes.byref(desc), n_top, float(temperature), _ptr(o["values"]), _ptr(o["ids"]),
+                                        _ptr(o["lse"]), ws.ptr, ws.nbytes, stream_handle()))
+    return o
+
+
+def distill_from_logits(logits: torch.Tensor, values: torch.Tensor, ids: torch.Tensor, ws: LogitsWorkspace,
+                        teacher_lse=None, temperature: float = 1.0, kl_share: float = 1.0, eta: float = 0.5, weight=None,
+                        last_row=None, want_grad: bool = True, grad=None, outs=None):
+    """Distillation loss of the student's logits [batch][rows][vocab] from a teacher's top logits (values, ids and,
+    over the teacher's whole row, teacher_lse: what top_logits returns), with its gradient in the same call.  See
+    nld_distill_from_logits in include/nld.h for the formula.  Returns dict: loss and accept f32 [batch][rows], grad
+    (the gradient of loss.sum() by the logits, in their dtype; ``grad=logits`` puts it in their place)."""
+    desc = _logits(logits, "logits")
+    teacher = _entries(values, ids, teacher_lse, logits, "teacher")
+    _check_ws(ws, logits)
+    B, T = logits.shape[:2]
+    dev = logits.device
+    _rows_of(weight, "weight", (B, T), torch.float32, logits)
+    _rows_of(last_row, "last_row", (B,), torch.int32, logits)
+    o = dict(outs or {})
+    o.setdefault("loss", torch.empty((B, T), dtype=torch.float32, device=dev))
+    o.setdefault("accept", torch.empty((B, T), dtype=torch.float32, device=dev))
+    _rows_of(o["loss"], "loss", (B, T), torch.float32, logits)
+    _rows_of(o["accept"], "accept", (B, T), torch.float32, logits)
+    g = _grad_for(logits, want_grad, grad, o)
+    with torch.cuda.device(dev):
+        C.check(C.load().nld_distill_from_logits(
+            ctypes.byref(desc), ctypes.byref(teacher), float(temperature), float(kl_share), float(eta), _ptr(weight),
+            _ptr(last_row), _ptr(o["loss"]), _ptr(o["accept"]), ctypes.byref(g) if g is not None else None, ws.ptr,
+            ws.nbytes, stream_handle()))
+    return o
+
+
+def policy_from_logits(logits: torch.Tensor, actions: torch.Tensor, advantage: torch.Tensor, ws: LogitsWorkspace,
+                       old_logp=None, ref_logp=None, temperature: float = 1.0, clip_low: float = 0.2,
+                       clip_high: float = 0.2, kl_coef: float = 0.0, weight=None, last_row=None, want_grad: bool = True,
+                       grad=None, outs=None):
+    """Clipped policy loss of the tokens ``actions`` (int32 [batch][rows], -1: none) under logits [batch][rows][vocab],
+    with its gradient in the same call.  See nld_policy_from_logits in include/nld.h for the formula.  Returns dict:
+    loss and logp f32 [batch][rows], grad (as distill_from_logits)."""
+    desc = _logits(logits, "logits")
+    _check_ws(ws, logits)
+    B, T = logits.shape[:2]
+    dev = logits.device
+    if actions is None or advantage is None:
+        raise ValueError("actions and advantage are needed")
+    _rows_of(actions, "actions", (B, T), torch.int32, logits)
+    for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")):
+        _rows_of(t, name, (B, T), torch.float32, logits)
+    _rows_of(last_row, "last_row", (B,), torch.int32, logits)
+    rollout = C.Rollout(_ptr(actions), _ptr(advantage), _ptr(old_logp), _ptr(ref_logp))
+    o = dict(outs or {})
+    o.setdefault("loss", torch.empty((B, T), dtype=torch.float32, device=dev))
+    o.setdefault("logp", torch.empty((B, T), dtype=torch.float32, device=dev))
+    _rows_of(o["loss"], "loss", (B, T), torch.float32, logits)
+    _rows_of(o["logp"], "logp", (B, T), torch.float32, logits)
+    g = _grad_for(logits, want_grad, grad, o)
+    with torch.cuda.device(dev):
+        C.check(C.load().nld_policy_from_logits(
+            ctypes.byref(desc), ctypes.byref(rollout), float(temperature), float(clip_low), float(clip_high),
+            float(kl_coef), _ptr(weight), _ptr(last_row), _ptr(o["loss"]), _ptr(o["logp"]),
+            ctypes.byref(g) if g is not None else None, ws.ptr, ws.nbytes, stream_handle()))
+    return o
+
+
+def drafter_loss(model, cache, ws, logits_ws: LogitsWorkspace, anchor: torch.Tensor, k: int, n_top: int = 200,
+                 temperature: float = 3.0, kl_share: float = 1.0, eta: float = 0.5, bidir_from: int = 0, weight=None,
+                 want_grad: bool = True):
+    """A self-speculation step that also gives the drafter's training loss (Sec. 3.3): the draft pass, the verify pass
+    with acceptance and commit, and the distillation of draft rows 1..k-1 from the verify rows that predict the same
+    positions (verify row j-1 for draft row j), over the accepted drafts and the first rejected one.  ``weight``
+    (optional, f32 [batch][k-1]) weighs the rows.  Returns the dict of verify_accept with loss and accept f32
+    [batch][k-1], draft_logits [batch][k][vocab] and drafts added; with ``want_grad`` also grad [batch][k-1][vocab],
+    the gradient of loss.sum() by draft_logits[:, 1:]."""
+    drafts, draft_logits = draft(model, cache, ws, anchor, k, bidir_from, want_logits=True)
+    out = verify_accept(model, cache, ws, anchor, drafts, k, want_logits=True)
+    top = top_logits(out["logits"][:, :k - 1], n_top, logits_ws, temperature)
+    o = distill_from_logits(draft_logits[:, 1:], top["values"], top["ids"], logits_ws, teacher_lse=top["lse"],
+                            temperature=temperature, kl_share=kl_share, eta=eta, weight=weight,
+                            last_row=out["accept_len"], want_grad=want_grad)
+    out.update(o, drafts=drafts, draft_logits=draft_logits)
+    return out
 
 
 def choose_block(ar_step_ms: float, ss_step_ms: float, expected_committed: float, k_ss: int) -> int:
