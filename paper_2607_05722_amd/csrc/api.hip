@@ -732,7 +732,7 @@ LogitsLayout make_logits_layout(int bf16, int n_rows, int vocab, int n_top) {
     for (int chunks : {L.top.chunks, L.loss.chunks})
         if (chunks > 1) shared = std::max(shared, (size_t)n_rows * chunks);
     L.part = 256;
-    L.entries = align256(L.part + 8 * shared);
+    L.entries = align256(L.part + sizeof(ChunkStat) * shared);
     L.total = align256(L.entries + 8 * shared * n_top);
     return L;
 }
@@ -810,7 +810,7 @@ nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperat
     a.aux = aux;
     a.status = at<uint32_t>(ws, 0);
     a.plan = L.loss;
-    a.part = at<float2>(ws, L.part);
+    a.part = at<ChunkStat>(ws, L.part);
     a.saved = at<uint2>(ws, L.entries);
     *out = a;
     return NLD_OK;
@@ -1202,7 +1202,7 @@ nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float tempera
     a.ids = ids;
     a.lse = lse;
     a.plan = L.top;
-    a.part = at<float2>(workspace, L.part);
+    a.part = at<ChunkStat>(workspace, L.part);
     a.keys = at<unsigned long long>(workspace, L.entries);
     HIP_TRY(launch_top(a, (hipStream_t)stream));
     return NLD_OK;

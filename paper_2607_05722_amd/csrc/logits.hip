@@ -4,12 +4,14 @@
 // All three read a row of `vocab` logits z once for its softmax statistics, q_j = exp(z_j / tau) / sum, and are bound
 // by that read (a few operations and one exponential per logit), the gradient by the read and the write.
 //
-// Exponents are taken in base 2, with c = log2(e) / tau.  A thread keeps a running reference m (the largest logit it
-// has seen) and s = sum exp2((z - m) * c); pairs (m, s) merge as s1 * exp2((m1 - m) * c) + s2 * exp2((m2 - m) * c).  The
-// difference is taken before the product, so that a row of the type's lowest values does not overflow.  The sum is f32:
-// 150 thousand positive terms in several hundred partial sums keep its relative error below 1e-5 at worst, near 1e-8
-// in the middle.  What comes after the sums, a few values per row and per teacher entry, is in f64, because the losses
-// are small differences of logarithms (a divergence of 1e-3 from logarithms near 10 keeps four digits in f32).
+// Exponents are taken in base 2, with c = float(log2(e) / tau).  A thread keeps a running reference m (the largest z * c it
+// has seen, rounded) and s = sum exp2(z * c - m): per logit one fused multiply-add, one exp2 and one addition (and for bf16
+// one operation to unpack it).  The sum is f32: 150 thousand positive terms in several hundred partial sums keep its
+// relative error below 1e-5 at worst, near 1e-8 in the middle.  What comes after the sums, a few values per row and per
+// teacher entry, is in f64, because the losses are small differences of logarithms (a divergence of 1e-3 from logarithms
+// near 10 keeps four digits in f32); there the reference counts as m * (c_exact / c), which takes c's rounding back.
+// Rows whose products with c do not fit f32 (a mask of the type's lowest value over all of a row) are taken again with
+// differences before products, out of the way of the others.
 //
 // A row is cut into 16-byte vectors on the addresses' own 16-byte grid, so that rows of any stride and start are read
 // with aligned wide loads: vector i holds elements [i * W - lead, (i + 1) * W - lead), W = 4 (f32) or 8 (bf16), and the
@@ -41,10 +43,12 @@ struct Elem<true> {
 };
 
 template <bool BF>
-__device__ __forceinline__ float load_elem(const typename Elem<BF>::type* p) {
-    if constexpr (BF) return bf16_to_f32(*p);
-    else return *p;
+__device__ __forceinline__ float to_float(typename Elem<BF>::type v) {
+    if constexpr (BF) return bf16_to_f32(v);
+    else return v;
 }
+template <bool BF>
+__device__ __forceinline__ float load_elem(const typename Elem<BF>::type* p) { return to_float<BF>(*p); }
 template <bool BF>
 __device__ __forceinline__ void store_elem(typename Elem<BF>::type* p, float v) {
     if constexpr (BF) *p = (uint16_t)f32_to_bf16(v);
@@ -102,48 +106,112 @@ struct Span {
     __device__ __forceinline__ int edge(int k) const { return k < f0 - v0 ? v0 + k : f1 + (k - (f0 - v0)); }
 };
 
+// a value that every lane holds alike, in scalar registers: rows are held in the vector registers meanwhile
+__device__ __forceinline__ float uniform(float v) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+__device__ __forceinline__ double uniform(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+
 // ---------------------------------------------------------------- softmax statistics
 struct Stat {
-    float m, s;   // reference (-inf: nothing yet) and sum of exp2((z - m) * c)
+    float m, s;   // reference and sum of exp2(z * c - m)
 };
-__device__ __forceinline__ Stat stat_merge(Stat a, Stat b, float c) {
+constexpr float STAT_EMPTY = -3.0e38f;   // the reference of no logit: finite, so that -inf adds nothing to a sum of it
+__device__ __forceinline__ Stat stat_merge(Stat a, Stat b) {
+    Stat o;
+    o.m = fmaxf(a.m, b.m);
+    o.s = a.s * __builtin_amdgcn_exp2f(a.m - o.m) + b.s * __builtin_amdgcn_exp2f(b.m - o.m);
+    return o;
+}
+// adds N logits and returns the largest of them; NaN, +inf or a product past f32 among them makes the sum NaN
+template <int N>
+__device__ __forceinline__ float stat_add(Stat& t, const float* z, float c) {
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
+    const float m = top * c;
+    if (m > t.m) {
+        t.s *= __builtin_amdgcn_exp2f(t.m - m);
+        t.m = m;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) t.s += __builtin_amdgcn_exp2f(fmaf(z[e], c, -t.m));
+    return top;
+}
+// the same with differences first: m is the largest logit itself (-inf: none yet), s = sum of exp2((z - m) * c)
+__device__ __forceinline__ Stat wide_merge(Stat a, Stat b, float c) {
     Stat o;
     o.m = fmaxf(a.m, b.m);
     const float ref = o.m == -INFINITY ? 0.f : o.m;   // both empty: the sums are 0 (or NaN, which stays)
     o.s = a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c);
     return o;
 }
-// adds N logits; a NaN or +inf among them makes the sum NaN
-template <int N>
-__device__ __forceinline__ void stat_add(Stat& t, const float* z, float c) {
-    float top = z[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-    if (top > t.m) {
-        t.s *= __builtin_amdgcn_exp2f((t.m - top) * c);
-        t.m = top;
-    }
-    const float ref = t.m == -INFINITY ? 0.f : t.m;
-#pragma unroll
-    for (int e = 0; e < N; ++e) t.s += __builtin_amdgcn_exp2f((z[e] - ref) * c);
-}
-// every thread's statistics -> the workgroup's, in every thread; red: NT / 64 pairs
-template <int NT>
-__device__ __forceinline__ Stat stat_block(Stat t, Stat* red, float c) {
+
+// every thread's statistics -> the workgroup's, in every thread, and the same of the maximum *top (optional); red: two
+// times NT / 64 pairs.  WIDE: by wide_merge.
+template <int NT, bool WIDE>
+__device__ __forceinline__ Stat stat_block(Stat t, Stat* red, float c, float* top) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto merge = [&](Stat x, Stat y) __attribute__((always_inline)) {
+        if constexpr (WIDE) return wide_merge(x, y, c);
+        else return stat_merge(x, y);
+    };
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) t = stat_merge(t, Stat{__shfl_xor(t.m, off), __shfl_xor(t.s, off)}, c);
-    if (lane == 0) red[wave] = t;
+    for (int off = 32; off >= 1; off >>= 1) t = merge(t, Stat{__shfl_xor(t.m, off), __shfl_xor(t.s, off)});
+    if (top)
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) *top = fmaxf(*top, __shfl_xor(*top, off));
     __syncthreads();
-    t = red[0];
+    if (lane == 0) {
+        red[wave] = t;
+        if (top) red[NT / 64 + wave].m = *top;
+    }
+    __syncthreads();
+    t = red[lane & (NT / 64 - 1)];
 #pragma unroll
-    for (int w = 1; w < NT / 64; ++w) t = stat_merge(t, red[w], c);
-    return t;
+    for (int off = NT / 128; off >= 1; off >>= 1) t = merge(t, Stat{__shfl_xor(t.m, off), __shfl_xor(t.s, off)});
+    if (top) {
+        float x = red[NT / 64 + (lane & (NT / 64 - 1))].m;
+#pragma unroll
+        for (int off = NT / 128; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+        *top = uniform(x);
+    }
+    return Stat{uniform(t.m), uniform(t.s)};
+}
+
+// The statistics of a row or a chunk of it: sum of exp2(z / tau * log2(e) - ref) = s.
+typedef ChunkStat RowStat;
+// From every thread's share; `again` takes the thread's logits once more, by wide_merge of Stat{z, 1}.
+template <int NT, class Again>
+__device__ __forceinline__ RowStat row_stat(Stat t, Stat* red, float c, double c_exact, float* top, const Again& again) {
+    t = stat_block<NT, false>(t, red, c, top);
+    if (t.s > 0.f && t.s < INFINITY) return RowStat{uniform((double)t.m * (c_exact / (double)c)), t.s};
+    t = stat_block<NT, true>(again(), red, c, nullptr);
+    return RowStat{t.m == -INFINITY ? 0.0 : uniform((double)t.m * c_exact), t.s};
+}
+// all chunks of row r, in every thread: a lane takes every 64th chunk, then the wavefront's lanes are added in a tree
+__device__ __forceinline__ RowStat merge_chunks(const ChunkStat* part, int r, int chunks) {
+    const int lane = threadIdx.x & 63;
+    const ChunkStat* p = part + (long long)r * chunks;
+    double ref = -(double)INFINITY;
+    for (int c = lane; c < chunks; c += 64)
+        if (p[c].s != 0.f) ref = fmax(ref, p[c].ref);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) ref = fmax(ref, __shfl_xor(ref, off));
+    if (ref == -(double)INFINITY) ref = 0.0;   // nothing anywhere
+    double s = 0.0;
+    for (int c = lane; c < chunks; c += 64)
+        if (p[c].s != 0.f) s += (double)p[c].s * exp2(p[c].ref - ref);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+    return RowStat{uniform(ref), uniform((float)s)};
 }
 // log2 of the sum of exp(z / tau)
-__device__ __forceinline__ double stat_log2(Stat t, double c_exact) {
-    return t.s == 0.f ? -(double)INFINITY : (double)t.m * c_exact + log2((double)t.s);
-}
+__device__ __forceinline__ double stat_log2(RowStat t) { return t.s == 0.f ? -(double)INFINITY : t.ref + log2((double)t.s); }
 
 // ---------------------------------------------------------------- the largest logits of a row
 // Order-preserving key of a logit at column n: larger value first, then lower column; -0.0 counts as +0.0 and a NaN
@@ -162,15 +230,17 @@ __device__ __forceinline__ unsigned long long key_of(uint32_t ord, int n) {
 constexpr uint32_t ORD_POS_INF = 0xFF800000u, ORD_NEG_INF = 0x007FFFFFu;
 
 constexpr int TOP_NT = 1024;     // threads
-constexpr int TOP_SEGS = 8;      // a thread's vectors are cut into this many segments, each with its maximum
+constexpr int TOP_SEGS = 16;     // a thread's vectors are cut into at most this many segments, each with its maximum
+constexpr int TOP_AHEAD = 4;     // vectors requested at once; a segment is a multiple of it
+constexpr int TOP_HITS = 4096;   // segments that may be looked at again
 constexpr int TOP_CAND = 2048;   // candidates that one ranking holds
 
 struct TopShared {
-    uint32_t seg[TOP_SEGS][TOP_NT];          // largest key of each thread's segments
-    uint16_t hits[TOP_SEGS * TOP_NT];        // segments that may hold one of the largest
+    uint16_t seg[TOP_SEGS][TOP_NT];          // largest key of each thread's segments, its upper half
+    uint16_t hits[TOP_HITS];                 // segments that may hold one of the largest
     unsigned long long cand[TOP_CAND];
     uint32_t hist[256];
-    Stat red[TOP_NT / 64];
+    Stat red[2 * TOP_NT / 64];
     int cnt[2][TOP_NT / 64];
     int n_hits, n_cand, digit, above;
 };
@@ -291,91 +361,116 @@ __device__ __forceinline__ void emit_top(const TopArgs& a, int r, int rank, unsi
     a.ids[(long long)r * a.n_top + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
 }
 // the row's log-sum-exp, from the largest key and the statistics (whose sum is NaN where +inf or NaN took part)
-__device__ __forceinline__ float lse_of(Stat t, uint32_t top, const TopArgs& a) {
+__device__ __forceinline__ float lse_of(RowStat t, uint32_t top) {
     if (top == 0xFFFFFFFFu) return NAN;
     if (top == ORD_POS_INF) return INFINITY;
     if (top == ORD_NEG_INF) return -INFINITY;
-    return (float)(stat_log2(t, a.c_exact) * 0.69314718055994530942);
+    return (float)(stat_log2(t) * 0.69314718055994530942);
 }
 
 // One pass over the row for the statistics and for the maximum of every thread's segments; then a lower bound of the
-// k-th largest from the threads' maxima; then a second look at the few segments that reach it (about k of 8192, a few
-// per cent of the row, which the first pass left in L2 or the memory-side cache); then the candidates are ranked.
+// k-th largest from the threads' maxima; then a second look at the few segments that reach it (about k of some
+// thousands, a few per cent of the row, which the first pass left in L2 or the memory-side cache); then the candidates
+// are ranked.
 template <bool BF>
 __global__ void __launch_bounds__(TOP_NT) top_kernel(TopArgs a) {
     constexpr int W = Elem<BF>::W;
     __shared__ TopShared sh;
     const int r = blockIdx.x / a.plan.chunks, chunk = blockIdx.x % a.plan.chunks, tid = threadIdx.x;
     const Span<BF> sp(a.in, r, chunk, a.plan.cv);
-    const int iters = (sp.v1 - sp.v0 + TOP_NT - 1) / TOP_NT, len = (iters + TOP_SEGS - 1) / TOP_SEGS;   // vectors per segment
+    const int nf = sp.f1 - sp.f0, iters = (nf + TOP_NT - 1) / TOP_NT;   // full vectors of the chunk, and of a thread
+    const int len = (iters + TOP_SEGS * TOP_AHEAD - 1) / (TOP_SEGS * TOP_AHEAD) * TOP_AHEAD;   // vectors per segment
+    const int segs = len ? (iters + len - 1) / len : 0;
     if (tid == 0) {
         sh.n_hits = 0;
         sh.n_cand = 0;
     }
-    Stat st{-INFINITY, 0.f};
-    uint32_t best = 0u;
-    for (int s = 0; s < TOP_SEGS; ++s) {
+    Stat part{STAT_EMPTY, 0.f};
+    float best_z = -INFINITY;
+    bool any = false;
+    float edge[W];
+    if (tid < sp.n_edges()) {
+        sp.load_edge(sp.edge(tid), edge);
+        best_z = stat_add<W>(part, edge, a.c);
+        any = true;
+    }
+    for (int s = 0; s < segs; ++s) {
         float top = -INFINITY;
-        bool any = false;
-        for (int u = s * len; u < min(iters, (s + 1) * len); ++u) {
-            const int i = sp.v0 + u * TOP_NT + tid;
-            if (i >= sp.v1) break;
+        for (int u0 = 0; u0 < len; u0 += TOP_AHEAD) {
+            const int i0 = tid + (s * len + u0) * TOP_NT;   // among the full vectors
+            uint4 v[TOP_AHEAD];
+#pragma unroll
+            for (int u = 0; u < TOP_AHEAD; ++u) v[u] = sp.load(sp.f0 + min(i0 + u * TOP_NT, nf - 1));
+#pragma unroll
+            for (int u = 0; u < TOP_AHEAD; ++u)
+                if (i0 + u * TOP_NT < nf) {
+                    float z[W];
+                    unpack<BF>(v[u], z);
+                    top = fmaxf(top, stat_add<W>(part, z, a.c));
+                    any = true;
+                }
+        }
+        sh.seg[s][tid] = tid + s * len * TOP_NT < nf ? (uint16_t)(order_of(top) >> 16) : (uint16_t)0;
+        best_z = fmaxf(best_z, top);
+    }
+    const RowStat st = row_stat<TOP_NT>(part, sh.red, a.c, a.c_exact, nullptr, [&]() {
+        Stat t{-INFINITY, 0.f};
+        for (int i = sp.v0 + tid; i < sp.v1; i += TOP_NT) {
             float z[W];
             if (sp.full(i)) unpack<BF>(sp.load(i), z);
             else sp.load_edge(i, z);
-            stat_add<W>(st, z, a.c);
 #pragma unroll
-            for (int e = 0; e < W; ++e) top = fmaxf(top, z[e]);
-            any = true;
+            for (int e = 0; e < W; ++e) t = wide_merge(t, Stat{z[e], 1.f}, a.c);
         }
-        const uint32_t o = any ? order_of(top) : 0u;
-        sh.seg[s][tid] = o;
-        best = max(best, o);
-    }
-    st = stat_block<TOP_NT>(st, sh.red, a.c);
+        return t;
+    });
     const int e0 = max(0, sp.v0 * W - sp.lead), e1 = min(sp.n, sp.v1 * W - sp.lead), n = max(0, e1 - e0);
     const int k = min(a.n_top, n);
-    uint32_t bound = 0u;
-    bool exact = st.s != st.s;   // NaN or +inf: the maxima above do not order these
+    bool exact = !(st.s < INFINITY);   // NaN or +inf: the maxima above do not order these
     if (!exact) {
-        bound = bound_below(best, k, sh);
-        __syncthreads();
-#pragma unroll
-        for (int s = 0; s < TOP_SEGS; ++s)
-            if (sh.seg[s][tid] != 0u && sh.seg[s][tid] >= bound) sh.hits[atomicAdd(&sh.n_hits, 1)] = (uint16_t)(s * TOP_NT + tid);
-        __syncthreads();
-        const int items = sh.n_hits * len;
-        for (int it = tid; it < items; it += TOP_NT) {
-            const int h = sh.hits[it / len], s = h / TOP_NT, u = s * len + it % len, i = sp.v0 + u * TOP_NT + h % TOP_NT;
-            if (u >= iters || i >= sp.v1) continue;
-            float z[W];
-            if (sp.full(i)) unpack<BF>(sp.load(i), z);
-            else sp.load_edge(i, z);
+        const uint32_t bound = bound_below(any ? order_of(best_z) : 0u, k, sh);
+        auto take = [&](const float* z, int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < W; ++e) {
                 const int j = i * W + e - sp.lead;
                 const uint32_t o = order_of(z[e]);
-                if (j >= 0 && j < sp.n && o >= bound) {
+                if (o >= bound && j >= 0 && j < sp.n) {
                     const int at = atomicAdd(&sh.n_cand, 1);
                     if (at < TOP_CAND) sh.cand[at] = key_of(o, j);
                 }
             }
+        };
+        __syncthreads();
+        if (tid < sp.n_edges()) take(edge, sp.edge(tid));
+        for (int s = 0; s < segs; ++s)
+            if (sh.seg[s][tid] != 0u && sh.seg[s][tid] >= bound >> 16) {
+                const int at = atomicAdd(&sh.n_hits, 1);
+                if (at < TOP_HITS) sh.hits[at] = (uint16_t)(s * TOP_NT + tid);
+            }
+        __syncthreads();
+        const int items = min(sh.n_hits, TOP_HITS) * len;
+        for (int it = tid; it < items; it += TOP_NT) {
+            const int h = sh.hits[it / len], i = h % TOP_NT + (h / TOP_NT * len + it % len) * TOP_NT;
+            if (i >= nf) continue;
+            float z[W];
+            unpack<BF>(sp.load(sp.f0 + i), z);
+            take(z, sp.f0 + i);
         }
         __syncthreads();
-        exact = sh.n_cand > TOP_CAND;
+        exact = sh.n_cand > TOP_CAND || sh.n_hits > TOP_HITS;
     }
     if (exact) select_exact(RowKeys<BF>{sp, e0}, n, k, sh);
     const int nc = sh.n_cand;
     if (a.plan.chunks == 1) {
         rank_candidates(nc, k, sh, [&](int rank, unsigned long long key) {
             emit_top(a, r, rank, key);
-            if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(key >> 32), a);
+            if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(key >> 32));
         });
     } else {
         unsigned long long* out = a.keys + ((long long)r * a.plan.chunks + chunk) * a.n_top;
         for (int i = k + tid; i < a.n_top; i += TOP_NT) out[i] = 0ull;
         rank_candidates(nc, k, sh, [&](int rank, unsigned long long key) { out[rank] = key; });
-        if (tid == 0) a.part[(long long)r * a.plan.chunks + chunk] = float2{st.m, st.s};
+        if (tid == 0) a.part[(long long)r * a.plan.chunks + chunk] = st;
     }
 }
 
@@ -385,14 +480,8 @@ __global__ void __launch_bounds__(TOP_NT) top_merge_kernel(TopArgs a) {
     const int r = blockIdx.x, tid = threadIdx.x, n = a.plan.chunks * a.n_top;
     const ListKeys key{a.keys + (long long)r * n};
     if (tid == 0) sh.n_cand = 0;
-    Stat st{-INFINITY, 0.f};
-    for (int p = tid; p < a.plan.chunks; p += TOP_NT) {
-        const float2 v = a.part[(long long)r * a.plan.chunks + p];
-        st = stat_merge(st, Stat{v.x, v.y}, a.c);
-    }
     uint32_t best = 0u;
     for (int i = tid; i < n; i += TOP_NT) best = max(best, (uint32_t)(key(i) >> 32));
-    st = stat_block<TOP_NT>(st, sh.red, a.c);
     const uint32_t bound = max(bound_below(best, a.n_top, sh), 1u);   // 0: an empty place of a short chunk
     __syncthreads();
     for (int i = tid; i < n; i += TOP_NT) {
@@ -403,9 +492,10 @@ __global__ void __launch_bounds__(TOP_NT) top_merge_kernel(TopArgs a) {
     }
     __syncthreads();
     if (sh.n_cand > TOP_CAND) select_exact(key, n, a.n_top, sh);
+    const RowStat st = merge_chunks(a.part, r, a.plan.chunks);
     rank_candidates(sh.n_cand, a.n_top, sh, [&](int rank, unsigned long long x) {
         emit_top(a, r, rank, x);
-        if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(x >> 32), a);
+        if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(x >> 32));
     });
 }
 
@@ -416,23 +506,23 @@ __global__ void __launch_bounds__(TOP_NT) top_merge_kernel(TopArgs a) {
 //   row values   in f64 from the entries' logits and (m, s): the loss, and the coefficients of the gradient, which is
 //                rest * exp2((z_j - m) * c) for every column outside the entries and a value of its own for each entry;
 //   gradient     one more pass over the row.
-constexpr int LOSS_NT = 512;   // a thread per entry
-static_assert(LOSS_NT >= TOP_MAX, "a thread per teacher entry");
+constexpr int LOSS_NT = TOP_MAX;   // threads: at least one per teacher entry
 
+template <int NT>
 struct LossShared {
-    Stat red[LOSS_NT / 64];
-    double sum[LOSS_NT / 64][5];
+    Stat red[2 * NT / 64];
+    double sum[TOP_MAX / 64][2];
     int32_t ids[TOP_MAX];
+    uint32_t mark[NT];   // per thread: which of its held vectors have an entry among their columns
     int repeated;
 };
 
-// sums (or maxima) of N values over the workgroup, in every thread; wavefronts without a teacher entry hold `none`
-template <int N, bool MAX>
-__device__ __forceinline__ void reduce_block(double* v, bool mine, LossShared& sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const double none = MAX ? -(double)INFINITY : 0.0;
-    if (mine) {
-#pragma unroll
+// sums (or maxima) of N values over the n threads of the entries, in every thread of the workgroup
+template <int N, bool MAX, int NT>
+__device__ __forceinline__ void reduce_entries(double* v, int n, LossShared<NT>& sh) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (n + 63) >> 6;
+    if (wave < waves) {
+#pragma unroll 1
         for (int off = 32; off >= 1; off >>= 1)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -441,78 +531,109 @@ __device__ __forceinline__ void reduce_block(double* v, bool mine, LossShared& s
             }
     }
     __syncthreads();
-    if (lane == 0)
+    if (lane == 0 && wave < waves)
 #pragma unroll
-        for (int i = 0; i < N; ++i) sh.sum[wave][i] = mine ? v[i] : none;
+        for (int i = 0; i < N; ++i) sh.sum[wave][i] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        double t = sh.sum[0][i];
-        for (int w = 1; w < LOSS_NT / 64; ++w) t = MAX ? fmax(t, sh.sum[w][i]) : t + sh.sum[w][i];
-        v[i] = t;
-    }
+    for (int i = 0; i < N; ++i) v[i] = sh.sum[0][i];
+#pragma unroll 1   // one at a time: the row may be held in registers meanwhile
+    for (int w = 1; w < waves; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = MAX ? fmax(v[i], sh.sum[w][i]) : v[i] + sh.sum[w][i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = uniform(v[i]);
 }
 
-// what a row's gradient needs: rest * exp2((z - m) * c) outside the entries, `entry` at this thread's entry
+// What a row's gradient needs: a column outside the entries gets its share of the rest, exp2(z / tau * log2(e) - ref) / s,
+// times `rest`; `entry` is what this thread's entry gets.
 struct RowGrad {
-    float m, rest, entry;
+    RowStat st;
+    double rest;
+    float entry;
     bool none;   // the gradient is zero throughout
 };
 
 // Distillation.  p: the teacher's probabilities of its entries and, with its log-sum-exp given, of everything else (the
-// rest, R); q: the student's.  Every thread calls this with its entry (counts: it is one).
+// rest, R); q: the student's.
 //   loss = w (lambda KL + (1 - lambda) TV),  KL = sum p log(p / q),  TV = 1/2 sum |p - q|,
 //   lambda = kl_share exp(-eta alpha), alpha = sum min(p, q), held constant in the gradient;
 //   d loss / d z_j = w / tau (q_j (lambda P + (1 - lambda) / 2 (s_j - mean)) - lambda p_j) for an entry, with P = sum p,
 //   s = sign(q - p), mean = sum s q, all sums over entries and rest, and in the rest, where every q_j has the same share
 //   of what the rest gets, w / tau q_j (lambda P + (1 - lambda) / 2 (s_R - mean) - lambda p_R / q_R).
-__device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, int trow, bool counts, float z, float t, bool whole,
-                                               Stat st, double weight, LossShared& sh) {
-    const bool mine = (int)(threadIdx.x & ~63u) < a.n_top;   // a wavefront with entries
+// KL is taken as sum p log p - sum p y + P log(sum of the student's exponentials), y = z / tau, so that all of the teacher's side is
+// done while the row is on its way, and TV as (P + 1) / 2 - alpha.
+
+// The teacher's side: this thread's p, and for the row the sums (base-2 logarithms) over entries and rest.
+struct Teacher {
+    double p, entries, rest, plogp;
+    bool none;   // no token at all
+};
+template <int NT>
+__device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, float t_lse, bool counts, bool whole, LossShared<NT>& sh) {
     const double none = -(double)INFINITY;
-    const double x = counts ? (double)t * a.c_exact : none, y = counts ? (double)z * a.c_exact : none;   // base-2 exponents
-    double top[2] = {x, y};
-    reduce_block<2, true>(top, mine, sh);
-    double tot[2];
-    tot[0] = x == none ? 0.0 : exp2(x - top[0]);
-    tot[1] = y == none ? 0.0 : exp2(y - top[1]);
-    reduce_block<2, false>(tot, mine, sh);
-    const double log_rest = stat_log2(st, a.c_exact);
-    const double ref = fmax(log_rest, top[1]);
-    const double lse = a.lse ? (double)a.lse[trow] * 1.44269504088896340736 : top[0] + log2(tot[0]);
-    RowGrad g{st.m == -INFINITY ? 0.f : st.m, 0.f, 0.f, true};
-    // a teacher or a student without any token: nothing to learn
-    if (lse == none || (ref == none && st.s == 0.f && tot[1] == 0.0)) {
+    const double x = counts ? (double)t * a.c_exact : none;
+    double lse;
+    if (a.lse) {
+        lse = uniform((double)t_lse * 1.44269504088896340736);
+    } else {
+        double top[1] = {x};
+        reduce_entries<1, true, NT>(top, a.n_top, sh);
+        double tot[1] = {x == none ? 0.0 : exp2(x - top[0])};
+        reduce_entries<1, false, NT>(tot, a.n_top, sh);
+        lse = uniform(tot[0] == 0.0 ? none : top[0] + log2(tot[0]));
+    }
+    Teacher o;
+    o.none = lse == none;
+    o.p = x == none ? 0.0 : exp2(x - lse);
+    double sums[2] = {o.p, o.p > 0.0 ? o.p * (x - lse) : 0.0};
+    reduce_entries<2, false, NT>(sums, a.n_top, sh);
+    o.entries = sums[0];
+    o.rest = a.lse && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;   // whole: the entries are every column
+    o.plogp = uniform(sums[1] + (o.rest > 0.0 ? o.rest * log2(o.rest) : 0.0));
+    if (!(sums[0] < (double)INFINITY)) o.entries = o.plogp = (double)NAN;
+    return o;
+}
+
+// The rest: every thread with its entry's logit z, the statistics of the columns outside the entries, and the largest
+// logit among the entries.
+template <int NT>
+__device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, const Teacher& t, bool counts, float z, float z_top,
+                                               RowStat st, double weight, LossShared<NT>& sh) {
+    RowGrad g{st, 0.0, 0.f, true};
+    const double y_top = uniform((double)z_top * a.c_exact);   // -inf: no entry has a probability
+    const double ref = st.s == 0.f ? (z_top == -INFINITY ? 0.0 : y_top) : uniform(fmax(st.ref, y_top));
+    const double er = st.s == 0.f ? 0.0 : uniform((double)st.s * exp2(st.ref - ref));
+    const double y = (double)z * a.c_exact - ref, ey = counts ? exp2(y) : 0.0;
+    double sums[2] = {ey, t.p > 0.0 ? t.p * y : 0.0};
+    reduce_entries<2, false, NT>(sums, a.n_top, sh);
+    const double total = er + sums[0];
+    if (t.none || total == 0.0) {   // a teacher or a student without any token: nothing to learn
         if (threadIdx.x == 0) {
             a.loss[r] = 0.f;
             if (a.aux) a.aux[r] = 0.f;
         }
         return g;
     }
-    const double log_all = ref + log2(exp2(log_rest - ref) + (top[1] > none ? tot[1] * exp2(top[1] - ref) : tot[1]));
-    const double lp = x - lse, lq = y - log_all;
-    const double p = counts ? exp2(lp) : 0.0, q = counts ? exp2(lq) : 0.0;
-    const double sgn = q > p ? 1.0 : (q < p ? -1.0 : 0.0);
-    double sums[5] = {p, p > 0.0 ? p * (lp - lq) : 0.0, fmin(p, q), fabs(p - q), sgn * q};
-    if (counts && !(p == p && q == q)) sums[2] = p + q;   // fmin would drop a NaN
-    reduce_block<5, false>(sums, mine, sh);
-    const double p_rest = a.lse && !whole ? fmax(0.0, 1.0 - sums[0]) : 0.0;
-    const double lq_rest = log_rest - log_all, q_rest = exp2(lq_rest);
-    const double s_rest = q_rest > p_rest ? 1.0 : (q_rest < p_rest ? -1.0 : 0.0);
-    const double kl = (sums[1] + (p_rest > 0.0 ? p_rest * (log2(p_rest) - lq_rest) : 0.0)) * 0.69314718055994530942;
-    const double tv = 0.5 * (sums[3] + fabs(p_rest - q_rest));
-    const double alpha = sums[2] + (q_rest == q_rest ? fmin(p_rest, q_rest) : q_rest);
-    const double mean = sums[4] + s_rest * q_rest, mass = sums[0] + p_rest;
-    const double lambda = (double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha);
+    const double inv = uniform(1.0 / total), q = ey * inv, q_rest = uniform(er * inv);
+    const double sgn = q > t.p ? 1.0 : (q < t.p ? -1.0 : 0.0);
+    double both[2] = {q == q && t.p == t.p ? fmin(t.p, q) : q + t.p, sgn * q};
+    reduce_entries<2, false, NT>(both, a.n_top, sh);
+    const double log_total = uniform(log2(total)), rest_y = uniform(stat_log2(st) - ref);
+    const double mass = t.entries + t.rest;
+    const double kl = (t.plogp - sums[1] - (t.rest > 0.0 ? t.rest * rest_y : 0.0) + mass * log_total) * 0.69314718055994530942;
+    const double alpha = both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest);
+    const double tv = 0.5 * (mass + 1.0) - alpha;
+    const double lambda = uniform((double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha));
+    const double s_rest = q_rest > t.rest ? 1.0 : (q_rest < t.rest ? -1.0 : 0.0);
+    const double mean = both[1] + s_rest * q_rest, half = 0.5 * (1.0 - lambda), f = weight * a.inv_tau;
     if (threadIdx.x == 0) {
         a.loss[r] = (float)(weight * ((lambda > 0.0 ? lambda * kl : 0.0) + (1.0 - lambda) * tv));
         if (a.aux) a.aux[r] = (float)alpha;
     }
-    const double f = weight * a.inv_tau, half = 0.5 * (1.0 - lambda);
     g.none = false;
-    g.entry = (float)(f * (q * (lambda * mass + half * (sgn - mean)) - lambda * p));
-    // exp2((z - m) c) / s is a column's share of the rest
-    if (st.s != 0.f) g.rest = (float)(f * (q_rest * (lambda * mass + half * (s_rest - mean)) - lambda * p_rest) / (double)st.s);
+    g.entry = (float)(f * (q * (lambda * mass + half * (sgn - mean)) - lambda * t.p));
+    g.rest = uniform(f * (q_rest * (lambda * mass + half * (s_rest - mean)) - lambda * t.rest));
     return g;
 }
 
@@ -520,9 +641,12 @@ __device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, int tro
 //   loss = w (-min(rho A, clip(rho, 1 - low, 1 + high) A) + beta (exp(d) - d - 1)),  d = ref - logp,
 //   d loss / d logp = w (-[rho A is the minimum] rho A + beta (1 - exp(d))),  d logp / d z_j = ([j = action] - q_j) / tau.
 // With the action apart, 1 - q of a likely action is the rest's share itself.
-__device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, float z, Stat st, double weight) {
-    RowGrad g{st.m == -INFINITY ? 0.f : st.m, 0.f, 0.f, true};
-    const double y = (double)z * a.c_exact, log_rest = stat_log2(st, a.c_exact);
+struct Rollout {
+    float advantage, old_logp, ref_logp;
+};
+__device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, const Rollout& in, float z, RowStat st, double weight) {
+    RowGrad g{st, 0.0, 0.f, true};
+    const double y = (double)z * a.c_exact, log_rest = stat_log2(st);
     const double ref = fmax(log_rest, y);
     if (ref == -(double)INFINITY && st.s == 0.f && z == z) {   // no token is possible
         if (threadIdx.x == 0) {
@@ -534,14 +658,14 @@ __device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, float z,
     const double er = exp2(log_rest - ref), ey = exp2(y - ref), all = er + ey;
     // log(ey / all), by the rest's share where that is the small part
     const double logp = y >= log_rest ? -log1p(er / ey) : (y - ref) * 0.69314718055994530942 - log(all);
-    const double adv = a.advantage[r];
-    const double rho = a.old_logp ? exp(logp - (double)a.old_logp[r]) : (logp == logp ? 1.0 : logp);
+    const double adv = in.advantage;
+    const double rho = a.old_logp ? exp(logp - (double)in.old_logp) : (logp == logp ? 1.0 : logp);
     const double free_ = adv == 0.0 ? 0.0 : rho * adv;
     const double held = fmin(fmax(rho, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
     double loss = free_ <= held ? -free_ : (free_ > held ? -held : (double)NAN);
     double dl = free_ <= held ? -free_ : (free_ > held ? 0.0 : (double)NAN);
     if (a.ref_logp) {
-        const double d = (double)a.ref_logp[r] - logp, beta = a.kl_coef;
+        const double d = (double)in.ref_logp - logp, beta = a.kl_coef;
         loss += beta * (expm1(d) - d);
         dl -= beta * expm1(d);
     }
@@ -552,42 +676,84 @@ __device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, float z,
     const double f = weight * a.inv_tau * dl;
     g.none = f == 0.0;   // clipped
     g.entry = (float)(f * (er / all));
-    if (st.s != 0.f) g.rest = (float)(-f * (er / all) / (double)st.s);
+    g.rest = -f * (er / all);
     return g;
 }
 
-// does row r take part, and with what weight
-__device__ __forceinline__ bool row_counts(const LossArgs& a, int r, double* weight) {
-    const float w = a.weight ? a.weight[r] : 1.f;
-    *weight = (double)w;
-    const int b = r / a.in.rows;
-    return w != 0.f && !(a.last_row && r - b * a.in.rows > a.last_row[b]);
+// What a row's loss needs besides its logits, requested at once: the loads of the logits follow them, and what was
+// asked for later would be waited for together with these.
+struct RowInputs {
+    float weight, t, t_lse;
+    int last, id, action;
+    Rollout rollout;
+};
+template <LossKind KIND>
+__device__ __forceinline__ RowInputs row_inputs(const LossArgs& a, int r) {
+    const int b = r / a.in.rows, tid = threadIdx.x;
+    RowInputs v{};
+    v.weight = a.weight ? a.weight[r] : 1.f;
+    v.last = a.last_row ? a.last_row[b] : a.in.rows;
+    v.id = v.action = -1;
+    if constexpr (KIND == LOSS_DISTILL) {
+        const long long row = (long long)b * a.t_seq_rows + (r - b * a.in.rows), e = row * a.n_top + min(tid, a.n_top - 1);
+        v.id = a.ids[e];
+        v.t = a.values[e];
+        v.t_lse = a.lse ? a.lse[row] : 0.f;
+    } else {
+        v.action = a.actions[r];
+        v.rollout = Rollout{a.advantage[r], a.old_logp ? a.old_logp[r] : 0.f, a.ref_logp ? a.ref_logp[r] : 0.f};
+    }
+    return v;
+}
+// does the row take part
+template <LossKind KIND>
+__device__ __forceinline__ bool row_counts(const LossArgs& a, int r, int chunk, const RowInputs& v) {
+    if (v.weight == 0.f || r % a.in.rows > v.last) return false;
+    if (KIND == LOSS_POLICY && (v.action < 0 || v.action >= a.in.vocab)) {
+        if (v.action != -1 && chunk == 0 && threadIdx.x == 0) atomicOr(a.status, DEV_BAD_TOKEN);
+        return false;
+    }
+    return true;
 }
 
-// The entries of this chunk: membership bits of its vectors' columns (distillation), and this thread's entry: *z its
-// logit where it lies in the chunk.  Returns whether the entry counts; *here: it lies in this chunk (an entry that
-// counts nowhere is chunk 0's to report).
-template <bool BF>
-__device__ __forceinline__ bool find_entries(const LossArgs& a, const Span<BF>& sp, long long trow, int chunk, uint32_t* bits,
-                                             LossShared& sh, float* z, bool* here) {
-    constexpr int W = Elem<BF>::W;
-    const int tid = threadIdx.x, words = (a.plan.cv * W + 31) / 32;
-    for (int w = tid; w < words; w += LOSS_NT) bits[w] = 0u;
-    if (tid == 0) sh.repeated = 0;
-    const int id = tid < a.n_top ? a.ids[trow * a.n_top + tid] : -1;
+// Waits for the row's inputs, before the loads of the logits are issued: a later wait for an input, on a path where the
+// compiler cannot count the loads in between, would wait for all of these.
+__device__ __forceinline__ void inputs_here() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A teacher's entries in this chunk: membership bits of its vectors' columns, the marks of the threads that hold them (the
+// first `held` vectors of each), and this thread's entry.  list_entries, then (a barrier lies between) mark_entries.
+template <bool BF, int NT>
+__device__ __forceinline__ void list_entries(const LossArgs& a, int id, uint32_t* bits, LossShared<NT>& sh) {
+    const int tid = threadIdx.x, words = (a.plan.cv * Elem<BF>::W + 31) / 32;
     if (tid < a.n_top) sh.ids[tid] = id;
+    for (int w = tid; w < words; w += NT) bits[w] = 0u;
+    sh.mark[tid] = 0u;
+    if (tid == 0) sh.repeated = 0;
+}
+// Returns whether the entry counts; *here: it lies in this chunk (an entry that counts nowhere is chunk 0's to report);
+// *z: its logit as stored, asked for but not looked at.
+template <bool BF, int NT>
+__device__ __forceinline__ bool mark_entries(const LossArgs& a, const Span<BF>& sp, int id, int chunk, int held, uint32_t* bits,
+                                             LossShared<NT>& sh, typename Elem<BF>::type* z, bool* here) {
+    constexpr int W = Elem<BF>::W;
+    const int tid = threadIdx.x;
     __syncthreads();
-    const bool valid = id >= 0 && id < sp.n;
+    const bool entry = tid < a.n_top, valid = entry && id >= 0 && id < sp.n;
     const int v = valid ? (id + sp.lead) / W : 0;
-    *here = valid ? v >= sp.v0 && v < sp.v1 : tid < a.n_top && chunk == 0;
+    *here = valid ? v >= sp.v0 && v < sp.v1 : entry && chunk == 0;
     bool counts = valid && *here;
     if (counts) {
-        *z = load_elem<BF>(sp.row + id);
-        const int bit = id + sp.lead - sp.v0 * W;
+        *z = sp.row[id];
+        const int bit = id + sp.lead - sp.v0 * W, at = v - sp.f0;
         if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1u) sh.repeated = 1;
+        if (at >= 0 && at < held * NT) atomicOr(&sh.mark[at % NT], 1u << (at / NT));
     }
     __syncthreads();
-    bool bad = tid < a.n_top && chunk == 0 && !valid && id != -1;
+    bool bad = entry && chunk == 0 && !valid && id != -1;
     if (sh.repeated && counts) {   // of equal ids the first counts
         for (int i = 0; i < tid; ++i)
             if (sh.ids[i] == id) counts = false;
@@ -610,180 +776,334 @@ __device__ __forceinline__ uint32_t members(const Span<BF>& sp, const uint32_t* 
     }
 }
 
-template <bool BF, LossKind KIND>
-__device__ __forceinline__ Stat rest_stats(const Span<BF>& sp, const uint32_t* bits, int action, float c) {
-    constexpr int W = Elem<BF>::W, U = 4;
-    Stat st{-INFINITY, 0.f};
-    auto add = [&](float* z, int i) __attribute__((always_inline)) {
-        const uint32_t mem = members<BF, KIND>(sp, bits, action, i);
-        if (mem)
-#pragma unroll
-            for (int e = 0; e < W; ++e) z[e] = (mem >> e) & 1u ? -INFINITY : z[e];
-        stat_add<W>(st, z, c);
-    };
-    if ((int)threadIdx.x < sp.n_edges()) {
-        float z[W];
-        const int i = sp.edge(threadIdx.x);
-        sp.load_edge(i, z);
-        add(z, i);
-    }
-    int i = sp.f0 + threadIdx.x;
-    for (; i + (U - 1) * LOSS_NT < sp.f1; i += U * LOSS_NT) {
-        uint4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = sp.load(i + u * LOSS_NT);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float z[W];
-            unpack<BF>(v[u], z);
-            add(z, i + u * LOSS_NT);
+// One pass over this thread's vectors of a chunk for the statistics of the columns outside the entries, and a second
+// one, through the same object, for their gradient.  The first CAP vectors of each thread stay in registers from the
+// one to the other; the rest of a longer chunk is read again.
+template <bool BF, LossKind KIND, int NT, int CAP>
+struct Columns {
+    static constexpr int W = Elem<BF>::W;
+    const Span<BF>& sp;
+    const uint32_t* bits;
+    int action;
+    uint32_t mark;   // which held vectors have an entry among their columns
+    uint4 held[CAP > 0 ? CAP : 1];
+    static_assert(CAP <= 32, "a bit per held vector");
+    __device__ __forceinline__ Columns(const Span<BF>& s, const uint32_t* b, int act) : sp(s), bits(b), action(act), mark(0u) {
+        if constexpr (KIND == LOSS_POLICY) {
+            const int at = (act + s.lead) / W - s.f0;
+            if (at >= 0 && at < CAP * NT && at % NT == (int)threadIdx.x) mark = 1u << (at / NT);
         }
     }
-    for (; i < sp.f1; i += LOSS_NT) {
-        float z[W];
-        unpack<BF>(sp.load(i), z);
-        add(z, i);
+    // Asks for held vector u, without a branch (a thread's last ones may be the chunk's last vector again), so that a wait
+    // for an earlier load does not wait for this one; past the caches, which are for what is read again (125 us with it, 131
+    // without, for 512 rows of 151936 f32 logits with gradient).  f1 > f0.
+    __device__ __forceinline__ void ask(int u) { held[u] = load_stream((const uint4*)sp.grid + min(sp.f0 + (int)threadIdx.x + u * NT, sp.f1 - 1)); }
+    // The first vectors; `each` asks for the others as it goes, AHEAD ahead: with all of them asked for at once a wavefront is
+    // held up until the memory has taken them, about as long as the row takes to come, and starts to work on it after that
+    // (4096 rows of 151936 bf16 logits, distillation with gradient: 593 us, and 539 with 8 ahead).
+    static constexpr int AHEAD = CAP < 8 ? CAP : 8;
+    __device__ __forceinline__ void fetch() {
+        if (sp.f1 <= sp.f0) return;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) ask(u);
     }
-    return st;
-}
-
-// The gradient of this chunk's columns outside the entries (none: zeros in all its columns).  A thread reads a
-// vector before it writes the same columns, so the gradient may take the logits' place.
-template <bool BF, LossKind KIND>
-__device__ __forceinline__ void write_rest(const LossArgs& a, const Span<BF>& sp, int r, const uint32_t* bits, int action,
-                                           RowGrad g) {
-    const bool zero = g.none;
-    typedef typename Elem<BF>::type T;
-    constexpr int W = Elem<BF>::W;
-    const int b = r / a.in.rows, j = r - b * a.in.rows;
-    T* out = (T*)a.grad + (long long)b * a.grad_seq_stride + (long long)j * a.grad_row_stride;
-    const bool wide = (((uintptr_t)out ^ (uintptr_t)sp.row) & 15u) == 0u;   // vectors line up with the logits'
-    auto put = [&](float* z, int i, bool full) __attribute__((always_inline)) {
-        const uint32_t mem = zero ? 0u : members<BF, KIND>(sp, bits, action, i);
+    __device__ __forceinline__ uint32_t mem(int i) const { return members<BF, KIND>(sp, bits, action, i); }
+    // f(vector index, its values, is it a full one, has it an entry, its place in `held` or -1) for every vector; FIRST: the
+    // pass that loads them.  The number of vectors is made opaque in each pass: the compiler would keep the comparisons with it, a
+    // register pair per vector, from the one to the other.
+    template <bool FIRST, class F>
+    __device__ __forceinline__ void each(const F& f) {
+        constexpr int U = CAP > 0 ? 2 : 4;
+        if ((int)threadIdx.x < sp.n_edges()) {
+            float z[W];
+            const int i = sp.edge(threadIdx.x);
+            sp.load_edge(i, z);
+            f(i, z, false, mem(i) != 0u, -1);
+        }
+        int count = sp.f1 - sp.f0 - (int)threadIdx.x;   // vectors from this thread's first on
+        asm volatile("" : "+v"(count));
+        if (sp.f1 > sp.f0) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) z[e] = zero ? 0.f : __builtin_amdgcn_exp2f((z[e] - g.m) * a.c) * g.rest;
-        if (full && wide && mem == 0u) {
-            uint4 v;
-            if constexpr (BF) v = uint4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])};
-            else v = uint4{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])};
-            *(uint4*)(out + ((long long)i * W - sp.lead)) = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < W; ++e) {
-                const int col = i * W + e - sp.lead;
-                if (col >= 0 && col < sp.n && !((mem >> e) & 1u)) store_elem<BF>(out + col, z[e]);
+            for (int u = 0; u < CAP; ++u) {
+                if (FIRST && u + AHEAD < CAP) {
+                    ask(u + AHEAD);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (count > u * NT) {
+                    float z[W];
+                    unpack<BF>(held[u], z);
+                    f(sp.f0 + (int)threadIdx.x + u * NT, z, true, (mark >> u & 1u) != 0u, u);
+                }
             }
         }
-    };
-    if ((int)threadIdx.x < sp.n_edges()) {
-        float z[W];
-        const int i = sp.edge(threadIdx.x);
-        if (!zero) sp.load_edge(i, z);
-        put(z, i, false);
+        int i = sp.f0 + (int)threadIdx.x + CAP * NT;
+        for (; i + (U - 1) * NT < sp.f1; i += U * NT) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = sp.load(i + u * NT);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float z[W];
+                unpack<BF>(v[u], z);
+                f(i + u * NT, z, true, mem(i + u * NT) != 0u, -1);
+            }
+        }
+        for (; i < sp.f1; i += NT) {
+            float z[W];
+            unpack<BF>(sp.load(i), z);
+            f(i, z, true, mem(i) != 0u, -1);
+        }
     }
-    for (int i = sp.f0 + threadIdx.x; i < sp.f1; i += LOSS_NT) {
-        float z[W];
-        if (!zero) unpack<BF>(sp.load(i), z);
-        put(z, i, true);
+    // the vectors of this thread one after the other, for what rarely runs: f(vector index, its values, entries among them)
+    template <class F>
+    __device__ __forceinline__ void each_slowly(const F& f) const {
+#pragma unroll 1
+        for (int i = sp.v0 + (int)threadIdx.x; i < sp.v1; i += NT) {
+            float z[W];
+            if (sp.full(i)) unpack<BF>(sp.load(i), z);
+            else sp.load_edge(i, z);
+            f(i, z, mem(i));
+        }
     }
-}
+    // entry(): this thread's entry's logit, whose maximum goes to *z_top (NULL: neither)
+    template <class E>
+    __device__ __forceinline__ RowStat stats(const LossArgs& a, LossShared<NT>& sh, const E& entry_logit, float* z_top) {
+        Stat st{STAT_EMPTY, 0.f};
+        each<true>([&](int i, float* z, bool, bool entry, int) __attribute__((always_inline)) {
+            if (entry) {
+                const uint32_t m = mem(i);
+#pragma unroll
+                for (int e = 0; e < W; ++e) z[e] = (m >> e) & 1u ? -INFINITY : z[e];
+            }
+            stat_add<W>(st, z, a.c);
+        });
+        if (z_top) *z_top = entry_logit();
+        return row_stat<NT>(st, sh.red, a.c, a.c_exact, z_top, [&]() __attribute__((always_inline)) {
+            Stat t{-INFINITY, 0.f};
+            each_slowly([&](int, float* z, uint32_t m) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) t = wide_merge(t, Stat{(m >> e) & 1u ? -INFINITY : z[e], 1.f}, a.c);
+            });
+            return t;
+        });
+    }
+};
 
 template <bool BF>
-__device__ __forceinline__ void write_entry(const LossArgs& a, int r, int col, float v) {
+struct GradRow {
     typedef typename Elem<BF>::type T;
-    const int b = r / a.in.rows, j = r - b * a.in.rows;
-    store_elem<BF>((T*)a.grad + (long long)b * a.grad_seq_stride + (long long)j * a.grad_row_stride + col, v);
-}
-
-// STEP 0: a workgroup takes a whole row.  Rows that several workgroups share: STEP 1 leaves every chunk's statistics and
-// entries in the workspace, STEP 2 takes them together, each workgroup for itself, and writes its chunk of the gradient.
-template <bool BF, LossKind KIND, int STEP>
-__global__ void __launch_bounds__(LOSS_NT) loss_kernel(LossArgs a) {
-    extern __shared__ uint32_t bits[];
-    __shared__ LossShared sh;
-    const int per_row = STEP == 2 && !a.grad ? 1 : a.plan.chunks;   // workgroups of a row in this launch
-    const int r = blockIdx.x / per_row, chunk = blockIdx.x % per_row, tid = threadIdx.x;
-    const Span<BF> sp(a.in, r, chunk, a.plan.cv);
-    double weight;
-    bool on = row_counts(a, r, &weight);
-    int action = -1;
-    if (KIND == LOSS_POLICY && on) {
-        action = a.actions[r];
-        if (action < 0 || action >= sp.n) {
-            if (action != -1 && chunk == 0 && tid == 0) atomicOr(a.status, DEV_BAD_TOKEN);
-            on = false;
+    static constexpr int W = Elem<BF>::W;
+    T* out;   // column 0
+    __device__ __forceinline__ GradRow(const LossArgs& a, int r) {
+        const int b = r / a.in.rows, j = r - b * a.in.rows;
+        out = (T*)a.grad + (long long)b * a.grad_seq_stride + (long long)j * a.grad_row_stride;
+    }
+    // All columns of vector i (of the logits' grid; the gradient's rows may lie otherwise, and global stores of any
+    // alignment are one instruction).  STREAM: past the caches.  Many rows' gradients are more than these hold, and would
+    // drive out the part of the logits that is read again: 512 rows of 151936 f32 logits take 131 us with it and 163 without,
+    // 4096 of bf16, which stay in registers, 424 and 438.
+    template <bool STREAM>
+    __device__ __forceinline__ void put(const Span<BF>& sp, int i, const float* g) const {
+        uint4 v;
+        if constexpr (BF) v = uint4{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7])};
+        else v = uint4{__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3])};
+        T* at = out + ((long long)i * W - sp.lead);
+        if constexpr (STREAM) {
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+            __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4*)at);
+        } else {
+            __builtin_memcpy(at, &v, 16);
         }
     }
-    if (!on) {
-        if (STEP == 1) return;
-        if (chunk == 0 && tid == 0) {
-            a.loss[r] = 0.f;
-            if (a.aux) a.aux[r] = 0.f;
+    // those that lie in the row and not in `skip`
+    __device__ __forceinline__ void put_some(const Span<BF>& sp, int i, const float* g, uint32_t skip) const {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const int col = i * W + e - sp.lead;
+            if (col >= 0 && col < sp.n && !((skip >> e) & 1u)) store_elem<BF>(out + col, g[e]);
         }
-        if (a.grad) write_rest<BF, KIND>(a, sp, r, bits, -1, RowGrad{0.f, 0.f, 0.f, true});
+    }
+    template <int NT>
+    __device__ __forceinline__ void zero(const Span<BF>& sp) const {
+        float g[W] = {};
+        if ((int)threadIdx.x < sp.n_edges()) put_some(sp, sp.edge(threadIdx.x), g, 0u);
+        for (int i = sp.f0 + (int)threadIdx.x; i < sp.f1; i += NT) put<true>(sp, i, g);
+    }
+};
+
+// The gradient of a chunk's columns: the rest's from `cols`, and the entry of this thread (col, where `mine`).  A thread
+// has read a vector when it writes the same columns, and the entries' logits were read before, so the gradient may
+// take the logits' place.  The few vectors with an entry among their columns are written column by column, after the
+// others: they are read once more for it, which keeps that code out of the unrolled part.
+template <bool BF, LossKind KIND, int NT, int CAP>
+__device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp, Columns<BF, KIND, NT, CAP>& cols, int r,
+                                           const RowGrad& g, bool mine, int col) {
+    constexpr int W = Elem<BF>::W;
+    const GradRow<BF> out(a, r);
+    if (g.none) {
+        out.template zero<NT>(sp);
         return;
     }
-    const int b = r / a.in.rows;
-    const long long trow = (long long)b * a.t_seq_rows + (r - b * a.in.rows);
-    float z = -INFINITY;
+    if (!(fabs(g.st.ref) < 1e8)) {   // products with c would lose the differences, or not fit f32: differences first
+        const float m = (float)(g.st.ref / a.c_exact);
+        const float scale = g.st.s == 0.f ? 0.f : (float)(g.rest / (double)g.st.s * exp2((double)m * a.c_exact - g.st.ref));
+        cols.each_slowly([&](int i, float* z, uint32_t mem) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - m) * a.c) * scale;
+            out.put_some(sp, i, z, mem);
+        });
+    } else {
+        // exp2(z c - m) * scale; m is the reference rounded to f32 (c's rounding taken back), and what it is off by belongs to
+        // scale
+        const float m = uniform((float)(g.st.ref * ((double)a.c / a.c_exact)));
+        const float scale = uniform(g.st.s == 0.f ? 0.f : (float)(g.rest / (double)g.st.s * exp2((double)m * (a.c_exact / (double)a.c) - g.st.ref)));
+        auto value = [&](float z) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(z, a.c, -m)) * scale; };
+        cols.template each<false>([&](int i, float* z, bool full, bool entry, int u) __attribute__((always_inline)) {
+            if (full && !entry) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) z[e] = value(z[e]);
+                out.template put<(CAP > 0)>(sp, i, z);
+            } else if (u < 0) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) z[e] = value(z[e]);
+                out.put_some(sp, i, z, cols.mem(i));
+            }
+        });
+#pragma unroll 1
+        for (uint32_t later = cols.mark; later; later &= later - 1u) {
+            const int i = sp.f0 + (int)threadIdx.x + NT * (__ffs(later) - 1);
+            float z[W];
+            unpack<BF>(sp.load(i), z);
+#pragma unroll
+            for (int e = 0; e < W; ++e) z[e] = value(z[e]);
+            out.put_some(sp, i, z, cols.mem(i));
+        }
+    }
+    if (mine) store_elem<BF>(out.out + col, g.entry);
+}
+
+// a row that takes no part, or has nothing to learn from
+template <bool BF, int NT>
+__device__ __forceinline__ void empty_row(const LossArgs& a, const Span<BF>& sp, int r, int chunk) {
+    if (chunk == 0 && threadIdx.x == 0) {
+        a.loss[r] = 0.f;
+        if (a.aux) a.aux[r] = 0.f;
+    }
+    if (a.grad) GradRow<BF>(a, r).template zero<NT>(sp);
+}
+
+// A workgroup takes a whole row and keeps it, or the first CAP * NT vectors of it, in registers from the statistics to
+// the gradient.
+template <bool BF, LossKind KIND, int NT, int CAP>
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) loss_row_kernel(LossArgs a) {
+    typedef typename Elem<BF>::type T;
+    extern __shared__ uint32_t bits[];
+    __shared__ LossShared<NT> sh;
+    const int r = blockIdx.x, tid = threadIdx.x;
+    const Span<BF> sp(a.in, r, 0, a.plan.cv);
+    const RowInputs in = row_inputs<KIND>(a, r);
+    if (!row_counts<KIND>(a, r, 0, in)) {
+        empty_row<BF, NT>(a, sp, r, 0);
+        return;
+    }
+    Columns<BF, KIND, NT, CAP> cols(sp, bits, in.action);
+    RowGrad g;
+    bool mine = tid == 0;
+    if constexpr (KIND == LOSS_DISTILL) {
+        list_entries<BF, NT>(a, in.id, bits, sh);
+        inputs_here();
+        cols.fetch();
+        T raw = 0;
+        bool here;
+        const bool counts = mark_entries<BF, NT>(a, sp, in.id, 0, CAP, bits, sh, &raw, &here);
+        cols.mark = sh.mark[tid];
+        const bool whole = __syncthreads_count(counts) == sp.n;
+        const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, whole, sh);
+        __builtin_amdgcn_sched_barrier(0);
+        // (z as stored is looked at after the row's vectors, which were asked for before it)
+        float z = -INFINITY, z_top;
+        const RowStat st = cols.stats(a, sh, [&]() __attribute__((always_inline)) { return z = counts ? to_float<BF>(raw) : -INFINITY; }, &z_top);
+        g = distill_row<NT>(a, r, te, counts, z, z_top, st, (double)in.weight, sh);
+        mine = counts;
+    } else {
+        const T raw = sp.row[in.action];
+        cols.fetch();
+        const RowStat st = cols.stats(a, sh, [] { return 0.f; }, nullptr);
+        g = policy_row(a, r, in.rollout, to_float<BF>(raw), st, (double)in.weight);
+    }
+    if (a.grad) write_grad<BF, KIND, NT, CAP>(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
+}
+
+// Few rows are shared by several workgroups.  STEP 1 leaves every chunk's statistics and entries in the workspace, STEP 2
+// takes them together, each workgroup for itself, and writes its chunk of the gradient.
+template <bool BF, LossKind KIND, int STEP>
+__global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
+    typedef typename Elem<BF>::type T;
+    constexpr int NT = LOSS_NT;
+    extern __shared__ uint32_t bits[];
+    __shared__ LossShared<NT> sh;
+    const int per_row = STEP == 2 && !a.grad ? 1 : a.plan.chunks;   // workgroups of a row in this launch
+    const int r = blockIdx.x / per_row, chunk = blockIdx.x % per_row, tid = threadIdx.x;
+    const int n_entries = KIND == LOSS_DISTILL ? a.n_top : 1;
+    const Span<BF> sp(a.in, r, chunk, a.plan.cv);
+    const RowInputs in = row_inputs<KIND>(a, r);
+    if (!row_counts<KIND>(a, r, chunk, in)) {
+        if (STEP == 2) empty_row<BF, NT>(a, sp, r, chunk);
+        return;
+    }
+    Columns<BF, KIND, NT, 0> cols(sp, bits, in.action);
+    T raw = 0;
     bool counts = false, here = false;
     if constexpr (KIND == LOSS_DISTILL) {
-        if (STEP != 2 || a.grad) counts = find_entries<BF>(a, sp, trow, STEP == 2 ? -1 : chunk, bits, sh, &z, &here);
+        if (STEP == 1 || a.grad) {
+            list_entries<BF, NT>(a, in.id, bits, sh);
+            counts = mark_entries<BF, NT>(a, sp, in.id, STEP == 1 ? chunk : -1, 0, bits, sh, &raw, &here);
+        }
     } else {
-        const int v = (action + sp.lead) / Elem<BF>::W;
-        counts = true;
+        const int v = (in.action + sp.lead) / Elem<BF>::W;
         here = v >= sp.v0 && v < sp.v1;
-        if (STEP != 2 && here) z = load_elem<BF>(sp.row + action);
+        counts = true;
+        if (STEP == 1 && here) raw = sp.row[in.action];
     }
-    Stat st;
-    if constexpr (STEP != 2) {
-        st = stat_block<LOSS_NT>(rest_stats<BF, KIND>(sp, bits, action, a.c), sh.red, a.c);
-        if constexpr (STEP == 1) {
-            const int n_entries = KIND == LOSS_DISTILL ? a.n_top : 1;
-            if (tid == 0) a.part[(long long)r * a.plan.chunks + chunk] = float2{st.m, st.s};
-            if (here && tid < n_entries) a.saved[(long long)r * n_entries + tid] = uint2{__float_as_uint(z), counts ? 1u : 0u};
-            return;
-        }
+    if constexpr (STEP == 1) {
+        const RowStat st = cols.stats(a, sh, [] { return 0.f; }, nullptr);
+        if (tid == 0) a.part[(long long)r * a.plan.chunks + chunk] = st;
+        if (here && tid < n_entries)
+            a.saved[(long long)r * n_entries + tid] = uint2{__float_as_uint(to_float<BF>(raw)), counts ? 1u : 0u};
     } else {
-        st = Stat{-INFINITY, 0.f};
-        for (int p = 0; p < a.plan.chunks; ++p) {
-            const float2 v = a.part[(long long)r * a.plan.chunks + p];
-            st = stat_merge(st, Stat{v.x, v.y}, a.c);
-        }
+        const RowStat st = merge_chunks(a.part, r, a.plan.chunks);
+        RowGrad g;
+        bool mine = here && tid == 0;
         if constexpr (KIND == LOSS_DISTILL) {
             const uint2 e = tid < a.n_top ? a.saved[(long long)r * a.n_top + tid] : uint2{0u, 0u};
-            z = __uint_as_float(e.x);
-            here = here && e.y != 0u;
             counts = e.y != 0u;
+            const bool whole = __syncthreads_count(counts) == sp.n;
+            const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, whole, sh);
+            const float z = counts ? __uint_as_float(e.x) : -INFINITY;
+            float z_top = z;
+            stat_block<NT, false>(Stat{STAT_EMPTY, 0.f}, sh.red, a.c, &z_top);
+            g = distill_row<NT>(a, r, te, counts, z, z_top, st, (double)in.weight, sh);
+            mine = here && counts;
         } else {
-            z = __uint_as_float(a.saved[r].x);
+            g = policy_row(a, r, in.rollout, __uint_as_float(a.saved[r].x), st, (double)in.weight);
         }
+        if (a.grad) write_grad<BF, KIND, NT, 0>(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
     }
-    RowGrad g;
-    if constexpr (KIND == LOSS_DISTILL) {
-        const int n_counts = __syncthreads_count(counts);
-        const float t = tid < a.n_top ? a.values[trow * a.n_top + tid] : 0.f;
-        g = distill_row(a, r, (int)trow, counts, z, t, n_counts == sp.n, st, weight, sh);
-    } else {
-        g = policy_row(a, r, z, st, weight);
-    }
-    if (!a.grad) return;
-    write_rest<BF, KIND>(a, sp, r, bits, action, g);
-    if (g.none) return;
-    if (KIND == LOSS_DISTILL ? counts && (STEP == 0 || here) : here && tid == 0)
-        write_entry<BF>(a, r, KIND == LOSS_DISTILL ? sh.ids[tid] : action, g.entry);
 }
 
 template <bool BF, LossKind KIND>
 void launch_loss_as(const LossArgs& a, hipStream_t s) {
+    constexpr int HELD = KIND == LOSS_DISTILL ? 19 : 21;   // vectors of a thread that stay in registers
     const int n = a.in.batch * a.in.rows;
     const size_t lds = KIND == LOSS_DISTILL ? (size_t)cdiv(a.plan.cv * Elem<BF>::W, 32) * 4 : 0;
     if (a.plan.chunks == 1) {
-        loss_kernel<BF, KIND, 0><<<n, LOSS_NT, lds, s>>>(a);
+        if (a.grad == nullptr) loss_row_kernel<BF, KIND, 512, 0><<<n, 512, lds, s>>>(a);
+        else if (a.plan.cv <= 512 * HELD) loss_row_kernel<BF, KIND, 512, HELD><<<n, 512, lds, s>>>(a);
+        else loss_row_kernel<BF, KIND, 1024, HELD><<<n, 1024, lds, s>>>(a);
         return;
     }
-    loss_kernel<BF, KIND, 1><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
-    loss_kernel<BF, KIND, 2><<<a.grad ? n * a.plan.chunks : n, LOSS_NT, lds, s>>>(a);
+    loss_chunk_kernel<BF, KIND, 1><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
+    loss_chunk_kernel<BF, KIND, 2><<<a.grad ? n * a.plan.chunks : n, LOSS_NT, lds, s>>>(a);
 }
 
 }  // namespace

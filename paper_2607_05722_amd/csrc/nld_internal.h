@@ -303,6 +303,12 @@ struct RowPlan {
     int chunks, cv;
 };
 
+// softmax statistics of a chunk of a row: sum of exp2(z / tau * log2(e) - ref) = s
+struct ChunkStat {
+    double ref;
+    float s;
+};
+
 struct TopArgs {
     LogitRows in;
     int n_top;
@@ -312,7 +318,7 @@ struct TopArgs {
     int32_t* ids;                // [batch * rows][n_top]
     float* lse;                  // optional [batch * rows]
     RowPlan plan;
-    float2* part;                // chunks > 1: softmax statistics [batch * rows][chunks]
+    ChunkStat* part;             // chunks > 1: [batch * rows][chunks]
     unsigned long long* keys;    // chunks > 1: the chunks' largest keys [batch * rows][chunks][n_top] (0: none)
 };
 
@@ -343,7 +349,7 @@ struct LossArgs {
     float clip_low, clip_high, kl_coef;
     uint32_t* status;
     RowPlan plan;
-    float2* part;                // chunks > 1: softmax statistics of the columns outside the entries [rows][chunks]
+    ChunkStat* part;             // chunks > 1: of the columns outside the entries [batch * rows][chunks]
     uint2* saved;                // chunks > 1: the entries' logits (bits, 1: it counts) [rows][n_top]
 };
 

@@ -62,6 +62,36 @@ def distill(z, values, ids, t_lse, tau, kl_share, eta, w):
     return w * loss, alpha, w / tau * g, abs(w) / tau * size
 
 
+def distill_undecided(z, values, ids, t_lse, tau, kl_share, eta, w, d):
+    """How far the gradient of each column may move where q and p are closer than rounding decides.  With q off by d
+    relative, sign(q - p) is open wherever |q - p| <= 2 d (p + q).  Each such sign moves by at most 2, so its own column by
+    2 x (1 - lambda) / 2 x q, and the mean by 2 q, hence every column by (1 - lambda) / 2 x q_j x 2 x (the open q's sum)."""
+    z = np.asarray(z, dtype=np.float64)
+    V = z.size
+    keep = valid_entries(ids, V)
+    S = np.asarray(ids)[keep].astype(np.int64)
+    t = np.asarray(values, dtype=np.float64)[keep] / tau
+    c = (float(t_lse) if t_lse is not None else (lse(t) if t.size else -np.inf))
+    y = z / tau
+    L = lse(y)
+    if w == 0 or not np.isfinite(c) or not np.isfinite(L):
+        return np.zeros(V)
+    q = np.exp(y - L)
+    R = np.ones(V, dtype=bool)
+    R[S] = False
+    p = np.exp(t - c)
+    pR = max(0.0, 1.0 - p.sum()) if t_lse is not None and R.any() else 0.0
+    qR = float(np.sum(q[R]))
+    pb, qb = np.append(p, pR), np.append(q[S], qR)
+    open_ = (np.abs(qb - pb) <= 2 * d * (pb + qb)) & (pb + qb > 0)
+    half = 0.5 * (1 - kl_share * np.exp(-eta * float(np.sum(np.minimum(pb, qb)))))
+    move = half * q * 2 * float(np.sum(qb[open_]))
+    move[S] += np.where(open_[:-1], 2 * half * q[S], 0.0)
+    if open_[-1]:
+        move[R] += 2 * half * q[R]
+    return abs(w) / tau * move
+
+
 def policy(z, action, adv, old, ref, tau, lo, hi, beta, w):
     """One row: loss, logp, gradient, sizes."""
     z = np.asarray(z, dtype=np.float64)

@@ -11,7 +11,8 @@ half a step, 2^-24 (f32) or 2^-8 (bf16) relative.  Hence with d = delta(V):
     alpha     d + 2^-24
     loss      |w| d (1 + 2 eta max(KL, TV)) + 2^-24 |loss|: all log q shift alike, by at most d, lambda by eta d
     gradient  each of its terms by 4 d relative (the term's own exponential, the sum, the rest's share, lambda), then
-              half a step of its type
+              half a step of its type; where q and p are
+              closer than d, the sign of TV's gradient is open (logits_ref.distill_undecided)
 and a bf16 logit is exact in f32.
 """
 import os
@@ -153,7 +154,7 @@ def rows_taking_part(B, T, weight, last_row):
     return w
 
 
-def compare(z, w, loss, aux, grad, plain, slack, aux_slack):
+def compare(z, w, loss, aux, grad, plain, slack, aux_slack, undecided=lambda r: 0.0):
     """Device results of all rows against plain(r) -> (loss, aux, gradient, sizes)."""
     B, T, V = z.shape
     d = delta(V)
@@ -165,7 +166,7 @@ def compare(z, w, loss, aux, grad, plain, slack, aux_slack):
         assert abs(L[r] - l) <= abs(w.reshape(-1)[r]) * d * slack(r) + HALF[F32] * abs(l) + 1e-37, (r, L[r], l)
         assert abs(A[r] - a) <= d * aux_slack + HALF[F32] * abs(a), (r, A[r], a)
         if G is not None:
-            off = np.abs(G[r] - g) - (4 * d * slack(r) * size + h * np.abs(g) + 1e-37)
+            off = np.abs(G[r] - g) - (4 * d * slack(r) * size + h * np.abs(g) + undecided(r) + 1e-37)
             assert off.max() <= 0, (r, int(off.argmax()), G[r][off.argmax()], g[off.argmax()])
 
 
@@ -191,7 +192,9 @@ def check_distill(z, k, tau=1.0, kl_share=1.0, eta=0.5, tail=True, weight=None, 
         return 1 + 2 * eta * max(kl, 1.0)
 
     assert R.read_device_status(ws) == status
-    compare(z if grad is not z else zz_like(zz, z), w, o["loss"], o["accept"], o.get("grad"), plain, slack, 1.0)
+    compare(z if grad is not z else zz_like(zz, z), w, o["loss"], o["accept"], o.get("grad"), plain, slack, 1.0,
+            lambda r: ref.distill_undecided(zz[r], vv[r], ii[r], ll[r] if tail else None, tau, kl_share, eta, w.reshape(-1)[r],
+                                            delta(V)))
     return o
 
 
@@ -306,7 +309,10 @@ def test_distill_infinities(shared, monkeypatch):
                 else:
                     # the rest's mass p_R = 1 - sum p is itself a difference of f32 inputs: taken alike on both sides
                     assert abs(L[r] - l) <= delta(V) + HALF[F32] * abs(l) * 2, (r, L[r], l)
-                assert np.all(np.abs(G[r] - g) <= 4 * delta(V) * size + HALF[F32] * np.abs(g) + 1e-37), r
+                # row 4 learns from itself: the signs of TV's gradient are open there
+                move = ref.distill_undecided(f64(z)[0, r], f64(vals)[0, r], ids.cpu().numpy()[0, r],
+                                             f64(lse)[0, r] if tail else None, 1.0, kl, 0.0, 1.0, delta(V))
+                assert np.all(np.abs(G[r] - g) <= 4 * delta(V) * size + HALF[F32] * np.abs(g) + move + 1e-37), r
 
 
 def test_distill_of_a_student_without_the_teachers_token_is_infinite():
@@ -582,8 +588,12 @@ def test_slices_of_longer_arrays():
     o = R.distill_from_logits(z[:, 1:], vals[:, :5], ids[:, :5], R.LogitsWorkspace(3, 5, 4099, 30), teacher_lse=lse[:, :5])
     w = R.distill_from_logits(z[:, 1:].contiguous(), vals[:, :5].contiguous(), ids[:, :5].contiguous(),
                               R.LogitsWorkspace(3, 5, 4099, 30), teacher_lse=lse[:, :5].contiguous())
-    assert torch.equal(o["loss"], w["loss"]) and torch.equal(o["accept"], w["accept"])
-    assert torch.allclose(o["grad"], w["grad"], rtol=1e-5, atol=1e-8)
+    # the rows lie on other 16-byte boundaries, so the sums run in another order: each side is off by delta at most (losses
+    # below 4 and eta 0.5: times 5)
+    d = delta(4099)
+    assert torch.allclose(o["loss"], w["loss"], rtol=2 * HALF[F32], atol=2 * 5 * d)
+    assert torch.allclose(o["accept"], w["accept"], rtol=2 * HALF[F32], atol=2 * d)
+    assert torch.allclose(o["grad"], w["grad"], rtol=8 * 5 * d, atol=8 * 5 * d * float(w["grad"].abs().max()))
 
 
 def test_binding_refusals():
