@@ -719,7 +719,7 @@ static_assert(TOP_MAX == NLD_TOP_MAX, "entries per row");
 // shared by up to SHARED_WGS workgroups per CU in all, and there is room for those whatever the rows, so that a
 // workspace also serves calls of fewer rows, columns and entries; very long rows are shared by as many as they need.
 struct LogitsLayout {
-    RowPlan top, loss;
+    RowPlan top, loss[2];   // without and with gradient
     size_t part, entries, total;
 };
 
@@ -727,9 +727,9 @@ LogitsLayout make_logits_layout(int bf16, int n_rows, int vocab, int n_top) {
     LogitsLayout L{};
     const int cus = device_cus();
     L.top = plan_top(bf16, n_rows, vocab, n_top, cus);
-    L.loss = plan_loss(bf16, n_rows, vocab, cus);
+    for (int g = 0; g < 2; ++g) L.loss[g] = plan_loss(bf16, n_rows, vocab, n_top, g != 0, cus);
     size_t shared = (size_t)SHARED_WGS * cus;
-    for (int chunks : {L.top.chunks, L.loss.chunks})
+    for (int chunks : {L.top.chunks, L.loss[0].chunks, L.loss[1].chunks})
         if (chunks > 1) shared = std::max(shared, (size_t)n_rows * chunks);
     L.part = 256;
     L.entries = align256(L.part + sizeof(ChunkStat) * shared);
@@ -759,7 +759,7 @@ nld_status validate_logits(const nld_logits* z, int n_top, float temperature, vo
     if (!ws) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     *out = make_logits_layout(z->dtype == NLD_BF16, z->batch * z->rows, z->vocab, n_top);
     // a launch holds less than 2^32 threads
-    if ((long long)z->batch * z->rows * std::max(out->top.chunks, out->loss.chunks) > (1 << 21))
+    if ((long long)z->batch * z->rows * std::max({out->top.chunks, out->loss[0].chunks, out->loss[1].chunks}) > (1 << 21))
         return fail(NLD_ERR_SHAPE, "%d rows of %d columns are too many for one call", z->batch * z->rows, z->vocab);
     if (ws_bytes < out->total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, out->total);
     return NLD_OK;
@@ -809,7 +809,7 @@ nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperat
     a.loss = loss;
     a.aux = aux;
     a.status = at<uint32_t>(ws, 0);
-    a.plan = L.loss;
+    a.plan = L.loss[grad != nullptr];
     a.part = at<ChunkStat>(ws, L.part);
     a.saved = at<uint2>(ws, L.entries);
     *out = a;

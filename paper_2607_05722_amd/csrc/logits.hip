@@ -19,6 +19,7 @@
 #include "nld_internal.h"
 
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -778,15 +779,18 @@ __device__ __forceinline__ uint32_t members(const Span<BF>& sp, const uint32_t* 
 
 // One pass over this thread's vectors of a chunk for the statistics of the columns outside the entries, and a second
 // one, through the same object, for their gradient.  The first CAP vectors of each thread stay in registers from the
-// one to the other; the rest of a longer chunk is read again.
-template <bool BF, LossKind KIND, int NT, int CAP>
+// one to the other; the rest of a longer chunk is read again.  STREAM: held vectors, and with CAP 0 all, are loaded past the
+// caches: those are for what is read again (125 us with it, 131 without, for 512 rows of 151936 f32 logits with gradient;
+// 97 and 110 us for 992 rows without).
+template <bool BF, LossKind KIND, int NT, int CAP, bool STREAM>
 struct Columns {
     static constexpr int W = Elem<BF>::W;
     const Span<BF>& sp;
     const uint32_t* bits;
     int action;
     uint32_t mark;   // which held vectors have an entry among their columns
-    uint4 held[CAP > 0 ? CAP : 1];
+    static constexpr int AHEAD = CAP ? (CAP < 8 ? CAP : 8) : 4;   // vectors asked for before the first is worked on
+    uint4 held[CAP ? CAP : AHEAD];   // CAP 0: a ring
     static_assert(CAP <= 32, "a bit per held vector");
     __device__ __forceinline__ Columns(const Span<BF>& s, const uint32_t* b, int act) : sp(s), bits(b), action(act), mark(0u) {
         if constexpr (KIND == LOSS_POLICY) {
@@ -795,13 +799,14 @@ struct Columns {
         }
     }
     // Asks for held vector u, without a branch (a thread's last ones may be the chunk's last vector again), so that a wait
-    // for an earlier load does not wait for this one; past the caches, which are for what is read again (125 us with it, 131
-    // without, for 512 rows of 151936 f32 logits with gradient).  f1 > f0.
-    __device__ __forceinline__ void ask(int u) { held[u] = load_stream((const uint4*)sp.grid + min(sp.f0 + (int)threadIdx.x + u * NT, sp.f1 - 1)); }
+    // for an earlier load does not wait for this one.  f1 > f0.
+    __device__ __forceinline__ void ask(int u) {
+        held[u] = get(min(sp.f0 + (int)threadIdx.x + u * NT, sp.f1 - 1));
+    }
+    __device__ __forceinline__ uint4 get(int i) const { return STREAM ? load_stream((const uint4*)sp.grid + i) : sp.load(i); }
     // The first vectors; `each` asks for the others as it goes, AHEAD ahead: with all of them asked for at once a wavefront is
     // held up until the memory has taken them, about as long as the row takes to come, and starts to work on it after that
     // (4096 rows of 151936 bf16 logits, distillation with gradient: 593 us, and 539 with 8 ahead).
-    static constexpr int AHEAD = CAP < 8 ? CAP : 8;
     __device__ __forceinline__ void fetch() {
         if (sp.f1 <= sp.f0) return;
 #pragma unroll
@@ -813,7 +818,6 @@ struct Columns {
     // register pair per vector, from the one to the other.
     template <bool FIRST, class F>
     __device__ __forceinline__ void each(const F& f) {
-        constexpr int U = CAP > 0 ? 2 : 4;
         if ((int)threadIdx.x < sp.n_edges()) {
             float z[W];
             const int i = sp.edge(threadIdx.x);
@@ -822,7 +826,7 @@ struct Columns {
         }
         int count = sp.f1 - sp.f0 - (int)threadIdx.x;   // vectors from this thread's first on
         asm volatile("" : "+v"(count));
-        if (sp.f1 > sp.f0) {
+        if (CAP > 0 && sp.f1 > sp.f0) {
 #pragma unroll
             for (int u = 0; u < CAP; ++u) {
                 if (FIRST && u + AHEAD < CAP) {
@@ -836,6 +840,25 @@ struct Columns {
                 }
             }
         }
+        if constexpr (CAP == 0) {
+            if (sp.f1 <= sp.f0) return;
+            if (!FIRST) fetch();
+            const int rounds = (sp.f1 - sp.f0 + NT - 1) / NT;
+            for (int u0 = 0; u0 < rounds; u0 += AHEAD)
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int i = sp.f0 + (int)threadIdx.x + (u0 + u) * NT;
+                    if (count > (u0 + u) * NT) {
+                        float z[W];
+                        unpack<BF>(held[u], z);
+                        f(i, z, true, mem(i) != 0u, -1);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    held[u] = get(min(i + AHEAD * NT, sp.f1 - 1));
+                }
+            return;
+        }
+        constexpr int U = 2;
         int i = sp.f0 + (int)threadIdx.x + CAP * NT;
         for (; i + (U - 1) * NT < sp.f1; i += U * NT) {
             uint4 v[U];
@@ -935,8 +958,8 @@ struct GradRow {
 // has read a vector when it writes the same columns, and the entries' logits were read before, so the gradient may
 // take the logits' place.  The few vectors with an entry among their columns are written column by column, after the
 // others: they are read once more for it, which keeps that code out of the unrolled part.
-template <bool BF, LossKind KIND, int NT, int CAP>
-__device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp, Columns<BF, KIND, NT, CAP>& cols, int r,
+template <bool BF, LossKind KIND, int NT, int CAP, bool STREAM>
+__device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp, Columns<BF, KIND, NT, CAP, STREAM>& cols, int r,
                                            const RowGrad& g, bool mine, int col) {
     constexpr int W = Elem<BF>::W;
     const GradRow<BF> out(a, r);
@@ -962,7 +985,7 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp
             if (full && !entry) {
 #pragma unroll
                 for (int e = 0; e < W; ++e) z[e] = value(z[e]);
-                out.template put<(CAP > 0)>(sp, i, z);
+                out.template put<STREAM>(sp, i, z);
             } else if (u < 0) {
 #pragma unroll
                 for (int e = 0; e < W; ++e) z[e] = value(z[e]);
@@ -995,7 +1018,7 @@ __device__ __forceinline__ void empty_row(const LossArgs& a, const Span<BF>& sp,
 // A workgroup takes a whole row and keeps it, or the first CAP * NT vectors of it, in registers from the statistics to
 // the gradient.
 template <bool BF, LossKind KIND, int NT, int CAP>
-__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) loss_row_kernel(LossArgs a) {
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(CAP ? 4 : 8))) loss_row_kernel(LossArgs a) {
     typedef typename Elem<BF>::type T;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared<NT> sh;
@@ -1006,7 +1029,7 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) lo
         empty_row<BF, NT>(a, sp, r, 0);
         return;
     }
-    Columns<BF, KIND, NT, CAP> cols(sp, bits, in.action);
+    Columns<BF, KIND, NT, CAP, true> cols(sp, bits, in.action);
     RowGrad g;
     bool mine = tid == 0;
     if constexpr (KIND == LOSS_DISTILL) {
@@ -1031,12 +1054,12 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) lo
         const RowStat st = cols.stats(a, sh, [] { return 0.f; }, nullptr);
         g = policy_row(a, r, in.rollout, to_float<BF>(raw), st, (double)in.weight);
     }
-    if (a.grad) write_grad<BF, KIND, NT, CAP>(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
+    if (a.grad) write_grad(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
 }
 
 // Few rows are shared by several workgroups.  STEP 1 leaves every chunk's statistics and entries in the workspace, STEP 2
 // takes them together, each workgroup for itself, and writes its chunk of the gradient.
-template <bool BF, LossKind KIND, int STEP>
+template <bool BF, LossKind KIND, int STEP, bool STREAM>
 __global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
     typedef typename Elem<BF>::type T;
     constexpr int NT = LOSS_NT;
@@ -1051,12 +1074,16 @@ __global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
         if (STEP == 2) empty_row<BF, NT>(a, sp, r, chunk);
         return;
     }
-    Columns<BF, KIND, NT, 0> cols(sp, bits, in.action);
+    Columns<BF, KIND, NT, 0, STREAM> cols(sp, bits, in.action);
     T raw = 0;
     bool counts = false, here = false;
     if constexpr (KIND == LOSS_DISTILL) {
         if (STEP == 1 || a.grad) {
             list_entries<BF, NT>(a, in.id, bits, sh);
+            if (STEP == 1) {
+                inputs_here();
+                cols.fetch();
+            }
             counts = mark_entries<BF, NT>(a, sp, in.id, STEP == 1 ? chunk : -1, 0, bits, sh, &raw, &here);
         }
     } else {
@@ -1064,6 +1091,7 @@ __global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
         here = v >= sp.v0 && v < sp.v1;
         counts = true;
         if (STEP == 1 && here) raw = sp.row[in.action];
+        if (STEP == 1) cols.fetch();
     }
     if constexpr (STEP == 1) {
         const RowStat st = cols.stats(a, sh, [] { return 0.f; }, nullptr);
@@ -1087,7 +1115,7 @@ __global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
         } else {
             g = policy_row(a, r, in.rollout, __uint_as_float(a.saved[r].x), st, (double)in.weight);
         }
-        if (a.grad) write_grad<BF, KIND, NT, 0>(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
+        if (a.grad) write_grad(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
     }
 }
 
@@ -1097,13 +1125,27 @@ void launch_loss_as(const LossArgs& a, hipStream_t s) {
     const int n = a.in.batch * a.in.rows;
     const size_t lds = KIND == LOSS_DISTILL ? (size_t)cdiv(a.plan.cv * Elem<BF>::W, 32) * 4 : 0;
     if (a.plan.chunks == 1) {
-        if (a.grad == nullptr) loss_row_kernel<BF, KIND, 512, 0><<<n, 512, lds, s>>>(a);
-        else if (a.plan.cv <= 512 * HELD) loss_row_kernel<BF, KIND, 512, HELD><<<n, 512, lds, s>>>(a);
-        else loss_row_kernel<BF, KIND, 1024, HELD><<<n, 1024, lds, s>>>(a);
+        const int nt = a.plan.threads;
+        if (a.grad) {
+            if (nt == 1024) loss_row_kernel<BF, KIND, 1024, HELD><<<n, 1024, lds, s>>>(a);
+            else if (nt == 512) loss_row_kernel<BF, KIND, 512, HELD><<<n, 512, lds, s>>>(a);
+            else loss_row_kernel<BF, KIND, 256, HELD><<<n, 256, lds, s>>>(a);
+        } else if (nt == 1024) {
+            loss_row_kernel<BF, KIND, 1024, 0><<<n, 1024, lds, s>>>(a);
+        } else if (nt == 512) {
+            loss_row_kernel<BF, KIND, 512, 0><<<n, 512, lds, s>>>(a);
+        } else {
+            loss_row_kernel<BF, KIND, 256, 0><<<n, 256, lds, s>>>(a);
+        }
         return;
     }
-    loss_chunk_kernel<BF, KIND, 1><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
-    loss_chunk_kernel<BF, KIND, 2><<<a.grad ? n * a.plan.chunks : n, LOSS_NT, lds, s>>>(a);
+    if (a.grad) {   // the second step reads what the first left in the caches
+        loss_chunk_kernel<BF, KIND, 1, false><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
+        loss_chunk_kernel<BF, KIND, 2, false><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
+    } else {
+        loss_chunk_kernel<BF, KIND, 1, true><<<n * a.plan.chunks, LOSS_NT, lds, s>>>(a);
+        loss_chunk_kernel<BF, KIND, 2, true><<<n, LOSS_NT, lds, s>>>(a);
+    }
 }
 
 }  // namespace
@@ -1128,13 +1170,40 @@ RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus) {
 
 constexpr int LOSS_MAX_COLS = 1 << 18;   // columns of one workgroup: their membership bits are 32 KB
 
-RowPlan plan_loss(int bf16, int n_rows, int vocab, int cus) {
+static int env_or(const char* name, int v) {
+    const char* e = getenv(name);
+    return e && *e ? atoi(e) : v;
+}
+
+// Rows shared by several workgroups, in two launches, or one each; and the threads of one.  us for n rows of 151936 columns,
+// shared and one each: with gradient f32 1 row 14 and 28, 32 rows 25 and 35, 64 rows 35 and 36, 128 rows 59 and 48, bf16 14.6 and 25,
+// 21 and 28, 27 and 29, 38 and 31; without, f32 1 row 11 and 21, 64 rows 18 and 22, 128 rows 24 and 25, bf16 64 rows 16 and 18,
+// 128 rows 19 and 19; of 16877 columns one each is never slower (1 f32 row with gradient 12 and 14).  Within
+// 2 us of these and of 50257 and 100000 columns, with nv vectors a row, n rows take
+//     with gradient    shared 13.5 + 1e-5 n nv,   one each 8 + 8e-4 nv,
+//     without          shared 11.3 + 2.7e-6 n nv, one each 8.3 + 4e-4 nv     (n of up to half the CUs)
+// Threads: smaller workgroups hide each other's latencies, larger ones hold more of a row.  With gradient, 4096 rows of 4000 bf16
+// columns take 60, 99 and 200 us on 256, 512 and 1024 threads, of 16877 106, 138 and 249, of 50257 214, 209 and 314, 1024 rows of
+// 100000 f32 columns 204 and 157 on 512 and 1024; without, 4096 rows of 50257 bf16 columns 95, 112 and 160, 64 of 151936 f32
+// columns 32, 22 and 23.
+// NLD_LOSS_CHUNKS (1: one each, else: shared) and NLD_LOSS_THREADS (256, 512, 1024) override.
+RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus) {
     const int W = bf16 ? 8 : 4, nv = row_vectors(bf16, vocab);
-    RowPlan p = spread(nv, n_rows, SHARED_WGS * cus, 1024);
+    const double n = (double)n_rows * 256 / cus;
+    bool share = grad ? 5.5 + 1e-5 * n * nv < 8e-4 * nv : 3.0 + 2.7e-6 * n * nv < 4e-4 * nv;
+    const int forced = env_or("NLD_LOSS_CHUNKS", 0);
+    if (forced) share = forced > 1;
+    RowPlan p{1, nv, 0};
+    if (share) p = spread(nv, n_rows, SHARED_WGS * cus, 1024);
     if (p.cv * W > LOSS_MAX_COLS) {
         p.cv = LOSS_MAX_COLS / W;
         p.chunks = cdiv(nv, p.cv);
     }
+    if (grad) p.threads = nv <= 256 * 19 ? 256 : (nv <= 512 * 26 ? 512 : 1024);
+    else p.threads = nv > 2048 && n_rows < 2 * cus ? 512 : 256;
+    p.threads = env_or("NLD_LOSS_THREADS", p.threads);
+    if (p.threads != 256 && p.threads != 1024) p.threads = 512;
+    if (p.threads == 256 && n_top > 256) p.threads = 512;   // a thread per entry
     return p;
 }
 

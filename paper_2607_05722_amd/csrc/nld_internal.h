@@ -298,9 +298,10 @@ struct LogitRows {
 constexpr int TOP_MAX = 512;    // entries per row of the top selection and of a teacher
 constexpr int SHARED_WGS = 2;   // few rows: at most this many workgroups per CU share them
 
-// How a call's rows are spread: `chunks` workgroups share a row, each taking cv 16-byte vectors of it.
+// How a call's rows are spread: `chunks` workgroups share a row, each taking cv 16-byte vectors of it; a workgroup of a
+// whole row has `threads` (the losses).
 struct RowPlan {
-    int chunks, cv;
+    int chunks, cv, threads;
 };
 
 // softmax statistics of a chunk of a row: sum of exp2(z / tau * log2(e) - ref) = s
@@ -402,7 +403,7 @@ hipError_t launch_quad_finish(const FinishArgs& a, hipStream_t s);
 // Most 16-byte vectors a row of this type and length covers, whatever its alignment.
 int row_vectors(int bf16, int vocab);
 RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus);
-RowPlan plan_loss(int bf16, int n_rows, int vocab, int cus);
+RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus);
 hipError_t launch_top(const TopArgs& a, hipStream_t s);
 hipError_t launch_loss(LossKind kind, const LossArgs& a, hipStream_t s);
 
