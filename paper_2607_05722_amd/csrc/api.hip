@@ -718,24 +718,28 @@ static_assert(TOP_MAX == NLD_TOP_MAX, "entries per row");
 // workgroups share, and their largest keys (the top selection) or the entries' logits (the losses).  Few rows are
 // shared by up to SHARED_WGS workgroups per CU in all, and there is room for those whatever the rows, so that a
 // workspace also serves calls of fewer rows, columns and entries; very long rows are shared by as many as they need.
+enum LogitsOp { OP_TOP = 0, OP_LOSS = 1, OP_LOSS_GRAD = 2 };
+
 struct LogitsLayout {
-    RowPlan top, loss[2];   // without and with gradient
+    RowPlan plan;
     size_t part, entries, total;
 };
 
-LogitsLayout make_logits_layout(int bf16, int n_rows, int vocab, int n_top) {
+LogitsLayout make_logits_layout(LogitsOp op, int bf16, int n_rows, int vocab, int n_top) {
     LogitsLayout L{};
     const int cus = device_cus();
-    L.top = plan_top(bf16, n_rows, vocab, n_top, cus);
-    for (int g = 0; g < 2; ++g) L.loss[g] = plan_loss(bf16, n_rows, vocab, n_top, g != 0, cus);
+    L.plan = op == OP_TOP ? plan_top(bf16, n_rows, vocab, n_top, cus) : plan_loss(bf16, n_rows, vocab, n_top, op == OP_LOSS_GRAD, cus);
     size_t shared = (size_t)SHARED_WGS * cus;
-    for (int chunks : {L.top.chunks, L.loss[0].chunks, L.loss[1].chunks})
-        if (chunks > 1) shared = std::max(shared, (size_t)n_rows * chunks);
+    if (L.plan.chunks > 1) shared = std::max(shared, (size_t)n_rows * L.plan.chunks);
     L.part = 256;
     L.entries = align256(L.part + sizeof(ChunkStat) * shared);
-    L.total = align256(L.entries + 8 * shared * n_top);
+    L.total = align256(L.entries + 8 * shared * top_places(n_top));
     return L;
 }
+
+// A launch holds less than 2^32 threads: 2^21 workgroups of up to 1024, and of a long row one takes at most LOSS_MAX_COLS
+// columns.
+bool one_launch(int n_rows, int vocab) { return (long long)n_rows * (vocab / LOSS_MAX_COLS + 2) <= (1 << 21); }
 
 nld_status check_logits(const nld_logits* z, const char* what) {
     if (!z || !z->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
@@ -747,20 +751,20 @@ nld_status check_logits(const nld_logits* z, const char* what) {
     if (z->vocab > NLD_LOGITS_MAX_VOCAB) return fail(NLD_ERR_SHAPE, "%s: vocab (%d) exceeds %d", what, z->vocab, NLD_LOGITS_MAX_VOCAB);
     if ((long long)z->batch * z->rows > MAX_LOGIT_ROWS)
         return fail(NLD_ERR_SHAPE, "%s: %lld rows exceed %d", what, (long long)z->batch * z->rows, MAX_LOGIT_ROWS);
+    if (!one_launch(z->batch * z->rows, z->vocab))
+        return fail(NLD_ERR_SHAPE, "%s: %d rows of %d columns are too many for one call", what, z->batch * z->rows, z->vocab);
     return NLD_OK;
 }
 
-nld_status validate_logits(const nld_logits* z, int n_top, float temperature, void* ws, size_t ws_bytes, LogitsLayout* out) {
+nld_status validate_logits(LogitsOp op, const nld_logits* z, int n_top, float temperature, void* ws, size_t ws_bytes,
+                           LogitsLayout* out) {
     nld_status st = check_logits(z, "logits");
     if (st != NLD_OK) return st;
     if (n_top < 1 || n_top > z->vocab) return fail(NLD_ERR_INVALID_ARG, "n_top must be in [1, vocab] (got %d)", n_top);
     if (n_top > NLD_TOP_MAX) return fail(NLD_ERR_SHAPE, "n_top (%d) exceeds %d", n_top, NLD_TOP_MAX);
     if (!(temperature >= 1e-3f && temperature <= 1e3f)) return fail(NLD_ERR_INVALID_ARG, "temperature must be in [1e-3, 1e3]");
     if (!ws) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
-    *out = make_logits_layout(z->dtype == NLD_BF16, z->batch * z->rows, z->vocab, n_top);
-    // a launch holds less than 2^32 threads
-    if ((long long)z->batch * z->rows * std::max({out->top.chunks, out->loss[0].chunks, out->loss[1].chunks}) > (1 << 21))
-        return fail(NLD_ERR_SHAPE, "%d rows of %d columns are too many for one call", z->batch * z->rows, z->vocab);
+    *out = make_logits_layout(op, z->dtype == NLD_BF16, z->batch * z->rows, z->vocab, n_top);
     if (ws_bytes < out->total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, out->total);
     return NLD_OK;
 }
@@ -809,7 +813,7 @@ nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperat
     a.loss = loss;
     a.aux = aux;
     a.status = at<uint32_t>(ws, 0);
-    a.plan = L.loss[grad != nullptr];
+    a.plan = L.plan;
     a.part = at<ChunkStat>(ws, L.part);
     a.saved = at<uint2>(ws, L.entries);
     *out = a;
@@ -1182,15 +1186,18 @@ nld_status nld_accept_from_logits(const float* logits, const int32_t* draft, int
 
 size_t nld_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab, int32_t n_top) {
     if (batch < 1 || rows < 1 || vocab < 1 || n_top < 1 || n_top > NLD_TOP_MAX || n_top > vocab ||
-        vocab > NLD_LOGITS_MAX_VOCAB || (long long)batch * rows > MAX_LOGIT_ROWS)
+        vocab > NLD_LOGITS_MAX_VOCAB || (long long)batch * rows > MAX_LOGIT_ROWS || !one_launch(batch * rows, vocab))
         return 0;
-    return std::max(make_logits_layout(0, batch * rows, vocab, n_top).total, make_logits_layout(1, batch * rows, vocab, n_top).total);
+    size_t total = 0;
+    for (LogitsOp op : {OP_TOP, OP_LOSS, OP_LOSS_GRAD})
+        for (int bf16 = 0; bf16 < 2; ++bf16) total = std::max(total, make_logits_layout(op, bf16, batch * rows, vocab, n_top).total);
+    return total;
 }
 
 nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float temperature, float* values, int32_t* ids,
                           float* lse, void* workspace, size_t ws_bytes, void* stream) {
     LogitsLayout L;
-    nld_status st = validate_logits(logits, n_top, temperature, workspace, ws_bytes, &L);
+    nld_status st = validate_logits(OP_TOP, logits, n_top, temperature, workspace, ws_bytes, &L);
     if (st != NLD_OK) return st;
     if (!values || !ids) return fail(NLD_ERR_INVALID_ARG, "values or ids is NULL");
     TopArgs a{};
@@ -1201,7 +1208,7 @@ nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float tempera
     a.values = values;
     a.ids = ids;
     a.lse = lse;
-    a.plan = L.top;
+    a.plan = L.plan;
     a.part = at<ChunkStat>(workspace, L.part);
     a.keys = at<unsigned long long>(workspace, L.entries);
     HIP_TRY(launch_top(a, (hipStream_t)stream));
@@ -1214,7 +1221,7 @@ nld_status nld_distill_from_logits(const nld_logits* student, const nld_teacher*
                                    size_t ws_bytes, void* stream) {
     if (!teacher || !teacher->values || !teacher->ids) return fail(NLD_ERR_INVALID_ARG, "teacher, its values or its ids is NULL");
     LogitsLayout L;
-    nld_status st = validate_logits(student, teacher->n_top, temperature, workspace, ws_bytes, &L);
+    nld_status st = validate_logits(grad ? OP_LOSS_GRAD : OP_LOSS, student, teacher->n_top, temperature, workspace, ws_bytes, &L);
     if (st != NLD_OK) return st;
     if (teacher->seq_rows < student->rows) return fail(NLD_ERR_INVALID_ARG, "teacher->seq_rows (%d) < rows (%d)", teacher->seq_rows, student->rows);
     if (!loss) return fail(NLD_ERR_INVALID_ARG, "loss is NULL");
@@ -1239,7 +1246,7 @@ nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* r
                                   const int32_t* last_row, float* loss, float* logp, const nld_logits* grad,
                                   void* workspace, size_t ws_bytes, void* stream) {
     LogitsLayout L;
-    nld_status st = validate_logits(policy, 1, temperature, workspace, ws_bytes, &L);
+    nld_status st = validate_logits(grad ? OP_LOSS_GRAD : OP_LOSS, policy, 1, temperature, workspace, ws_bytes, &L);
     if (st != NLD_OK) return st;
     if (!rollout || !rollout->actions || !rollout->advantage)
         return fail(NLD_ERR_INVALID_ARG, "rollout, its actions or its advantage is NULL");

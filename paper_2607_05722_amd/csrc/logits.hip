@@ -230,57 +230,100 @@ __device__ __forceinline__ unsigned long long key_of(uint32_t ord, int n) {
 }
 constexpr uint32_t ORD_POS_INF = 0xFF800000u, ORD_NEG_INF = 0x007FFFFFu;
 
-constexpr int TOP_NT = 1024;     // threads
 constexpr int TOP_SEGS = 16;     // a thread's vectors are cut into at most this many segments, each with its maximum
 constexpr int TOP_AHEAD = 4;     // vectors requested at once; a segment is a multiple of it
-constexpr int TOP_HITS = 4096;   // segments that may be looked at again
 constexpr int TOP_CAND = 2048;   // candidates that one ranking holds
 
+template <int NT>
 struct TopShared {
-    uint16_t seg[TOP_SEGS][TOP_NT];          // largest key of each thread's segments, its upper half
-    uint16_t hits[TOP_HITS];                 // segments that may hold one of the largest
-    unsigned long long cand[TOP_CAND];
-    uint32_t hist[256];
-    Stat red[2 * TOP_NT / 64];
-    int cnt[2][TOP_NT / 64];
-    int n_hits, n_cand, digit, above;
+    uint16_t seg[TOP_SEGS][NT];          // largest key of each thread's segments, its upper half
+    uint16_t hits[4 * NT];               // segments that may hold one of the largest
+    alignas(16) unsigned long long cand[TOP_CAND];
+    alignas(16) uint32_t hist[256];
+    Stat red[2 * NT / 64];
+    uint32_t lo[NT / 64], hi[NT / 64];
+    int n_hits, n_cand;
 };
 
-// threads with `in`, summed over the workgroup (which: two buffers used in turn, so that one barrier does)
-__device__ __forceinline__ int count_block(bool in, TopShared& sh, int which) {
-    const int n = __popcll(__ballot(in));
-    if ((threadIdx.x & 63) == 0) sh.cnt[which][threadIdx.x >> 6] = n;
-    __syncthreads();
-    int t = 0;
+// The highest of 256 bins from which on there are at least k (hist), in every wavefront alike: *from: the count from it on,
+// *past: from the next one on.  -1: there are not so many.
+__device__ __forceinline__ int bin_from_top(const uint32_t* hist, int k, int* from, int* past) {
+    const int lane = threadIdx.x & 63;
+    const uint4 h = ((const uint4*)hist)[63 - lane];   // lane 0: the last four bins
+    int n[4] = {(int)h.w, (int)h.z, (int)h.y, (int)h.x};
+    n[1] += n[0];
+    n[2] += n[1];
+    n[3] += n[2];
+    int before = n[3];
 #pragma unroll
-    for (int w = 0; w < TOP_NT / 64; ++w) t += sh.cnt[which][w];
-    return t;
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(before, off);
+        before += lane >= off ? o : 0;
+    }
+    before -= n[3];   // in the bins of the lanes below
+    const unsigned long long reach = __ballot(before + n[3] >= k);
+    if (reach == 0ull) return -1;
+    const int l = __ffsll((long long)reach) - 1;
+    int q = 3;
+#pragma unroll
+    for (int i = 2; i >= 0; --i) q = before + n[i] >= k ? i : q;
+    const int here = before + (q == 0 ? n[0] : q == 1 ? n[1] : q == 2 ? n[2] : n[3]);
+    const int prev = before + (q == 0 ? 0 : q == 1 ? n[0] : q == 2 ? n[1] : n[2]);
+    *from = __shfl(here, l);
+    *past = __shfl(prev, l);
+    return 255 - 4 * l - __shfl(q, l);
 }
 
-// A key that at least k threads' maxima reach, and not many more: bisection over the keys.  0 when fewer than k
-// threads have anything.  At least k elements of the row reach it, so the k largest all do.
-__device__ __forceinline__ uint32_t bound_below(uint32_t mine, int k, TopShared& sh) {
-    uint32_t lo = 0u, hi = 0xFFFFFFFFu;   // k threads reach lo
-    int which = 0;
-    while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        const int n = count_block(mine >= mid, sh, which);
-        which ^= 1;
-        if (n >= k) {
-            lo = mid;
-            if (n <= k + (k >> 3) + 4) break;
-        } else {
-            hi = mid - 1;
-        }
+// A key that at least k threads' maxima reach, and not many more: the keys from the least to the largest are cut into 256
+// bins, and the bin of the k-th again while it holds many more than are wanted.  0 when fewer than k threads have
+// anything.  At least k elements of the row reach it, so the k largest all do.
+template <int NT>
+__device__ __forceinline__ uint32_t bound_below(uint32_t mine, int k, TopShared<NT>& sh) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t lo = mine ? mine : 0xFFFFFFFFu, hi = mine;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, off));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, off));
     }
-    return lo;
+    if (lane == 0) {
+        sh.lo[wave] = lo;
+        sh.hi[wave] = hi;
+    }
+    if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0u;
+    __syncthreads();
+    lo = sh.lo[lane & (NT / 64 - 1)];
+    hi = sh.hi[lane & (NT / 64 - 1)];
+#pragma unroll
+    for (int off = NT / 128; off >= 1; off >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, off));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, off));
+    }
+    int above = 0;   // threads beyond hi
+    while (lo <= hi) {
+        const int shift = max(0, 24 - __clz((int)(hi - lo)));
+        if (mine >= lo && mine <= hi) atomicAdd(&sh.hist[(mine - lo) >> shift], 1u);
+        __syncthreads();
+        int from = 0, past = 0;
+        const int bin = bin_from_top(sh.hist, k - above, &from, &past);
+        if (bin < 0) return 0u;
+        const uint32_t bound = lo + ((uint32_t)bin << shift);
+        if (shift == 0 || above + from <= k + (k >> 2) + 8) return bound;
+        above += past;
+        lo = bound;
+        hi = bound + min(hi - bound, (1u << shift) - 1u);
+        __syncthreads();
+        if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0u;
+        __syncthreads();
+    }
+    return 0u;
 }
 
 // The k largest of n distinct keys, whatever their order and ties: radix selection from the top byte down, each byte
 // one pass over the keys.  Leaves them in sh.cand (any order).  For rows whose bound lets too many candidates through
 // (many equal logits, a vocabulary masked down to few tokens, NaN).
-template <class Keys>
-__device__ void select_exact(const Keys& key, int n, int k, TopShared& sh) {
+template <int NT, class Keys>
+__device__ void select_exact(const Keys& key, int n, int k, TopShared<NT>& sh) {
     unsigned long long prefix = 0ull;
     int need = k;
     int shift = 56;
@@ -288,7 +331,7 @@ __device__ void select_exact(const Keys& key, int n, int k, TopShared& sh) {
         __syncthreads();
         if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0u;
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += TOP_NT) {
+        for (int i = threadIdx.x; i < n; i += NT) {
             const unsigned long long x = key(i);
             const bool in = shift == 56 || (x >> (shift + 8)) == prefix;
             const int d = (int)((x >> shift) & 255u);
@@ -301,22 +344,18 @@ __device__ void select_exact(const Keys& key, int n, int k, TopShared& sh) {
             if ((threadIdx.x & 63) == __ffsll((long long)act) - 1) atomicAdd(&sh.hist[d0], (uint32_t)__popcll(same));
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            int above = 0, d = 255;
-            while (d > 0 && above + (int)sh.hist[d] < need) above += (int)sh.hist[d--];
-            sh.digit = d;
-            sh.above = above;
-        }
-        __syncthreads();
-        need -= sh.above;
-        prefix = (prefix << 8) | (unsigned long long)sh.digit;
-        if ((int)sh.hist[sh.digit] == need) break;   // the whole bin belongs to the k largest
+        int from = 0, past = 0;
+        const int digit = max(bin_from_top(sh.hist, need, &from, &past), 0);
+        const int in_bin = (int)sh.hist[digit];
+        need -= past;
+        prefix = (prefix << 8) | (unsigned long long)digit;
+        if (in_bin == need) break;   // the whole bin belongs to the k largest
     }
     const unsigned long long least = prefix << (shift < 0 ? 0 : shift);
     __syncthreads();
     if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += TOP_NT) {
+    for (int i = threadIdx.x; i < n; i += NT) {
         const unsigned long long x = key(i);
         if (x >= least) {
             const int at = atomicAdd(&sh.n_cand, 1);
@@ -326,19 +365,29 @@ __device__ void select_exact(const Keys& key, int n, int k, TopShared& sh) {
     __syncthreads();
 }
 
-// Ranks the candidates (distinct keys) by counting, for each, the larger ones, and hands those of rank < k to
-// `emit(rank, key)`.  Several threads share a candidate where there are few.
-template <class Emit>
-__device__ __forceinline__ void rank_candidates(int n, int k, TopShared& sh, const Emit& emit) {
-    int share = 1;   // threads per candidate, a power of two up to 16
-    while (share < 16 && n * share * 2 <= TOP_NT) share *= 2;
-    for (int c0 = 0; c0 < n; c0 += TOP_NT / share) {
-        const int c = c0 + (int)threadIdx.x / share, part = (int)threadIdx.x & (share - 1);
+// Ranks the n candidates (distinct keys) by counting, for each, the larger ones, and hands those of rank < k to
+// `emit(rank, key)`.  SHARE threads count for a candidate, each AT keys at once; places past the last one are filled up
+// with keys below all.
+template <int NT, class Emit>
+__device__ __forceinline__ void rank_candidates(int n, int k, TopShared<NT>& sh, const Emit& emit) {
+    constexpr int AT = 8, SHARE = 8;
+    static_assert(TOP_CAND % (AT * SHARE) == 0, "room to fill up");
+    const int filled = (n + AT * SHARE - 1) / (AT * SHARE) * (AT * SHARE);
+    if (n + (int)threadIdx.x < filled) sh.cand[n + threadIdx.x] = 0ull;
+    __syncthreads();
+    for (int c0 = 0; c0 < n; c0 += NT / SHARE) {
+        const int c = c0 + (int)threadIdx.x / SHARE, part = (int)threadIdx.x & (SHARE - 1);
         const unsigned long long mine = c < n ? sh.cand[c] : 0ull;
         int rank = 0;
-        if (c < n)
-            for (int j = part; j < n; j += share) rank += sh.cand[j] > mine ? 1 : 0;
-        for (int off = share >> 1; off >= 1; off >>= 1) rank += __shfl_xor(rank, off);
+        for (int j = part; j < filled; j += AT * SHARE) {
+            unsigned long long x[AT];
+#pragma unroll
+            for (int u = 0; u < AT; ++u) x[u] = sh.cand[j + u * SHARE];
+#pragma unroll
+            for (int u = 0; u < AT; ++u) rank += x[u] > mine ? 1 : 0;
+        }
+#pragma unroll
+        for (int off = SHARE >> 1; off >= 1; off >>= 1) rank += __shfl_xor(rank, off);
         if (c < n && part == 0 && rank < k) emit(rank, mine);
     }
 }
@@ -373,13 +422,13 @@ __device__ __forceinline__ float lse_of(RowStat t, uint32_t top) {
 // k-th largest from the threads' maxima; then a second look at the few segments that reach it (about k of some
 // thousands, a few per cent of the row, which the first pass left in L2 or the memory-side cache); then the candidates
 // are ranked.
-template <bool BF>
-__global__ void __launch_bounds__(TOP_NT) top_kernel(TopArgs a) {
+template <bool BF, int NT>
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8))) top_kernel(TopArgs a) {
     constexpr int W = Elem<BF>::W;
-    __shared__ TopShared sh;
+    __shared__ TopShared<NT> sh;
     const int r = blockIdx.x / a.plan.chunks, chunk = blockIdx.x % a.plan.chunks, tid = threadIdx.x;
     const Span<BF> sp(a.in, r, chunk, a.plan.cv);
-    const int nf = sp.f1 - sp.f0, iters = (nf + TOP_NT - 1) / TOP_NT;   // full vectors of the chunk, and of a thread
+    const int nf = sp.f1 - sp.f0, iters = (nf + NT - 1) / NT;   // full vectors of the chunk, and of a thread
     const int len = (iters + TOP_SEGS * TOP_AHEAD - 1) / (TOP_SEGS * TOP_AHEAD) * TOP_AHEAD;   // vectors per segment
     const int segs = len ? (iters + len - 1) / len : 0;
     if (tid == 0) {
@@ -398,25 +447,25 @@ __global__ void __launch_bounds__(TOP_NT) top_kernel(TopArgs a) {
     for (int s = 0; s < segs; ++s) {
         float top = -INFINITY;
         for (int u0 = 0; u0 < len; u0 += TOP_AHEAD) {
-            const int i0 = tid + (s * len + u0) * TOP_NT;   // among the full vectors
+            const int i0 = tid + (s * len + u0) * NT;   // among the full vectors
             uint4 v[TOP_AHEAD];
 #pragma unroll
-            for (int u = 0; u < TOP_AHEAD; ++u) v[u] = sp.load(sp.f0 + min(i0 + u * TOP_NT, nf - 1));
+            for (int u = 0; u < TOP_AHEAD; ++u) v[u] = load_stream((const uint4*)sp.grid + sp.f0 + min(i0 + u * NT, nf - 1));
 #pragma unroll
             for (int u = 0; u < TOP_AHEAD; ++u)
-                if (i0 + u * TOP_NT < nf) {
+                if (i0 + u * NT < nf) {
                     float z[W];
                     unpack<BF>(v[u], z);
                     top = fmaxf(top, stat_add<W>(part, z, a.c));
                     any = true;
                 }
         }
-        sh.seg[s][tid] = tid + s * len * TOP_NT < nf ? (uint16_t)(order_of(top) >> 16) : (uint16_t)0;
+        sh.seg[s][tid] = tid + s * len * NT < nf ? (uint16_t)(order_of(top) >> 16) : (uint16_t)0;
         best_z = fmaxf(best_z, top);
     }
-    const RowStat st = row_stat<TOP_NT>(part, sh.red, a.c, a.c_exact, nullptr, [&]() {
+    const RowStat st = row_stat<NT>(part, sh.red, a.c, a.c_exact, nullptr, [&]() {
         Stat t{-INFINITY, 0.f};
-        for (int i = sp.v0 + tid; i < sp.v1; i += TOP_NT) {
+        for (int i = sp.v0 + tid; i < sp.v1; i += NT) {
             float z[W];
             if (sp.full(i)) unpack<BF>(sp.load(i), z);
             else sp.load_edge(i, z);
@@ -446,19 +495,29 @@ __global__ void __launch_bounds__(TOP_NT) top_kernel(TopArgs a) {
         for (int s = 0; s < segs; ++s)
             if (sh.seg[s][tid] != 0u && sh.seg[s][tid] >= bound >> 16) {
                 const int at = atomicAdd(&sh.n_hits, 1);
-                if (at < TOP_HITS) sh.hits[at] = (uint16_t)(s * TOP_NT + tid);
+                if (at < 4 * NT) sh.hits[at] = (uint16_t)(s * NT + tid);
             }
         __syncthreads();
-        const int items = min(sh.n_hits, TOP_HITS) * len;
-        for (int it = tid; it < items; it += TOP_NT) {
-            const int h = sh.hits[it / len], i = h % TOP_NT + (h / TOP_NT * len + it % len) * TOP_NT;
-            if (i >= nf) continue;
-            float z[W];
-            unpack<BF>(sp.load(sp.f0 + i), z);
-            take(z, sp.f0 + i);
+        const int items = min(sh.n_hits, 4 * NT) * len;
+        for (int it = tid; it < items; it += TOP_AHEAD * NT) {
+            int at[TOP_AHEAD];
+            uint4 v[TOP_AHEAD];
+#pragma unroll
+            for (int u = 0; u < TOP_AHEAD; ++u) {
+                const int x = it + u * NT, h = x < items ? sh.hits[x / len] : 0;
+                at[u] = x < items ? h % NT + (h / NT * len + x % len) * NT : nf;
+                v[u] = sp.load(sp.f0 + min(at[u], nf - 1));
+            }
+#pragma unroll
+            for (int u = 0; u < TOP_AHEAD; ++u)
+                if (at[u] < nf) {
+                    float z[W];
+                    unpack<BF>(v[u], z);
+                    take(z, sp.f0 + at[u]);
+                }
         }
         __syncthreads();
-        exact = sh.n_cand > TOP_CAND || sh.n_hits > TOP_HITS;
+        exact = sh.n_cand > TOP_CAND || sh.n_hits > 4 * NT;
     }
     if (exact) select_exact(RowKeys<BF>{sp, e0}, n, k, sh);
     const int nc = sh.n_cand;
@@ -468,32 +527,47 @@ __global__ void __launch_bounds__(TOP_NT) top_kernel(TopArgs a) {
             if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(key >> 32));
         });
     } else {
-        unsigned long long* out = a.keys + ((long long)r * a.plan.chunks + chunk) * a.n_top;
-        for (int i = k + tid; i < a.n_top; i += TOP_NT) out[i] = 0ull;
-        rank_candidates(nc, k, sh, [&](int rank, unsigned long long key) { out[rank] = key; });
+        // the merge does not mind their order, so that only more candidates than there are places are ranked
+        const int places = top_places(a.n_top);
+        unsigned long long* out = a.keys + ((long long)r * a.plan.chunks + chunk) * places;
+        if (nc <= places) {
+            for (int i = tid; i < places; i += NT) out[i] = i < nc ? sh.cand[i] : 0ull;
+        } else {
+            for (int i = k + tid; i < places; i += NT) out[i] = 0ull;
+            rank_candidates(nc, k, sh, [&](int rank, unsigned long long key) { out[rank] = key; });
+        }
         if (tid == 0) a.part[(long long)r * a.plan.chunks + chunk] = st;
     }
 }
 
-// The chunks' largest keys -> the row's.
-__global__ void __launch_bounds__(TOP_NT) top_merge_kernel(TopArgs a) {
-    __shared__ TopShared sh;
-    const int r = blockIdx.x, tid = threadIdx.x, n = a.plan.chunks * a.n_top;
+// The chunks' largest keys -> the row's.  As many as MERGE_HELD per thread are read once, side by side.
+constexpr int MERGE_HELD = 8;
+__global__ void __launch_bounds__(1024) top_merge_kernel(TopArgs a) {
+    constexpr int NT = 1024;
+    __shared__ TopShared<NT> sh;
+    const int r = blockIdx.x, tid = threadIdx.x, n = a.plan.chunks * top_places(a.n_top);
     const ListKeys key{a.keys + (long long)r * n};
     if (tid == 0) sh.n_cand = 0;
+    unsigned long long held[MERGE_HELD];
     uint32_t best = 0u;
-    for (int i = tid; i < n; i += TOP_NT) best = max(best, (uint32_t)(key(i) >> 32));
-    const uint32_t bound = max(bound_below(best, a.n_top, sh), 1u);   // 0: an empty place of a short chunk
-    __syncthreads();
-    for (int i = tid; i < n; i += TOP_NT) {
-        const unsigned long long x = key(i);
-        if ((uint32_t)(x >> 32) < bound) continue;
+#pragma unroll
+    for (int u = 0; u < MERGE_HELD; ++u) held[u] = tid + u * NT < n ? key(tid + u * NT) : 0ull;
+#pragma unroll
+    for (int u = 0; u < MERGE_HELD; ++u) best = max(best, (uint32_t)(held[u] >> 32));
+    for (int i = tid + MERGE_HELD * NT; i < n; i += NT) best = max(best, (uint32_t)(key(i) >> 32));
+    const RowStat st = merge_chunks(a.part, r, a.plan.chunks);
+    const uint32_t bound = max(bound_below(best, a.n_top, sh), 1u);   // 0: an empty place
+    auto take = [&](unsigned long long x) __attribute__((always_inline)) {
+        if ((uint32_t)(x >> 32) < bound) return;
         const int at = atomicAdd(&sh.n_cand, 1);
         if (at < TOP_CAND) sh.cand[at] = x;
-    }
+    };
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < MERGE_HELD; ++u) take(held[u]);
+    for (int i = tid + MERGE_HELD * NT; i < n; i += NT) take(key(i));
     __syncthreads();
     if (sh.n_cand > TOP_CAND) select_exact(key, n, a.n_top, sh);
-    const RowStat st = merge_chunks(a.part, r, a.plan.chunks);
     rank_candidates(sh.n_cand, a.n_top, sh, [&](int rank, unsigned long long x) {
         emit_top(a, r, rank, x);
         if (rank == 0 && a.lse) a.lse[r] = lse_of(st, (uint32_t)(x >> 32));
@@ -1164,15 +1238,28 @@ static RowPlan spread(int nv, int n_rows, int target, int least) {
     return p;
 }
 
-RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus) {
-    return spread(row_vectors(bf16, vocab), n_rows, SHARED_WGS * cus / 2, std::max(2048, n_top * 16 / (bf16 ? 8 : 4)));
-}
-
-constexpr int LOSS_MAX_COLS = 1 << 18;   // columns of one workgroup: their membership bits are 32 KB
-
 static int env_or(const char* name, int v) {
     const char* e = getenv(name);
     return e && *e ? atoi(e) : v;
+}
+
+// Rows shared by several workgroups, in two launches, or one each.  us for n rows, top 200 of 151936 columns (50 of fewer),
+// shared and one each: f32 151936 columns 1 row 17 and 31, 64 rows 25 and 31, 128 rows 32 and 31, 50257 columns 1 row 13 and 17,
+// 128 rows 19 and 17, 16877 columns 13 and 11; bf16 151936 columns 1 row 17 and 25, 64 rows 23 and 25, 128 rows 27 and 26.
+// Threads of one: as many as keep a segment at TOP_AHEAD vectors, since each of these lies on a line of its own when it is looked
+// at again (4096 bf16 rows of 50257 columns 106 us on 512, 136 on 1024; f32 of 151936 527 and 451).  NLD_TOP_CHUNKS (1: one each,
+// else: shared) and NLD_TOP_THREADS (512, 1024) override.
+RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus) {
+    const int nv = row_vectors(bf16, vocab);
+    const double n = (double)n_rows * 256 / cus;
+    bool share = nv * ((bf16 ? 7e-4 : 5e-4) - 3.7e-6 * n) > 5.0;
+    const int forced = env_or("NLD_TOP_CHUNKS", 0);
+    if (forced) share = forced > 1;
+    RowPlan p{1, nv, 0};
+    if (share) p = spread(nv, n_rows, SHARED_WGS * cus / 2, std::max(2048, n_top * 16 / (bf16 ? 8 : 4)));
+    p.threads = env_or("NLD_TOP_THREADS", p.cv <= 512 * TOP_SEGS * TOP_AHEAD ? 512 : 1024);
+    if (p.threads != 512 || n_top > 256) p.threads = 1024;   // the bound on the n_top-th comes from the threads' maxima
+    return p;
 }
 
 // Rows shared by several workgroups, in two launches, or one each; and the threads of one.  us for n rows of 151936 columns,
@@ -1197,7 +1284,7 @@ RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus
     if (share) p = spread(nv, n_rows, SHARED_WGS * cus, 1024);
     if (p.cv * W > LOSS_MAX_COLS) {
         p.cv = LOSS_MAX_COLS / W;
-        p.chunks = cdiv(nv, p.cv);
+        p.chunks = cdiv(nv, p.cv);   // at most vocab / LOSS_MAX_COLS + 2
     }
     if (grad) p.threads = nv <= 256 * 19 ? 256 : (nv <= 512 * 26 ? 512 : 1024);
     else p.threads = nv > 2048 && n_rows < 2 * cus ? 512 : 256;
@@ -1209,9 +1296,15 @@ RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus
 
 hipError_t launch_top(const TopArgs& a, hipStream_t s) {
     const int n = a.in.batch * a.in.rows;
-    if (a.in.bf16) top_kernel<true><<<n * a.plan.chunks, TOP_NT, 0, s>>>(a);
-    else top_kernel<false><<<n * a.plan.chunks, TOP_NT, 0, s>>>(a);
-    if (a.plan.chunks > 1) top_merge_kernel<<<n, TOP_NT, 0, s>>>(a);
+    const int wgs = n * a.plan.chunks;
+    if (a.plan.threads == 512) {
+        if (a.in.bf16) top_kernel<true, 512><<<wgs, 512, 0, s>>>(a);
+        else top_kernel<false, 512><<<wgs, 512, 0, s>>>(a);
+    } else {
+        if (a.in.bf16) top_kernel<true, 1024><<<wgs, 1024, 0, s>>>(a);
+        else top_kernel<false, 1024><<<wgs, 1024, 0, s>>>(a);
+    }
+    if (a.plan.chunks > 1) top_merge_kernel<<<n, 1024, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -296,6 +296,8 @@ struct LogitRows {
     long long seq_stride, row_stride;
 };
 constexpr int TOP_MAX = 512;    // entries per row of the top selection and of a teacher
+__host__ __device__ constexpr int top_places(int n_top) { return 2 * n_top; }   // keys that a chunk of a row hands on
+constexpr int LOSS_MAX_COLS = 1 << 18;   // columns of one workgroup: their membership bits are 32 KB
 constexpr int SHARED_WGS = 2;   // few rows: at most this many workgroups per CU share them
 
 // How a call's rows are spread: `chunks` workgroups share a row, each taking cv 16-byte vectors of it; a workgroup of a
@@ -320,7 +322,7 @@ struct TopArgs {
     float* lse;                  // optional [batch * rows]
     RowPlan plan;
     ChunkStat* part;             // chunks > 1: [batch * rows][chunks]
-    unsigned long long* keys;    // chunks > 1: the chunks' largest keys [batch * rows][chunks][n_top] (0: none)
+    unsigned long long* keys;    // chunks > 1: the chunks' largest keys [batch * rows][chunks][top_places] (0: none)
 };
 
 enum LossKind { LOSS_DISTILL = 0, LOSS_POLICY = 1 };
