@@ -117,17 +117,58 @@ __device__ __forceinline__ double uniform(double v) {
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
 
+// Reductions over a wavefront by cross-lane moves of the vector unit (an LDS permute takes several times as long, and these
+// stand one after the other at the end of every row): within rows of 16 lanes by shifts of 1, 2, 4 and 8, then lane 15 of
+// a row into the next one and lane 31 into the upper half; lane 63 has the whole.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_move(uint32_t none, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T lane_from(T none, T v) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, lane_move<CTRL, ROWS>(__builtin_bit_cast(uint32_t, none), __builtin_bit_cast(uint32_t, v)));
+    } else {
+        const uint2 n = __builtin_bit_cast(uint2, none), x = __builtin_bit_cast(uint2, v);
+        return __builtin_bit_cast(T, uint2{lane_move<CTRL, ROWS>(n.x, x.x), lane_move<CTRL, ROWS>(n.y, x.y)});
+    }
+}
+template <class T>
+__device__ __forceinline__ T lane63(T v) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    } else {
+        const uint2 x = __builtin_bit_cast(uint2, v);
+        return __builtin_bit_cast(T, uint2{(uint32_t)__builtin_amdgcn_readlane((int)x.x, 63), (uint32_t)__builtin_amdgcn_readlane((int)x.y, 63)});
+    }
+}
+// op over all lanes, in every lane; none: op's neutral value
+template <class T, class Op>
+__device__ __forceinline__ T wave_reduce(T v, T none, const Op& op) {
+    v = op(v, lane_from<0x111, 0xF>(none, v));
+    v = op(v, lane_from<0x112, 0xF>(none, v));
+    v = op(v, lane_from<0x114, 0xF>(none, v));
+    v = op(v, lane_from<0x118, 0xF>(none, v));
+    v = op(v, lane_from<0x142, 0xA>(none, v));
+    v = op(v, lane_from<0x143, 0xC>(none, v));
+    return lane63(v);
+}
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+    return wave_reduce(v, (T)0, [](T a, T b) __attribute__((always_inline)) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+    return wave_reduce(v, -INFINITY, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ double wave_max(double v) {
+    return wave_reduce(v, -(double)INFINITY, [](double a, double b) __attribute__((always_inline)) { return fmax(a, b); });
+}
+
 // ---------------------------------------------------------------- softmax statistics
 struct Stat {
     float m, s;   // reference and sum of exp2(z * c - m)
 };
 constexpr float STAT_EMPTY = -3.0e38f;   // the reference of no logit: finite, so that -inf adds nothing to a sum of it
-__device__ __forceinline__ Stat stat_merge(Stat a, Stat b) {
-    Stat o;
-    o.m = fmaxf(a.m, b.m);
-    o.s = a.s * __builtin_amdgcn_exp2f(a.m - o.m) + b.s * __builtin_amdgcn_exp2f(b.m - o.m);
-    return o;
-}
 // adds N logits and returns the largest of them; NaN, +inf or a product past f32 among them makes the sum NaN
 template <int N>
 __device__ __forceinline__ float stat_add(Stat& t, const float* z, float c) {
@@ -153,35 +194,26 @@ __device__ __forceinline__ Stat wide_merge(Stat a, Stat b, float c) {
 }
 
 // every thread's statistics -> the workgroup's, in every thread, and the same of the maximum *top (optional); red: two
-// times NT / 64 pairs.  WIDE: by wide_merge.
+// times NT / 64 pairs.  WIDE: as wide_merge takes them.
 template <int NT, bool WIDE>
 __device__ __forceinline__ Stat stat_block(Stat t, Stat* red, float c, float* top) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    auto merge = [&](Stat x, Stat y) __attribute__((always_inline)) {
-        if constexpr (WIDE) return wide_merge(x, y, c);
-        else return stat_merge(x, y);
+    // the largest reference first, then every sum is scaled once
+    auto all = [&](Stat x) __attribute__((always_inline)) {
+        const float m = wave_max(x.m), ref = WIDE && m == -INFINITY ? 0.f : m;
+        return Stat{m, wave_sum(x.s * __builtin_amdgcn_exp2f(WIDE ? (x.m - ref) * c : x.m - ref))};
     };
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) t = merge(t, Stat{__shfl_xor(t.m, off), __shfl_xor(t.s, off)});
-    if (top)
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) *top = fmaxf(*top, __shfl_xor(*top, off));
+    t = all(t);
+    if (top) *top = wave_max(*top);
     __syncthreads();
     if (lane == 0) {
         red[wave] = t;
         if (top) red[NT / 64 + wave].m = *top;
     }
     __syncthreads();
-    t = red[lane & (NT / 64 - 1)];
-#pragma unroll
-    for (int off = NT / 128; off >= 1; off >>= 1) t = merge(t, Stat{__shfl_xor(t.m, off), __shfl_xor(t.s, off)});
-    if (top) {
-        float x = red[NT / 64 + (lane & (NT / 64 - 1))].m;
-#pragma unroll
-        for (int off = NT / 128; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
-        *top = uniform(x);
-    }
-    return Stat{uniform(t.m), uniform(t.s)};
+    t = all(lane < NT / 64 ? red[lane] : Stat{WIDE ? -INFINITY : STAT_EMPTY, 0.f});
+    if (top) *top = wave_max(lane < NT / 64 ? red[NT / 64 + lane].m : -INFINITY);
+    return t;
 }
 
 // The statistics of a row or a chunk of it: sum of exp2(z / tau * log2(e) - ref) = s.
@@ -201,15 +233,12 @@ __device__ __forceinline__ RowStat merge_chunks(const ChunkStat* part, int r, in
     double ref = -(double)INFINITY;
     for (int c = lane; c < chunks; c += 64)
         if (p[c].s != 0.f) ref = fmax(ref, p[c].ref);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) ref = fmax(ref, __shfl_xor(ref, off));
+    ref = wave_max(ref);
     if (ref == -(double)INFINITY) ref = 0.0;   // nothing anywhere
     double s = 0.0;
     for (int c = lane; c < chunks; c += 64)
         if (p[c].s != 0.f) s += (double)p[c].s * exp2(p[c].ref - ref);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
-    return RowStat{uniform(ref), uniform((float)s)};
+    return RowStat{ref, uniform((float)wave_sum(s))};
 }
 // log2 of the sum of exp(z / tau)
 __device__ __forceinline__ double stat_log2(RowStat t) { return t.s == 0.f ? -(double)INFINITY : t.ref + log2((double)t.s); }
@@ -281,24 +310,18 @@ template <int NT>
 __device__ __forceinline__ uint32_t bound_below(uint32_t mine, int k, TopShared<NT>& sh) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t lo = mine ? mine : 0xFFFFFFFFu, hi = mine;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, off));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, off));
-    }
+    auto least = [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return min(a, b); };
+    auto most = [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return max(a, b); };
+    lo = wave_reduce(lo, 0xFFFFFFFFu, least);
+    hi = wave_reduce(hi, 0u, most);
     if (lane == 0) {
         sh.lo[wave] = lo;
         sh.hi[wave] = hi;
     }
     if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0u;
     __syncthreads();
-    lo = sh.lo[lane & (NT / 64 - 1)];
-    hi = sh.hi[lane & (NT / 64 - 1)];
-#pragma unroll
-    for (int off = NT / 128; off >= 1; off >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, off));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, off));
-    }
+    lo = wave_reduce(sh.lo[lane & (NT / 64 - 1)], 0xFFFFFFFFu, least);
+    hi = wave_reduce(sh.hi[lane & (NT / 64 - 1)], 0u, most);
     int above = 0;   // threads beyond hi
     while (lo <= hi) {
         const int shift = max(0, 24 - __clz((int)(hi - lo)));
@@ -596,15 +619,9 @@ struct LossShared {
 template <int N, bool MAX, int NT>
 __device__ __forceinline__ void reduce_entries(double* v, int n, LossShared<NT>& sh) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (n + 63) >> 6;
-    if (wave < waves) {
-#pragma unroll 1
-        for (int off = 32; off >= 1; off >>= 1)
+    if (wave < waves)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const double o = __shfl_xor(v[i], off);
-                v[i] = MAX ? fmax(v[i], o) : v[i] + o;
-            }
-    }
+        for (int i = 0; i < N; ++i) v[i] = MAX ? wave_max(v[i]) : wave_sum(v[i]);
     __syncthreads();
     if (lane == 0 && wave < waves)
 #pragma unroll
@@ -697,7 +714,7 @@ __device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, const T
     const double log_total = uniform(log2(total)), rest_y = uniform(stat_log2(st) - ref);
     const double mass = t.entries + t.rest;
     const double kl = (t.plogp - sums[1] - (t.rest > 0.0 ? t.rest * rest_y : 0.0) + mass * log_total) * 0.69314718055994530942;
-    const double alpha = both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest);
+    const double alpha = mass < (double)INFINITY ? both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest) : (double)NAN;
     const double tv = 0.5 * (mass + 1.0) - alpha;
     const double lambda = uniform((double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha));
     const double s_rest = q_rest > t.rest ? 1.0 : (q_rest < t.rest ? -1.0 : 0.0);

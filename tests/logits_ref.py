@@ -52,11 +52,12 @@ def distill(z, values, ids, t_lse, tau, kl_share, eta, w):
     s = np.sign(qb - pb)
     mean, mass = float(np.sum(s * qb)), float(pb.sum())
     g = np.zeros(V)
-    ratio = pR / qb[-1] if pR > 0 else 0.0
-    g[R] = q[R] * (lam * mass + 0.5 * (1 - lam) * (s[-1] - mean) - lam * ratio)
+    # p_R / q_R q_j as p_R times the column's share of the rest, which is there when q_R is too small for a number
+    taken = pR * np.exp(y[R] - lse(y[R])) if pR > 0 and np.isfinite(lqR) else 0.0
+    g[R] = q[R] * (lam * mass + 0.5 * (1 - lam) * (s[-1] - mean)) - lam * taken
     g[S] = q[S] * (lam * mass + 0.5 * (1 - lam) * (s[:-1] - mean)) - lam * p
     size = np.zeros(V)
-    size[R] = q[R] * (1 + ratio)
+    size[R] = q[R] + taken
     size[S] = q[S] + p
     loss = (lam * kl if lam > 0 else 0.0) + (1 - lam) * tv
     return w * loss, alpha, w / tau * g, abs(w) / tau * size

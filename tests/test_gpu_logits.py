@@ -15,8 +15,6 @@ half a step, 2^-24 (f32) or 2^-8 (bf16) relative.  Hence with d = delta(V):
               closer than d, the sign of TV's gradient is open (logits_ref.distill_undecided)
 and a bf16 logit is exact in f32.
 """
-import os
-
 import logits_ref as ref
 import numpy as np
 import pytest
@@ -53,12 +51,27 @@ def place(z, lead=0, pad_row=0, pad_seq=0):
     return view
 
 
+PLANS = ["shared", "256", "512", "1024"]
+
+
+def use_plan(monkeypatch, plan):
+    """Rows shared by several workgroups (two launches), or one workgroup of so many threads each."""
+    monkeypatch.setenv("NLD_LOSS_CHUNKS", "2" if plan == "shared" else "1")
+    monkeypatch.setenv("NLD_LOSS_THREADS", "512" if plan == "shared" else plan)
+
+
 def f64(t):
     return t.detach().double().cpu().numpy()
 
 
 # ------------------------------------------------------------------------------------------ top logits
+def as_f32(x):
+    """The number that a call taking a float gets (1e-3 is not one: 5e-8 off, which exponents near 10^4 show)."""
+    return float(np.float32(x))
+
+
 def check_top(z, k, tau=1.0, ws=None):
+    tau = as_f32(tau)
     B, T, V = z.shape
     ws = ws or R.LogitsWorkspace(B, T, V, k)
     o = R.top_logits(z, k, ws, temperature=tau)
@@ -89,6 +102,16 @@ SIZES = [(1, 1, 1, 1), (1, 2, 7, 7), (2, 3, 1000, 20), (1, 5, 1024, 512), (3, 2,
 @pytest.mark.parametrize("B,T,V,k", SIZES)
 def test_top(B, T, V, k, dtype):
     check_top(place(draw((B, T, V), dtype, V + k)), k, tau=3.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("chunks,threads", [("1", "512"), ("1", "1024"), ("2", "512"), ("2", "1024")])
+@pytest.mark.parametrize("V,k", [(100003, 256), (50021, 33), (400009, 8)])
+def test_top_plans(V, k, chunks, threads, dtype, monkeypatch):
+    """One workgroup a row and several, of either size; 400009 columns: segments longer than one request."""
+    monkeypatch.setenv("NLD_TOP_CHUNKS", chunks)
+    monkeypatch.setenv("NLD_TOP_THREADS", threads)
+    check_top(place(draw((1, 3, V), dtype, V), 1, 1), k)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -123,9 +146,11 @@ def special_rows(V, dtype):
 @pytest.mark.parametrize("V,k", [(3001, 20), (20011, 200), (151936, 512)])
 def test_top_special_rows(V, k, dtype, monkeypatch):
     z = place(special_rows(V, dtype), lead=1)
-    check_top(z, k)                              # rows shared by several workgroups where they are long
-    monkeypatch.setenv("NLD_CUS", "1")           # and by one each
-    check_top(z, k)
+    for chunks in ("1", "2"):                    # one workgroup a row, and several where it is long
+        for threads in ("512", "1024"):
+            monkeypatch.setenv("NLD_TOP_CHUNKS", chunks)
+            monkeypatch.setenv("NLD_TOP_THREADS", threads)
+            check_top(z, k)
 
 
 def test_top_tiny_k_of_equal_rows_is_the_lowest_columns():
@@ -173,6 +198,7 @@ def compare(z, w, loss, aux, grad, plain, slack, aux_slack, undecided=lambda r: 
 def check_distill(z, k, tau=1.0, kl_share=1.0, eta=0.5, tail=True, weight=None, last_row=None, grad=None, want_grad=True,
                   entries=None, ws=None, status=0):
     B, T, V = z.shape
+    tau = as_f32(tau)
     zz = f64(z).reshape(-1, V)
     vals, ids, lse = entries or teacher_of(z, k, tau, V + k)
     ws = ws or R.LogitsWorkspace(B, T, V, k)
@@ -212,24 +238,22 @@ def test_distill(B, T, V, k, dtype):
     check_distill(place(draw((B, T, V), dtype, V)), k, tau=3.0)
 
 
-@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("plan", PLANS)
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("kl_share,eta,tail,tau", [(1.0, 0.0, True, 1.0), (1.0, 0.0, False, 2.0), (0.0, 0.0, True, 1.0),
                                                    (0.4, 2.0, False, 0.7), (1.0, 0.5, True, 3.0)])
-def test_distill_mixtures(kl_share, eta, tail, tau, dtype, shared, monkeypatch):
-    """Rows shared by several workgroups, and rows of one workgroup each."""
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    check_distill(place(draw((2, 3, 9001), dtype, 3), lead=1), 50, tau, kl_share, eta, tail)
+def test_distill_mixtures(kl_share, eta, tail, tau, dtype, plan, monkeypatch):
+    """50021 columns: more than 256 threads hold, two or more chunks where the rows are shared."""
+    use_plan(monkeypatch, plan)
+    check_distill(place(draw((2, 3, 50021), dtype, 3), lead=1), 50, tau, kl_share, eta, tail)
 
 
-@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("plan", PLANS)
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_distill_rows_that_take_no_part(dtype, shared, monkeypatch):
+def test_distill_rows_that_take_no_part(dtype, plan, monkeypatch):
     """Weights (0, negative, absent), last_row, and rows of NaN that have weight 0 or lie past last_row."""
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    B, T, V, k = 3, 4, 9001, 20
+    use_plan(monkeypatch, plan)
+    B, T, V, k = 3, 4, 50021, 20
     z = draw((B, T, V), dtype, 8)
     entries = teacher_of(place(z), k, 1.0, 1)
     weight = torch.tensor([[1.0, 0.0, -2.0, 0.5]] * B, device="cuda")
@@ -242,13 +266,12 @@ def test_distill_rows_that_take_no_part(dtype, shared, monkeypatch):
     assert not o["grad"][1].any() and not o["loss"][1].any() and not o["accept"][1].any()
 
 
-@pytest.mark.parametrize("shared", [True, False])
-def test_distill_entries_that_do_not_count(shared, monkeypatch):
+@pytest.mark.parametrize("plan", PLANS)
+def test_distill_entries_that_do_not_count(plan, monkeypatch):
     """-1 is no entry; ids out of range and repeated ones are left out and reported; no entry at all: with the tail the
     teacher knows nothing but "some token", without it there is no teacher."""
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    V, k = 9001, 70
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 70
     z = place(draw((1, 6, V), F32, 9))
     for row, bad in ((0, None), (1, V), (2, -7), (3, "twice"), (4, "thrice")):
         vals, ids, lse = teacher_of(z, k, 1.0, 2)
@@ -265,13 +288,12 @@ def test_distill_entries_that_do_not_count(shared, monkeypatch):
             check_distill(z, k, entries=(vals, ids, lse), tail=tail, status=0 if bad is None else C.NLD_DEV_BAD_TOKEN)
 
 
-@pytest.mark.parametrize("shared", [True, False])
-def test_distill_infinities(shared, monkeypatch):
+@pytest.mark.parametrize("plan", PLANS)
+def test_distill_infinities(plan, monkeypatch):
     """Masked students and teachers: columns of -inf in the rest and among the entries, rows of nothing else, a rest far
     below the entries, entries far below the rest, every column an entry."""
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    V, k = 5003, 40
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 40
     z = draw((1, 7, V), F32, 10)
     inf = float("inf")
     z[0, 0, ::3] = -inf
@@ -340,23 +362,94 @@ def test_not_a_number_stays_in_its_row(bad, column):
         assert torch.isfinite(x["loss"][0, [0, 2]]).all() and torch.isfinite(x["grad"][0, [0, 2]]).all()
 
 
-@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("where", ["values", "lse"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_not_a_number_of_the_teacher_stays_in_its_row(bad, where):
+    z = place(draw((1, 3, 4001), F32, 4))
+    vals, ids, lse = teacher_of(z, 10, 1.0, 3)
+    if where == "values":
+        vals[0, 1, 4] = bad
+    else:
+        lse[0, 1] = bad if bad != bad else float("-inf")     # no token at all
+    o = R.distill_from_logits(z, vals, ids, R.LogitsWorkspace(1, 3, 4001, 10), teacher_lse=lse)
+    if where == "lse" and bad == bad:
+        assert o["loss"][0, 1] == 0 and o["accept"][0, 1] == 0 and not o["grad"][0, 1].any()
+    else:
+        assert torch.isnan(o["loss"][0, 1]) and torch.isnan(o["accept"][0, 1]) and torch.isnan(o["grad"][0, 1]).all()
+    assert torch.isfinite(o["loss"][0, [0, 2]]).all() and torch.isfinite(o["grad"][0, [0, 2]]).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_gradient_in_place_and_strided(dtype, shared, monkeypatch):
+def test_the_longest_row(dtype):
+    """2^24 columns: top, and both losses with gradient, against 64-bit sums on the device."""
+    V, k = 1 << 24, 100
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.randn((1, 1, V), generator=g, device="cuda").mul_(2.5).to(dtype)
+    d = z[0, 0].double()
+    ws = R.LogitsWorkspace(1, 1, V, k)
+    t = R.top_logits(z, k, ws)
+    v, i = torch.sort(d, descending=True, stable=True)
+    assert torch.equal(t["ids"][0, 0].long(), i[:k]) and torch.equal(t["values"][0, 0].double(), v[:k])
+    L = torch.logsumexp(d, 0)
+    assert abs(t["lse"].item() - L.item()) <= delta(V) + HALF[F32] * L.item()
+    a = i[:1].to(torch.int32).view(1, 1)
+    p = R.policy_from_logits(z, a, torch.ones((1, 1), device="cuda"), ws)
+    q = torch.exp(d - L)
+    want = q.clone()
+    want[i[0]] -= 1.0
+    assert abs(p["logp"].item() - (v[0] - L).item()) <= delta(V) + HALF[F32] * abs((v[0] - L).item())
+    assert bool(((p["grad"][0, 0].double() - want).abs() <= 4 * delta(V) * (q + (want < 0)) + HALF[dtype] * want.abs() + 1e-37).all())
+    # cross-entropy of the same token: the same gradient
+    c = R.distill_from_logits(z, t["values"][..., :1].contiguous(), t["ids"][..., :1].contiguous(), ws, eta=0.0)
+    assert abs(c["loss"].item() + (v[0] - L).item()) <= delta(V) + HALF[F32] * abs((v[0] - L).item())
+    assert bool(((c["grad"][0, 0].double() - want).abs() <= 4 * delta(V) * (q + (want < 0)) + HALF[dtype] * want.abs() + 1e-37).all())
+
+
+def test_very_many_short_rows():
+    """2^20 rows of 5 columns, the most of one call."""
+    R_, V = 1 << 20, 5
+    g = torch.Generator(device="cuda").manual_seed(2)
+    z = torch.randn((1, R_, V), generator=g, device="cuda")
+    ws = R.LogitsWorkspace(1, R_, V, 2)
+    t = R.top_logits(z, 2, ws)
+    v, i = torch.sort(z, dim=-1, descending=True, stable=True)
+    assert torch.equal(t["ids"].long(), i[..., :2]) and torch.equal(t["values"], v[..., :2])
+    lp = torch.log_softmax(z.double(), -1)
+    p = R.policy_from_logits(z, t["ids"][..., 1].contiguous(), torch.ones((1, R_), device="cuda"), ws)
+    want = lp.gather(-1, i[..., 1:2])[..., 0]
+    assert bool(((p["logp"].double() - want).abs() <= delta(V) + HALF[F32] * want.abs()).all())
+    grad = torch.exp(lp)
+    grad.scatter_add_(-1, i[..., 1:2], torch.full((1, R_, 1), -1.0, dtype=torch.float64, device="cuda"))
+    assert bool(((p["grad"].double() - grad).abs() <= 4 * delta(V) * 2 + HALF[F32] * grad.abs()).all())
+    assert R.read_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("tau", [1e-3, 1e3])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_extreme_temperatures(tau, dtype):
+    z = place(draw((1, 4, 3001), dtype, 90))
+    check_top(z, 20, tau=tau)
+    check_distill(z, 20, tau=tau, eta=0.0)
+    check_policy(z, tau=tau, old=False)
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradient_in_place_and_strided(dtype, plan, monkeypatch):
     """The gradient in the logits' place, and into views of other alignment whose surroundings stay as they were."""
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    z = draw((2, 3, 9001), dtype, 21)
+    use_plan(monkeypatch, plan)
+    V = 50021
+    z = draw((2, 3, V), dtype, 21)
     for lead, pr, ps in ((0, 0, 0), (1, 3, 5)):
         zd = place(z, lead, pr, ps)
         check_distill(zd, 30, grad=zd)
     for lead, pr, ps in ((0, 0, 0), (2, 7, 0), (5, 1, 4)):
         out = place(torch.zeros_like(z), lead, pr, ps)
         check_distill(place(z, 1, 2, 3), 30, grad=out)
-        gap = torch.as_strided(out, (2, 3, pr), (out.stride(0), out.stride(1), 1), out.storage_offset() + 9001)
+        gap = torch.as_strided(out, (2, 3, pr), (out.stride(0), out.stride(1), 1), out.storage_offset() + V)
         assert torch.isnan(gap).all()
     # sequences inside the rows: [rows][batch] in memory
-    buf = torch.empty((3, 2, 9001), dtype=dtype, device="cuda").transpose(0, 1)
+    buf = torch.empty((3, 2, V), dtype=dtype, device="cuda").transpose(0, 1)
     check_distill(place(z), 30, grad=buf)
 
 
@@ -388,6 +481,7 @@ def test_offsets_past_32_bits():
 def check_policy(z, seed=0, tau=1.0, lo=0.2, hi=0.3, beta=0.0, old=True, refp=False, weight=None, last_row=None, grad=None,
                  actions=None, status=0):
     B, T, V = z.shape
+    tau = as_f32(tau)
     zz = f64(z).reshape(-1, V)
     rng = np.random.default_rng(seed + V)
     a = rng.integers(0, V, size=(B, T)) if actions is None else np.asarray(actions).reshape(B, T)
@@ -426,13 +520,12 @@ def test_policy(B, T, V, k, dtype):
     check_policy(place(draw((B, T, V), dtype, V + 1)), beta=0.05, refp=True)
 
 
-@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("plan", PLANS)
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("tau,old,refp", [(1.0, False, False), (0.7, True, False), (3.0, False, True), (1.0, True, True)])
-def test_policy_terms(tau, old, refp, dtype, shared, monkeypatch):
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    z = place(draw((2, 40, 9001), dtype, 40), 1, 1, 3)
+def test_policy_terms(tau, old, refp, dtype, plan, monkeypatch):
+    use_plan(monkeypatch, plan)
+    z = place(draw((2, 40, 50021), dtype, 40), 1, 1, 3)
     check_policy(z, tau=tau, old=old, refp=refp, beta=0.1 if refp else 0.0)
     weight = torch.rand((2, 40), device="cuda") - 0.3
     weight[:, ::3] = 0.0
@@ -441,13 +534,12 @@ def test_policy_terms(tau, old, refp, dtype, shared, monkeypatch):
     check_policy(z, tau=tau, old=old, refp=refp, beta=0.1 if refp else 0.0, grad=z)
 
 
-@pytest.mark.parametrize("shared", [True, False])
-def test_policy_actions_that_do_not_count(shared, monkeypatch):
-    if not shared:
-        monkeypatch.setenv("NLD_CUS", "1")
-    z = place(draw((1, 4, 9001), F32, 41))
-    check_policy(z, actions=[-1, 0, 9000, -1])
-    check_policy(z, actions=[5, 9001, 3, 8], status=C.NLD_DEV_BAD_TOKEN)
+@pytest.mark.parametrize("plan", PLANS)
+def test_policy_actions_that_do_not_count(plan, monkeypatch):
+    use_plan(monkeypatch, plan)
+    z = place(draw((1, 4, 20011), F32, 41))
+    check_policy(z, actions=[-1, 0, 20010, -1])
+    check_policy(z, actions=[5, 20011, 3, 8], status=C.NLD_DEV_BAD_TOKEN)
     check_policy(z, actions=[5, -2, 3, 8], status=C.NLD_DEV_BAD_TOKEN)
 
 
@@ -618,14 +710,18 @@ def test_binding_refusals():
             call()
 
 
-@pytest.mark.parametrize("batch", [1, 3])
-def test_drafter_loss_on_the_tiny_model(batch):
-    """The whole run: draft pass, verify pass and commit, the teacher's entries and the loss with its gradient, against
-    the plain version on the two passes' own logits, and against the calls made one by one."""
-    from synth.workloads import LazyWeights, WORKLOADS, prefix_kv, tokens
+@pytest.mark.parametrize("batch,lora", [(1, False), (3, False), (2, True)])
+def test_drafter_loss_on_the_tiny_model(batch, lora):
+    """The whole run: draft pass (with the adapter of the LoRA-enhanced drafter, or without), verify pass and commit, the
+    teacher's entries and the loss with its gradient, against the plain version on the two passes' own logits, and against the
+    calls made one by one."""
+    from synth.workloads import LazyWeights, ModelShape, WORKLOADS, lora_weights, prefix_kv, tokens
     wl = WORKLOADS["tiny"]
     shape, k, n_top = wl.shape, 8, 50
     model = R.DeviceModel(shape, LazyWeights(shape, wl.seed))
+    if lora:
+        lshape = ModelShape(**{**shape.__dict__, "lora_rank": 32, "lora_alpha": 128.0})
+        model = model.with_lora(lshape, lambda l: lora_weights(lshape, wl.seed, l))
     caches = []
     for _ in range(2):
         c = R.DeviceCache(shape, batch, 256)
