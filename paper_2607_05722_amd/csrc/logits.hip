@@ -609,33 +609,49 @@ constexpr int LOSS_NT = TOP_MAX;   // threads: at least one per teacher entry
 template <int NT>
 struct LossShared {
     Stat red[2 * NT / 64];
-    double sum[TOP_MAX / 64][2];
+    double sum[5][TOP_MAX / 64][2];   // the entries' sums, one place for each of a row's reductions
+    double rest;                      // RowGrad's, from the wavefronts that work it out
+    int none;
     int32_t ids[TOP_MAX];
     uint32_t mark[NT];   // per thread: which of its held vectors have an entry among their columns
     int repeated;
 };
 
-// sums (or maxima) of N values over the n threads of the entries, in every thread of the workgroup
-template <int N, bool MAX, int NT>
-__device__ __forceinline__ void reduce_entries(double* v, int n, LossShared<NT>& sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (n + 63) >> 6;
-    if (wave < waves)
+// The values of a row, all in f64, are worked out by the wavefronts that have teacher entries (n_top threads), while the
+// others wait: with all of them at it, each with the row's values, the few vector units would do the same work many times
+// (2.7 us of a row on 16 wavefronts).  A reduction over the entries: post_sums in these wavefronts, meet in all, take_sums in
+// these again.
+template <int NT>
+struct Entries {
+    const int n, waves, wave, lane;
+    LossShared<NT>& sh;
+    __device__ __forceinline__ Entries(int n_top, LossShared<NT>& s)
+        : n(n_top), waves((n_top + 63) >> 6), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), sh(s) {}
+    __device__ __forceinline__ bool here() const { return wave < waves; }
+    template <int N, bool MAX>
+    __device__ __forceinline__ void post(double* v, int slot) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = MAX ? wave_max(v[i]) : wave_sum(v[i]);
-    __syncthreads();
-    if (lane == 0 && wave < waves)
+        if (waves > 1 && lane == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) sh.sum[wave][i] = v[i];
-    __syncthreads();
+            for (int i = 0; i < N; ++i) sh.sum[slot][wave][i] = v[i];
+    }
+    __device__ __forceinline__ void meet() const {
+        if (waves > 1) __syncthreads();
+    }
+    template <int N, bool MAX>
+    __device__ __forceinline__ void take(double* v, int slot) const {
+        if (waves == 1) return;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = sh.sum[0][i];
-#pragma unroll 1   // one at a time: the row may be held in registers meanwhile
-    for (int w = 1; w < waves; ++w)
+        for (int i = 0; i < N; ++i) v[i] = sh.sum[slot][0][i];
+#pragma unroll 1   // one at a time: the row is held in registers meanwhile
+        for (int w = 1; w < waves; ++w)
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = MAX ? fmax(v[i], sh.sum[w][i]) : v[i] + sh.sum[w][i];
+            for (int i = 0; i < N; ++i) v[i] = MAX ? fmax(v[i], sh.sum[slot][w][i]) : v[i] + sh.sum[slot][w][i];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = uniform(v[i]);
-}
+        for (int i = 0; i < N; ++i) v[i] = uniform(v[i]);
+    }
+};
 
 // What a row's gradient needs: a column outside the entries gets its share of the rest, exp2(z / tau * log2(e) - ref) / s,
 // times `rest`; `entry` is what this thread's entry gets.
@@ -656,77 +672,111 @@ struct RowGrad {
 // KL is taken as sum p log p - sum p y + P log(sum of the student's exponentials), y = z / tau, so that all of the teacher's side is
 // done while the row is on its way, and TV as (P + 1) / 2 - alpha.
 
-// The teacher's side: this thread's p, and for the row the sums (base-2 logarithms) over entries and rest.
+// The teacher's side: this thread's p, and for the row the sums (base-2 logarithms) over entries and rest; in the
+// wavefronts with entries, and its first half.
 struct Teacher {
     double p, entries, rest, plogp;
     bool none;   // no token at all
 };
 template <int NT>
-__device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, float t_lse, bool counts, bool whole, LossShared<NT>& sh) {
+__device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, float t_lse, bool counts, LossShared<NT>& sh) {
+    const Entries<NT> en(a.n_top, sh);
     const double none = -(double)INFINITY;
     const double x = counts ? (double)t * a.c_exact : none;
-    double lse;
+    double lse = none;
     if (a.lse) {
         lse = uniform((double)t_lse * 1.44269504088896340736);
     } else {
-        double top[1] = {x};
-        reduce_entries<1, true, NT>(top, a.n_top, sh);
-        double tot[1] = {x == none ? 0.0 : exp2(x - top[0])};
-        reduce_entries<1, false, NT>(tot, a.n_top, sh);
-        lse = uniform(tot[0] == 0.0 ? none : top[0] + log2(tot[0]));
+        double top[1] = {x}, tot[1] = {0.0};
+        if (en.here()) en.template post<1, true>(top, 0);
+        en.meet();
+        if (en.here()) {
+            en.template take<1, true>(top, 0);
+            tot[0] = x == none ? 0.0 : exp2(x - top[0]);
+            en.template post<1, false>(tot, 1);
+        }
+        en.meet();
+        if (en.here()) {
+            en.template take<1, false>(tot, 1);
+            lse = uniform(tot[0] == 0.0 ? none : top[0] + log2(tot[0]));
+        }
     }
-    Teacher o;
-    o.none = lse == none;
-    o.p = x == none ? 0.0 : exp2(x - lse);
-    double sums[2] = {o.p, o.p > 0.0 ? o.p * (x - lse) : 0.0};
-    reduce_entries<2, false, NT>(sums, a.n_top, sh);
+    Teacher o{0.0, 0.0, 0.0, 0.0, lse == none};
+    if (en.here()) {
+        o.p = x == none ? 0.0 : exp2(x - lse);
+        double sums[2] = {o.p, o.p > 0.0 ? o.p * (x - lse) : 0.0};
+        en.template post<2, false>(sums, 2);
+        o.entries = sums[0];
+        o.plogp = sums[1];
+    }
+    return o;
+}
+// and the second half of it, with a barrier between: the statistics have some, and the wavefronts without entries need not
+// wait for one before them.  whole: the entries are every column.
+template <int NT>
+__device__ __forceinline__ void teacher_sums(const LossArgs& a, Teacher& o, bool whole, const Entries<NT>& en) {
+    double sums[2] = {o.entries, o.plogp};
+    en.template take<2, false>(sums, 2);
     o.entries = sums[0];
-    o.rest = a.lse && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;   // whole: the entries are every column
+    o.rest = a.lse && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;
     o.plogp = uniform(sums[1] + (o.rest > 0.0 ? o.rest * log2(o.rest) : 0.0));
     if (!(sums[0] < (double)INFINITY)) o.entries = o.plogp = (double)NAN;
-    return o;
 }
 
 // The rest: every thread with its entry's logit z, the statistics of the columns outside the entries, and the largest
 // logit among the entries.
 template <int NT>
-__device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, const Teacher& t, bool counts, float z, float z_top,
+__device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, Teacher t, bool counts, bool whole, float z, float z_top,
                                                RowStat st, double weight, LossShared<NT>& sh) {
-    RowGrad g{st, 0.0, 0.f, true};
-    const double y_top = uniform((double)z_top * a.c_exact);   // -inf: no entry has a probability
-    const double ref = st.s == 0.f ? (z_top == -INFINITY ? 0.0 : y_top) : uniform(fmax(st.ref, y_top));
-    const double er = st.s == 0.f ? 0.0 : uniform((double)st.s * exp2(st.ref - ref));
-    const double y = (double)z * a.c_exact - ref, ey = counts ? exp2(y) : 0.0;
-    double sums[2] = {ey, t.p > 0.0 ? t.p * y : 0.0};
-    reduce_entries<2, false, NT>(sums, a.n_top, sh);
-    const double total = er + sums[0];
-    if (t.none || total == 0.0) {   // a teacher or a student without any token: nothing to learn
+    const Entries<NT> en(a.n_top, sh);
+    double ref = 0.0, er = 0.0, ey = 0.0, q = 0.0, q_rest = 0.0, sgn = 0.0, total = 0.0;
+    double sums[2] = {0.0, 0.0}, both[2] = {0.0, 0.0};
+    if (en.here()) {
+        teacher_sums<NT>(a, t, whole, en);
+        const double y_top = uniform((double)z_top * a.c_exact);   // -inf: no entry has a probability
+        ref = st.s == 0.f ? (z_top == -INFINITY ? 0.0 : y_top) : uniform(fmax(st.ref, y_top));
+        er = st.s == 0.f ? 0.0 : uniform((double)st.s * exp2(st.ref - ref));
+        const double y = (double)z * a.c_exact - ref;
+        ey = counts ? exp2(y) : 0.0;
+        sums[0] = ey;
+        sums[1] = t.p > 0.0 ? t.p * y : 0.0;
+        en.template post<2, false>(sums, 3);
+    }
+    en.meet();
+    if (en.here()) {
+        en.template take<2, false>(sums, 3);
+        total = er + sums[0];
+        const double inv = uniform(1.0 / total);
+        q = ey * inv;
+        q_rest = uniform(er * inv);
+        sgn = q > t.p ? 1.0 : (q < t.p ? -1.0 : 0.0);
+        both[0] = q == q && t.p == t.p ? fmin(t.p, q) : q + t.p;
+        both[1] = sgn * q;
+        en.template post<2, false>(both, 4);
+    }
+    en.meet();
+    float entry = 0.f;
+    if (en.here()) {
+        en.template take<2, false>(both, 4);
+        const bool none = t.none || total == 0.0;   // a teacher or a student without any token: nothing to learn
+        const double log_total = uniform(log2(total)), rest_y = uniform(stat_log2(st) - ref);
+        const double mass = t.entries + t.rest;
+        const double kl = (t.plogp - sums[1] - (t.rest > 0.0 ? t.rest * rest_y : 0.0) + mass * log_total) * 0.69314718055994530942;
+        const double alpha = mass < (double)INFINITY ? both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest) : (double)NAN;
+        const double tv = 0.5 * (mass + 1.0) - alpha;
+        const double lambda = uniform((double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha));
+        const double s_rest = q_rest > t.rest ? 1.0 : (q_rest < t.rest ? -1.0 : 0.0);
+        const double mean = both[1] + s_rest * q_rest, half = 0.5 * (1.0 - lambda), f = weight * a.inv_tau;
+        entry = (float)(f * (q * (lambda * mass + half * (sgn - mean)) - lambda * t.p));
         if (threadIdx.x == 0) {
-            a.loss[r] = 0.f;
-            if (a.aux) a.aux[r] = 0.f;
+            a.loss[r] = none ? 0.f : (float)(weight * ((lambda > 0.0 ? lambda * kl : 0.0) + (1.0 - lambda) * tv));
+            if (a.aux) a.aux[r] = none ? 0.f : (float)alpha;
+            sh.rest = f * (q_rest * (lambda * mass + half * (s_rest - mean)) - lambda * t.rest);
+            sh.none = none;
         }
-        return g;
     }
-    const double inv = uniform(1.0 / total), q = ey * inv, q_rest = uniform(er * inv);
-    const double sgn = q > t.p ? 1.0 : (q < t.p ? -1.0 : 0.0);
-    double both[2] = {q == q && t.p == t.p ? fmin(t.p, q) : q + t.p, sgn * q};
-    reduce_entries<2, false, NT>(both, a.n_top, sh);
-    const double log_total = uniform(log2(total)), rest_y = uniform(stat_log2(st) - ref);
-    const double mass = t.entries + t.rest;
-    const double kl = (t.plogp - sums[1] - (t.rest > 0.0 ? t.rest * rest_y : 0.0) + mass * log_total) * 0.69314718055994530942;
-    const double alpha = mass < (double)INFINITY ? both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest) : (double)NAN;
-    const double tv = 0.5 * (mass + 1.0) - alpha;
-    const double lambda = uniform((double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha));
-    const double s_rest = q_rest > t.rest ? 1.0 : (q_rest < t.rest ? -1.0 : 0.0);
-    const double mean = both[1] + s_rest * q_rest, half = 0.5 * (1.0 - lambda), f = weight * a.inv_tau;
-    if (threadIdx.x == 0) {
-        a.loss[r] = (float)(weight * ((lambda > 0.0 ? lambda * kl : 0.0) + (1.0 - lambda) * tv));
-        if (a.aux) a.aux[r] = (float)alpha;
-    }
-    g.none = false;
-    g.entry = (float)(f * (q * (lambda * mass + half * (sgn - mean)) - lambda * t.p));
-    g.rest = uniform(f * (q_rest * (lambda * mass + half * (s_rest - mean)) - lambda * t.rest));
-    return g;
+    __syncthreads();
+    return RowGrad{st, uniform(sh.rest), entry, sh.none != 0};
 }
 
 // Clipped policy loss of the action's log-probability.  rho = exp(logp - old),
@@ -736,40 +786,39 @@ __device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, const T
 struct Rollout {
     float advantage, old_logp, ref_logp;
 };
-__device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, const Rollout& in, float z, RowStat st, double weight) {
-    RowGrad g{st, 0.0, 0.f, true};
-    const double y = (double)z * a.c_exact, log_rest = stat_log2(st);
-    const double ref = fmax(log_rest, y);
-    if (ref == -(double)INFINITY && st.s == 0.f && z == z) {   // no token is possible
-        if (threadIdx.x == 0) {
-            a.loss[r] = 0.f;
-            if (a.aux) a.aux[r] = 0.f;
+template <int NT>
+__device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, const Rollout& in, float z, RowStat st, double weight,
+                                              LossShared<NT>& sh) {
+    float entry = 0.f;
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == 0) {   // one wavefront, as above
+        const double y = (double)z * a.c_exact, log_rest = stat_log2(st);
+        const double ref = fmax(log_rest, y);
+        const bool none = ref == -(double)INFINITY && st.s == 0.f && z == z;   // no token is possible
+        const double er = exp2(log_rest - ref), ey = exp2(y - ref), all = er + ey;
+        // log(ey / all), by the rest's share where that is the small part
+        const double logp = y >= log_rest ? -log1p(er / ey) : (y - ref) * 0.69314718055994530942 - log(all);
+        const double adv = in.advantage;
+        const double rho = a.old_logp ? exp(logp - (double)in.old_logp) : (logp == logp ? 1.0 : logp);
+        const double free_ = adv == 0.0 ? 0.0 : rho * adv;
+        const double held = fmin(fmax(rho, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
+        double loss = free_ <= held ? -free_ : (free_ > held ? -held : (double)NAN);
+        double dl = free_ <= held ? -free_ : (free_ > held ? 0.0 : (double)NAN);
+        if (a.ref_logp) {
+            const double d = (double)in.ref_logp - logp, beta = a.kl_coef, e = expm1(d);
+            loss += beta * (e - d);
+            dl -= beta * e;
         }
-        return g;
+        const double f = weight * a.inv_tau * dl;
+        entry = (float)(f * (er / all));
+        if (threadIdx.x == 0) {
+            a.loss[r] = none ? 0.f : (float)(weight * loss);
+            if (a.aux) a.aux[r] = none ? 0.f : (float)logp;
+            sh.rest = -f * (er / all);
+            sh.none = none || f == 0.0;   // 0: clipped
+        }
     }
-    const double er = exp2(log_rest - ref), ey = exp2(y - ref), all = er + ey;
-    // log(ey / all), by the rest's share where that is the small part
-    const double logp = y >= log_rest ? -log1p(er / ey) : (y - ref) * 0.69314718055994530942 - log(all);
-    const double adv = in.advantage;
-    const double rho = a.old_logp ? exp(logp - (double)in.old_logp) : (logp == logp ? 1.0 : logp);
-    const double free_ = adv == 0.0 ? 0.0 : rho * adv;
-    const double held = fmin(fmax(rho, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
-    double loss = free_ <= held ? -free_ : (free_ > held ? -held : (double)NAN);
-    double dl = free_ <= held ? -free_ : (free_ > held ? 0.0 : (double)NAN);
-    if (a.ref_logp) {
-        const double d = (double)in.ref_logp - logp, beta = a.kl_coef;
-        loss += beta * (expm1(d) - d);
-        dl -= beta * expm1(d);
-    }
-    if (threadIdx.x == 0) {
-        a.loss[r] = (float)(weight * loss);
-        if (a.aux) a.aux[r] = (float)logp;
-    }
-    const double f = weight * a.inv_tau * dl;
-    g.none = f == 0.0;   // clipped
-    g.entry = (float)(f * (er / all));
-    g.rest = -f * (er / all);
-    return g;
+    __syncthreads();
+    return RowGrad{st, uniform(sh.rest), entry, sh.none != 0};
 }
 
 // What a row's loss needs besides its logits, requested at once: the loads of the logits follow them, and what was
@@ -1132,18 +1181,18 @@ __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(CAP ? 4
         const bool counts = mark_entries<BF, NT>(a, sp, in.id, 0, CAP, bits, sh, &raw, &here);
         cols.mark = sh.mark[tid];
         const bool whole = __syncthreads_count(counts) == sp.n;
-        const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, whole, sh);
+        const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, sh);
         __builtin_amdgcn_sched_barrier(0);
         // (z as stored is looked at after the row's vectors, which were asked for before it)
         float z = -INFINITY, z_top;
         const RowStat st = cols.stats(a, sh, [&]() __attribute__((always_inline)) { return z = counts ? to_float<BF>(raw) : -INFINITY; }, &z_top);
-        g = distill_row<NT>(a, r, te, counts, z, z_top, st, (double)in.weight, sh);
+        g = distill_row<NT>(a, r, te, counts, whole, z, z_top, st, (double)in.weight, sh);
         mine = counts;
     } else {
         const T raw = sp.row[in.action];
         cols.fetch();
         const RowStat st = cols.stats(a, sh, [] { return 0.f; }, nullptr);
-        g = policy_row(a, r, in.rollout, to_float<BF>(raw), st, (double)in.weight);
+        g = policy_row(a, r, in.rollout, to_float<BF>(raw), st, (double)in.weight, sh);
     }
     if (a.grad) write_grad(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
 }
@@ -1197,14 +1246,14 @@ __global__ void __launch_bounds__(LOSS_NT) loss_chunk_kernel(LossArgs a) {
             const uint2 e = tid < a.n_top ? a.saved[(long long)r * a.n_top + tid] : uint2{0u, 0u};
             counts = e.y != 0u;
             const bool whole = __syncthreads_count(counts) == sp.n;
-            const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, whole, sh);
+            const Teacher te = teacher_side<NT>(a, in.t, in.t_lse, counts, sh);
             const float z = counts ? __uint_as_float(e.x) : -INFINITY;
             float z_top = z;
             stat_block<NT, false>(Stat{STAT_EMPTY, 0.f}, sh.red, a.c, &z_top);
-            g = distill_row<NT>(a, r, te, counts, z, z_top, st, (double)in.weight, sh);
+            g = distill_row<NT>(a, r, te, counts, whole, z, z_top, st, (double)in.weight, sh);
             mine = here && counts;
         } else {
-            g = policy_row(a, r, in.rollout, __uint_as_float(a.saved[r].x), st, (double)in.weight);
+            g = policy_row(a, r, in.rollout, __uint_as_float(a.saved[r].x), st, (double)in.weight, sh);
         }
         if (a.grad) write_grad(a, sp, cols, r, g, mine, KIND == LOSS_POLICY ? in.action : mine ? sh.ids[tid] : -1);
     }
