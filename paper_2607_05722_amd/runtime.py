@@ -449,15 +449,18 @@ def _out(outs, name: str, shape, dtype, device):
 def _entries(values, ids, lse, shape, device) -> C.Teacher:
     """Descriptor of a teacher's entries [batch][rows][n_top]; a leading slice [:, :rows] of longer arrays will do."""
     B, T = shape
-    for t, dt, nd in ((values, torch.float32, 3), (ids, torch.int32, 3), (lse, torch.float32, 2)):
-        if t is not None and (t.dim() != nd or t.shape[0] != B or t.shape[1] != T or t.dtype != dt or t.device != device):
-            raise ValueError("teacher: values f32 and ids int32 [batch][rows][n_top] and lse f32 [batch][rows] on %s" % device)
-    n = values.shape[2]
-    if ids.shape[2] != n or n < 1:
-        raise ValueError("teacher: values and ids must have the same entries, at least one")
+    n = values.shape[-1]
+    full = (B, T, n)
+    if values.shape != full or ids.shape != full or (lse is not None and lse.shape != shape) or n < 1:
+        raise ValueError("teacher: values and ids must be [batch][rows][n_top] and lse [batch][rows] for the logits' rows")
+    if values.dtype != torch.float32 or ids.dtype != torch.int32 or values.device != device or ids.device != device or \
+            (lse is not None and (lse.dtype != torch.float32 or lse.device != device)):
+        raise ValueError("teacher: values must be float32, ids int32 and lse float32, on %s" % device)
 
     def seq_rows(t, width):
         # rows from a sequence to the next, where the rows of one lie one behind the other
+        if t.is_contiguous():
+            return T
         st = t.stride()
         ok = (width == 1 or t.dim() == 2 or st[2] == 1) and (T == 1 or st[1] == width)
         if B == 1:
