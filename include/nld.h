@@ -395,6 +395,8 @@ typedef struct {
  * entries and R every other column taken as one event,
  *   p_i = exp(t_i / temperature - lse), p_R = max(0, 1 - sum p_i)  (lse NULL: over S
  *         alone, p_R = 0),    q_i as above, q_R = sum of q over R,
+ *         (p_R of at most what rounding lse to f32 can leave, 2^-22 + 2^-24 |lse|, is 0
+ *         where q_R is 0: teacher and student masked down to the same tokens),
  *   KL = sum p log(p / q), TV = 1/2 sum |p - q|, alpha = sum min(p, q), each over S and R,
  *   lambda = kl_share * exp(-eta * alpha), held constant in the gradient,
  *   loss = weight * (lambda * KL + (1 - lambda) * TV).
@@ -403,12 +405,13 @@ typedef struct {
  * weight (optional, 1) f32 [batch][rows]; last_row (optional) int32 [batch]: rows past
  * last_row[b] take no part (accept_len of nld_verify_accept: the accepted drafts and
  * the first rejected one).  A row of weight 0 or past last_row is not read; it, and a
- * row whose teacher or student has no token at all, has loss 0 and gradient 0.
+ * row whose teacher or student has no token at all, has loss 0 and gradient 0.  A
+ * teacher's lse of at most -2^24 is that of a row masked throughout, so of no token.
  * loss f32 [batch][rows]; accept (optional) f32 [batch][rows] = alpha, the chance that
  * speculative sampling would accept the student's token.  grad (optional): the
  * gradient of the sum of loss by the logits, in the logits' dtype and sizes; it may be
- * the logits' own buffer with the same strides, else it must not overlap it, and its
- * rows must not overlap each other.
+ * the logits' own buffer with the same strides, else the two ranges of addresses
+ * must be apart; its rows must not overlap each other.
  * An id outside [-1, vocab), or one that an earlier entry of the row has, is left out
  * and sets NLD_DEV_BAD_TOKEN.  A NaN or +inf that takes part makes loss, accept and
  * gradient of its row NaN.
@@ -431,7 +434,7 @@ typedef struct {
  * exp(logp - old_logp),
  *   loss = weight * (-min(rho * A, clip(rho, 1 - clip_low, 1 + clip_high) * A)
  *                    + kl_coef * (exp(d) - d - 1)),   d = ref_logp - logp
- * (the KL term only with ref_logp).  weight, last_row, loss and grad as above;
+ * (the KL term only with ref_logp and kl_coef > 0; +inf for an action of probability 0).  weight, last_row, loss and grad as above;
  * logp (optional) f32 [batch][rows], 0 for rows that take no part.  An action outside
  * [-1, vocab) takes no part and sets NLD_DEV_BAD_TOKEN.
  * Errors: as nld_top_logits, INVALID_ARG for a clip_low outside [0, 1], a clip_high or kl_coef < 0

@@ -117,6 +117,13 @@ __device__ __forceinline__ double uniform(double v) {
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
 
+// z / tau * log2(e), rounded: equal logits of any size have a difference of 0, which a product fused into the difference
+// would not give (rows of the type's lowest value)
+__device__ __forceinline__ double base2(float z, double c_exact) {
+#pragma clang fp contract(off)
+    return (double)z * c_exact;
+}
+
 // Reductions over a wavefront by cross-lane moves of the vector unit (an LDS permute takes several times as long, and these
 // stand one after the other at the end of every row): within rows of 16 lanes by shifts of 1, 2, 4 and 8, then lane 15 of
 // a row into the next one and lane 31 into the upper half; lane 63 has the whole.
@@ -218,13 +225,15 @@ __device__ __forceinline__ Stat stat_block(Stat t, Stat* red, float c, float* to
 
 // The statistics of a row or a chunk of it: sum of exp2(z / tau * log2(e) - ref) = s.
 typedef ChunkStat RowStat;
-// From every thread's share; `again` takes the thread's logits once more, by wide_merge of Stat{z, 1}.
+constexpr float WIDE_FROM = 1e8f;
+// From every thread's share; `again` takes the thread's logits once more, by wide_merge of Stat{z, 1}, where products with c
+// do not fit f32 or are so large that their rounding costs many binary orders.
 template <int NT, class Again>
 __device__ __forceinline__ RowStat row_stat(Stat t, Stat* red, float c, double c_exact, float* top, const Again& again) {
     t = stat_block<NT, false>(t, red, c, top);
-    if (t.s > 0.f && t.s < INFINITY) return RowStat{uniform((double)t.m * (c_exact / (double)c)), t.s};
+    if (t.s > 0.f && t.s < INFINITY && fabsf(t.m) < WIDE_FROM) return RowStat{uniform((double)t.m * (c_exact / (double)c)), t.s};
     t = stat_block<NT, true>(again(), red, c, nullptr);
-    return RowStat{t.m == -INFINITY ? 0.0 : uniform((double)t.m * c_exact), t.s};
+    return RowStat{t.m == -INFINITY ? 0.0 : uniform(base2(t.m, c_exact)), t.s};
 }
 // all chunks of row r, in every thread: a lane takes every 64th chunk, then the wavefront's lanes are added in a tree
 __device__ __forceinline__ RowStat merge_chunks(const ChunkStat* part, int r, int chunks) {
@@ -602,7 +611,8 @@ __global__ void __launch_bounds__(1024) top_merge_kernel(TopArgs a) {
 //   statistics   (m, s) over the rest, the entries apart, so that neither a rest that has next to nothing nor an entry
 //                that has next to all loses its digits in a difference from the row's sum;
 //   row values   in f64 from the entries' logits and (m, s): the loss, and the coefficients of the gradient, which is
-//                rest * exp2((z_j - m) * c) for every column outside the entries and a value of its own for each entry;
+//                the column's share of the rest times one number for every column outside the entries, and a value of its
+//                own for each entry;
 //   gradient     one more pass over the row.
 constexpr int LOSS_NT = TOP_MAX;   // threads: at least one per teacher entry
 
@@ -675,17 +685,21 @@ struct RowGrad {
 // The teacher's side: this thread's p, and for the row the sums (base-2 logarithms) over entries and rest; in the
 // wavefronts with entries, and its first half.
 struct Teacher {
-    double p, entries, rest, plogp;
-    bool none;   // no token at all
+    double p, entries, rest, plogp;   // plogp: without the rest's
+    double slack;   // what the rounding of an f32 log-sum-exp can leave of 1 - sum p
+    bool none;      // no token at all
 };
+// A log-sum-exp at or below it is that of a row masked throughout by a finite value: rounded to f32 by 1 and more, it says
+// nothing of the entries, and counts as -inf.
+constexpr float NO_LSE = -(float)(1 << 24);
 template <int NT>
 __device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, float t_lse, bool counts, LossShared<NT>& sh) {
     const Entries<NT> en(a.n_top, sh);
     const double none = -(double)INFINITY;
-    const double x = counts ? (double)t * a.c_exact : none;
-    double lse = none;
+    const double x = counts ? base2(t, a.c_exact) : none;
+    double lse = none, more = 0.0;   // the log-sum-exp in two parts: beside a large one the other would be lost
     if (a.lse) {
-        lse = uniform((double)t_lse * 1.44269504088896340736);
+        lse = t_lse <= NO_LSE ? none : uniform((double)t_lse * 1.44269504088896340736);
     } else {
         double top[1] = {x}, tot[1] = {0.0};
         if (en.here()) en.template post<1, true>(top, 0);
@@ -698,13 +712,15 @@ __device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, floa
         en.meet();
         if (en.here()) {
             en.template take<1, false>(tot, 1);
-            lse = uniform(tot[0] == 0.0 ? none : top[0] + log2(tot[0]));
+            lse = tot[0] == 0.0 ? none : top[0];
+            more = uniform(log2(tot[0]));
         }
     }
-    Teacher o{0.0, 0.0, 0.0, 0.0, lse == none};
+    Teacher o{0.0, 0.0, 0.0, 0.0, fabs(lse) * (0.69314718055994530942 / (1 << 24)) + 1.0 / (1 << 22), lse == none};
     if (en.here()) {
-        o.p = x == none ? 0.0 : exp2(x - lse);
-        double sums[2] = {o.p, o.p > 0.0 ? o.p * (x - lse) : 0.0};
+        const double log_p = x - lse - more;
+        o.p = x == none ? 0.0 : exp2(log_p);
+        double sums[2] = {o.p, o.p > 0.0 ? o.p * log_p : 0.0};
         en.template post<2, false>(sums, 2);
         o.entries = sums[0];
         o.plogp = sums[1];
@@ -719,7 +735,7 @@ __device__ __forceinline__ void teacher_sums(const LossArgs& a, Teacher& o, bool
     en.template take<2, false>(sums, 2);
     o.entries = sums[0];
     o.rest = a.lse && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;
-    o.plogp = uniform(sums[1] + (o.rest > 0.0 ? o.rest * log2(o.rest) : 0.0));
+    o.plogp = sums[1];
     if (!(sums[0] < (double)INFINITY)) o.entries = o.plogp = (double)NAN;
 }
 
@@ -733,10 +749,10 @@ __device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, Teacher
     double sums[2] = {0.0, 0.0}, both[2] = {0.0, 0.0};
     if (en.here()) {
         teacher_sums<NT>(a, t, whole, en);
-        const double y_top = uniform((double)z_top * a.c_exact);   // -inf: no entry has a probability
+        const double y_top = uniform(base2(z_top, a.c_exact));   // -inf: no entry has a probability
         ref = st.s == 0.f ? (z_top == -INFINITY ? 0.0 : y_top) : uniform(fmax(st.ref, y_top));
         er = st.s == 0.f ? 0.0 : uniform((double)st.s * exp2(st.ref - ref));
-        const double y = (double)z * a.c_exact - ref;
+        const double y = base2(z, a.c_exact) - ref;
         ey = counts ? exp2(y) : 0.0;
         sums[0] = ey;
         sums[1] = t.p > 0.0 ? t.p * y : 0.0;
@@ -759,9 +775,11 @@ __device__ __forceinline__ RowGrad distill_row(const LossArgs& a, int r, Teacher
     if (en.here()) {
         en.template take<2, false>(both, 4);
         const bool none = t.none || total == 0.0;   // a teacher or a student without any token: nothing to learn
-        const double log_total = uniform(log2(total)), rest_y = uniform(stat_log2(st) - ref);
+        // Teacher and student masked down to the same tokens: what rounding left of the teacher's rest is no rest
+        if (q_rest == 0.0 && t.rest <= t.slack) t.rest = 0.0;
+        const double log_total = uniform(log2(total)), rest_y = st.s == 0.f ? -(double)INFINITY : uniform(st.ref - ref + log2((double)st.s));
         const double mass = t.entries + t.rest;
-        const double kl = (t.plogp - sums[1] - (t.rest > 0.0 ? t.rest * rest_y : 0.0) + mass * log_total) * 0.69314718055994530942;
+        const double kl = (t.plogp - sums[1] + (t.rest > 0.0 ? t.rest * (log2(t.rest) - rest_y) : 0.0) + mass * log_total) * 0.69314718055994530942;
         const double alpha = mass < (double)INFINITY ? both[0] + (q_rest == q_rest ? fmin(t.rest, q_rest) : q_rest) : (double)NAN;
         const double tv = 0.5 * (mass + 1.0) - alpha;
         const double lambda = uniform((double)a.kl_share * exp2(-(double)a.eta * 1.44269504088896340736 * alpha));
@@ -791,21 +809,20 @@ __device__ __forceinline__ RowGrad policy_row(const LossArgs& a, int r, const Ro
                                               LossShared<NT>& sh) {
     float entry = 0.f;
     if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == 0) {   // one wavefront, as above
-        const double y = (double)z * a.c_exact, log_rest = stat_log2(st);
-        const double ref = fmax(log_rest, y);
-        const bool none = ref == -(double)INFINITY && st.s == 0.f && z == z;   // no token is possible
-        const double er = exp2(log_rest - ref), ey = exp2(y - ref), all = er + ey;
+        const double y = base2(z, a.c_exact), y_rest = st.s == 0.f ? -(double)INFINITY : st.ref, ref = uniform(fmax(y_rest, y));
+        const bool none = ref == -(double)INFINITY && z == z;   // no token is possible
+        const double er = uniform((double)st.s * exp2(y_rest - ref)), ey = uniform(exp2(y - ref)), all = uniform(er + ey);
         // log(ey / all), by the rest's share where that is the small part
-        const double logp = y >= log_rest ? -log1p(er / ey) : (y - ref) * 0.69314718055994530942 - log(all);
+        const double logp = ey >= er ? -log1p(er / ey) : (y - ref) * 0.69314718055994530942 - log(all);
         const double adv = in.advantage;
         const double rho = a.old_logp ? exp(logp - (double)in.old_logp) : (logp == logp ? 1.0 : logp);
-        const double free_ = adv == 0.0 ? 0.0 : rho * adv;
+        const double free_ = adv == 0.0 && rho == rho ? 0.0 : rho * adv;   // also of an infinite ratio
         const double held = fmin(fmax(rho, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high) * adv;
         double loss = free_ <= held ? -free_ : (free_ > held ? -held : (double)NAN);
         double dl = free_ <= held ? -free_ : (free_ > held ? 0.0 : (double)NAN);
-        if (a.ref_logp) {
+        if (a.ref_logp && a.kl_coef > 0.f) {
             const double d = (double)in.ref_logp - logp, beta = a.kl_coef, e = expm1(d);
-            loss += beta * (e - d);
+            loss += beta * (d == (double)INFINITY ? d : e - d);
             dl -= beta * e;
         }
         const double f = weight * a.inv_tau * dl;
@@ -1107,9 +1124,9 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp
         out.template zero<NT>(sp);
         return;
     }
-    if (!(fabs(g.st.ref) < 1e8)) {   // products with c would lose the differences, or not fit f32: differences first
+    if (!(fabs(g.st.ref) < (double)WIDE_FROM)) {   // differences first, as in the statistics; m is the row's largest logit
         const float m = (float)(g.st.ref / a.c_exact);
-        const float scale = g.st.s == 0.f ? 0.f : (float)(g.rest / (double)g.st.s * exp2((double)m * a.c_exact - g.st.ref));
+        const float scale = g.st.s == 0.f ? (float)(0.0 * g.rest) : (float)(g.rest / (double)g.st.s * exp2(base2(m, a.c_exact) - g.st.ref));
         cols.each_slowly([&](int i, float* z, uint32_t mem) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < W; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - m) * a.c) * scale;
@@ -1119,7 +1136,7 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp
         // exp2(z c - m) * scale; m is the reference rounded to f32 (c's rounding taken back), and what it is off by belongs to
         // scale
         const float m = uniform((float)(g.st.ref * ((double)a.c / a.c_exact)));
-        const float scale = uniform(g.st.s == 0.f ? 0.f : (float)(g.rest / (double)g.st.s * exp2((double)m * (a.c_exact / (double)a.c) - g.st.ref)));
+        const float scale = uniform(g.st.s == 0.f ? (float)(0.0 * g.rest) : (float)(g.rest / (double)g.st.s * exp2((double)m * (a.c_exact / (double)a.c) - g.st.ref)));
         auto value = [&](float z) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(z, a.c, -m)) * scale; };
         cols.template each<false>([&](int i, float* z, bool full, bool entry, int u) __attribute__((always_inline)) {
             if (full && !entry) {

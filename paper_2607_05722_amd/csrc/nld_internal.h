@@ -301,7 +301,7 @@ constexpr int LOSS_MAX_COLS = 1 << 18;   // columns of one workgroup: their memb
 constexpr int SHARED_WGS = 2;   // few rows: at most this many workgroups per CU share them
 
 // How a call's rows are spread: `chunks` workgroups share a row, each taking cv 16-byte vectors of it; a workgroup of a
-// whole row has `threads` (the losses).
+// whole row, and one of the top selection, has `threads`.
 struct RowPlan {
     int chunks, cv, threads;
 };

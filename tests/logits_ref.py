@@ -24,6 +24,12 @@ def valid_entries(ids, vocab):
     return np.asarray(keep, dtype=np.int64)
 
 
+def rest_of(p, qR, t_lse):
+    """The teacher's rest; nothing where the student has none and it is no more than rounding t_lse to f32 leaves."""
+    pR = max(0.0, 1.0 - p.sum())
+    return 0.0 if qR == 0 and pR <= 2.0 ** -22 + 2.0 ** -24 * abs(t_lse) else pR
+
+
 def distill(z, values, ids, t_lse, tau, kl_share, eta, w):
     """One row: loss, alpha, gradient, and per column the size of the terms that the gradient is a difference of."""
     z = np.asarray(z, dtype=np.float64)
@@ -41,7 +47,7 @@ def distill(z, values, ids, t_lse, tau, kl_share, eta, w):
     R[S] = False
     lqR = lse(y[R]) - L if R.any() else -np.inf
     p = np.exp(t - c)
-    pR = max(0.0, 1.0 - p.sum()) if t_lse is not None and R.any() else 0.0
+    pR = rest_of(p, np.exp(lqR), float(t_lse)) if t_lse is not None and R.any() else 0.0
     pb, qb = np.append(p, pR), np.append(q[S], np.exp(lqR))
     lq = np.append(y[S] - L, lqR)
     on = pb > 0
@@ -81,8 +87,8 @@ def distill_undecided(z, values, ids, t_lse, tau, kl_share, eta, w, d):
     R = np.ones(V, dtype=bool)
     R[S] = False
     p = np.exp(t - c)
-    pR = max(0.0, 1.0 - p.sum()) if t_lse is not None and R.any() else 0.0
     qR = float(np.sum(q[R]))
+    pR = rest_of(p, qR, float(t_lse)) if t_lse is not None and R.any() else 0.0
     pb, qb = np.append(p, pR), np.append(q[S], qR)
     open_ = (np.abs(qb - pb) <= 2 * d * (pb + qb)) & (pb + qb > 0)
     half = 0.5 * (1 - kl_share * np.exp(-eta * float(np.sum(np.minimum(pb, qb)))))

@@ -345,6 +345,78 @@ def test_distill_of_a_student_without_the_teachers_token_is_infinite():
     assert o["loss"].item() == float("inf") and o["grad"][0, 0, 7].item() == -1.0
 
 
+@pytest.mark.parametrize("mask", [float("-inf"), torch.finfo(F32).min, -1e5])
+@pytest.mark.parametrize("plan", PLANS)
+def test_distill_of_a_shared_mask(plan, mask, monkeypatch):
+    """Teacher and student masked down to the same tokens, fewer than there are entries and with a log-sum-exp that f32
+    rounds: the loss is that of these tokens, not the infinite one of a token that only the teacher has."""
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 40
+    z, t = draw((1, 6, V), F32, 12) + 20.0, draw((1, 6, V), F32, 13) + 20.0
+    off = torch.ones(V, dtype=torch.bool)
+    off[[5, 900, 901, V - 1, 7000]] = False
+    z[..., off] = t[..., off] = mask
+    ws = R.LogitsWorkspace(1, 6, V, k)
+    top = R.top_logits(place(t), k, ws)
+    o = check_distill(place(z), k, eta=0.0, entries=(top["values"], top["ids"], top["lse"]), ws=ws)
+    assert torch.isfinite(o["loss"]).all() and (o["loss"] > 1e-3).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", ["lowest", "highest", 2.0 ** 31, -2.0 ** 28, 2.0 ** 27])
+@pytest.mark.parametrize("tau", [1.0, 0.3])
+@pytest.mark.parametrize("plan", PLANS)
+def test_rows_of_one_large_value(plan, tau, value, dtype, monkeypatch):
+    """Every logit alike and so large that sums beside it vanish: all tokens are as likely.  A teacher's log-sum-exp of the
+    lowest value is no teacher; its entries alone are one."""
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 40
+    big = {"lowest": torch.finfo(dtype).min, "highest": torch.finfo(dtype).max}.get(value, value)
+    z = place(torch.full((1, 2, V), big, dtype=dtype), lead=1)
+    ids = torch.arange(100, 100 + k, dtype=torch.int32, device="cuda").expand(1, 2, k).contiguous()
+    vals = torch.full((1, 2, k), torch.finfo(F32).min, device="cuda")
+    a, adv = ids[..., 0].contiguous(), torch.ones((1, 2), device="cuda")
+    ws, d, h = R.LogitsWorkspace(1, 2, V, k), delta(V), HALF[dtype]
+    p = R.policy_from_logits(z, a, adv, ws, temperature=tau)
+    assert ((p["logp"].double() + np.log(V)).abs() <= d + HALF[F32] * np.log(V)).all()
+    want = np.full(V, 1.0 / V / tau)
+    want[100] -= 1.0 / tau
+    assert np.all(np.abs(f64(p["grad"])[0] - want) <= 4 * d * 2 / tau * np.where(want < 0, 1.0, 1.0 / V) + h * np.abs(want))
+    o = R.distill_from_logits(z, vals, ids, ws, temperature=tau, eta=0.0)    # uniform over the entries
+    assert ((o["loss"].double() - np.log(V / k)).abs() <= d + HALF[F32] * np.log(V / k)).all()
+    want = np.full(V, 1.0 / V / tau)
+    want[100:100 + k] -= 1.0 / k / tau
+    assert np.all(np.abs(f64(o["grad"])[0] - want) <= 4 * d * 2 / tau * np.where(want < 0, 1.0 / k, 1.0 / V) + h * np.abs(want))
+    lse = R.top_logits(torch.full_like(z, torch.finfo(dtype).min), k, ws, temperature=tau)["lse"]
+    o = R.distill_from_logits(z, vals, ids, ws, teacher_lse=lse, temperature=tau)
+    assert not o["loss"].any() and not o["accept"].any() and not o["grad"].any()
+
+
+def test_not_a_number_beside_an_empty_rest():
+    """Every column outside the entries masked, a NaN among the entries: the whole gradient is NaN."""
+    z = torch.full((1, 1, 5001), float("-inf"), device="cuda")
+    z[0, 0, :3] = torch.tensor([1.0, float("nan"), 2.0])
+    vals, ids = torch.zeros((1, 1, 3), device="cuda"), torch.arange(3, dtype=torch.int32, device="cuda").view(1, 1, 3)
+    o = R.distill_from_logits(z, vals, ids, R.LogitsWorkspace(1, 1, 5001, 3))
+    assert torch.isnan(o["loss"]).all() and torch.isnan(o["grad"]).all()
+
+
+def test_policy_corners():
+    """An advantage of 0 hides no NaN; an action of probability 0 costs +inf against a reference, nothing with kl_coef 0."""
+    z = torch.zeros((1, 3, 3000), device="cuda")
+    z[0, 0, 9] = float("nan")
+    z[0, 1, 17] = float("-inf")
+    a = torch.full((1, 3), 17, dtype=torch.int32, device="cuda")
+    adv, refp = torch.zeros((1, 3), device="cuda"), torch.full((1, 3), -2.0, device="cuda")
+    ws = R.LogitsWorkspace(1, 3, 3000, 1)
+    o = R.policy_from_logits(z, a, adv, ws, ref_logp=refp)
+    assert torch.isnan(o["loss"][0, 0]) and torch.isnan(o["grad"][0, 0]).all()
+    assert not o["loss"][0, 1:].any() and not o["grad"][0, 1:].any()
+    o = R.policy_from_logits(z, a, adv, ws, ref_logp=refp, kl_coef=0.1)
+    assert o["loss"][0, 1].item() == float("inf") and o["grad"][0, 1, 17].item() == float("-inf")
+    assert torch.isfinite(o["loss"][0, 2]) and torch.isfinite(o["grad"][0, 2]).all()
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("column", [3, 777])
 def test_not_a_number_stays_in_its_row(bad, column):
