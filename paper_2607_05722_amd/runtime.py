@@ -550,6 +550,23 @@ def policy_from_logits(logits: torch.Tensor, actions: torch.Tensor, advantage: t
     return {"loss": loss, "logp": logp, "grad": grad}
 
 
+def _check_drafter_loss(model, logits_ws, anchor, k, n_top, temperature, kl_share, eta, weight):
+    """What the loss would refuse after the verify pass has committed."""
+    batch, vocab, dev = anchor.shape[0], model.shape.vocab, anchor.device
+    if k < 2:
+        raise ValueError("k must be at least 2: row 0 is the anchor's")
+    need = C.load().nld_logits_workspace_bytes(batch, k - 1, vocab, n_top)
+    if need == 0:
+        raise ValueError("no loss for batch %d, k %d, vocab %d, n_top %d" % (batch, k, vocab, n_top))
+    if need > logits_ws.nbytes:
+        raise ValueError("the logits workspace holds %d bytes, these sizes need %d" % (logits_ws.nbytes, need))
+    if logits_ws.buf.device != dev:
+        raise ValueError("the logits workspace is on %s, the anchors on %s" % (logits_ws.buf.device, dev))
+    if not 1e-3 <= np.float32(temperature) <= np.float32(1e3) or not 0.0 <= kl_share <= 1.0 or not 0.0 <= eta < float("inf"):
+        raise ValueError("temperature must be in [1e-3, 1e3], kl_share in [0, 1], eta >= 0 and finite")
+    _rows_of(weight, "weight", (batch, k - 1), torch.float32, dev)
+
+
 def drafter_loss(model, cache, ws, logits_ws: LogitsWorkspace, anchor: torch.Tensor, k: int, n_top: int = 200,
                  temperature: float = 3.0, kl_share: float = 1.0, eta: float = 0.5, bidir_from: int = 0, weight=None,
                  want_grad: bool = True):
@@ -558,7 +575,9 @@ def drafter_loss(model, cache, ws, logits_ws: LogitsWorkspace, anchor: torch.Ten
     positions (verify row j-1 for draft row j), over the accepted drafts and the first rejected one.  ``weight``
     (optional, f32 [batch][k-1]) weighs the rows.  Returns the dict of verify_accept with loss and accept f32
     [batch][k-1], draft_logits [batch][k][vocab] and drafts added; with ``want_grad`` also grad [batch][k-1][vocab],
-    the gradient of loss.sum() by draft_logits[:, 1:]."""
+    the gradient of loss.sum() by draft_logits[:, 1:].  Arguments are checked before the passes: a call that raises
+    ValueError has not moved the cache."""
+    _check_drafter_loss(model, logits_ws, anchor, k, n_top, temperature, kl_share, eta, weight)
     drafts, draft_logits = draft(model, cache, ws, anchor, k, bidir_from, want_logits=True)
     out = verify_accept(model, cache, ws, anchor, drafts, k, want_logits=True)
     top = top_logits(out["logits"][:, :k - 1], n_top, logits_ws, temperature)

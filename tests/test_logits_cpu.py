@@ -1,12 +1,15 @@
 """The operators on rows of logits: argument checks (nothing is enqueued), and the plain versions that the GPU tests
 compare with, against differences and closed forms.  No GPU needed."""
 import ctypes
+from types import SimpleNamespace
 
 import logits_ref as ref
 import numpy as np
 import pytest
+import torch
 
 from paper_2607_05722_amd import _lib as C
+from paper_2607_05722_amd import runtime
 
 P = 0x1000
 WS = 1 << 40
@@ -154,3 +157,33 @@ def test_plain_policy_gradient_against_differences(adv, old, refp):
         e = np.zeros(V)
         e[j] = h
         assert abs((f(z + e) - f(z - e)) / (2 * h) - g[j]) < 1e-7
+
+
+def test_plain_distill_of_a_shared_mask():
+    """Teacher and student masked to the same three tokens: what rounding the teacher's log-sum-exp to f32 leaves of
+    1 - sum p is no token that the student could lack; more than that is."""
+    z = np.full(50, -np.inf)
+    z[:3] = [1.0, 2.0, 3.0]
+    c = float(np.float32(ref.lse(z + 20.0)))
+    for off in (0.0, 1e-6):
+        loss, alpha, g, _ = ref.distill(z, z[:3] + 20.0, [0, 1, 2], c + off, 1.0, 1.0, 0.0, 1.0)
+        assert abs(loss) < 3e-6 and abs(alpha - 1) < 3e-6 and np.max(np.abs(g)) < 3e-6
+    assert ref.distill(z, z[:3] + 20.0, [0, 1, 2], c + 1e-5, 1.0, 1.0, 0.0, 1.0)[0] == np.inf
+
+
+BAD_DRAFTER_LOSS = [dict(k=1), dict(n_top=0), dict(n_top=513), dict(n_top=301), dict(temperature=0.0), dict(temperature=NAN),
+                    dict(kl_share=1.5), dict(eta=-1.0), dict(eta=INF), dict(nbytes=0), dict(weight=(2, 8)), dict(device="meta")]
+
+
+@pytest.mark.parametrize("bad", BAD_DRAFTER_LOSS, ids=lambda b: "-".join("%s_%s" % x for x in b.items()))
+def test_drafter_loss_refuses_before_any_pass(bad):
+    """The cache would have moved on otherwise: no model, cache or workspace is touched."""
+    bad = dict(bad)
+    model = SimpleNamespace(shape=SimpleNamespace(vocab=300))
+    ws = SimpleNamespace(nbytes=bad.pop("nbytes", WS), buf=torch.empty(0, device=bad.pop("device", "cpu")))
+    args = dict(k=8, n_top=50)
+    args.update(bad)
+    if "weight" in args:
+        args["weight"] = torch.ones(args["weight"])
+    with pytest.raises(ValueError):
+        runtime.drafter_loss(model, None, None, ws, torch.zeros(2, dtype=torch.int32), **args)
