@@ -437,13 +437,26 @@ def _rows_of(t, name: str, shape, dtype, device):
     return t.data_ptr()
 
 
-def _out(outs, name: str, shape, dtype, device):
-    """The caller's output tensor of this name, or a new one."""
+def _out(outs, name: str, shape, dtype, device, like=None):
+    """The caller's output tensor of this name, or a new one.  like: a tensor of this type on this device (0.4 us less than
+    naming both)."""
     t = outs.get(name) if outs is not None else None
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=device) if like is None else like.new_empty(*shape)
     _rows_of(t, name, shape, dtype, device)
     return t
+
+
+def _seq_rows(t, shape, width):
+    """Rows from a sequence to the next, where the rows of one lie one behind the other; else None."""
+    B, T = shape
+    if t.is_contiguous():
+        return T
+    st = t.stride()
+    ok = (width == 1 or t.dim() == 2 or st[2] == 1) and (T == 1 or st[1] == width)
+    if B == 1:
+        return T if ok else None
+    return st[0] // width if ok and st[0] % width == 0 and st[0] >= T * width else None
 
 
 def _entries(values, ids, lse, shape, device) -> C.Teacher:
@@ -457,28 +470,24 @@ def _entries(values, ids, lse, shape, device) -> C.Teacher:
             (lse is not None and (lse.dtype != torch.float32 or lse.device != device)):
         raise ValueError("teacher: values must be float32, ids int32 and lse float32, on %s" % device)
 
-    def seq_rows(t, width):
-        # rows from a sequence to the next, where the rows of one lie one behind the other
-        if t.is_contiguous():
-            return T
-        st = t.stride()
-        ok = (width == 1 or t.dim() == 2 or st[2] == 1) and (T == 1 or st[1] == width)
-        if B == 1:
-            return T if ok else None
-        return st[0] // width if ok and st[0] % width == 0 and st[0] >= T * width else None
-
-    rows = seq_rows(values, n)
-    if rows is None or seq_rows(ids, n) != rows or (lse is not None and seq_rows(lse, 1) != rows):
-        raise ValueError("teacher: values, ids and lse must be whole arrays or the same leading rows of such")
+    rows = T
+    if not (values.is_contiguous() and ids.is_contiguous() and (lse is None or lse.is_contiguous())):
+        rows = _seq_rows(values, shape, n)
+        if rows is None or _seq_rows(ids, shape, n) != rows or (lse is not None and _seq_rows(lse, shape, 1) != rows):
+            raise ValueError("teacher: values, ids and lse must be whole arrays or the same leading rows of such")
     return C.Teacher(values.data_ptr(), ids.data_ptr(), 0 if lse is None else lse.data_ptr(), n, rows)
 
 
-def _grad_for(logits, want_grad, grad):
+def _grad_for(logits, desc, want_grad, grad):
+    """The gradient's tensor (the caller's, a new contiguous one, or None) and its descriptor."""
     if grad is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if want_grad else None
+        if not want_grad:
+            return None, None
+        grad = logits.new_empty(desc.batch, desc.rows, desc.vocab)
+        return grad, C.Logits(grad.data_ptr(), desc.dtype, desc.batch, desc.rows, desc.vocab, desc.rows * desc.vocab, desc.vocab)
     if grad.device != logits.device:
         raise ValueError("grad must be on %s" % logits.device)
-    return grad
+    return grad, _logits(grad, "grad")
 
 
 def _call(fn, device, ws, *args):
@@ -502,7 +511,7 @@ def top_logits(logits: torch.Tensor, n_top: int, ws: LogitsWorkspace, temperatur
     dev, rows = logits.device, (desc.batch, desc.rows)
     values = _out(outs, "values", rows + (n_top,), torch.float32, dev)
     ids = _out(outs, "ids", rows + (n_top,), torch.int32, dev)
-    lse = _out(outs, "lse", rows, torch.float32, dev)
+    lse = _out(outs, "lse", rows, torch.float32, dev, values)
     _call(C.load().nld_top_logits, dev, ws, desc, n_top, temperature, values.data_ptr(), ids.data_ptr(), lse.data_ptr())
     return {"values": values, "ids": ids, "lse": lse}
 
@@ -519,11 +528,11 @@ def distill_from_logits(logits: torch.Tensor, values: torch.Tensor, ids: torch.T
     teacher = _entries(values, ids, teacher_lse, rows, dev)
     w = _rows_of(weight, "weight", rows, torch.float32, dev)
     last = _rows_of(last_row, "last_row", rows[:1], torch.int32, dev)
-    loss = _out(outs, "loss", rows, torch.float32, dev)
-    accept = _out(outs, "accept", rows, torch.float32, dev)
-    grad = _grad_for(logits, want_grad, grad)
+    loss = _out(outs, "loss", rows, torch.float32, dev, values)
+    accept = _out(outs, "accept", rows, torch.float32, dev, values)
+    grad, grad_desc = _grad_for(logits, desc, want_grad, grad)
     _call(C.load().nld_distill_from_logits, dev, ws, desc, teacher, temperature, kl_share, eta, w, last, loss.data_ptr(),
-          accept.data_ptr(), None if grad is None else _logits(grad, "grad"))
+          accept.data_ptr(), grad_desc)
     return {"loss": loss, "accept": accept, "grad": grad}
 
 
@@ -542,11 +551,11 @@ def policy_from_logits(logits: torch.Tensor, actions: torch.Tensor, advantage: t
                         _rows_of(old_logp, "old_logp", rows, f32, dev), _rows_of(ref_logp, "ref_logp", rows, f32, dev))
     w = _rows_of(weight, "weight", rows, f32, dev)
     last = _rows_of(last_row, "last_row", rows[:1], torch.int32, dev)
-    loss = _out(outs, "loss", rows, f32, dev)
-    logp = _out(outs, "logp", rows, f32, dev)
-    grad = _grad_for(logits, want_grad, grad)
+    loss = _out(outs, "loss", rows, f32, dev, advantage)
+    logp = _out(outs, "logp", rows, f32, dev, advantage)
+    grad, grad_desc = _grad_for(logits, desc, want_grad, grad)
     _call(C.load().nld_policy_from_logits, dev, ws, desc, rollout, temperature, clip_low, clip_high, kl_coef, w, last,
-          loss.data_ptr(), logp.data_ptr(), None if grad is None else _logits(grad, "grad"))
+          loss.data_ptr(), logp.data_ptr(), grad_desc)
     return {"loss": loss, "logp": logp, "grad": grad}
 
 
