@@ -345,7 +345,8 @@ nld_status nld_commit_from_logits(const float* logits, int32_t* block, int32_t b
  * Logits are rows of `vocab` adjacent columns, [batch][rows], of any strides
  * (in elements), so that a slice of a pass's logits or a trainer's tensor is
  * taken as it is.  q_j = exp(z_j / temperature) / sum, sums in f32, everything
- * per row in f64.  -inf is a column of probability 0. */
+ * per row in f64.  -inf is a column of probability 0.  Outputs must not overlap
+ * inputs, except as grad says. */
 #define NLD_F32 0
 #define NLD_BF16 1
 typedef struct {
