@@ -883,7 +883,7 @@ __device__ __forceinline__ void inputs_here() {
 }
 
 // A teacher's entries in this chunk: membership bits of its vectors' columns, the marks of the threads that hold them (the
-// first `held` vectors of each), and this thread's entry.  list_entries, then (a barrier lies between) mark_entries.
+// first `held` full vectors of each), and this thread's entry.  list_entries, then (a barrier lies between) mark_entries.
 template <bool BF, int NT>
 __device__ __forceinline__ void list_entries(const LossArgs& a, int id, uint32_t* bits, LossShared<NT>& sh) {
     const int tid = threadIdx.x, words = (a.plan.cv * Elem<BF>::W + 31) / 32;
@@ -908,7 +908,7 @@ __device__ __forceinline__ bool mark_entries(const LossArgs& a, const Span<BF>& 
         *z = sp.row[id];
         const int bit = id + sp.lead - sp.v0 * W, at = v - sp.f0;
         if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1u) sh.repeated = 1;
-        if (at >= 0 && at < held * NT) atomicOr(&sh.mark[at % NT], 1u << (at / NT));
+        if (sp.full(v) && at < held * NT) atomicOr(&sh.mark[at % NT], 1u << (at / NT));   // a partial vector is nobody's to hold
     }
     __syncthreads();
     bool bad = entry && chunk == 0 && !valid && id != -1;
@@ -951,8 +951,8 @@ struct Columns {
     static_assert(CAP <= 32, "a bit per held vector");
     __device__ __forceinline__ Columns(const Span<BF>& s, const uint32_t* b, int act) : sp(s), bits(b), action(act), mark(0u) {
         if constexpr (KIND == LOSS_POLICY) {
-            const int at = (act + s.lead) / W - s.f0;
-            if (at >= 0 && at < CAP * NT && at % NT == (int)threadIdx.x) mark = 1u << (at / NT);
+            const int v = (act + s.lead) / W, at = v - s.f0;
+            if (s.full(v) && at < CAP * NT && at % NT == (int)threadIdx.x) mark = 1u << (at / NT);
         }
     }
     // Asks for held vector u, without a branch (a thread's last ones may be the chunk's last vector again), so that a wait
@@ -1113,8 +1113,10 @@ struct GradRow {
 
 // The gradient of a chunk's columns: the rest's from `cols`, and the entry of this thread (col, where `mine`).  A thread
 // has read a vector when it writes the same columns, and the entries' logits were read before, so the gradient may
-// take the logits' place.  The few vectors with an entry among their columns are written column by column, after the
-// others: they are read once more for it, which keeps that code out of the unrolled part.
+// take the logits' place.  The few full vectors with an entry among their columns are written column by column, after the
+// others: they are read once more for it, which keeps that code out of the unrolled part.  The partial ones at the row's
+// ends are written with the others, by the thread that reads them element by element, and only there: a second look at
+// them would find gradients where the logits were.
 template <bool BF, LossKind KIND, int NT, int CAP, bool STREAM>
 __device__ __forceinline__ void write_grad(const LossArgs& a, const Span<BF>& sp, Columns<BF, KIND, NT, CAP, STREAM>& cols, int r,
                                            const RowGrad& g, bool mine, int col) {

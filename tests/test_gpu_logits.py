@@ -829,3 +829,25 @@ def test_drafter_loss_on_the_tiny_model(batch, lora):
 def g_rest(size):
     """A change of every p by e relative changes p_R by e (1 - p_R) / p_R of itself: the rest's terms by that much more."""
     return size * 4.0
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [3, 5, 1003, 16877, 50257])
+@pytest.mark.parametrize("from_end", [0, 1, None])
+def test_entries_at_the_ends_of_a_row_in_place(from_end, V, dtype, plan, monkeypatch):
+    """The action and the teacher's first entry in the last column, the last but one, or the first: eight adjacent rows of
+    an odd length end at every place of the 16-byte grid, so in a vector that is partly another row's.  In the logits' place
+    the gradient has the same bits as in a buffer of its own, where it is checked."""
+    use_plan(monkeypatch, plan)
+    col = 0 if from_end is None else V - 1 - from_end
+    z = draw((1, 8, V), dtype, V + col)
+    z[..., col] += 9.0
+    actions, k = [col] * 8, 1 if V == 3 else 4
+    entries = teacher_of(place(z), k, 1.0, 11)
+    entries[1][..., 0] = torch.where((entries[1] == col).any(-1), entries[1][..., 0], col)
+    for check in (lambda x, g: check_policy(x, actions=actions, beta=0.05, refp=True, grad=g),
+                  lambda x, g: check_distill(x, k, entries=entries, grad=g)):
+        apart = check(place(z), None)
+        x = place(z)
+        assert torch.equal(check(x, x)["grad"], apart["grad"])
