@@ -15,6 +15,8 @@ half a step, 2^-24 (f32) or 2^-8 (bf16) relative.  Hence with d = delta(V):
               closer than d, the sign of TV's gradient is open (logits_ref.distill_undecided)
 and a bf16 logit is exact in f32.
 """
+import functools
+
 import logits_ref as ref
 import numpy as np
 import pytest
@@ -851,3 +853,116 @@ def test_entries_at_the_ends_of_a_row_in_place(from_end, V, dtype, plan, monkeyp
         apart = check(place(z), None)
         x = place(z)
         assert torch.equal(check(x, x)["grad"], apart["grad"])
+
+
+# ------------------------------------------------------------------------------------------ without a gradient
+@pytest.fixture
+def forward_only(monkeypatch):
+    """Both losses without their gradient, for the checks above."""
+    for name in ("distill_from_logits", "policy_from_logits"):
+        monkeypatch.setattr(R, name, functools.partial(getattr(R, name), want_grad=False))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,V,k", LOSS_SIZES)
+def test_losses_without_gradient(B, T, V, k, dtype, forward_only):
+    z = place(draw((B, T, V), dtype, V + 2), lead=1)
+    assert check_distill(z, k, tau=3.0, want_grad=False)["grad"] is None
+    assert check_policy(z, beta=0.05, refp=True)["grad"] is None
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [1003, 50021, 151936])
+def test_losses_without_gradient_by_plan(V, dtype, plan, monkeypatch, forward_only):
+    """From less than one vector per thread to 149 of them, with rows that take no part, weights and strides."""
+    use_plan(monkeypatch, plan)
+    z = place(draw((2, 5, V), dtype, V + 3), 3, 1, 2)
+    weight = torch.tensor([[1.0, 0.0, -2.0, 0.5, 3.0]] * 2, device="cuda")
+    last = torch.tensor([4, 2], dtype=torch.int32, device="cuda")
+    check_distill(z, 50, tau=2.0, kl_share=0.6, weight=weight, last_row=last, want_grad=False)
+    check_distill(z, 300, tail=False, eta=0.0, want_grad=False)
+    check_policy(z, weight=weight, last_row=last, actions=[V - 1, 0, V - 2, 1, V // 2] * 2)
+    check_policy(z, tau=0.7, refp=True, beta=0.1, old=False)
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("mask", [float("-inf"), torch.finfo(F32).min])
+def test_masked_rows_without_gradient(mask, plan, monkeypatch, forward_only):
+    """Teacher and student masked down to the same tokens; rows of nothing but the mask."""
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 40
+    z, t = draw((1, 4, V), F32, 14), draw((1, 4, V), F32, 15)
+    off = torch.ones(V, dtype=torch.bool)
+    off[[0, 900, 901, V - 1]] = False
+    z[..., off] = t[..., off] = mask
+    t[0, 2] = mask
+    ws = R.LogitsWorkspace(1, 4, V, k)
+    top = R.top_logits(place(t), k, ws)
+    entries = (top["values"], top["ids"], top["lse"])
+    rows = torch.tensor([[1.0, 1.0, 0.0, 1.0]], device="cuda")
+    check_distill(place(z), k, eta=0.0, entries=entries, ws=ws, weight=rows, want_grad=False)
+    o = R.distill_from_logits(place(z), *entries[:2], ws, teacher_lse=entries[2])
+    assert o["loss"][0, 2] == 0 and o["accept"][0, 2] == 0
+    check_policy(place(z), actions=[0, 900, 901, V - 1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_longest_row_without_gradient(dtype, forward_only):
+    V, k = 1 << 24, 100
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn((1, 1, V), generator=g, device="cuda").mul_(2.5).to(dtype)
+    d, ws = z[0, 0].double(), R.LogitsWorkspace(1, 1, V, k)
+    L = torch.logsumexp(d, 0).item()
+    t = R.top_logits(z, k, ws)
+    a = torch.full((1, 1), V - 1, dtype=torch.int32, device="cuda")
+    p = R.policy_from_logits(z, a, torch.ones((1, 1), device="cuda"), ws)
+    want = d[V - 1].item() - L
+    assert abs(p["logp"].item() - want) <= delta(V) + HALF[F32] * abs(want)
+    # a teacher that is the student, by its log-sum-exp alone: KL 0 and everything accepted, within what each side is off by
+    o = R.distill_from_logits(z, t["values"], t["ids"], ws, teacher_lse=t["lse"], eta=0.0)
+    assert abs(o["loss"].item()) <= 3 * delta(V) and abs(o["accept"].item() - 1.0) <= 3 * delta(V)
+
+
+def test_gradients_of_rows_past_32_bits():
+    """The last rows of more than 2^32 bytes, in place and apart, against the 64-bit gradient column by column; the rows
+    before them hold other logits."""
+    T, V, k = 14200, 151936, 64
+    tail = draw((1, 2, V), BF16, 7)
+    z = torch.empty((1, T, V), dtype=BF16, device="cuda")
+    z[:, :-2] = tail[0, 0].roll(7).cuda()
+    z[:, -2:] = tail.cuda()
+    entries = teacher_of(tail, k, 1.0, 5)
+    ws, d, h = R.LogitsWorkspace(1, T, V, k), delta(V), HALF[BF16]
+    many = lambda t, fill: torch.cat([torch.full((1, T - 2) + t.shape[2:], fill, dtype=t.dtype, device="cuda"), t], 1)    # noqa: E731
+    vals, ids, lse = (many(t, 0) for t in entries)
+    weight = many(torch.ones((1, 2), device="cuda"), 0.0)
+    top = R.top_logits(z, k, ws)
+    actions = many(top["ids"][:, -2:, 5].contiguous(), -1)
+    adv = torch.ones((1, T), device="cuda")
+    zz = f64(tail)[0]
+    plain = {"p": [ref.policy(zz[r], int(actions[0, T - 2 + r]), 1.0, None, None, 1.0, 0.2, 0.2, 0.0, 1.0) for r in range(2)],
+             "d": [ref.distill(zz[r], f64(vals)[0, T - 2 + r], ids.cpu().numpy()[0, T - 2 + r], f64(lse)[0, T - 2 + r], 1.0, 1.0,
+                               0.5, 1.0) for r in range(2)]}
+    for r in range(2):
+        assert np.array_equal(top["ids"][0, T - 2 + r].cpu().numpy(), ref.top(zz[r], k))
+    grad = torch.empty_like(z)
+    for name, call in (("p", lambda g: R.policy_from_logits(z, actions, adv, ws, grad=g)),
+                       ("d", lambda g: R.distill_from_logits(z, vals, ids, ws, teacher_lse=lse, weight=weight, grad=g)),
+                       ("d", lambda g: R.distill_from_logits(z, vals, ids, ws, teacher_lse=lse, weight=weight, grad=z))):
+        o = call(grad)
+        assert not o["grad"][:, :-2].any() and not o["loss"][:, :-2].any()
+        G, L = f64(o["grad"][:, -2:])[0], f64(o["loss"])[0, -2:]
+        for r, (l, a, g, size) in enumerate(plain[name]):
+            slack = 1 + 2 * 0.5 * max(l, 1.0) if name == "d" else 2.0
+            move = ref.distill_undecided(zz[r], f64(vals)[0, T - 2 + r], ids.cpu().numpy()[0, T - 2 + r], f64(lse)[0, T - 2 + r],
+                                         1.0, 1.0, 0.5, 1.0, d) if name == "d" else 0.0
+            assert abs(L[r] - l) <= d * slack + HALF[F32] * abs(l)
+            assert np.all(np.abs(G[r] - g) <= 4 * d * slack * size + h * np.abs(g) + move + 1e-37)
+    assert R.read_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_top_of_logits_below_the_normal_range(dtype):
+    z = (torch.arange(3001, dtype=torch.float32) - 1500.0).roll(700) * 2.0 ** -133
+    check_top(place(z.to(dtype)[None, None].expand(1, 2, 3001).clone()), 40)
