@@ -386,7 +386,7 @@ nld_status nld_top_logits(const nld_logits* logits, int32_t n_top, float tempera
 typedef struct {
     const float* values;
     const int32_t* ids;    /* -1: no entry */
-    const float* lse;      /* optional: at the same temperature, over the teacher's whole row */
+    const float* lse;      /* optional: at the same temperature, over the teacher's whole row, below 2^24 in size */
     int32_t n_top;
     int32_t seq_rows;      /* >= rows */
 } nld_teacher;
@@ -406,8 +406,11 @@ typedef struct {
  * weight (optional, 1) f32 [batch][rows]; last_row (optional) int32 [batch]: rows past
  * last_row[b] take no part (accept_len of nld_verify_accept: the accepted drafts and
  * the first rejected one).  A row of weight 0 or past last_row is not read; it, and a
- * row whose teacher or student has no token at all, has loss 0 and gradient 0.  A
- * teacher's lse of at most -2^24 is that of a row masked throughout, so of no token.
+ * row whose teacher or student has no token at all, has loss 0 and gradient 0.
+ * The teacher's lse is taken as it is given, so p is off by lse's rounding to f32, up
+ * to 2^-24 |lse| relative.  From 2^24 on that says nothing of the entries: an lse of
+ * 2^24 or more counts as none given, one of at most -2^24 is that of a row masked
+ * throughout, so of no token.
  * loss f32 [batch][rows]; accept (optional) f32 [batch][rows] = alpha, the chance that
  * speculative sampling would accept the student's token.  grad (optional): the
  * gradient of the sum of loss by the logits, in the logits' dtype and sizes; it may be

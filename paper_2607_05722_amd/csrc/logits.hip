@@ -688,18 +688,22 @@ struct Teacher {
     double p, entries, rest, plogp;   // plogp: without the rest's
     double slack;   // what the rounding of an f32 log-sum-exp can leave of 1 - sum p
     bool none;      // no token at all
+    bool tail;      // the log-sum-exp is given, and counts
 };
-// A log-sum-exp at or below it is that of a row masked throughout by a finite value: rounded to f32 by 1 and more, it says
-// nothing of the entries, and counts as -inf.
-constexpr float NO_LSE = -(float)(1 << 24);
+// A log-sum-exp of this size is rounded to f32 by half a unit and more, so that it says nothing of the entries.  At or below
+// -LSE_ROUNDED it is that of a row masked throughout by a finite value, and counts as -inf; from LSE_ROUNDED on the entries
+// alone are the teacher, as where none is given.
+constexpr float LSE_ROUNDED = (float)(1 << 24);
 template <int NT>
 __device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, float t_lse, bool counts, LossShared<NT>& sh) {
     const Entries<NT> en(a.n_top, sh);
     const double none = -(double)INFINITY;
     const double x = counts ? base2(t, a.c_exact) : none;
     double lse = none, more = 0.0;   // the log-sum-exp in two parts: beside a large one the other would be lost
-    if (a.lse) {
-        lse = t_lse <= NO_LSE ? none : uniform((double)t_lse * 1.44269504088896340736);
+    t_lse = uniform(t_lse);
+    const bool tail = a.lse && !(t_lse >= LSE_ROUNDED && t_lse < INFINITY);
+    if (tail) {
+        lse = t_lse <= -LSE_ROUNDED ? none : uniform((double)t_lse * 1.44269504088896340736);
     } else {
         double top[1] = {x}, tot[1] = {0.0};
         if (en.here()) en.template post<1, true>(top, 0);
@@ -716,7 +720,7 @@ __device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, floa
             more = uniform(log2(tot[0]));
         }
     }
-    Teacher o{0.0, 0.0, 0.0, 0.0, fabs(lse) * (0.69314718055994530942 / (1 << 24)) + 1.0 / (1 << 22), lse == none};
+    Teacher o{0.0, 0.0, 0.0, 0.0, fabs(lse) * (0.69314718055994530942 / (1 << 24)) + 1.0 / (1 << 22), lse == none, tail};
     if (en.here()) {
         const double log_p = x - lse - more;
         o.p = x == none ? 0.0 : exp2(log_p);
@@ -734,7 +738,7 @@ __device__ __forceinline__ void teacher_sums(const LossArgs& a, Teacher& o, bool
     double sums[2] = {o.entries, o.plogp};
     en.template take<2, false>(sums, 2);
     o.entries = sums[0];
-    o.rest = a.lse && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;
+    o.rest = o.tail && !whole ? uniform(fmax(0.0, 1.0 - sums[0])) : 0.0;
     o.plogp = sums[1];
     if (!(sums[0] < (double)INFINITY)) o.entries = o.plogp = (double)NAN;
 }

@@ -966,3 +966,29 @@ def test_gradients_of_rows_past_32_bits():
 def test_top_of_logits_below_the_normal_range(dtype):
     z = (torch.arange(3001, dtype=torch.float32) - 1500.0).roll(700) * 2.0 ** -133
     check_top(place(z.to(dtype)[None, None].expand(1, 2, 3001).clone()), 40)
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("tau", [1.0, 0.3])
+def test_teacher_of_logits_whose_log_sum_exp_is_rounded_away(tau, plan, monkeypatch):
+    """From 2^24 on an f32 log-sum-exp says nothing of the entries, which then are the teacher: row 0 has equal logits, row 1
+    one token."""
+    use_plan(monkeypatch, plan)
+    V, k, tau = 20011, 40, as_f32(tau)
+    t = torch.full((1, 2, V), 2.0 ** 27)
+    t[0, 1] = 0.0
+    t[0, 1, 5] = 2.0 ** 27
+    ws, d, h = R.LogitsWorkspace(1, 2, V, k), delta(V), HALF[F32]
+    top = R.top_logits(place(t), k, ws, temperature=tau)
+    assert (top["lse"] >= 2.0 ** 24).all()
+    for grad in (True, False):
+        o = R.distill_from_logits(torch.zeros((1, 2, V), device="cuda"), top["values"], top["ids"], ws, teacher_lse=top["lse"],
+                                  temperature=tau, eta=0.0, want_grad=grad)
+        for r, n in ((0, k), (1, 1)):
+            assert abs(o["loss"][0, r].item() - np.log(V / n)) <= d + h * np.log(V / n)
+            assert abs(o["accept"][0, r].item() - n / V) <= d
+            if grad:
+                p = np.zeros(V)
+                p[5 if n == 1 else slice(0, k)] = 1.0 / n
+                want = (1.0 / V - p) / tau
+                assert np.all(np.abs(f64(o["grad"])[0, r] - want) <= 4 * d * (1.0 / V + p) / tau + h * np.abs(want))
