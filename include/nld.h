@@ -417,8 +417,8 @@ typedef struct {
  * the logits' own buffer with the same strides, else the two ranges of addresses
  * must be apart; its rows must not overlap each other.
  * An id outside [-1, vocab), or one that an earlier entry of the row has, is left out
- * and sets NLD_DEV_BAD_TOKEN.  A NaN or +inf that takes part makes loss, accept and
- * gradient of its row NaN.
+ * and sets NLD_DEV_BAD_TOKEN.  A NaN or +inf that takes part, lse's too, makes loss,
+ * accept and gradient of its row NaN.
  * Errors: as nld_top_logits, INVALID_ARG for kl_share outside [0, 1], eta < 0 or not
  * finite, seq_rows < rows, a grad of other sizes or dtype, or one that overlaps. */
 nld_status nld_distill_from_logits(const nld_logits* student, const nld_teacher* teacher, float temperature,

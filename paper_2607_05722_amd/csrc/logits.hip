@@ -724,7 +724,7 @@ __device__ __forceinline__ Teacher teacher_side(const LossArgs& a, float t, floa
     if (en.here()) {
         const double log_p = x - lse - more;
         o.p = x == none ? 0.0 : exp2(log_p);
-        double sums[2] = {o.p, o.p > 0.0 ? o.p * log_p : 0.0};
+        double sums[2] = {o.p + 0.0 * lse, o.p > 0.0 ? o.p * log_p : 0.0};   // an infinite lse, or NaN, of no entry too
         en.template post<2, false>(sums, 2);
         o.entries = sums[0];
         o.plogp = sums[1];

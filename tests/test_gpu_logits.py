@@ -992,3 +992,18 @@ def test_teacher_of_logits_whose_log_sum_exp_is_rounded_away(tau, plan, monkeypa
                 p[5 if n == 1 else slice(0, k)] = 1.0 / n
                 want = (1.0 / V - p) / tau
                 assert np.all(np.abs(f64(o["grad"])[0, r] - want) <= 4 * d * (1.0 / V + p) / tau + h * np.abs(want))
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("entries", [0, 10])
+def test_a_log_sum_exp_that_is_no_number(entries, bad, plan, monkeypatch):
+    """The teacher's own, with entries that are numbers or with none: NaN throughout the row and nowhere else."""
+    use_plan(monkeypatch, plan)
+    z = place(draw((1, 3, 20011), F32, 4))
+    vals, ids, lse = teacher_of(z, 10, 1.0, 3)
+    lse[0, 1] = bad
+    ids[0, 1, entries:] = -1
+    o = R.distill_from_logits(z, vals, ids, R.LogitsWorkspace(1, 3, 20011, 10), teacher_lse=lse)
+    assert torch.isnan(o["loss"][0, 1]) and torch.isnan(o["accept"][0, 1]) and torch.isnan(o["grad"][0, 1]).all()
+    assert torch.isfinite(o["loss"][0, [0, 2]]).all() and torch.isfinite(o["grad"][0, [0, 2]]).all()
