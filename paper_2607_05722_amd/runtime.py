@@ -10,6 +10,7 @@ import ctypes
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import _lib as C
 
@@ -490,6 +491,15 @@ def _grad_for(logits, desc, want_grad, grad):
     return grad, _logits(grad, "grad")
 
 
+def _written(outs, names, grad=None):
+    """Tells autograd that the caller's tensors were written, as torch's own operations in place do: what kept one of them
+    for its backward pass raises there."""
+    if outs is not None:
+        increment_version([outs[n] for n in names if outs.get(n) is not None])
+    if grad is not None:
+        increment_version(grad)
+
+
 def _call(fn, device, ws, *args):
     """fn(*args, workspace, its size, stream) on `device` and its current stream."""
     if ws.buf.device != device:
@@ -506,13 +516,14 @@ def _call(fn, device, ws, *args):
 def top_logits(logits: torch.Tensor, n_top: int, ws: LogitsWorkspace, temperature: float = 1.0, outs=None):
     """The n_top largest logits of every row of logits [batch][rows][vocab] (f32 or bf16), largest first, the lower
     column first among equal ones.  Returns dict: values f32 and ids int32 [batch][rows][n_top], lse f32
-    [batch][rows] (log-sum-exp of logits / temperature over the whole row)."""
+    [batch][rows] (log-sum-exp of logits / temperature over the whole row).  No gradient flows through them."""
     desc = _logits(logits, "logits")
     dev, rows = logits.device, (desc.batch, desc.rows)
     values = _out(outs, "values", rows + (n_top,), torch.float32, dev)
     ids = _out(outs, "ids", rows + (n_top,), torch.int32, dev)
     lse = _out(outs, "lse", rows, torch.float32, dev, values)
     _call(C.load().nld_top_logits, dev, ws, desc, n_top, temperature, values.data_ptr(), ids.data_ptr(), lse.data_ptr())
+    _written(outs, ("values", "ids", "lse"))
     return {"values": values, "ids": ids, "lse": lse}
 
 
@@ -522,7 +533,10 @@ def distill_from_logits(logits: torch.Tensor, values: torch.Tensor, ids: torch.T
     """Distillation loss of the student's logits [batch][rows][vocab] from a teacher's top logits (values, ids and,
     over the teacher's whole row, teacher_lse: what top_logits returns), with its gradient in the same call.  See
     nld_distill_from_logits in include/nld.h for the formula.  Returns dict: loss and accept f32 [batch][rows], grad
-    (the gradient of loss.sum() by the logits, in their dtype; ``grad=logits`` puts it in their place; None without)."""
+    (the gradient of loss.sum() by the logits, in their dtype; ``grad=logits`` puts it in their place; None without).
+    The loss hangs on no autograd graph: a trainer goes on with ``logits.backward(grad)``.  ``grad=logits`` is a change in place
+    of them, so an operation that kept them for its own backward pass (tanh, softmax) raises there; give such logits a
+    gradient of its own."""
     desc = _logits(logits, "logits")
     dev, rows = logits.device, (desc.batch, desc.rows)
     teacher = _entries(values, ids, teacher_lse, rows, dev)
@@ -530,9 +544,11 @@ def distill_from_logits(logits: torch.Tensor, values: torch.Tensor, ids: torch.T
     last = _rows_of(last_row, "last_row", rows[:1], torch.int32, dev)
     loss = _out(outs, "loss", rows, torch.float32, dev, values)
     accept = _out(outs, "accept", rows, torch.float32, dev, values)
+    given = grad
     grad, grad_desc = _grad_for(logits, desc, want_grad, grad)
     _call(C.load().nld_distill_from_logits, dev, ws, desc, teacher, temperature, kl_share, eta, w, last, loss.data_ptr(),
           accept.data_ptr(), grad_desc)
+    _written(outs, ("loss", "accept"), given)
     return {"loss": loss, "accept": accept, "grad": grad}
 
 
@@ -542,7 +558,7 @@ def policy_from_logits(logits: torch.Tensor, actions: torch.Tensor, advantage: t
                        grad=None, outs=None):
     """Clipped policy loss of the tokens ``actions`` (int32 [batch][rows], -1: none) under logits [batch][rows][vocab],
     with its gradient in the same call.  See nld_policy_from_logits in include/nld.h for the formula.  Returns dict:
-    loss and logp f32 [batch][rows], grad (as distill_from_logits)."""
+    loss and logp f32 [batch][rows], grad (as distill_from_logits, also as to autograd)."""
     desc = _logits(logits, "logits")
     dev, rows, f32 = logits.device, (desc.batch, desc.rows), torch.float32
     if actions is None or advantage is None:
@@ -553,9 +569,11 @@ def policy_from_logits(logits: torch.Tensor, actions: torch.Tensor, advantage: t
     last = _rows_of(last_row, "last_row", rows[:1], torch.int32, dev)
     loss = _out(outs, "loss", rows, f32, dev, advantage)
     logp = _out(outs, "logp", rows, f32, dev, advantage)
+    given = grad
     grad, grad_desc = _grad_for(logits, desc, want_grad, grad)
     _call(C.load().nld_policy_from_logits, dev, ws, desc, rollout, temperature, clip_low, clip_high, kl_coef, w, last,
           loss.data_ptr(), logp.data_ptr(), grad_desc)
+    _written(outs, ("loss", "logp"), given)
     return {"loss": loss, "logp": logp, "grad": grad}
 
 

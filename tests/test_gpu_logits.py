@@ -1007,3 +1007,35 @@ def test_a_log_sum_exp_that_is_no_number(entries, bad, plan, monkeypatch):
     o = R.distill_from_logits(z, vals, ids, R.LogitsWorkspace(1, 3, 20011, 10), teacher_lse=lse)
     assert torch.isnan(o["loss"][0, 1]) and torch.isnan(o["accept"][0, 1]) and torch.isnan(o["grad"][0, 1]).all()
     assert torch.isfinite(o["loss"][0, [0, 2]]).all() and torch.isfinite(o["grad"][0, [0, 2]]).all()
+
+
+def test_autograd_sees_what_a_call_writes():
+    """A loss hangs on no graph; its gradient is handed on by logits.backward.  In the logits' place it is a change that
+    autograd knows of, so that an operation which kept these logits for its own backward pass raises."""
+    V, k = 1003, 8
+    a, adv = torch.full((1, 2), 3, dtype=torch.int32, device="cuda"), torch.ones((1, 2), device="cuda")
+    ws = R.LogitsWorkspace(1, 2, V, k)
+    top = R.top_logits(torch.randn((1, 2, V), device="cuda"), k, ws)
+    calls = (lambda z, **kw: R.distill_from_logits(z, top["values"], top["ids"], ws, teacher_lse=top["lse"], **kw),
+             lambda z, **kw: R.policy_from_logits(z, a, adv, ws, **kw))
+    for call in calls:
+        x = torch.randn((1, 2, V), device="cuda", requires_grad=True)
+        z = 2.0 * x
+        o = call(z)
+        assert not o["loss"].requires_grad and z._version == 0
+        z.backward(o["grad"])
+        assert torch.equal(x.grad, 2.0 * o["grad"])
+        capped = torch.tanh(x)
+        call(capped, grad=capped)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            capped.sum().backward()
+    outs = {n: torch.empty_like(t) for n, t in top.items()}
+    R.top_logits(torch.randn((1, 2, V), device="cuda"), k, ws, outs=outs)
+    loss = {n: torch.empty((1, 2), device="cuda") for n in ("loss", "accept", "logp")}
+    for call in calls:
+        call(torch.randn((1, 2, V), device="cuda"), outs=loss)
+    assert all(t._version > 0 for t in list(outs.values()) + list(loss.values()))
+    before = [t._version for t in loss.values()]
+    with pytest.raises(C.NLDError):
+        calls[0](torch.randn((1, 2, V), device="cuda"), outs=loss, temperature=0.0)
+    assert before == [t._version for t in loss.values()]       # a refused call wrote nothing
