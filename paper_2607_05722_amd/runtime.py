@@ -589,7 +589,8 @@ def _check_drafter_loss(model, logits_ws, anchor, k, n_top, temperature, kl_shar
         raise ValueError("the logits workspace holds %d bytes, these sizes need %d" % (logits_ws.nbytes, need))
     if logits_ws.buf.device != dev:
         raise ValueError("the logits workspace is on %s, the anchors on %s" % (logits_ws.buf.device, dev))
-    if not 1e-3 <= np.float32(temperature) <= np.float32(1e3) or not 0.0 <= kl_share <= 1.0 or not 0.0 <= eta < float("inf"):
+    eta32 = ctypes.c_float(eta).value   # as the call gets it
+    if not 1e-3 <= np.float32(temperature) <= np.float32(1e3) or not 0.0 <= kl_share <= 1.0 or not 0.0 <= eta32 < float("inf"):
         raise ValueError("temperature must be in [1e-3, 1e3], kl_share in [0, 1], eta >= 0 and finite")
     _rows_of(weight, "weight", (batch, k - 1), torch.float32, dev)
 

@@ -187,3 +187,11 @@ def test_drafter_loss_refuses_before_any_pass(bad):
         args["weight"] = torch.ones(args["weight"])
     with pytest.raises(ValueError):
         runtime.drafter_loss(model, None, None, ws, torch.zeros(2, dtype=torch.int32), **args)
+
+
+def test_drafter_loss_refuses_an_eta_past_f32_before_any_pass():
+    """1e39 is finite here and infinite in the call, which would refuse it after the verify pass."""
+    ws = SimpleNamespace(nbytes=WS, buf=torch.empty(0))
+    with pytest.raises(ValueError):
+        runtime.drafter_loss(SimpleNamespace(shape=SimpleNamespace(vocab=300)), None, None, ws,
+                             torch.zeros(2, dtype=torch.int32), k=8, n_top=50, eta=1e39)
