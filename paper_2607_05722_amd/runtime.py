@@ -415,6 +415,7 @@ class LogitsWorkspace:
         self.ptr = _ptr(self.buf)
 
 
+_INT32_MAX = 2 ** 31 - 1   # a descriptor's field keeps the lower half of a larger number, without an error
 _DTYPES = {torch.float32: C.NLD_F32, torch.bfloat16: C.NLD_BF16}
 
 
@@ -426,6 +427,8 @@ def _logits(t: torch.Tensor, name: str) -> C.Logits:
     (batch, rows, vocab), (seq, row, col) = t.shape, t.stride()
     if col != 1 and vocab > 1:
         raise ValueError("%s: the columns of a row must be adjacent" % name)
+    if (batch | rows | vocab) > _INT32_MAX:
+        raise ValueError("%s: sizes must be int32" % name)
     return C.Logits(t.data_ptr(), dtype, batch, rows, vocab, seq, row)
 
 
@@ -476,6 +479,8 @@ def _entries(values, ids, lse, shape, device) -> C.Teacher:
         rows = _seq_rows(values, shape, n)
         if rows is None or _seq_rows(ids, shape, n) != rows or (lse is not None and _seq_rows(lse, shape, 1) != rows):
             raise ValueError("teacher: values, ids and lse must be whole arrays or the same leading rows of such")
+    if n > _INT32_MAX or rows > _INT32_MAX:
+        raise ValueError("teacher: sizes must be int32")
     return C.Teacher(values.data_ptr(), ids.data_ptr(), 0 if lse is None else lse.data_ptr(), n, rows)
 
 
@@ -518,6 +523,8 @@ def top_logits(logits: torch.Tensor, n_top: int, ws: LogitsWorkspace, temperatur
     column first among equal ones.  Returns dict: values f32 and ids int32 [batch][rows][n_top], lse f32
     [batch][rows] (log-sum-exp of logits / temperature over the whole row).  No gradient flows through them."""
     desc = _logits(logits, "logits")
+    if not 0 <= n_top <= _INT32_MAX:
+        raise ValueError("n_top must be in [1, vocab] (got %d)" % n_top)
     dev, rows = logits.device, (desc.batch, desc.rows)
     values = _out(outs, "values", rows + (n_top,), torch.float32, dev)
     ids = _out(outs, "ids", rows + (n_top,), torch.int32, dev)

@@ -195,3 +195,28 @@ def test_drafter_loss_refuses_an_eta_past_f32_before_any_pass():
     with pytest.raises(ValueError):
         runtime.drafter_loss(SimpleNamespace(shape=SimpleNamespace(vocab=300)), None, None, ws,
                              torch.zeros(2, dtype=torch.int32), k=8, n_top=50, eta=1e39)
+
+
+def like_logits(shape, stride):
+    """What the binding looks at of a device tensor."""
+    return SimpleNamespace(dtype=torch.float32, shape=shape, is_cuda=True, device=torch.device("cuda", 0), dim=lambda: 3,
+                           stride=lambda: stride, data_ptr=lambda: P)
+
+
+@pytest.mark.parametrize("shape", [(1 << 32, 1, 5), (1, (1 << 32) + 3, 5), (1, 1, (1 << 32) + 5), (1 << 31, 1, 5)])
+def test_binding_refuses_sizes_past_int32(shape):
+    """The descriptor's fields would keep their lower halves: a call on the first few rows or columns, with no error."""
+    with pytest.raises(ValueError):
+        runtime._logits(like_logits(shape, (shape[1] * shape[2], shape[2], 1)), "logits")
+
+
+def test_binding_refuses_entries_past_int32():
+    meta = torch.device("meta")
+    many = lambda B, T, n, seq, dt: torch.empty_strided((B, T, n), (seq, n, 1), dtype=dt, device=meta)    # noqa: E731
+    for args in ((2, 3, 1, (1 << 32) + 3), (1, 1, (1 << 32) + 5, (1 << 32) + 5)):
+        with pytest.raises(ValueError):
+            runtime._entries(many(*args, torch.float32), many(*args, torch.int32), None, args[:2], meta)
+    runtime._entries(many(2, 3, 4, 40, torch.float32), many(2, 3, 4, 40, torch.int32), None, (2, 3), meta)
+    for n in ((1 << 32) + 5, -1):
+        with pytest.raises(ValueError):
+            runtime.top_logits(like_logits((1, 1, 100), (100, 100, 1)), n, None)
