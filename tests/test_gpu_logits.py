@@ -1039,3 +1039,62 @@ def test_autograd_sees_what_a_call_writes():
     with pytest.raises(C.NLDError):
         calls[0](torch.randn((1, 2, V), device="cuda"), outs=loss, temperature=0.0)
     assert before == [t._version for t in loss.values()]       # a refused call wrote nothing
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("column", [0, 9000, 20010])
+def test_not_a_number_by_plan(column, bad, dtype, plan, monkeypatch):
+    """In the first, a middle and the last column, which is an entry in one row and none in the other: NaN all over these
+    rows, with a gradient and without one, and numbers in the rows beside them."""
+    use_plan(monkeypatch, plan)
+    V, k = 20011, 10
+    z = draw((1, 5, V), dtype, 16)
+    vals, ids, lse = teacher_of(z, k, 1.0, 17)
+    ids[0, 1] = torch.arange(100, 100 + k, dtype=torch.int32)
+    ids[0, 3] = ids[0, 1]
+    ids[0, 3, 7] = column
+    z[0, [1, 3], column] = bad
+    zd = place(z, lead=1)
+    a = torch.tensor([[5, 5, 5, column, 5]], dtype=torch.int32, device="cuda")
+    ws = R.LogitsWorkspace(1, 5, V, k)
+    for grad in (True, False):
+        o = R.distill_from_logits(zd, vals, ids, ws, teacher_lse=lse, want_grad=grad)
+        p = R.policy_from_logits(zd, a, torch.ones((1, 5), device="cuda"), ws, want_grad=grad)
+        for x in [o["loss"], o["accept"], p["loss"], p["logp"]] + ([o["grad"], p["grad"]] if grad else []):
+            assert torch.isnan(x[0, [1, 3]]).all() and torch.isfinite(x[0, [0, 2, 4]]).all()
+
+
+@pytest.mark.parametrize("plan", PLANS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_the_lowest_value_in_place(dtype, plan, monkeypatch):
+    """Rows whose statistics take differences first: masked by the type's lowest value but for a few tokens, the last column among
+    them, and throughout.  In the logits' place as in a buffer of its own."""
+    use_plan(monkeypatch, plan)
+    V = 20011
+    z = draw((1, 8, V), dtype, 18)
+    off = torch.ones(V, dtype=torch.bool)
+    off[[0, 77, V - 4, V - 1]] = False
+    z[0, ::2, off] = torch.finfo(dtype).min
+    z[0, [2, 5]] = torch.finfo(dtype).min
+    z[0, 7] = 2.0 ** 40
+    k = 4
+    ids = torch.tensor([0, V - 1, 77, 9], dtype=torch.int32, device="cuda").expand(1, 8, k).contiguous()
+    vals, lse = torch.zeros((1, 8, k), device="cuda"), torch.full((1, 8), float(np.float32(np.log(5))), device="cuda")
+    a, adv = torch.full((1, 8), V - 1, dtype=torch.int32, device="cuda"), torch.ones((1, 8), device="cuda")
+    ws, one, d = R.LogitsWorkspace(1, 8, V, k), np.ones((1, 8)), delta(V)
+    # less the row's largest, which is exact here and changes no softmax: beside 3e38 the logarithm of a sum is lost in 64 bits too
+    zz = f64(z)[0]
+    zz = zz - zz.max(-1, keepdims=True)
+    t = float(lse[0, 0])
+    for call, aux, plain, move in (
+            (lambda x, g: R.policy_from_logits(x, a, adv, ws, grad=g), "logp",
+             lambda r: ref.policy(zz[r], V - 1, 1.0, None, None, 1.0, 0.2, 0.2, 0.0, 1.0), lambda r: 0.0),
+            (lambda x, g: R.distill_from_logits(x, vals, ids, ws, teacher_lse=lse, kl_share=0.0, eta=0.0, grad=g), "accept",
+             lambda r: ref.distill(zz[r], np.zeros(k), ids[0, 0].cpu().numpy(), t, 1.0, 0.0, 0.0, 1.0),
+             lambda r: ref.distill_undecided(zz[r], np.zeros(k), ids[0, 0].cpu().numpy(), t, 1.0, 0.0, 0.0, 1.0, d))):
+        apart = call(place(z), None)
+        compare(z, one, apart["loss"], apart[aux], apart["grad"], plain, lambda r: 2.0 if aux == "logp" else 1.0, 1.0, move)
+        x = place(z)
+        assert torch.equal(call(x, x)["grad"], apart["grad"])
