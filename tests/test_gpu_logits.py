@@ -1098,3 +1098,27 @@ def test_rows_of_the_lowest_value_in_place(dtype, plan, monkeypatch):
         compare(z, one, apart["loss"], apart[aux], apart["grad"], plain, lambda r: 2.0 if aux == "logp" else 1.0, 1.0, move)
         x = place(z)
         assert torch.equal(call(x, x)["grad"], apart["grad"])
+
+
+def test_policy_on_what_a_verify_pass_commits():
+    """committed, with its -1 behind the accepted drafts, is taken as actions as it is."""
+    from synth.workloads import LazyWeights, WORKLOADS, prefix_kv, tokens
+    wl = WORKLOADS["tiny"]
+    shape, batch, k = wl.shape, 3, 8
+    model = R.DeviceModel(shape, LazyWeights(shape, wl.seed))
+    cache = R.DeviceCache(shape, batch, 256)
+    for l in range(shape.n_layers):
+        cache.load_prefix(l, *prefix_kv(shape, wl.seed, l, batch, 100))
+    cache.set_lengths([100 - 7 * b for b in range(batch)])
+    anchor = torch.from_numpy(tokens(shape, 3, "anchor", (batch,))).cuda()
+    ws = R.Workspace(model, batch, k, 256)
+    d, _ = R.draft(model, cache, ws, anchor, k)
+    v = R.verify_accept(model, cache, ws, anchor, d, k, want_logits=True)
+    adv, lws = torch.ones((batch, k), device="cuda"), R.LogitsWorkspace(batch, k, shape.vocab)
+    o = R.policy_from_logits(v["logits"], v["committed"], adv, lws)
+    a, zz = v["committed"].cpu().numpy().reshape(-1), f64(v["logits"]).reshape(-1, shape.vocab)
+    compare(v["logits"], np.ones((batch, k)), o["loss"], o["logp"], o["grad"],
+            lambda r: ref.policy(zz[r], int(a[r]), 1.0, None, None, 1.0, 0.2, 0.2, 0.0, 1.0), lambda r: 2.0, 1.0)
+    behind = torch.arange(k, device="cuda")[None] > v["accept_len"][:, None]
+    assert bool((v["committed"][behind] == -1).all()) and not o["grad"][behind].any()
+    assert R.read_device_status(lws) == 0
