@@ -66,12 +66,6 @@ struct TraceScope {
 int device_cus();
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-inline int cdiv(int a, int b) { return (a + b - 1) / b; }
-
-int env_int(const char* name, int dflt) {
-    const char* v = getenv(name);
-    return (v && *v) ? atoi(v) : dflt;
-}
 
 // Operand sites carried in plain bf16 instead of split form: NLD_PLAIN_SITES, a comma-separated list
 // of norm, final, q, kv, p, o, act (precision knob; default: none, every site split).

@@ -19,7 +19,6 @@
 #include "nld_internal.h"
 
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -27,8 +26,6 @@ namespace nld {
 namespace {
 
 constexpr uint32_t DEV_BAD_TOKEN = 0x1u;
-
-inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 
 template <bool BF>
 struct Elem;
@@ -633,10 +630,10 @@ struct LossShared {
 // these again.
 template <int NT>
 struct Entries {
-    const int n, waves, wave, lane;
+    const int waves, wave, lane;
     LossShared<NT>& sh;
     __device__ __forceinline__ Entries(int n_top, LossShared<NT>& s)
-        : n(n_top), waves((n_top + 63) >> 6), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), sh(s) {}
+        : waves((n_top + 63) >> 6), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), sh(s) {}
     __device__ __forceinline__ bool here() const { return wave < waves; }
     template <int N, bool MAX>
     __device__ __forceinline__ void post(double* v, int slot) const {
@@ -1327,11 +1324,6 @@ static RowPlan spread(int nv, int n_rows, int target, int least) {
     return p;
 }
 
-static int env_or(const char* name, int v) {
-    const char* e = getenv(name);
-    return e && *e ? atoi(e) : v;
-}
-
 // Rows shared by several workgroups, in two launches, or one each.  us for n rows, top 200 of 151936 columns (50 of fewer),
 // shared and one each: f32 151936 columns 1 row 17 and 31, 64 rows 25 and 31, 128 rows 32 and 31, 50257 columns 1 row 13 and 17,
 // 128 rows 19 and 17, 16877 columns 13 and 11; bf16 151936 columns 1 row 17 and 25, 64 rows 23 and 25, 128 rows 27 and 26.
@@ -1342,11 +1334,11 @@ RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus) {
     const int nv = row_vectors(bf16, vocab);
     const double n = (double)n_rows * 256 / cus;
     bool share = nv * ((bf16 ? 7e-4 : 5e-4) - 3.7e-6 * n) > 5.0;
-    const int forced = env_or("NLD_TOP_CHUNKS", 0);
+    const int forced = env_int("NLD_TOP_CHUNKS", 0);
     if (forced) share = forced > 1;
     RowPlan p{1, nv, 0};
     if (share) p = spread(nv, n_rows, SHARED_WGS * cus / 2, std::max(2048, n_top * 16 / (bf16 ? 8 : 4)));
-    p.threads = env_or("NLD_TOP_THREADS", p.cv <= 512 * TOP_SEGS * TOP_AHEAD ? 512 : 1024);
+    p.threads = env_int("NLD_TOP_THREADS", p.cv <= 512 * TOP_SEGS * TOP_AHEAD ? 512 : 1024);
     if (p.threads != 512 || n_top > 256) p.threads = 1024;   // the bound on the n_top-th comes from the threads' maxima
     return p;
 }
@@ -1367,7 +1359,7 @@ RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus
     const int W = bf16 ? 8 : 4, nv = row_vectors(bf16, vocab);
     const double n = (double)n_rows * 256 / cus;
     bool share = grad ? 5.5 + 1e-5 * n * nv < 8e-4 * nv : 3.0 + 2.7e-6 * n * nv < 4e-4 * nv;
-    const int forced = env_or("NLD_LOSS_CHUNKS", 0);
+    const int forced = env_int("NLD_LOSS_CHUNKS", 0);
     if (forced) share = forced > 1;
     RowPlan p{1, nv, 0};
     if (share) p = spread(nv, n_rows, SHARED_WGS * cus, 1024);
@@ -1377,7 +1369,7 @@ RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus
     }
     if (grad) p.threads = nv <= 256 * 19 ? 256 : (nv <= 512 * 26 ? 512 : 1024);
     else p.threads = nv > 2048 && n_rows < 2 * cus ? 512 : 256;
-    p.threads = env_or("NLD_LOSS_THREADS", p.threads);
+    p.threads = env_int("NLD_LOSS_THREADS", p.threads);
     if (p.threads != 256 && p.threads != 1024) p.threads = 512;
     if (p.threads == 256 && n_top > 256) p.threads = 512;   // a thread per entry
     return p;
