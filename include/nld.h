@@ -440,7 +440,9 @@ typedef struct {
  *                    + kl_coef * (exp(d) - d - 1)),   d = ref_logp - logp
  * (the KL term only with ref_logp and kl_coef > 0; +inf for an action of probability 0).  weight, last_row, loss and grad as above;
  * logp (optional) f32 [batch][rows], 0 for rows that take no part.  An action outside
- * [-1, vocab) takes no part and sets NLD_DEV_BAD_TOKEN.
+ * [-1, vocab) takes no part and sets NLD_DEV_BAD_TOKEN.  The logits [batch][k] and the
+ * committed tokens of nld_verify_accept are taken as they are: verify row j decodes
+ * committed[b][j], which is -1 behind the accepted drafts.
  * Errors: as nld_top_logits, INVALID_ARG for a clip_low outside [0, 1], a clip_high or kl_coef < 0
  * or not finite, and grad as above. */
 nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* rollout, float temperature,
