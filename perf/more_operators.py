@@ -1,0 +1,502 @@
+"""Performance cases of the operators on a paged key/value cache: storing new rows and reading rows back, the
+attention of a chunk of new rows, and the sparse attention over the pages that a cheap score selects.
+
+The cache of a layer is a pool of pages of 64 positions; a table gives the pages of each sequence, in no order.
+Pages hold bfloat16, or 8-bit floats (e4m3) with a power of two for each position and head as their scale.  Keys
+drift from page to page, so that a query's weight sits on some of them.  Lengths and row counts of ragged cases
+follow from the case; the seed makes the values and the order of the pages.
+
+Case keys: op (store: write new rows and read them back; read; attend; sparse: select, then attend), pages (bf16,
+e4m3), dtype (of the rows: bf16, f32), batch, q_heads, kv_heads, dim, ctx (most committed positions of a sequence),
+rows (most new rows of a sequence), ragged (lengths and row counts differ), draft (every new row sees every other
+one; else each sees those up to itself), top, first, group (sparse: pages per selection, leading pages always taken,
+new rows that share a selection).
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+PAGE = 64
+_TYPES = {"bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+
+
+def _case(name, op, pages, dtype, batch, heads, ctx, rows, ragged=False, draft=False, top=0, first=0, group=1):
+    c = {"op": op, "pages": pages, "dtype": dtype, "batch": batch, "q_heads": heads[0], "kv_heads": heads[1],
+         "dim": heads[2], "ctx": ctx, "rows": rows, "ragged": ragged, "draft": draft, "top": top, "first": first,
+         "group": group}
+    return dict({"name": name}, **c) if name else c
+
+
+TINY, H8B, H14B = (4, 2, 64), (32, 8, 128), (40, 8, 128)
+
+
+def listed():
+    return [
+        # one decoded token of a tiny model: latency is all there is
+        _case("store_token_tiny", "store", "bf16", "f32", 1, TINY, 128, 1),
+        # a part of eight prompts behind what is cached of them, quantised, with the bounds that selection reads
+        _case("store_chunk_e4m3", "store", "e4m3", "bf16", 8, H8B, 4096, 512, ragged=True),
+        # eight idle sequences that return from 8 bits
+        _case("read_parked_e4m3", "read", "e4m3", "bf16", 8, H8B, 16384, 16384, ragged=True),
+        # the head of one sequence, odd length, at full precision
+        _case("read_prefix_odd", "read", "bf16", "f32", 1, H14B, 333, 333),
+        # one token of a tiny model in the passes' own precision
+        _case("attend_token_tiny", "attend", "bf16", "f32", 1, TINY, 128, 1),
+        # one token of one sequence: few rows, one long axis
+        _case("attend_token_b1", "attend", "bf16", "bf16", 1, H8B, 4096, 1),
+        # decoding a batch of ragged sequences from 8 bits
+        _case("attend_token_b32_e4m3", "attend", "e4m3", "bf16", 32, H8B, 8192, 1, ragged=True),
+        # the verify blocks of a ragged batch, in the passes' own precision
+        _case("attend_verify_b32_k16", "attend", "bf16", "f32", 32, H8B, 8192, 16, ragged=True),
+        # draft blocks over long prefixes in 8 bits, five query heads to a key head
+        _case("attend_draft_14b_e4m3", "attend", "e4m3", "bf16", 8, H14B, 16384, 32, draft=True),
+        # parts of prompts that are read in, the largest case
+        _case("attend_prefill_b4", "attend", "bf16", "bf16", 4, H8B, 8192, 2048, ragged=True),
+        # a token of each of eight long sequences, 64 pages of up to 1024
+        _case("sparse_token_b8", "sparse", "bf16", "bf16", 8, H8B, 65536, 1, ragged=True, top=64, first=1),
+        # verify blocks that share a selection, over long sequences in 8 bits
+        _case("sparse_block_e4m3", "sparse", "e4m3", "bf16", 4, H8B, 131072, 16, top=128, first=1, group=16),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng: random.Random):
+    most = [max(work(c)[k] for c in listed()) for k in ("bytes", "flops")]
+    while True:
+        op = rng.choice(["store", "read", "attend", "attend", "sparse"])
+        pages, dtype = rng.choice(["bf16", "e4m3"]), rng.choice(["bf16", "bf16", "f32"])
+        heads = rng.choice([TINY, H8B, H8B, H14B, (8, 8, 64), (16, 1, 128)])
+        batch = 1 if rng.random() < 0.3 else _log_int(rng, 2, 64)
+        ctx = 0 if op in ("store", "attend") and rng.random() < 0.1 else _log_int(rng, 1, 131072)
+        rows = 1 if op in ("attend", "sparse") and rng.random() < 0.4 else _log_int(rng, 1, 2048)
+        if op == "read":
+            rows = ctx
+        ragged, draft = rng.random() < 0.6, op in ("attend", "sparse") and rng.random() < 0.3
+        top, first, group = 0, 0, 1
+        if op == "sparse":
+            top, first, group = _log_int(rng, 1, 256), rng.choice([0, 1, 1, 4]), min(rows, rng.choice([1, 1, 4, 8, 16]))
+            if group * (heads[0] // heads[1]) > 128:
+                continue
+        c = _case(None, op, pages, dtype, batch, heads, ctx, rows, ragged, draft, top, first, group)
+        w = work(c)
+        positions = batch * (ctx + rows)
+        scores = positions * rows * heads[0] if op != "sparse" else batch * -(-rows // group) * heads[1] * (top + 8) * 64 * 128
+        if w["bytes"] <= most[0] and w["flops"] <= most[1] and positions <= 1 << 20 and scores <= 1 << 31:
+            return c
+
+
+def _spread(n, lo, hi):
+    """n numbers of [lo, hi], the first of them hi: a fixed sequence that fills the range evenly."""
+    return [hi if i == 0 else lo + int((hi - lo + 1) * ((i * 0.6180339887498949) % 1.0)) for i in range(n)]
+
+
+def _lengths(case):
+    """Committed positions and new rows of each sequence."""
+    B, ctx, rows = case["batch"], case["ctx"], case["rows"]
+    if case["op"] == "read":
+        ends = _spread(B, ctx // 16, ctx) if case["ragged"] else [ctx] * B
+        return [0] * B, ends
+    lens = _spread(B, ctx // 16, ctx) if case["ragged"] else [ctx] * B
+    news = _spread(B, max(1, rows // 4), rows)[::-1] if case["ragged"] else [rows] * B
+    return lens, news
+
+
+def _pages_of(n):
+    return -(-n // PAGE)
+
+
+def work(case):
+    H, Hq, D = case["kv_heads"], case["q_heads"], case["dim"]
+    es = 2 if case["dtype"] == "bf16" else 4
+    ps = 2 if case["pages"] == "bf16" else 1
+    lens, news = _lengths(case)
+    stored = 2 * H * (D * ps + (1 if ps == 1 else 0))     # a position's keys and values
+    n = sum(news)
+    if case["op"] in ("store", "read"):
+        rows = 2 * n * H * D * es
+        return {"bytes": n * stored + rows * (1 if case["op"] == "read" else 2) + (n * stored if case["op"] == "store" else 0),
+                "flops": 8 * n * H * D}
+    bytes_, keys, extra = 2 * n * Hq * D * es, 0, 0
+    for p, m in zip(lens, news):
+        if case["op"] == "attend":
+            bytes_ += (p + m) * stored
+            keys += m * (p + m) if case["draft"] else m * p + m * (m + 1) // 2
+            continue
+        per = _pages_of(p + m)
+        bytes_ += per * H * (2 * D + 4)
+        # the pages of a group, read once for a key head; groups of one sequence may share pages
+        took = min(p + m, PAGE * (case["top"] + case["first"]) + (m if case["draft"] else case["group"]))
+        bytes_ += min(-(-m // case["group"]) * took, p + m) * stored
+        keys += m * took
+        extra += 4 * m * Hq * D * per
+    return {"bytes": bytes_, "flops": 4 * keys * Hq * D + extra}
+
+
+# ------------------------------------------------------------------------------------------ seeded inputs
+def _gen(seed, tag):
+    g = torch.Generator(device="cuda")
+    g.manual_seed((seed * 1000003 + tag * 8191) & 0x7FFFFFFF)
+    return g
+
+
+def _layout(case, seed):
+    """The table of the sequences' pages, in a shuffled order, and the places of the packed new rows."""
+    lens, news = _lengths(case)
+    need = [_pages_of(p + m) for p, m in zip(lens, news)]
+    n_pages, width = max(1, sum(need)), max(1, max(need))
+    order = torch.randperm(n_pages, generator=_gen(seed, 1), device="cuda").to(torch.int32)
+    table = torch.full((case["batch"], width), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, k in enumerate(need):
+        table[b, :k] = order[at:at + k]
+        at += k
+    start = torch.tensor([0] + news, device="cuda").cumsum(0).to(torch.int32)
+    return table, n_pages, torch.tensor(lens, dtype=torch.int32, device="cuda"), start
+
+
+def _places(case, which):
+    """Sequence and position of every committed position ("old"), of every new row ("new"), or of both."""
+    lens, news = _lengths(case)
+    lo = [0] * len(lens) if which != "new" else lens
+    hi = lens if which == "old" else [p + m for p, m in zip(lens, news)]
+    n = torch.tensor([b - a for a, b in zip(lo, hi)], device="cuda")
+    seq = torch.repeat_interleave(torch.arange(len(lens), device="cuda"), n)
+    begin = torch.cumsum(n, 0) - n
+    pos = torch.arange(int(n.sum()), device="cuda") - begin[seq] + torch.tensor(lo, device="cuda")[seq]
+    return seq, pos
+
+
+def _kv_rows(case, seed, tag, seq, pos):
+    """Keys or values of these positions in the rows' type: normal, the keys with a drift of their own on every page."""
+    H, D = case["kv_heads"], case["dim"]
+    x = torch.randn((len(seq), H, D), generator=_gen(seed, tag), device="cuda", dtype=torch.bfloat16)
+    if tag == 2 and len(seq):
+        width = int(pos.max()) // PAGE + 1
+        drift = torch.randn((case["batch"] * width, H, D), generator=_gen(seed, 3), device="cuda", dtype=torch.bfloat16)
+        x = x + drift[seq * width + pos // PAGE]
+    return x.to(_TYPES[case["dtype"]])
+
+
+def _quantise(x):
+    """Rows in 8 bits: codes and the rows' scales, the least power of two by which no magnitude is over 448 = 0.875 * 2^9."""
+    x = x.float()
+    m, e = torch.frexp(x.abs().amax(-1))
+    e = torch.where(m > 0, e - 9 + (m > 0.875), -100).clamp(min=-100)
+    scale = ((e + 127) << 23).to(torch.int32).view(torch.float32)
+    return (x / scale[..., None]).to(torch.float8_e4m3fn), scale
+
+
+def _bounds(lo, hi):
+    """Least and largest key of a page, rounded outwards to 8 bits, and their scale."""
+    scale = torch.maximum(lo.abs(), hi.abs()).amax(-1) / 127.0
+    by = torch.where(scale > 0, scale, 1.0)[..., None]
+    return torch.stack([torch.floor(lo / by), torch.ceil(hi / by)], -2).clamp_(-127, 127).to(torch.int8), scale
+
+
+class _Pool:
+    """The plain form's cache of a layer: [page][slot][head][dim], scales, and the bounds of each page's keys."""
+
+    def __init__(self, case, n_pages):
+        H, D = case["kv_heads"], case["dim"]
+        dev, self.e4m3 = "cuda", case["pages"] == "e4m3"
+        self.k = torch.zeros((n_pages, PAGE, H, D), dtype=_TYPES[case["pages"]], device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.ks = torch.zeros((n_pages, PAGE, H), device=dev)
+        self.vs = torch.zeros_like(self.ks)
+        self.bounds = torch.zeros((n_pages, H, 2, D), dtype=torch.int8, device=dev)
+        self.bound_scale = torch.zeros((n_pages, H), device=dev)
+
+    def write(self, page, slot, k, v):
+        for x, data, scale in ((k, self.k, self.ks), (v, self.v, self.vs)):
+            if self.e4m3:
+                code, s = _quantise(x)
+                data.view(torch.uint8)[page, slot] = code.view(torch.uint8)
+                scale[page, slot] = s
+            else:
+                data[page, slot] = x.to(data.dtype)
+
+    def values(self, which, *index):
+        data, scale = (self.k, self.ks) if which == "k" else (self.v, self.vs)
+        x = data.view(torch.uint8)[index].view(data.dtype).float() if self.e4m3 else data[index].float()
+        return x * scale[index][..., None] if self.e4m3 else x
+
+    def bound(self, page, filled):
+        """The bounds of these pages, of which so many positions are filled."""
+        k = self.values("k", page)
+        empty = (torch.arange(PAGE, device=k.device) >= filled[:, None])[..., None, None]
+        lo, hi = k.masked_fill(empty, torch.inf).amin(1), k.masked_fill(empty, -torch.inf).amax(1)
+        self.bounds[page], self.bound_scale[page] = _bounds(lo, hi)
+
+
+def prepare(case, seed):
+    table, n_pages, lens, start = _layout(case, seed)
+    new_seq, new_pos = _places(case, "new")
+    st = {"case": case, "table": table, "lens": lens, "start": start, "seq": new_seq, "pos": new_pos,
+          "scale": 1.0 / math.sqrt(case["dim"])}
+    seq, pos = _places(case, "old" if case["op"] == "store" else "both")
+    k, v = _kv_rows(case, seed, 2, seq, pos), _kv_rows(case, seed, 4, seq, pos)
+    if case["op"] == "store":
+        st["k"], st["v"] = _kv_rows(case, seed + 1, 2, new_seq, new_pos), _kv_rows(case, seed + 1, 4, new_seq, new_pos)
+    if case["op"] in ("attend", "sparse"):
+        q = torch.randn((len(new_seq), case["q_heads"], case["dim"]), generator=_gen(seed, 5), device="cuda")
+        st["q"] = (1.5 * q).to(_TYPES[case["dtype"]])
+    if own:
+        from paper_2607_05722_amd import runtime as rt
+
+        c = rt.PagedCache(kv_heads=case["kv_heads"], head_dim=case["dim"], batch=case["batch"], max_len=PAGE * table.shape[1],
+                          n_pages=n_pages, dtype=_TYPES[case["pages"]], bounds=True)
+        c.table.copy_(table)
+        ws = rt.PagesWorkspace(c, case["q_heads"], case["rows"], case["group"])
+        if len(seq):
+            # the sequences as they were read in: every row of the prefix is new
+            counts = torch.bincount(seq, minlength=case["batch"])
+            old = torch.cat([counts.new_zeros(1), counts.cumsum(0)]).to(torch.int32)
+            rt.write_pages(c, 0, k, v, ws, row_start=old, max_rows=int(counts.max()))
+        c.lengths.copy_(lens)
+        st["cache"], st["ws"] = c, ws
+    else:
+        p = _Pool(case, n_pages)
+        page = table[seq, pos // PAGE].long()
+        p.write(page, pos % PAGE, k, v)
+        ends = lens if case["op"] == "store" else lens + (start[1:] - start[:-1])
+        at = torch.arange(table.shape[1], device="cuda") * PAGE
+        filled = (ends[:, None] - at).clamp(0, PAGE)
+        p.bound(table[filled > 0].long(), filled[filled > 0])
+        st["pool"] = p
+    return st
+
+
+# ------------------------------------------------------------------------------------------ one pass
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"store": _plain_store, "read": _plain_read, "attend": _plain_attend, "sparse": _plain_sparse}[state["case"]["op"]](state)
+
+
+def _run_own(st):
+    from paper_2607_05722_amd import runtime as rt
+
+    case, c, ws, start, most = st["case"], st["cache"], st["ws"], st["start"], st["case"]["rows"]
+    if case["op"] == "store":
+        rt.write_pages(c, 0, st["k"], st["v"], ws, row_start=start, max_rows=most)
+        k, v = rt.read_pages(c, 0, len(st["seq"]), ws, dtype=st["k"].dtype, first=st["lens"], row_start=start, max_rows=most)
+        return [k, v, c.bounds[0], c.bound_scale[0]]
+    if case["op"] == "read":
+        return list(rt.read_pages(c, 0, len(st["seq"]), ws, dtype=_TYPES[case["dtype"]], row_start=start, max_rows=most))
+    mode = rt.DRAFT if case["draft"] else rt.VERIFY
+    if case["op"] == "attend":
+        return list(rt.attend_pages(c, 0, st["q"], ws, mode=mode, row_start=start, max_rows=most, want_lse=True))
+    pages = rt.select_pages(c, 0, st["q"], ws, case["top"], group=case["group"], n_first=case["first"], mode=mode,
+                            row_start=start, max_rows=most)
+    out, lse = rt.attend_pages(c, 0, st["q"], ws, mode=mode, row_start=start, max_rows=most, pages=pages,
+                               group=case["group"], want_lse=True)
+    return [pages, out, lse]
+
+
+def _plain_read(st):
+    page, slot = st["table"][st["seq"], st["pos"] // PAGE].long(), st["pos"] % PAGE
+    to = _TYPES[st["case"]["dtype"]]
+    return [st["pool"].values(x, page, slot).to(to) for x in ("k", "v")]
+
+
+def _plain_store(st):
+    p, seq, pos = st["pool"], st["seq"], st["pos"]
+    page = st["table"][seq, pos // PAGE].long()
+    p.write(page, pos % PAGE, st["k"], st["v"])
+    last = torch.zeros(p.k.shape[0], dtype=torch.int64, device=pos.device)
+    last.scatter_reduce_(0, page, pos % PAGE + 1, "amax")
+    new = torch.nonzero(last)[:, 0]
+    p.bound(new, last[new])
+    return _plain_read(st) + [p.bounds, p.bound_scale]
+
+
+def _padded(st):
+    """The place of row t of each sequence [batch][rows], which of them there are, and how many keys each sees."""
+    case, start = st["case"], st["start"].long()
+    t = torch.arange(case["rows"], device=start.device)
+    n = start[1:] - start[:-1]
+    there = t < n[:, None]
+    at = torch.where(there, start[:-1, None] + t, 0)
+    sees = st["lens"][:, None].long() + (n[:, None].expand_as(at) if case["draft"] else t + 1)
+    return at, there, torch.where(there, sees, 0)
+
+
+def _softmax_sum(s, v):
+    """Rows of scores (-inf: not seen) against values: the weighted means and the log-sum-exps."""
+    m = s.amax(-1, keepdim=True)
+    m = torch.where(torch.isinf(m), 0.0, m)
+    e = torch.exp(s - m)
+    total = e.sum(-1, keepdim=True)
+    o = torch.matmul(e, v) / torch.where(total > 0, total, 1.0)
+    return o, (m + torch.log(total))[..., 0]
+
+
+def _plain_attend(st):
+    case, q = st["case"], st["q"].float()
+    B, T, H, D = case["batch"], case["rows"], case["kv_heads"], case["dim"]
+    at, there, sees = _padded(st)
+    page = st["table"].long().clamp(min=0)
+    k, v = (st["pool"].values(x, page).reshape(B, -1, H, D).transpose(1, 2).contiguous() for x in ("k", "v"))
+    G = case["q_heads"] // H
+    qp = q[at].view(B, T, H, G, D).permute(0, 2, 1, 3, 4).reshape(B, H, T * G, D)
+    s = torch.matmul(qp, k.transpose(-1, -2)).view(B, H, T, G, -1) * st["scale"]
+    s.masked_fill_((torch.arange(s.shape[-1], device=s.device) >= sees[..., None])[:, None, :, None], -torch.inf)
+    o, lse = _softmax_sum(s.view(B, H, T * G, -1), v)
+    o = o.view(B, H, T, G, D).permute(0, 2, 1, 3, 4).reshape(B, T, -1, D)
+    lse = lse.view(B, H, T, G).permute(0, 2, 1, 3).reshape(B, T, -1)
+    return [o[there].to(st["q"].dtype), lse[there]]
+
+
+def _plain_select(st):
+    """The pages of each group [batch][groups][head][n], ascending, -1 behind the last.  Scores are whole numbers times
+    two scales, so that their order does not hang on how they are summed."""
+    case = st["case"]
+    B, T, H, D, N = case["batch"], case["rows"], case["kv_heads"], case["dim"], case["group"]
+    G, S = case["q_heads"] // H, -(-T // N)
+    at, there, sees = _padded(st)
+    q = st["q"].float()
+    qs = q.abs().amax(-1) / 127.0
+    qi = torch.round(q / torch.where(qs > 0, qs, 1.0)[..., None]).clamp_(-127, 127)
+    page = st["table"].long().clamp(min=0)
+    b = st["pool"].bounds[page].float().permute(0, 2, 3, 1, 4)          # [batch][head][least, largest][page][dim]
+    qp = qi[at].view(B, T, H, G, D).permute(0, 2, 1, 3, 4).reshape(B, H, T * G, D)
+    acc = torch.matmul(qp.clamp(min=0), b[:, :, 1].transpose(-1, -2)) + torch.matmul(qp.clamp(max=0), b[:, :, 0].transpose(-1, -2))
+    acc = acc.view(B, H, T, G, -1) * qs[at].view(B, T, H, G).permute(0, 2, 1, 3)[..., None]
+    acc = acc.masked_fill(~there[:, None, :, None, None], -torch.inf).amax(3)
+    pad = S * N - T
+    acc = torch.nn.functional.pad(acc, (0, 0, 0, pad), value=-torch.inf).view(B, H, S, N, -1).amax(3)
+    score = acc * st["pool"].bound_scale[page].transpose(1, 2)[:, :, None]
+    # the group's own pages, from its first row's position to the last one that it sees
+    p0 = (st["lens"][:, None].long() + torch.arange(S, device=q.device) * N) // PAGE
+    last = torch.nn.functional.pad(sees, (0, pad)).view(B, S, N).amax(-1)
+    used = last > 0
+    i = torch.arange(page.shape[1], device=q.device)
+    free = (i >= case["first"]) & (i < p0[..., None])
+    own_or_first = ((i < case["first"]) | (i >= p0[..., None])) & (i < ((last + PAGE - 1) // PAGE)[..., None])
+    score = score.masked_fill(~free[:, None], -torch.inf)
+    order = torch.sort(score, dim=-1, descending=True, stable=True)[1][..., :case["top"]]
+    taken = torch.zeros(score.shape, dtype=torch.bool, device=q.device).scatter_(-1, order, True) & free[:, None]
+    taken = ((taken | own_or_first[:, None]) & used[:, None, :, None]).transpose(1, 2)      # [batch][group][head][page]
+    span = T if case["draft"] else N
+    n = case["first"] + case["top"] + (span + PAGE - 2) // PAGE + 1
+    i = torch.sort(torch.where(taken, i, 1 << 30), dim=-1)[0]
+    i = torch.nn.functional.pad(i, (0, max(0, n - i.shape[-1])), value=1 << 30)[..., :n]
+    return torch.where(i < 1 << 30, i, -1).to(torch.int32)
+
+
+def _plain_sparse(st):
+    case = st["case"]
+    pages = _plain_select(st)
+    B, T, H, D, N = case["batch"], case["rows"], case["kv_heads"], case["dim"], case["group"]
+    G, S = case["q_heads"] // H, -(-T // N)
+    at, there, sees = _padded(st)
+    i = pages.long()
+    page = st["table"].long()[torch.arange(B, device=i.device)[:, None, None, None], i.clamp(min=0)].clamp(min=0)
+    head = torch.arange(H, device=i.device)[:, None]
+    slot = torch.arange(PAGE, device=i.device)
+    k, v = (st["pool"].values(x, page[..., None], slot, head[..., None]).reshape(B, S, H, -1, D) for x in ("k", "v"))
+    pos = torch.where(i[..., None] >= 0, i[..., None] * PAGE + slot, 1 << 30).reshape(B, S, H, 1, 1, -1)
+    pad = S * N - T
+    qp = torch.nn.functional.pad(st["q"].float()[at], (0, 0, 0, 0, 0, pad)).view(B, S, N, H, G, D).transpose(2, 3)
+    s = torch.matmul(qp.reshape(B, S, H, N * G, D), k.transpose(-1, -2)).view(B, S, H, N, G, -1) * st["scale"]
+    s = s.masked_fill(pos >= torch.nn.functional.pad(sees, (0, pad)).view(B, S, 1, N, 1, 1), -torch.inf)
+    o, lse = _softmax_sum(s.view(B, S, H, N * G, -1), v)
+    o = o.view(B, S, H, N, G, D).transpose(2, 3).reshape(B, S * N, -1, D)[:, :T]
+    lse = lse.view(B, S, H, N, G).transpose(2, 3).reshape(B, S * N, -1)[:, :T]
+    return [pages, o[there].to(st["q"].dtype), lse[there]]
+
+
+# ------------------------------------------------------------------------------------------ 64-bit results
+def _exact_stored(case, x):
+    """What the cache holds of these rows, in 64 bits."""
+    x = x.double()
+    if case["pages"] == "bf16":
+        return x.to(torch.bfloat16).double()
+    top = x.abs().amax(-1, keepdim=True) / 448.0
+    scale = torch.exp2(torch.ceil(torch.log2(torch.clamp(top, min=2.0 ** -100))))
+    y = x / scale
+    # e4m3: 3 bits behind the leading one, the least exponent -6
+    unit = torch.exp2(torch.floor(torch.log2(torch.clamp(y.abs(), min=2.0 ** -6))) - 3.0)
+    return torch.clamp(torch.round(y / unit) * unit, -448.0, 448.0) * scale
+
+
+def exact(case, seed):
+    lens, news = _lengths(case)
+    H, Hq, D = case["kv_heads"], case["q_heads"], case["dim"]
+    if case["op"] == "sparse" and sum(-(-m // case["group"]) for m in news) * H > 4096:
+        return None
+    rows = _places(case, "new")
+    seq, pos = _places(case, "old" if case["op"] == "store" else "both")
+    k, v = _kv_rows(case, seed, 2, seq, pos), _kv_rows(case, seed, 4, seq, pos)
+    if case["op"] == "store":
+        return [_exact_stored(case, _kv_rows(case, seed + 1, tag, *rows)) for tag in (2, 4)] + [None, None]
+    if case["op"] == "read":
+        return [_exact_stored(case, k), _exact_stored(case, v)]
+    q = (1.5 * torch.randn((len(rows[0]), Hq, D), generator=_gen(seed, 5), device="cuda")).to(_TYPES[case["dtype"]])
+    G, N, dev = Hq // H, case["group"], "cuda"
+    picked = _exact_pages(case, q, k, seq, lens, news) if case["op"] == "sparse" else None
+    outs, lses, r0, k0 = [], [], 0, 0
+    for b, (p, m) in enumerate(zip(lens, news)):
+        kb, vb = (_exact_stored(case, x[k0:k0 + p + m]) for x in (k, v))
+        o, l = torch.zeros((m, Hq, D), dtype=torch.float64, device=dev), torch.zeros((m, Hq), dtype=torch.float64, device=dev)
+        step = max(1, min(m, (1 << 25) // (p + m))) if picked is None else N
+        for t in range(0, m, step):
+            n = min(step, m - t)
+            for h in range(H):
+                key = torch.arange(p + m, device=dev) if picked is None else _positions(picked[b, t // N, h], p + m)
+                qq = q[r0 + t:r0 + t + n, h * G:(h + 1) * G].double().reshape(n * G, D)
+                s = qq @ kb[key, h].T / math.sqrt(D)
+                see = torch.full((n,), p + m, device=dev) if case["draft"] else p + t + torch.arange(n, device=dev) + 1
+                s.masked_fill_(key[None, :] >= see.repeat_interleave(G)[:, None], -torch.inf)
+                l[t:t + n, h * G:(h + 1) * G] = torch.logsumexp(s, -1).view(n, G)
+                o[t:t + n, h * G:(h + 1) * G] = (torch.softmax(s, -1) @ vb[key, h]).view(n, G, D)
+        outs.append(o)
+        lses.append(l)
+        r0, k0 = r0 + m, k0 + p + m
+    return ([] if picked is None else [picked]) + [torch.cat(outs), torch.cat(lses)]
+
+
+def _positions(pages, end):
+    i = pages[pages >= 0].long()
+    key = (i[:, None] * PAGE + torch.arange(PAGE, device=i.device)).reshape(-1)
+    return key[key < end]
+
+
+def _exact_pages(case, q, k, seq, lens, news):
+    H, D, N, T = case["kv_heads"], case["dim"], case["group"], case["rows"]
+    G = case["q_heads"] // H
+    width = max(case["first"] + case["top"] + ((T if case["draft"] else N) + PAGE - 2) // PAGE + 1, 1)
+    got = torch.full((case["batch"], -(-T // N), H, width), -1, dtype=torch.int32, device="cuda")
+    q32 = q.float()
+    qs = q32.abs().amax(-1) / 127.0
+    qi = torch.clamp(torch.round(q32 / torch.where(qs > 0, qs, 1.0)[..., None]), -127, 127).double()
+    r0 = k0 = 0
+    for b, (p, m) in enumerate(zip(lens, news)):
+        kb = _exact_stored(case, k[k0:k0 + p + m]).float()
+        n = _pages_of(p + m)
+        pages = torch.arange(n, device="cuda")
+        whole = torch.nn.functional.pad(kb, (0, 0, 0, 0, 0, n * PAGE - (p + m)), value=torch.nan).view(n, PAGE, H, D)
+        lo, hi = torch.nan_to_num(whole, nan=torch.inf).amin(1), torch.nan_to_num(whole, nan=-torch.inf).amax(1)
+        bound, scale = _bounds(lo, hi)
+        bound = bound.double()
+        for t in range(0, m, N):
+            cnt = min(N, m - t)
+            x = qi[r0 + t:r0 + t + cnt].view(cnt, H, G, D).transpose(0, 1).reshape(H, cnt * G, D)
+            u = torch.einsum("hrd,phd->hrp", x.clamp(min=0), bound[:, :, 1]) + torch.einsum("hrd,phd->hrp", x.clamp(max=0), bound[:, :, 0])
+            u = (u.float() * qs[r0 + t:r0 + t + cnt].view(cnt, H, G).transpose(0, 1).reshape(H, cnt * G, 1)).amax(1) * scale.T
+            first, end = (p + t) // PAGE, _pages_of(p + m if case["draft"] else p + t + cnt)
+            u[:, (pages < case["first"]) | (pages >= first)] = -torch.inf
+            order = torch.sort(u, dim=1, descending=True, stable=True)
+            for h in range(H):
+                best = order[1][h, :case["top"]][torch.isfinite(order[0][h, :case["top"]])]
+                always = pages[((pages < case["first"]) | (pages >= first)) & (pages < end)]
+                have = torch.sort(torch.cat([best, always]))[0]
+                got[b, t // N, h, :len(have)] = have.to(torch.int32)
+        r0, k0 = r0 + m, k0 + p + m
+    return got
