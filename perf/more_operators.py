@@ -192,9 +192,14 @@ def _quantise(x):
     return (x / scale[..., None]).to(torch.float8_e4m3fn), scale
 
 
+def _over_127(x):
+    """A division: by a plain number torch would multiply by its rounded reciprocal, which is another number now and then."""
+    return x / torch.full_like(x, 127.0)
+
+
 def _bounds(lo, hi):
     """Least and largest key of a page, rounded outwards to 8 bits, and their scale."""
-    scale = torch.maximum(lo.abs(), hi.abs()).amax(-1) / 127.0
+    scale = _over_127(torch.maximum(lo.abs(), hi.abs()).amax(-1))
     by = torch.where(scale > 0, scale, 1.0)[..., None]
     return torch.stack([torch.floor(lo / by), torch.ceil(hi / by)], -2).clamp_(-127, 127).to(torch.int8), scale
 
@@ -361,7 +366,7 @@ def _plain_select(st):
     G, S = case["q_heads"] // H, -(-T // N)
     at, there, sees = _padded(st)
     q = st["q"].float()
-    qs = q.abs().amax(-1) / 127.0
+    qs = _over_127(q.abs().amax(-1))
     qi = torch.round(q / torch.where(qs > 0, qs, 1.0)[..., None]).clamp_(-127, 127)
     page = st["table"].long().clamp(min=0)
     b = st["pool"].bounds[page].float().permute(0, 2, 3, 1, 4)          # [batch][head][least, largest][page][dim]
@@ -474,7 +479,7 @@ def _exact_pages(case, q, k, seq, lens, news):
     width = max(case["first"] + case["top"] + ((T if case["draft"] else N) + PAGE - 2) // PAGE + 1, 1)
     got = torch.full((case["batch"], -(-T // N), H, width), -1, dtype=torch.int32, device="cuda")
     q32 = q.float()
-    qs = q32.abs().amax(-1) / 127.0
+    qs = _over_127(q32.abs().amax(-1))
     qi = torch.clamp(torch.round(q32 / torch.where(qs > 0, qs, 1.0)[..., None]), -127, 127).double()
     r0 = k0 = 0
     for b, (p, m) in enumerate(zip(lens, news)):
