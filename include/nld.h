@@ -65,6 +65,9 @@ typedef enum {
                                       written, and a commit that would pass max_len stops the length there */
 #define NLD_DEV_BAD_LENGTH 0x4u    /* a negative committed length was read */
 #define NLD_DEV_MASK_LEFT 0x8u     /* nld_refresh_block found a mask token in block rows 1..k-1 */
+#define NLD_DEV_BAD_PAGE 0x10u     /* a table entry outside [0, n_pages), or a list entry outside [-1, max_pages), where a page is
+                                      needed: its positions were not written or read, and no row saw them */
+#define NLD_DEV_BAD_ROWS 0x20u     /* row_start descends, leaves [0, rows] or gives a sequence more than max_rows: the rows outside were left out */
 
 typedef enum {
     NLD_MODE_VERIFY = 0,   /* AR verify: causal within the block */
@@ -449,6 +452,105 @@ nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* r
                                   float clip_low, float clip_high, float kl_coef, const float* weight,
                                   const int32_t* last_row, float* loss, float* logp, const nld_logits* grad,
                                   void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- a paged cache, and attention over it ------------------------------------------
+ * Keys and values of ragged sequences in pages of 64 positions, in bf16 or in 8 bits, with the attention of a chunk of new
+ * tokens over them: for prompts read in by chunks of any length, for batches whose sequences share one pool of
+ * memory, for prefixes too long to be read whole at every step.
+ *
+ * Arrays (device; the contents of a page are the library's: nld_pages_write and nld_pages_read go between them and rows):
+ *   k, v         [n_layers][n_pages][n_kv_heads][64 * head_dim] of dtype, 16-byte aligned
+ *   scale        NLD_E4M3 only: uint8 [n_layers][n_pages][n_kv_heads][2][64], biased exponents of the positions' scales (keys, values)
+ *   bounds       optional: int8 [n_layers][n_pages][n_kv_heads][2][head_dim], with
+ *   bound_scale  f32 [n_layers][n_pages][n_kv_heads]: least and largest key of a page (nld_pages_select)
+ *   table        int32 [batch][max_pages]: the page of positions 64 i .. 64 i + 63 of a sequence.  Entries behind a sequence's
+ *                last position are not looked at, and may be -1.  Sequences may share pages that none of them writes.
+ *   lengths      int32 [batch]: committed positions P_b.  New row i of sequence b stands at position P_b + i.
+ * No call but the passes below changes lengths: a caller that keeps the rows of a chunk adds their number.
+ *
+ * NLD_E4M3: a row of a head is held as e4m3 numbers (4 bits of exponent, 3 of mantissa, no infinity, largest 448) times 2^e, e the
+ * least by which no finite magnitude of the row is over 448 (at least -100), rounded to nearest, ties to even; NaN and
+ * infinities become NaN (and what would round to 2^128 is 1.875 * 2^127).  Stored values are exact in bf16.
+ * Bounds: the least and the largest stored key of each dim among the page's positions up to the last one written, divided by
+ * bound_scale = largest magnitude / 127, rounded down and up; bound_scale is +inf where a key is not finite. */
+#define NLD_E4M3 2
+#define NLD_PAGE 64
+typedef struct {
+    void* k;
+    void* v;
+    uint8_t* scale;
+    int8_t* bounds;
+    float* bound_scale;
+    int32_t dtype;           /* NLD_BF16 or NLD_E4M3 */
+    int32_t n_layers, n_pages, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+    const int32_t* table;
+    int32_t* lengths;
+    int32_t batch, max_pages;
+} nld_pages;
+
+/* The new rows of all sequences, packed: those of sequence b are rows row_start[b] .. row_start[b + 1] - 1 (device int32
+ * [batch + 1], ascending; rows before, between and behind them are neither read nor written), at most max_rows.
+ * row_start NULL: max_rows of every sequence, rows = batch * max_rows. */
+typedef struct {
+    int32_t rows, max_rows;
+    const int32_t* row_start;
+} nld_chunk;
+
+/* Rows [rows][heads][head_dim] of any strides (in elements), head_dim adjacent.  Fastest where every row of a head is 16-byte aligned. */
+typedef struct {
+    void* data;
+    int32_t dtype;           /* NLD_F32 or NLD_BF16 */
+    int64_t row_stride, head_stride;   /* in [0, 2^38) */
+} nld_heads;
+
+/* Workspace of the calls below for chunks of up to max_rows rows per sequence and selections of groups of at least `group`
+ * tokens (0: none), on the current device; to be initialized with nld_workspace_init once.  0 for what the calls refuse. */
+size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int32_t max_rows, int32_t group);
+
+/* Writes the chunk's keys and values into the pages, at positions P_b + i, and updates the bounds (where given) of the pages it touches.
+ * A row's stored values hang on that row alone.  Two sequences must not write one page.
+ * Device errors: CAPACITY (rows past the table are not written), BAD_LENGTH, BAD_PAGE, BAD_ROWS.
+ * Errors: INVALID_ARG (NULL pointer, sizes < 1, max_rows > rows, a layer outside [0, n_layers), an unknown dtype, 8-bit pages
+ * without scale, bounds without bound_scale, misaligned data, a stride out of range, k and v of two dtypes), SHAPE (head_dim not 64 or
+ * 128, max_pages or rows over 2^24, more rows than one launch takes), CAPACITY (workspace). */
+nld_status nld_pages_write(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* k, const nld_heads* v,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* Reads positions first[b] + i back into the chunk's rows (first: int32 [batch]; NULL: from 0), committed or not, in f32 or bf16,
+ * both exact.  k and v must not overlap each other.  Device errors: as above (a negative first: BAD_LENGTH); what is not read is left as it was.
+ * Errors: as above, INVALID_ARG for rows that overlap each other. */
+nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const int32_t* first, const nld_heads* k,
+                          const nld_heads* v, void* workspace, size_t ws_bytes, void* stream);
+
+/* Attention of the chunk's queries q [rows][n_q_heads][head_dim] over the pages; the chunk's own keys and values have been written before.
+ * Row i of sequence b sees the positions below P_b + i + 1 (NLD_MODE_VERIFY), or in NLD_MODE_DRAFT, from row bidir_from on, all
+ * below P_b + n_b; query head h reads KV head h / (n_q_heads / n_kv_heads):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse (optional) f32 [rows][n_q_heads] = log sum_j exp(scale * q . k_j).
+ * q and out are both bf16 or both f32 (f32 queries and weights are carried in three bf16 pieces, sums are f32 throughout).
+ * A row that sees nothing gets 0 and -inf.  What a row does not see does not reach it, whatever it is.
+ * list (optional): only positions of the pages in the list of the row's group are seen: int32 [batch][ceil(max_rows / group)]
+ * [n_kv_heads][n_list], places in the sequence's table, -1: none; each of them counts as often as it stands there.  Group j holds tokens
+ * j * group .. of its sequence.  n_list and group are not looked at without a list.
+ * Device errors: as nld_pages_write.  Errors: as nld_pages_write, INVALID_ARG for an unknown mode, bidir_from outside [0, max_rows], a
+ * scale that is not finite, q and out of two dtypes or overlapping, n_list < 1, group < 1, SHAPE for n_q_heads not a multiple of n_kv_heads, or
+ * group * (n_q_heads / n_kv_heads) > 128. */
+nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* q, int32_t n_q_heads,
+                            float scale, int32_t mode, int32_t bidir_from, const int32_t* list, int32_t n_list, int32_t group,
+                            const nld_heads* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/* The pages that each group of `group` adjacent tokens of a sequence attends to, for each KV head: the n_first first ones, the group's
+ * own (from that of its first token's position to the last that one of its rows sees) and the n_top others with the largest scores, ascending, -1 behind
+ * the last: list int32 [batch][ceil(max_rows / group)][n_kv_heads][n_list], n_list at least nld_pages_list_len.
+ * With qs = max |q| / 127 and qi = q / qs rounded to nearest for each row and head,
+ *   score of a page = bound_scale * max over the group's rows and query heads of qs * sum_d max(qi_d * least_d, qi_d * largest_d),
+ * sums in whole numbers, the products in f32; the lower page first among equal scores.  A page with a key that is not finite
+ * scores +inf; a row that is not finite takes no part.
+ * Device errors: as nld_pages_write.  Errors: as nld_pages_attend, INVALID_ARG for pages without bounds, a NULL list, n_top or n_first < 0,
+ * n_list too small. */
+int32_t nld_pages_list_len(int32_t max_rows, int32_t group, int32_t n_top, int32_t n_first, int32_t mode);
+nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* q, int32_t n_q_heads,
+                            int32_t n_top, int32_t n_first, int32_t group, int32_t mode, int32_t bidir_from, int32_t* list, int32_t n_list,
+                            void* workspace, size_t ws_bytes, void* stream);
 
 /* ---- tracing aid -------------------------------------------------------------
  * While enabled, every kernel launch made by the block-decode calls records a

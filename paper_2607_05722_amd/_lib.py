@@ -23,6 +23,8 @@ NLD_DEV_BAD_TOKEN = 0x1
 NLD_DEV_CAPACITY = 0x2
 NLD_DEV_BAD_LENGTH = 0x4
 NLD_DEV_MASK_LEFT = 0x8
+NLD_DEV_BAD_PAGE = 0x10
+NLD_DEV_BAD_ROWS = 0x20
 
 NLD_PACK_LINEAR = 0
 NLD_PACK_QKV = 1
@@ -36,11 +38,14 @@ EXPORTED = [
     "nld_decode_steps", "nld_choose_block", "nld_quad_workspace_bytes", "nld_quad_step",
     "nld_read_device_status", "nld_trace_enable", "nld_trace_read", "nld_verify_accept_noalloc",
     "nld_hbm_read_probe", "nld_logits_workspace_bytes", "nld_top_logits", "nld_distill_from_logits",
-    "nld_policy_from_logits",
+    "nld_policy_from_logits", "nld_pages_list_len", "nld_pages_workspace_bytes", "nld_pages_write", "nld_pages_read",
+    "nld_pages_attend", "nld_pages_select",
 ]
 
 NLD_F32 = 0
 NLD_BF16 = 1
+NLD_E4M3 = 2
+NLD_PAGE = 64
 NLD_TOP_MAX = 512
 
 NLD_NOALLOC_SCRATCH_BYTES = 64 << 20
@@ -78,6 +83,20 @@ class Teacher(ctypes.Structure):
 
 class Rollout(ctypes.Structure):
     _fields_ = [("actions", c_vp), ("advantage", c_vp), ("old_logp", c_vp), ("ref_logp", c_vp)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", c_vp), ("v", c_vp), ("scale", c_vp), ("bounds", c_vp), ("bound_scale", c_vp), ("dtype", c_i32),
+                ("n_layers", c_i32), ("n_pages", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32), ("table", c_vp),
+                ("lengths", c_vp), ("batch", c_i32), ("max_pages", c_i32)]
+
+
+class Chunk(ctypes.Structure):
+    _fields_ = [("rows", c_i32), ("max_rows", c_i32), ("row_start", c_vp)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("dtype", c_i32), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class NLDError(RuntimeError):
@@ -178,6 +197,20 @@ def load(path: str = None):
     L.nld_policy_from_logits.restype = c_i32
     L.nld_policy_from_logits.argtypes = [P(Logits), P(Rollout), c_f32, c_f32, c_f32, c_f32, c_vp, c_vp, c_vp, c_vp,
                                          P(Logits), c_vp, c_sz, c_vp]
+    L.nld_pages_list_len.restype = c_i32
+    L.nld_pages_list_len.argtypes = [c_i32] * 5
+    L.nld_pages_workspace_bytes.restype = c_sz
+    L.nld_pages_workspace_bytes.argtypes = [P(Pages), c_i32, c_i32, c_i32]
+    L.nld_pages_write.restype = c_i32
+    L.nld_pages_write.argtypes = [P(Pages), c_i32, P(Chunk), P(Heads), P(Heads), c_vp, c_sz, c_vp]
+    L.nld_pages_read.restype = c_i32
+    L.nld_pages_read.argtypes = [P(Pages), c_i32, P(Chunk), c_vp, P(Heads), P(Heads), c_vp, c_sz, c_vp]
+    L.nld_pages_attend.restype = c_i32
+    L.nld_pages_attend.argtypes = [P(Pages), c_i32, P(Chunk), P(Heads), c_i32, c_f32, c_i32, c_i32, c_vp, c_i32, c_i32, P(Heads),
+                                   c_vp, c_vp, c_sz, c_vp]
+    L.nld_pages_select.restype = c_i32
+    L.nld_pages_select.argtypes = [P(Pages), c_i32, P(Chunk), P(Heads), c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp,
+                                   c_sz, c_vp]
     _lib = L
     return L
 

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnld.so")
-SOURCES = ["kernels.hip", "logits.hip", "api.hip", "probe.hip"]
+SOURCES = ["kernels.hip", "logits.hip", "pages.hip", "api.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

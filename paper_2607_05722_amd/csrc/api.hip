@@ -814,6 +814,150 @@ nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperat
     return NLD_OK;
 }
 
+// ---------------------------------------------------------------- paged cache
+constexpr int MAX_PAGE_WGS = 1 << 23;    // workgroups of 256 threads in one launch
+constexpr int MAX_SEQ_PAGES = 1 << 24;   // 2^30 positions
+constexpr int MAX_CHUNK_ROWS = 1 << 24;
+
+nld_status check_pages(const nld_pages* c, int layer) {
+    if (!c || !c->k || !c->v || !c->table || !c->lengths) return fail(NLD_ERR_INVALID_ARG, "pages or one of its pointers is NULL");
+    if (c->dtype != NLD_BF16 && c->dtype != NLD_E4M3) return fail(NLD_ERR_INVALID_ARG, "pages: dtype must be NLD_BF16 or NLD_E4M3");
+    if (c->dtype == NLD_E4M3 && !c->scale) return fail(NLD_ERR_INVALID_ARG, "pages: 8-bit pages need their scales");
+    if (!c->bounds != !c->bound_scale) return fail(NLD_ERR_INVALID_ARG, "pages: bounds and bound_scale go together");
+    if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1)
+        return fail(NLD_ERR_INVALID_ARG, "pages: sizes must be positive");
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(NLD_ERR_SHAPE, "pages: head_dim must be 64 or 128");
+    if (c->max_pages > MAX_SEQ_PAGES) return fail(NLD_ERR_SHAPE, "pages: max_pages (%d) exceeds %d", c->max_pages, MAX_SEQ_PAGES);
+    if (layer < 0 || layer >= c->n_layers) return fail(NLD_ERR_INVALID_ARG, "layer must be in [0, %d) (got %d)", c->n_layers, layer);
+    if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->scale | (uintptr_t)c->bounds) % 16 || (uintptr_t)c->bound_scale % 4)
+        return fail(NLD_ERR_INVALID_ARG, "pages: arrays must be 16-byte aligned");
+    return NLD_OK;
+}
+
+PageCache page_layer(const nld_pages* c, int layer) {
+    const size_t heads = (size_t)layer * c->n_pages * c->n_kv_heads, page = (size_t)64 * c->head_dim * (c->dtype == NLD_BF16 ? 2 : 1);
+    PageCache p{};
+    p.k = (char*)c->k + heads * page;
+    p.v = (char*)c->v + heads * page;
+    p.scale = c->dtype == NLD_E4M3 ? (uint8_t*)c->scale + heads * 128 : nullptr;
+    p.bounds = c->bounds ? (int8_t*)c->bounds + heads * 2 * c->head_dim : nullptr;
+    p.bound_scale = c->bounds ? c->bound_scale + heads : nullptr;
+    p.e4m3 = c->dtype == NLD_E4M3;
+    p.n_pages = c->n_pages;
+    p.n_kv_heads = c->n_kv_heads;
+    p.head_dim = c->head_dim;
+    p.table = c->table;
+    p.lengths = c->lengths;
+    p.batch = c->batch;
+    p.max_pages = c->max_pages;
+    return p;
+}
+
+nld_status check_chunk(const nld_pages* c, const nld_chunk* ch) {
+    if (!ch) return fail(NLD_ERR_INVALID_ARG, "chunk is NULL");
+    if (ch->rows < 1 || ch->max_rows < 1 || ch->max_rows > ch->rows)
+        return fail(NLD_ERR_INVALID_ARG, "chunk: max_rows must be in [1, rows] (got %d of %d)", ch->max_rows, ch->rows);
+    if (!ch->row_start && (long long)ch->max_rows * c->batch != ch->rows)
+        return fail(NLD_ERR_INVALID_ARG, "chunk: without row_start, rows (%d) must be batch * max_rows (%d * %d)", ch->rows, c->batch, ch->max_rows);
+    if (ch->rows > MAX_CHUNK_ROWS) return fail(NLD_ERR_SHAPE, "chunk: %d rows exceed %d", ch->rows, MAX_CHUNK_ROWS);
+    return NLD_OK;
+}
+
+// elements from the first one to past the last one
+long long heads_extent(const nld_heads* x, int rows, int heads, int dim) {
+    return (rows - 1) * x->row_stride + (heads - 1) * x->head_stride + dim;
+}
+
+// out: rows and heads must be apart from each other
+nld_status check_heads(const nld_heads* x, const char* what, int rows, int heads, int dim, bool out) {
+    if (!x || !x->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
+    if (x->dtype != NLD_F32 && x->dtype != NLD_BF16) return fail(NLD_ERR_INVALID_ARG, "%s: dtype must be NLD_F32 or NLD_BF16", what);
+    if (x->row_stride < 0 || x->head_stride < 0 || x->row_stride >> 38 || x->head_stride >> 38)
+        return fail(NLD_ERR_INVALID_ARG, "%s: strides must be in [0, 2^38)", what);
+    if ((uintptr_t)x->data % (x->dtype == NLD_BF16 ? 2 : 4)) return fail(NLD_ERR_INVALID_ARG, "%s: data is not aligned to its type", what);
+    if (out) {
+        const long long rs = rows > 1 ? x->row_stride : LLONG_MAX, hs = heads > 1 ? x->head_stride : LLONG_MAX;
+        const long long inner = std::min(rs, hs), outer = std::max(rs, hs), n_inner = rs <= hs ? rows : heads;
+        if (inner < dim || (outer != LLONG_MAX && outer < (n_inner - 1) * inner + dim))
+            return fail(NLD_ERR_INVALID_ARG, "%s: its rows overlap each other", what);
+    }
+    return NLD_OK;
+}
+
+HeadRows head_rows(const nld_heads* x) { return HeadRows{x->data, x->dtype == NLD_F32, 0, x->row_stride, x->head_stride}; }
+PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows, c->row_start}; }
+
+// The attention's plan and workspace: the status word, then the parts of units that workgroups share, or a selection's scores.
+// Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
+// registers) and are what hides the loads' latency.
+struct PagesPlan {
+    int row_tiles, n_blk, grid, slices;
+    size_t part_ml, total;
+};
+
+bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, PagesPlan* out) {
+    PagesPlan p{};
+    const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
+    p.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    const long long blocks = group ? cdiv(max_rows, group) : (rows + 32 * p.row_tiles - 1) / (32 * p.row_tiles);
+    if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
+    p.n_blk = (int)blocks;
+    p.grid = 2 * device_cus();
+    // the second launch: a few thousand workgroups at most, and one where units are that many
+    const int turns = cdiv((int)std::min<long long>(rows, 32 * p.row_tiles), 1024 / head_dim);
+    p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
+    const size_t part_rows = (size_t)2 * p.grid * 32 * p.row_tiles;
+    p.part_ml = 256 + part_rows * head_dim * 4;
+    p.total = align256(p.part_ml + part_rows * 8);
+    *out = p;
+    return true;
+}
+
+size_t score_bytes(const nld_pages* c, int max_rows, int group) {
+    return (size_t)c->batch * cdiv(max_rows, group) * c->n_kv_heads * c->max_pages * 4;
+}
+
+nld_status check_mode(int mode, int bidir_from, int max_rows) {
+    if (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT) return fail(NLD_ERR_INVALID_ARG, "mode must be 0 or 1");
+    if (bidir_from < 0 || bidir_from > max_rows) return fail(NLD_ERR_INVALID_ARG, "bidir_from must be in [0, max_rows]");
+    return NLD_OK;
+}
+
+nld_status check_group(const nld_pages* c, int n_q_heads, int group) {
+    if (group < 1) return fail(NLD_ERR_INVALID_ARG, "group must be >= 1 (got %d)", group);
+    if ((long long)group * (n_q_heads / c->n_kv_heads) > PAGES_GROUP_ROWS)
+        return fail(NLD_ERR_SHAPE, "group * (n_q_heads / n_kv_heads) = %lld exceeds %d", (long long)group * (n_q_heads / c->n_kv_heads), PAGES_GROUP_ROWS);
+    return NLD_OK;
+}
+
+nld_status check_q_heads(const nld_pages* c, int n_q_heads) {
+    if (n_q_heads < 1 || n_q_heads % c->n_kv_heads)
+        return fail(NLD_ERR_SHAPE, "n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", n_q_heads, c->n_kv_heads);
+    return NLD_OK;
+}
+
+// the launch of an attention: what does not hang on where queries come from and outputs go
+PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_heads, int mode, int bidir_from, float scale, const PagesPlan& p, void* ws,
+                         size_t off) {
+    PagesAttnArgs a{};
+    a.c = c;
+    a.ch = ch;
+    a.group_heads = group_heads;
+    a.draft = mode == NLD_MODE_DRAFT;
+    a.bidir_from = bidir_from;
+    a.scale_log2 = (float)(LOG2E * (double)scale);
+    a.row_tiles = p.row_tiles;
+    a.n_blk = p.n_blk;
+    a.n_entries = c.batch * p.n_blk;
+    a.grid = p.grid;
+    a.slices = p.slices;
+    a.least_steps = 4 / p.row_tiles;
+    a.part_o = at<float>(ws, off + 256);
+    a.part_ml = at<float>(ws, off + p.part_ml);
+    a.status = at<uint32_t>(ws, 0);
+    return a;
+}
+
 }  // namespace
 
 // =====================================================================================
@@ -1259,6 +1403,142 @@ nld_status nld_policy_from_logits(const nld_logits* policy, const nld_rollout* r
     a.clip_high = clip_high;
     a.kl_coef = kl_coef;
     HIP_TRY(launch_loss(LOSS_POLICY, a, (hipStream_t)stream));
+    return NLD_OK;
+}
+
+int32_t nld_pages_list_len(int32_t max_rows, int32_t group, int32_t n_top, int32_t n_first, int32_t mode) {
+    if (max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 1 || group > MAX_CHUNK_ROWS || n_top < 0 || n_first < 0 ||
+        n_top > MAX_SEQ_PAGES || n_first > MAX_SEQ_PAGES || (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT))
+        return 0;
+    return n_first + n_top + ((mode == NLD_MODE_DRAFT ? max_rows : group) + 62) / 64 + 1;
+}
+
+size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int32_t max_rows, int32_t group) {
+    if (check_pages(pages, 0) != NLD_OK || check_q_heads(pages, n_q_heads) != NLD_OK || max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 0)
+        return 0;
+    PagesPlan p;
+    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, max_rows, 0, &p)) return 0;
+    size_t n = p.total;
+    if (group) {
+        if (check_group(pages, n_q_heads, group) != NLD_OK ||
+            !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, max_rows, group, &p))
+            return 0;
+        n = std::max(n, align256(256 + score_bytes(pages, max_rows, group)));
+    }
+    return n;
+}
+
+nld_status nld_pages_write(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* k, const nld_heads* v, void* workspace,
+                           size_t ws_bytes, void* stream) {
+    nld_status st = check_pages(pages, layer);
+    if (st == NLD_OK) st = check_chunk(pages, chunk);
+    if (st == NLD_OK) st = check_heads(k, "k", chunk->rows, pages->n_kv_heads, pages->head_dim, false);
+    if (st == NLD_OK) st = check_heads(v, "v", chunk->rows, pages->n_kv_heads, pages->head_dim, false);
+    if (st != NLD_OK) return st;
+    if (k->dtype != v->dtype) return fail(NLD_ERR_INVALID_ARG, "k and v must have one dtype");
+    if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
+    if (ws_bytes < 256) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs 256", ws_bytes);
+    if (((long long)(chunk->max_rows + 62) / 64 + 1) * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS)
+        return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
+    HIP_TRY(launch_pages_write(page_layer(pages, layer), head_rows(k), head_rows(v), nullptr, nullptr, page_chunk(chunk), at<uint32_t>(workspace, 0),
+                               (hipStream_t)stream));
+    return NLD_OK;
+}
+
+nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const int32_t* first, const nld_heads* k, const nld_heads* v,
+                          void* workspace, size_t ws_bytes, void* stream) {
+    nld_status st = check_pages(pages, layer);
+    if (st == NLD_OK) st = check_chunk(pages, chunk);
+    if (st == NLD_OK) st = check_heads(k, "k", chunk->rows, pages->n_kv_heads, pages->head_dim, true);
+    if (st == NLD_OK) st = check_heads(v, "v", chunk->rows, pages->n_kv_heads, pages->head_dim, true);
+    if (st != NLD_OK) return st;
+    if (k->dtype != v->dtype || k->data == v->data) return fail(NLD_ERR_INVALID_ARG, "k and v must have one dtype and be apart");
+    if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
+    if (ws_bytes < 256) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs 256", ws_bytes);
+    if (((long long)(chunk->max_rows + 62) / 64 + 1) * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS)
+        return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
+    HIP_TRY(launch_pages_read(page_layer(pages, layer), head_rows(k), head_rows(v), page_chunk(chunk), first, at<uint32_t>(workspace, 0),
+                              (hipStream_t)stream));
+    return NLD_OK;
+}
+
+nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* q, int32_t n_q_heads, float scale,
+                            int32_t mode, int32_t bidir_from, const int32_t* list, int32_t n_list, int32_t group, const nld_heads* out, float* lse,
+                            void* workspace, size_t ws_bytes, void* stream) {
+    nld_status st = check_pages(pages, layer);
+    if (st == NLD_OK) st = check_chunk(pages, chunk);
+    if (st == NLD_OK) st = check_q_heads(pages, n_q_heads);
+    if (st == NLD_OK) st = check_heads(q, "q", chunk->rows, n_q_heads, pages->head_dim, false);
+    if (st == NLD_OK) st = check_heads(out, "out", chunk->rows, n_q_heads, pages->head_dim, true);
+    if (st == NLD_OK) st = check_mode(mode, bidir_from, chunk->max_rows);
+    if (st != NLD_OK) return st;
+    if (!(fabsf(scale) < INFINITY)) return fail(NLD_ERR_INVALID_ARG, "scale must be finite");
+    if (q->dtype != out->dtype) return fail(NLD_ERR_INVALID_ARG, "q and out must have one dtype");
+    {
+        const size_t es = q->dtype == NLD_BF16 ? 2 : 4;
+        const char *q0 = (const char*)q->data, *q1 = q0 + heads_extent(q, chunk->rows, n_q_heads, pages->head_dim) * es;
+        const char *o0 = (const char*)out->data, *o1 = o0 + heads_extent(out, chunk->rows, n_q_heads, pages->head_dim) * es;
+        if (o0 < q1 && q0 < o1) return fail(NLD_ERR_INVALID_ARG, "out overlaps q");
+    }
+    if (list) {
+        st = check_group(pages, n_q_heads, group);
+        if (st != NLD_OK) return st;
+        if (n_list < 1 || n_list > MAX_SEQ_PAGES) return fail(NLD_ERR_INVALID_ARG, "n_list must be in [1, %d] (got %d)", MAX_SEQ_PAGES, n_list);
+    }
+    if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
+    PagesPlan p;
+    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, chunk->max_rows, list ? group : 0, &p))
+        return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
+    if (ws_bytes < p.total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, p.total);
+    PagesAttnArgs a = pages_args(page_layer(pages, layer), page_chunk(chunk), n_q_heads / pages->n_kv_heads, mode, bidir_from, scale, p, workspace, 0);
+    a.q = head_rows(q);
+    a.out = head_rows(out);
+    a.list = list;
+    a.n_list = n_list;
+    a.group = group;
+    a.lse = lse;
+    HIP_TRY(launch_pages_attend(a, (hipStream_t)stream));
+    return NLD_OK;
+}
+
+nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* q, int32_t n_q_heads, int32_t n_top,
+                            int32_t n_first, int32_t group, int32_t mode, int32_t bidir_from, int32_t* list, int32_t n_list, void* workspace,
+                            size_t ws_bytes, void* stream) {
+    nld_status st = check_pages(pages, layer);
+    if (st == NLD_OK) st = check_chunk(pages, chunk);
+    if (st == NLD_OK) st = check_q_heads(pages, n_q_heads);
+    if (st == NLD_OK) st = check_heads(q, "q", chunk->rows, n_q_heads, pages->head_dim, false);
+    if (st == NLD_OK) st = check_mode(mode, bidir_from, chunk->max_rows);
+    if (st == NLD_OK) st = check_group(pages, n_q_heads, group);
+    if (st != NLD_OK) return st;
+    if (!pages->bounds) return fail(NLD_ERR_INVALID_ARG, "a selection needs the pages' bounds");
+    if (!list) return fail(NLD_ERR_INVALID_ARG, "list is NULL");
+    if (n_top < 0 || n_first < 0) return fail(NLD_ERR_INVALID_ARG, "n_top and n_first must be >= 0");
+    const int need = nld_pages_list_len(chunk->max_rows, group, n_top, n_first, mode);
+    if (need < 1) return fail(NLD_ERR_SHAPE, "n_top (%d) or n_first (%d) exceeds %d", n_top, n_first, MAX_SEQ_PAGES);
+    if (n_list < need) return fail(NLD_ERR_INVALID_ARG, "n_list is %d, this call needs %d", n_list, need);
+    const int n_groups = cdiv(chunk->max_rows, group);
+    if ((long long)pages->batch * n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
+        return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
+    if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
+    const size_t bytes = align256(256 + (n_top ? score_bytes(pages, chunk->max_rows, group) : 0));
+    if (ws_bytes < bytes) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, bytes);
+    PagesSelectArgs a{};
+    a.c = page_layer(pages, layer);
+    a.ch = page_chunk(chunk);
+    a.q = head_rows(q);
+    a.group_heads = n_q_heads / pages->n_kv_heads;
+    a.draft = mode == NLD_MODE_DRAFT;
+    a.bidir_from = bidir_from;
+    a.n_top = n_top;
+    a.n_first = n_first;
+    a.group = group;
+    a.n_groups = n_groups;
+    a.n_list = n_list;
+    a.scores = at<float>(workspace, 256);
+    a.list = list;
+    a.status = at<uint32_t>(workspace, 0);
+    HIP_TRY(launch_pages_select(a, (hipStream_t)stream));
     return NLD_OK;
 }
 

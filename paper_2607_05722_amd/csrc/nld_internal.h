@@ -365,6 +365,64 @@ struct LossArgs {
     uint2* saved;                // chunks > 1: the entries' logits (bits, 1: it counts) [rows][n_top]
 };
 
+// ---------------------------------------------------------------- paged cache (pages.hip)
+// One layer of a paged cache; arrays as in nld_pages.
+struct PageCache {
+    void* k;
+    void* v;
+    uint8_t* scale;
+    int8_t* bounds;
+    float* bound_scale;
+    int e4m3, n_pages, n_kv_heads, head_dim;
+    const int32_t* table;
+    const int32_t* lengths;
+    int batch, max_pages;
+};
+
+// Rows [row][head][head_dim] in f32 or bf16, strides in elements.  vec: every row of a head is 16-byte aligned.
+struct HeadRows {
+    void* data;
+    int f32, vec;
+    long long row_stride, head_stride;
+};
+
+struct PageChunk {
+    int rows, max_rows;
+    const int32_t* row_start;   // NULL: max_rows of every sequence
+};
+
+struct PagesAttnArgs {
+    PageCache c;
+    PageChunk ch;
+    HeadRows q, out;
+    const uint16_t* q_split;    // a pass: split queries (q_index with q_row_tiles) and split output (split_index with o_ksteps)
+    uint16_t* o_split;
+    int q_row_tiles, o_ksteps, plain_o;
+    int group_heads;            // query heads per KV head
+    int draft, bidir_from;
+    float scale_log2;
+    const int32_t* list;        // optional [batch][n_blk][kv head][n_list]: the pages of each group of tokens
+    int n_list, group;
+    float* lse;                 // optional [rows][query head]
+    int row_tiles, n_blk, n_entries;   // 32-row tiles of a workgroup (1, 2, 4); blocks of rows per sequence, of all
+    int grid, least_steps, slices;
+    float* part_o;              // [2 * grid][32 * row_tiles][head_dim]
+    float* part_ml;             // [2 * grid][32 * row_tiles][2]
+    uint32_t* status;
+};
+
+constexpr int PAGES_GROUP_ROWS = 128;   // rows (tokens x query heads of a KV head) that share a list of pages
+
+struct PagesSelectArgs {
+    PageCache c;
+    PageChunk ch;
+    HeadRows q;
+    int group_heads, draft, bidir_from, n_top, n_first, group, n_groups, n_list, chunks;
+    float* scores;              // [batch][n_groups][kv head][max_pages]
+    int32_t* list;              // [batch][n_groups][kv head][n_list]
+    uint32_t* status;
+};
+
 // ---------------------------------------------------------------- launch tracing (api.hip)
 // While tracing is on, returns true with a fresh pair of events for the next launch, which
 // then records them on its own dispatch (start and end of the kernel itself).
@@ -417,5 +475,14 @@ RowPlan plan_top(int bf16, int n_rows, int vocab, int n_top, int cus);
 RowPlan plan_loss(int bf16, int n_rows, int vocab, int n_top, bool grad, int cus);
 hipError_t launch_top(const TopArgs& a, hipStream_t s);
 hipError_t launch_loss(LossKind kind, const LossArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- launchers (pages.hip)
+// blk_k, blk_v: the split block K/V of a pass in the place of k and v
+hipError_t launch_pages_write(const PageCache& c, const HeadRows& k, const HeadRows& v, const uint16_t* blk_k, const uint16_t* blk_v,
+                              const PageChunk& ch, uint32_t* status, hipStream_t s);
+hipError_t launch_pages_read(const PageCache& c, const HeadRows& k, const HeadRows& v, const PageChunk& ch, const int32_t* first, uint32_t* status,
+                             hipStream_t s);
+hipError_t launch_pages_attend(const PagesAttnArgs& a, hipStream_t s);
+hipError_t launch_pages_select(const PagesSelectArgs& a, hipStream_t s);
 
 }  // namespace nld

@@ -1,0 +1,1194 @@
+// Paged key/value cache: writing and reading rows, the attention of a chunk of new rows over the pages, and the selection
+// of pages by a cheap score.
+//
+// A page holds 64 positions of one layer: per KV head the keys, then (another array) the values, in the order in which the
+// matrix instruction takes them, so that a wavefront's operand is one contiguous load of 16 bytes per lane and nothing is
+// shuffled on the way.  Keys are the A operand of S^T = K Q^T (32 keys x 16 dims a step), values that of
+// O^T = V^T P^T (32 dims x 16 keys a step).  The result of the first product leaves a lane with one row and the keys
+// 8j + 4 hf + i of 32 (hf = lane / 32; i, j = 0..3), so the values' steps take their keys in that order and the weights P
+// need no exchange between lanes.
+#include <type_traits>
+
+#include "nld_internal.h"
+
+namespace nld {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(16))) int i32x16_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+
+namespace {
+
+// status bits, as in nld.h
+constexpr uint32_t ST_CAPACITY = 2u, ST_LENGTH = 4u, ST_PAGE = 16u, ST_ROWS = 32u;
+
+__device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) { atomicOr(status, bit); }
+
+// ---------------------------------------------------------------- places in a page
+// Element offset of (key, dim) in a head's keys, and of the 8 elements that a lane takes of them in one step.  Both
+// types: blocks of 64 lanes (32 keys x 2), a lane's elements adjacent, 8 for bf16 and 16 (two steps) for e4m3.
+template <int D, bool E4M3>
+__device__ __forceinline__ int key_at(int key, int d) {
+    const int blk = (key >> 5) * (D / 32) + (d >> 5), lane = ((d >> 4) & 1) * 32 + (key & 31), f = (d >> 3) & 1, e = d & 7;
+    return E4M3 ? blk * 1024 + lane * 16 + f * 8 + e : (blk * 2 + f) * 512 + lane * 8 + e;
+}
+// of (key, dim) in a head's values
+template <int D, bool E4M3>
+__device__ __forceinline__ int value_at(int key, int d) {
+    const int k = key & 31, j = k >> 3, hf = (k >> 2) & 1, s = j >> 1, e = (j & 1) * 4 + (k & 3);
+    const int blk = (key >> 5) * (D / 32) + (d >> 5), lane = hf * 32 + (d & 31);
+    return E4M3 ? blk * 1024 + lane * 16 + s * 8 + e : (blk * 2 + s) * 512 + lane * 8 + e;
+}
+// key of element e of a lane's values in step s of 32 keys
+__device__ __forceinline__ int value_key(int s, int hf, int e) { return 16 * s + 4 * hf + (e & 3) + ((e & 4) << 1); }
+
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// two e4m3 numbers (the low or the high half of a word) times a power of two -> bf16 pair, exact
+template <bool HI>
+__device__ __forceinline__ uint32_t pair_bf16(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, HI));
+}
+__device__ __forceinline__ uint4 eight_bf16(uint32_t a, uint32_t b, float scale) {
+    return uint4{pair_bf16<false>(a, scale), pair_bf16<true>(a, scale), pair_bf16<false>(b, scale), pair_bf16<true>(b, scale)};
+}
+
+__device__ __forceinline__ f32x16_t mfma_32x32x16(uint4 a, uint4 b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- rows of a chunk
+struct SeqRows {
+    int r0, n;   // first packed row, rows
+};
+__device__ __forceinline__ SeqRows seq_rows(const PageChunk& c, int b, uint32_t* status) {
+    if (!c.row_start) return SeqRows{b * c.max_rows, c.max_rows};
+    const int s = c.row_start[b], e = c.row_start[b + 1];
+    const int r0 = min(max(s, 0), c.rows), n = max(0, min(min(e, c.rows) - r0, c.max_rows));
+    if (status && (r0 != s || r0 + n != e)) flag(status, ST_ROWS);
+    return SeqRows{r0, n};
+}
+
+// committed length; of a block of new rows, no position past what the table has room for
+__device__ __forceinline__ int seq_length(const PageCache& c, int b, uint32_t* status) {
+    const int p = c.lengths[b];
+    if (p >= 0 && p <= c.max_pages * 64) return p;
+    if (status) flag(status, p < 0 ? ST_LENGTH : ST_CAPACITY);
+    return p < 0 ? 0 : c.max_pages * 64;
+}
+
+__device__ __forceinline__ int page_id(const PageCache& c, int b, int page) {
+    const int id = c.table[(size_t)b * c.max_pages + page];
+    return (unsigned)id < (unsigned)c.n_pages ? id : -1;
+}
+
+// 8 adjacent elements of a row as f32; vec: 16-byte aligned rows
+__device__ __forceinline__ void load8(const HeadRows& r, long long row, int head, int d, float* x) {
+    const size_t at = (size_t)(row * r.row_stride + head * r.head_stride + d);
+    if (r.f32) {
+        const float* p = (const float*)r.data + at;
+        if (r.vec) {
+            const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[i];
+        }
+    } else {
+        const uint16_t* p = (const uint16_t*)r.data + at;
+        if (r.vec) {
+            const uint4 a = *(const uint4*)p;
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[2 * i] = bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]);
+        }
+    }
+}
+__device__ __forceinline__ void store4(const HeadRows& r, long long row, int head, int d, const float* x) {
+    const size_t at = (size_t)(row * r.row_stride + head * r.head_stride + d);
+    if (r.f32) {
+        float* p = (float*)r.data + at;
+        if (r.vec) {
+            *(float4*)p = float4{x[0], x[1], x[2], x[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = x[i];
+        }
+    } else {
+        uint16_t* p = (uint16_t*)r.data + at;
+        if (r.vec) {
+            *(uint2*)p = uint2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = (uint16_t)f32_to_bf16(x[i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- writing rows
+// One workgroup per page that a sequence's new rows touch, and KV head.  A thread takes 8 dims of a row: the keys go to
+// their place at once, the values through LDS, where a lane's 8 keys of one dim meet.  e4m3: the row's power of two is the
+// least by which no finite magnitude is over 448 (at least 2^-100); a row's codes hang on nothing but the row, so a
+// row written alone and one written in a chunk are the same.  NaN and infinities become NaN, e4m3 has no others.
+// Bounds: the least and largest stored key of each dim among the page's positions up to the last one written, rounded
+// outwards to 8 bits; earlier positions are read back.  The bound scale of a page with a key that is not finite is +inf.
+struct KvSource {        // the rows to write: strided tensors, or the split block K/V of a pass
+    HeadRows k, v;
+    const uint16_t* blk_k;   // [unit][hi, lo][64][D]
+    const uint16_t* blk_v;   // [unit][hi, lo][D][64]
+};
+
+template <int D>
+__device__ __forceinline__ void load_kv8(const KvSource& src, bool value, long long row, int t, int b, int head, int heads, int d, float* x) {
+    if (!src.blk_k) {
+        load8(value ? src.v : src.k, row, head, d, x);
+        return;
+    }
+    const size_t unit = (size_t)(b * heads + head) * 2 * 64 * D;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint16_t* p = value ? src.blk_v + unit + (d + i) * 64 + t : src.blk_k + unit + t * D + d + i;
+        x[i] = bf16_to_f32(p[0]) + bf16_to_f32(p[64 * D]);
+    }
+}
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+
+// four values as e4m3 numbers of x * 2^-e, at most `most`
+__device__ __forceinline__ uint32_t four_e4m3(const float* x, float inv, float most) {
+    uint32_t w = 0;
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = finite(x[i]) ? fminf(fmaxf(x[i] * inv, -most), most) : __uint_as_float(0x7FC00000u);
+    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], (int)w, false);
+    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)w, true);
+    return w;
+}
+
+// biased exponent of a row's power of two
+__device__ __forceinline__ uint32_t row_exponent(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u);   // 448 = 1.75 * 2^8
+    return (uint32_t)max(e, 27);
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256) pages_write_kernel(PageCache c, KvSource src, PageChunk ch, int touched, uint32_t* status) {
+    constexpr int C = D / 8, TOK = 256 / C;   // threads per row, rows per turn
+    using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
+    __shared__ __align__(16) Elem vt[64][D + (E4M3 ? 16 : 8)];
+    __shared__ float red[2][TOK][D];
+    __shared__ float top[4];
+    __shared__ int bad;
+
+    const int h = blockIdx.x % c.n_kv_heads, i = blockIdx.x / c.n_kv_heads % touched, b = blockIdx.x / c.n_kv_heads / touched;
+    const int tid = threadIdx.x, chunk = tid % C, d0 = chunk * 8;
+    const bool tell = h == 0 && i == 0 && tid == 0;
+    const SeqRows sr = seq_rows(ch, b, tell ? status : nullptr);
+    const int P = seq_length(c, b, tell && sr.n ? status : nullptr);
+    if (tell && sr.n && P + sr.n > c.max_pages * 64) flag(status, ST_CAPACITY);
+    const int page = P / 64 + i, end = min(min(P + sr.n, c.max_pages * 64) - page * 64, 64);   // positions of the page
+    const int begin = max(P - page * 64, 0);
+    if (begin >= end) return;
+    const int id = page_id(c, b, page);
+    if (id < 0) {
+        if (tid == 0 && h == 0) flag(status, ST_PAGE);
+        return;
+    }
+    const size_t head = (size_t)id * c.n_kv_heads + h;
+    Elem* kp = (Elem*)c.k + head * 64 * D;
+    Elem* vp = (Elem*)c.v + head * 64 * D;
+    if (tid == 0) bad = 0;
+
+    float lo[8], hi[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lo[e] = INFINITY, hi[e] = -INFINITY;
+    bool odd = false;   // a stored key that is not finite
+
+    for (int t = begin + tid / C;; t += TOK) {
+        const bool there = t < end;
+        if (__all(!there)) break;
+        float x[2][8];
+        float amax[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[w][e] = 0.0f;
+            if (there) load_kv8<D>(src, w == 1, sr.r0 + (page * 64 + t - P), page * 64 + t - P, b, h, c.n_kv_heads, d0, x[w]);
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax[w] = fmaxf(amax[w], finite(x[w][e]) ? fabsf(x[w][e]) : 0.0f);
+#pragma unroll
+                for (int m = 1; m < C; m <<= 1) amax[w] = fmaxf(amax[w], __shfl_xor(amax[w], m));
+            }
+        }
+        if (!there) continue;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            if constexpr (E4M3) {
+                const uint32_t ex = row_exponent(amax[w]);
+                const float inv = __uint_as_float((254u - ex) << 23), sc = scale_of(ex);
+                const float most = ex == 247u ? 240.0f : 448.0f;   // 256 * 2^120 would not be finite
+                const uint2 q{four_e4m3(x[w], inv, most), four_e4m3(x[w] + 4, inv, most)};
+                if (chunk == 0) c.scale[(head * 2 + w) * 64 + t] = (uint8_t)ex;
+                if (w == 0) {
+                    *(uint2*)(kp + key_at<D, true>(t, d0)) = q;
+                    if (c.bounds) {
+                        const uint4 s = eight_bf16(q.x, q.y, sc);
+                        const uint32_t u[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float f = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+                            odd |= !finite(f);
+                            lo[e] = fminf(lo[e], f), hi[e] = fmaxf(hi[e], f);
+                        }
+                    }
+                } else {
+                    *(uint2*)&vt[t][d0] = q;
+                }
+            } else {
+                uint32_t u[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = pack_bf16x2(x[w][2 * e], x[w][2 * e + 1]);
+                if (w == 0) {
+                    *(uint4*)(kp + key_at<D, false>(t, d0)) = uint4{u[0], u[1], u[2], u[3]};
+                    if (c.bounds) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float f = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+                            odd |= !finite(f);
+                            lo[e] = fminf(lo[e], f), hi[e] = fmaxf(hi[e], f);
+                        }
+                    }
+                } else {
+                    *(uint4*)&vt[t][d0] = uint4{u[0], u[1], u[2], u[3]};
+                }
+            }
+        }
+    }
+    __syncthreads();
+
+    // values: a lane's 8 keys of one dim, whole where all of them are new
+    for (int at = tid; at < 64 * D / 8; at += 256) {
+        const int lane = at & 63, s = (at >> 6) & 1, blk = at >> 7, kt = blk / (D / 32), d = (blk % (D / 32)) * 32 + (lane & 31);
+        const int k0 = kt * 32 + value_key(s, lane >> 5, 0), k1 = kt * 32 + value_key(s, lane >> 5, 7);
+        if (k1 < begin || k0 >= end) continue;
+        Elem* to = vp + value_at<D, E4M3>(k0, d);
+        if (k0 >= begin && k1 < end) {
+            Elem g[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = vt[kt * 32 + value_key(s, lane >> 5, e)][d];
+            if constexpr (E4M3)
+                *(uint2*)to = uint2{(uint32_t)g[0] | (uint32_t)g[1] << 8 | (uint32_t)g[2] << 16 | (uint32_t)g[3] << 24,
+                                    (uint32_t)g[4] | (uint32_t)g[5] << 8 | (uint32_t)g[6] << 16 | (uint32_t)g[7] << 24};
+            else
+                *(uint4*)to = uint4{(uint32_t)g[0] | (uint32_t)g[1] << 16, (uint32_t)g[2] | (uint32_t)g[3] << 16,
+                                    (uint32_t)g[4] | (uint32_t)g[5] << 16, (uint32_t)g[6] | (uint32_t)g[7] << 16};
+        } else {
+            for (int e = 0; e < 8; ++e) {
+                const int k = kt * 32 + value_key(s, lane >> 5, e);
+                if (k >= begin && k < end) to[e] = vt[k][d];
+            }
+        }
+    }
+    if (!c.bounds) return;
+
+    // earlier positions of the page, as they are stored
+    for (int t = tid / C; t < begin; t += TOK) {
+        uint32_t u[4];
+        if constexpr (E4M3) {
+            const uint2 q = *(const uint2*)(kp + key_at<D, true>(t, d0));
+            const uint4 s = eight_bf16(q.x, q.y, scale_of(c.scale[head * 2 * 64 + t]));
+            u[0] = s.x, u[1] = s.y, u[2] = s.z, u[3] = s.w;
+        } else {
+            const uint4 q = *(const uint4*)(kp + key_at<D, false>(t, d0));
+            u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float f = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+            odd |= !finite(f);
+            lo[e] = fminf(lo[e], f), hi[e] = fmaxf(hi[e], f);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[0][tid / C][d0 + e] = lo[e], red[1][tid / C][d0 + e] = hi[e];
+    if (odd) atomicOr(&bad, 1);
+    __syncthreads();
+    float a = 0.0f, l = 0.0f, g = 0.0f;
+    if (tid < D) {
+        l = red[0][0][tid], g = red[1][0][tid];
+        for (int r = 1; r < TOK; ++r) l = fminf(l, red[0][r][tid]), g = fmaxf(g, red[1][r][tid]);
+        a = fmaxf(fabsf(l), fabsf(g));
+    }
+    for (int m = 32; m; m >>= 1) a = fmaxf(a, __shfl_xor(a, m));
+    if ((tid & 63) == 0) top[tid >> 6] = a;
+    __syncthreads();
+    if (tid >= D) return;
+    a = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    const float sc = bad ? INFINITY : a / 127.0f, by = sc > 0.0f ? sc : 1.0f;
+    int8_t* bd = c.bounds + head * 2 * D;
+    bd[tid] = bad ? 0 : (int8_t)fmaxf(-127.0f, fminf(127.0f, floorf(l / by)));
+    bd[D + tid] = bad ? 0 : (int8_t)fmaxf(-127.0f, fminf(127.0f, ceilf(g / by)));
+    if (tid == 0) c.bound_scale[head] = sc;
+}
+
+// ---------------------------------------------------------------- reading rows
+// One workgroup per page that the positions first[b] .. first[b] + n_b touch, and KV head.  Every stored value is a bf16
+// number, also a scaled 8-bit one, so rows of either type are exact.
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k, HeadRows v, PageChunk ch, const int32_t* first, int touched,
+                                                         uint32_t* status) {
+    using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
+    constexpr int C = D / 8, TOK = 256 / C;
+    __shared__ __align__(16) uint16_t vt[64][D + 8];
+    const int h = blockIdx.x % c.n_kv_heads, i = blockIdx.x / c.n_kv_heads % touched, b = blockIdx.x / c.n_kv_heads / touched;
+    const int tid = threadIdx.x, d0 = tid % C * 8;
+    const bool tell = h == 0 && i == 0 && tid == 0;
+    const SeqRows sr = seq_rows(ch, b, tell ? status : nullptr);
+    int P = first ? first[b] : 0;
+    if (P < 0) {
+        if (tell) flag(status, ST_LENGTH);
+        return;
+    }
+    P = min(P, c.max_pages * 64);
+    if (tell && P + sr.n > c.max_pages * 64) flag(status, ST_CAPACITY);
+    const int page = P / 64 + i, end = min(min(P + sr.n, c.max_pages * 64) - page * 64, 64), begin = max(P - page * 64, 0);
+    if (begin >= end) return;
+    const int id = page_id(c, b, page);
+    if (id < 0) {
+        if (tid == 0 && h == 0) flag(status, ST_PAGE);
+        return;
+    }
+    const size_t head = (size_t)id * c.n_kv_heads + h;
+    const Elem* kp = (const Elem*)c.k + head * 64 * D;
+    const Elem* vp = (const Elem*)c.v + head * 64 * D;
+    const long long row0 = sr.r0 + (page * 64 - P);   // row of the page's first position
+
+    for (int at = tid; at < 64 * D / 8; at += 256) {
+        const int lane = at & 63, s = (at >> 6) & 1, blk = at >> 7, kt = blk / (D / 32), d = (blk % (D / 32)) * 32 + (lane & 31);
+        const int k0 = kt * 32 + value_key(s, lane >> 5, 0);
+        if constexpr (E4M3) {
+            const uint2 q = *(const uint2*)(vp + value_at<D, true>(k0, d));
+            const uint8_t* sc = c.scale + (head * 2 + 1) * 64 + k0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t w = ((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 0xFFu;
+                const uint32_t x = pair_bf16<false>(w, scale_of(sc[(e & 3) + ((e & 4) << 1)]));
+                vt[kt * 32 + value_key(s, lane >> 5, e)][d] = (uint16_t)x;
+            }
+        } else {
+            const uint4 q = *(const uint4*)(vp + value_at<D, false>(k0, d));
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vt[kt * 32 + value_key(s, lane >> 5, e)][d] = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+        }
+    }
+    for (int t = begin + tid / C; t < end; t += TOK) {
+        uint4 s;
+        if constexpr (E4M3) {
+            const uint2 q = *(const uint2*)(kp + key_at<D, true>(t, d0));
+            s = eight_bf16(q.x, q.y, scale_of(c.scale[head * 2 * 64 + t]));
+        } else {
+            s = *(const uint4*)(kp + key_at<D, false>(t, d0));
+        }
+        const uint32_t u[4] = {s.x, s.y, s.z, s.w};
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+        store4(k, row0 + t, h, d0, x);
+        store4(k, row0 + t, h, d0 + 4, x + 4);
+    }
+    __syncthreads();
+    for (int t = begin + tid / C; t < end; t += TOK) {
+        const uint4 s = *(const uint4*)&vt[t][d0];
+        const uint32_t u[4] = {s.x, s.y, s.z, s.w};
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+        store4(v, row0 + t, h, d0, x);
+        store4(v, row0 + t, h, d0 + 4, x + 4);
+    }
+}
+
+// ---------------------------------------------------------------- work of the attention
+// An entry is a block of a sequence's rows: 32 * row_tiles rows (token, query head of the group) of a KV head, or the
+// rows of a group of tokens that share a list of pages.  A unit is an entry and a KV head; its work is counted in steps of
+// 8 KB of keys and 8 KB of values at 128 dims (32 bf16 positions, 64 in 8 bits).  All units' steps, one behind the other, are cut into
+// equal shares, one per workgroup, whatever the lengths are: the committed lengths live on the device, so the kernels work
+// the shares out themselves, and a unit that lies in one share is finished there.  The others' parts meet in a second launch.
+struct Entry {
+    int b, blk;         // sequence, block of its rows
+    int r0, n, P;       // packed rows, committed length
+    int t0, t1;         // its tokens (first, past the last)
+    int rows0, rows1;   // its rows (t * G + g)
+    int steps;          // per KV head
+};
+
+template <int STEP>
+__device__ __forceinline__ Entry entry_of(const PagesAttnArgs& a, int e, uint32_t* status) {
+    Entry x;
+    x.b = e / a.n_blk;
+    x.blk = e % a.n_blk;
+    const SeqRows sr = seq_rows(a.ch, x.b, status);
+    x.r0 = sr.r0, x.n = sr.n;
+    x.P = seq_length(a.c, x.b, sr.n ? status : nullptr);
+    const int G = a.group_heads;
+    if (a.list) {
+        x.t0 = min(x.blk * a.group, x.n), x.t1 = min(x.t0 + a.group, x.n);
+        x.rows0 = x.t0 * G, x.rows1 = x.t1 * G;
+    } else {
+        x.rows0 = min(x.blk * 32 * a.row_tiles, x.n * G), x.rows1 = min(x.rows0 + 32 * a.row_tiles, x.n * G);
+        x.t0 = x.rows0 / G, x.t1 = (x.rows1 + G - 1) / G;
+    }
+    x.steps = 0;
+    if (x.rows1 > x.rows0) {
+        if (a.list) x.steps = a.n_list * (64 / STEP);
+        else {
+            const int sees = a.draft && x.t1 > a.bidir_from ? x.n : x.t1;
+            if (status && x.P + sees > a.c.max_pages * 64) flag(status, ST_CAPACITY);
+            x.steps = (min(x.P + sees, a.c.max_pages * 64) + STEP - 1) / STEP;
+        }
+    }
+    return x;
+}
+
+// how many positions a token sees
+__device__ __forceinline__ int sees_of(const PagesAttnArgs& a, int P, int n, int t) {
+    return min(P + (a.draft && t >= a.bidir_from ? n : t + 1), a.c.max_pages * 64);
+}
+
+__device__ __forceinline__ long long block_sum(long long v, long long* lds) {
+    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) v += lds[i];
+    return v;
+}
+
+struct Share {
+    long long total;   // steps of all units
+    int wgs;           // shares
+    __device__ long long begin(int w) const { return total * w / wgs; }
+    // the share that step s is in
+    __device__ int of(long long s) const {
+        int w = (int)(s * wgs / total);
+        while (w + 1 < wgs && begin(w + 1) <= s) ++w;
+        while (begin(w) > s) --w;
+        return w;
+    }
+};
+// shares of `total` steps, of `units` units: at least `least` steps each, but not fewer shares than units
+__device__ __forceinline__ Share share_of(long long total, long long units, int grid, int least) {
+    return Share{total, (int)max(1LL, min((long long)grid, max(units, total / least)))};
+}
+
+// Sum of the steps (per KV head) of the entries before `upto` and of all, and the number of entries that have rows.
+template <int STEP>
+__device__ __forceinline__ void sum_entries(const PagesAttnArgs& a, int upto, long long* lds, long long* before, long long* all, long long* live,
+                                            uint32_t* status) {
+    long long mine = 0, first = 0, some = 0;
+    for (int e = threadIdx.x; e < a.n_entries; e += blockDim.x) {
+        const int s = entry_of<STEP>(a, e, status).steps;
+        mine += s;
+        some += s > 0;
+        if (e < upto) first += s;
+    }
+    *all = block_sum(mine, lds);
+    *live = block_sum(some, lds);
+    if (before) *before = block_sum(first, lds);
+}
+
+// The entry that holds step `s` (per KV head: s / heads) and the steps before it.
+template <int STEP>
+__device__ __forceinline__ void find_entry(const PagesAttnArgs& a, long long s, long long* lds, int* entry, long long* before) {
+    __shared__ long long found_before;
+    __shared__ int found;
+    long long base = 0;
+    if (threadIdx.x == 0) found = a.n_entries;
+    for (int e0 = 0;; e0 += blockDim.x) {
+        const int e = e0 + threadIdx.x;
+        const long long own = e < a.n_entries ? (long long)entry_of<STEP>(a, e, nullptr).steps * a.c.n_kv_heads : 0;
+        long long up = own;
+        for (int m = 1; m < 64; m <<= 1) {
+            const long long o = __shfl_up(up, m);
+            if ((int)(threadIdx.x & 63) >= m) up += o;
+        }
+        __syncthreads();
+        if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = up;
+        __syncthreads();
+        long long ahead = base, sum = 0;
+        for (int i = 0; i < (int)blockDim.x / 64; ++i) {
+            if (i < (int)threadIdx.x / 64) ahead += lds[i];
+            sum += lds[i];
+        }
+        const long long lo = ahead + up - own;
+        if (own && lo <= s && s < lo + own) found = e, found_before = lo;
+        base += sum;
+        __syncthreads();
+        if (found < a.n_entries || e0 + (int)blockDim.x >= a.n_entries) break;
+    }
+    *entry = found;
+    *before = found_before;
+}
+
+// four dims of a finished row (token t of sequence b, query head), and its log-sum-exp: a row that sees nothing is 0
+template <int D>
+__device__ __forceinline__ void finish_row(const PagesAttnArgs& a, int b, int r0, int n, int t, int head, int d, float m, float l, const float* x) {
+    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = x[i] * by;
+    if (a.o_split) {
+        const size_t at = split_index(b * n + t, head * D + d, a.o_ksteps);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_split(a.o_split, at + i, y[i], a.plain_o);
+    } else {
+        store4(a.out, r0 + t, head, d, y);
+    }
+    if (a.lse && d == 0) a.lse[(size_t)(r0 + t) * (a.group_heads * a.c.n_kv_heads) + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.693147180559945309f;
+}
+
+// ---------------------------------------------------------------- attention
+// A workgroup of 4 wavefronts walks its share unit by unit: row_tiles x (4 / row_tiles) wavefronts, one 32-row tile and
+// every (4 / row_tiles)-th step each.  A step's keys and values go straight from memory to the registers of the wavefront, in operand
+// order; while a step is worked on, the next one's are under way, so that two workgroups per CU keep about 128 KB in flight.  Running
+// maximum and sum per row in base-2 exponents; the weights are carried in two bf16 pieces (three for f32 queries, which are
+// split likewise), so that P V is as exact as the f32 sums.  A unit's wavefronts meet in LDS at its end.
+// Positions that a row does not see have weight 0; a value there that is not finite must not reach the row, and 0 times it
+// would: in steps that some row of the tile does not see whole, values behind every row's last position count as 0, and any
+// other that is not finite is left out of the product and added to the rows that see it.
+template <int D, bool E4M3>
+__device__ __forceinline__ void add_not_finite(f32x16_t* o, const void* values, int base, int lane, int sees, int most) {
+    using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
+    const Elem* v = (const Elem*)values;
+    const int hf = lane >> 5;
+    for (int key = 0; key < (E4M3 ? 64 : 32); ++key) {
+        const int pos = base + key;
+        if (pos >= most) break;
+        const int slot = pos & 63;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t w = v[value_at<D, E4M3>(slot, dt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3))];
+                const float f = E4M3 ? ((w & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : 0.0f) : bf16_to_f32(w);
+                if (!finite(f) && pos < sees) o[dt][r] += f;
+            }
+    }
+}
+
+__device__ __forceinline__ bool four_not_finite(uint32_t w) {   // of four e4m3 numbers
+    bool r = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= ((w >> (8 * i)) & 0x7Fu) == 0x7Fu;
+    return r;
+}
+
+template <int D, bool E4M3, int NQ>   // NQ: bf16 pieces of a query (1: bf16, 2: split, 3: f32)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 && !(E4M3 && D == 128) ? 2 : 1))) pages_attend_kernel(PagesAttnArgs a) {
+    constexpr int STEP = E4M3 ? 64 : 32, KT = STEP / 32, KS = D / 16, DT = D / 32, NP = NQ == 3 ? 3 : 2;
+    constexpr int NL = E4M3 ? KT * DT : KS;   // 16-byte loads per lane of a step's keys, and of its values
+    constexpr int PITCH = D + 4;
+    __shared__ __align__(16) float so[4][32][PITCH];
+    __shared__ float sml[4][32][2];
+    __shared__ long long lds[4];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, row = lane & 31;
+    const int rt = wave % a.row_tiles, ks = wave / a.row_tiles, n_ks = 4 / a.row_tiles;
+    const int heads = a.c.n_kv_heads, G = a.group_heads;
+
+    long long total, live;
+    sum_entries<STEP>(a, 0, lds, nullptr, &total, &live, blockIdx.x == 0 ? a.status : nullptr);
+    total *= heads;
+    if (total == 0) return;
+    const Share sh = share_of(total, live * heads, gridDim.x, a.least_steps);
+    if ((int)blockIdx.x >= sh.wgs) return;
+    const long long first = sh.begin(blockIdx.x), last = sh.begin(blockIdx.x + 1);
+    int e;
+    long long before;
+    find_entry<STEP>(a, first, lds, &e, &before);
+    if (e >= a.n_entries) return;   // not unless the lengths change meanwhile
+    Entry en = entry_of<STEP>(a, e, nullptr);
+
+    for (long long at = first; at < last;) {
+        while (at >= before + (long long)en.steps * heads) {   // entries without rows have no steps
+            before += (long long)en.steps * heads;
+            if (++e >= a.n_entries) return;
+            en = entry_of<STEP>(a, e, nullptr);
+        }
+        const int h = (int)((at - before) / en.steps);
+        const long long unit0 = before + (long long)h * en.steps;
+        const int s0 = __builtin_amdgcn_readfirstlane((int)(at - unit0));
+        const int s1 = __builtin_amdgcn_readfirstlane((int)min(last - unit0, (long long)en.steps));
+        const bool whole = s0 == 0 && s1 == en.steps;
+        const int slot = 2 * blockIdx.x + (at > first ? 1 : 0);
+        at = unit0 + s1;
+
+        // this wavefront's rows
+        const int myrow = en.rows0 + rt * 32 + row;
+        const bool have = myrow < en.rows1;
+        const int t = have ? myrow / G : 0, g = have ? myrow % G : 0;
+        const int sees = have ? sees_of(a, en.P, en.n, t) : 0;
+        int least = have ? sees : 0x7FFFFFFF, most = sees;
+        for (int m = 16; m; m >>= 1) least = min(least, __shfl_xor(least, m)), most = max(most, __shfl_xor(most, m));
+        least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
+
+        uint4 q[NQ][KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = 32 * (s >> 1) + 16 * hf + 8 * (s & 1);
+            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
+                uint4 z{0u, 0u, 0u, 0u};
+                q[0][s] = q[1][s] = z;
+                if (have) {
+                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                    q[0][s] = *(const uint4*)p;
+                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
+                }
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
+#pragma unroll
+                for (int p = 0; p < NQ; ++p) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                    }
+                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
+                }
+            }
+        }
+
+        f32x16_t o[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
+        float m_run = -INFINITY, l_run = 0.0f;
+
+        // the unit's pages: lane i of the window holds the place and the id of page win + i
+        const int32_t* list = a.list ? a.list + ((size_t)(en.b * a.n_blk + en.blk) * heads + h) * a.n_list : nullptr;
+        int win = -1, w_page = -1, w_id = -1;
+        int s = s0 + ks;
+        int base = 0;          // first position of the step
+        size_t head = 0;       // page and KV head
+        // The next step that has keys for this wavefront, its position and page; false behind the last.
+        auto next = [&]() -> bool {
+            for (; s < s1; s += n_ks) {
+                const int pg = s * STEP >> 6;
+                if (win < 0 || pg >= win + 64) {
+                    win = pg;
+                    const int i = pg + lane;
+                    w_page = i * (64 / STEP) < s1 ? (list ? list[i] : i) : -1;
+                    w_id = w_page >= 0 && w_page < a.c.max_pages ? a.c.table[(size_t)en.b * a.c.max_pages + w_page] : -1;
+                    const bool bad = w_page >= a.c.max_pages || w_page < -1 || (w_page >= 0 && (unsigned)w_id >= (unsigned)a.c.n_pages);
+                    if (bad) {
+                        // a page that no row sees may be one that the sequence does not have yet
+                        if (w_page < -1 || w_page * 64LL < most) flag(a.status, ST_PAGE);
+                        w_id = -1;
+                    }
+                }
+                const int page = __builtin_amdgcn_readlane(w_page, pg - win), id = __builtin_amdgcn_readlane(w_id, pg - win);
+                if (id < 0 || page * 64 + (s * STEP & 63) >= most) continue;
+                base = page * 64 + (s * STEP & 63);
+                head = (size_t)id * heads + h;
+                s += n_ks;
+                return true;
+            }
+            return false;
+        };
+        uint4 kf[NL], vf[NL];
+        uint32_t ksc[KT], vsc[KT * 4];
+        auto load_k = [&](size_t hd, int bs) {
+            const uint4* p = (const uint4*)((const char*)a.c.k + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + lane;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) kf[i] = p[i * 64];
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) ksc[kt] = a.c.scale[hd * 128 + kt * 32 + row];
+            }
+        };
+        auto load_v = [&](size_t hd, int bs) {
+            const uint4* p = (const uint4*)((const char*)a.c.v + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + lane;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) vf[i] = p[i * 64];
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int i = 0; i < KT * 4; ++i) vsc[i] = *(const uint32_t*)(a.c.scale + hd * 128 + 64 + i * 8 + 4 * hf);
+            }
+        };
+
+        bool more = next();
+        int cur_base = base;
+        size_t cur_head = head;
+        if (more) {
+            load_k(cur_head, cur_base);
+            load_v(cur_head, cur_base);
+        }
+        while (more) {
+            f32x16_t sc[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[kt][r] = 0.0f;
+                // the small pieces first
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+#pragma unroll
+                        for (int f = 0; f < 2; ++f) {
+                            uint4 k;
+                            if constexpr (E4M3) {
+                                const uint4 w = kf[kt * DT + i];
+                                k = f ? eight_bf16(w.z, w.w, scale_of(ksc[kt])) : eight_bf16(w.x, w.y, scale_of(ksc[kt]));
+                            } else {
+                                k = kf[i * 2 + f];
+                            }
+                            sc[kt] = mfma_32x32x16(k, q[p][i * 2 + f], sc[kt]);
+                        }
+            }
+            const bool masked = cur_base + STEP > least;
+            more = next();
+            if (more) load_k(head, base);
+
+            // scores in base-2 exponents, their maximum
+            float top = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float x = sc[kt][r] * a.scale_log2;
+                    if (masked && cur_base + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3) >= sees) x = -INFINITY;
+                    sc[kt][r] = x;
+                    top = fmaxf(top, x);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any(top > m_run)) {
+                const float m = fmaxf(m_run, top), f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
+                l_run *= f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+                m_run = m;
+            }
+            const float ref = m_run == -INFINITY ? 0.0f : m_run;
+            float sum = 0.0f;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float p = __builtin_amdgcn_exp2f(sc[kt][r] - ref);
+                    sum += p;
+                    if constexpr (E4M3) {
+                        const float w = scale_of((vsc[kt * 4 + (r >> 2)] >> (8 * (r & 3))) & 0xFFu);
+                        p = p > 0.0f || p != p ? p * w : 0.0f;   // scales of empty places may be anything
+                    }
+                    sc[kt][r] = p;
+                }
+            l_run += sum;
+
+            bool odd = false;
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    uint32_t w[4] = {vf[i].x, vf[i].y, vf[i].z, vf[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (E4M3) {   // four keys of step j / 2: 8 (j & 1) + 4 hf + 0..3
+                            const int pos = cur_base + (i / DT) * 32 + 16 * (j >> 1) + 8 * (j & 1) + 4 * hf;
+#pragma unroll
+                            for (int b = 0; b < 4; ++b)
+                                if (pos + b >= most) w[j] &= ~(0xFFu << (8 * b));
+                            if (four_not_finite(w[j])) {
+                                odd = true;
+#pragma unroll
+                                for (int b = 0; b < 4; ++b)
+                                    if (((w[j] >> (8 * b)) & 0x7Fu) == 0x7Fu) w[j] &= ~(0xFFu << (8 * b));
+                            }
+                        } else {   // i = (dt, step), two keys
+                            const int pos = cur_base + value_key(i & 1, hf, 2 * j);
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                if (pos + b >= most) w[j] &= ~(0xFFFFu << (16 * b));
+                                if (((w[j] >> (16 * b)) & 0x7F80u) == 0x7F80u) odd = true, w[j] &= ~(0xFFFFu << (16 * b));
+                            }
+                        }
+                    }
+                    vf[i] = uint4{w[0], w[1], w[2], w[3]};
+                }
+            }
+
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = sc[kt][st * 8 + i];
+                    uint4 pf[NP];
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                            x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                        }
+                        pf[p] = uint4{w[0], w[1], w[2], w[3]};
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        uint4 v;
+                        if constexpr (E4M3) {
+                            const uint4 w = vf[kt * DT + dt];
+                            v = st ? eight_bf16(w.z, w.w, 1.0f) : eight_bf16(w.x, w.y, 1.0f);
+                        } else {
+                            v = vf[dt * 2 + st];
+                        }
+#pragma unroll
+                        for (int p = NP - 1; p >= 0; --p) o[dt] = mfma_32x32x16(v, pf[p], o[dt]);
+                    }
+                }
+            if (masked && __any(odd))
+                add_not_finite<D, E4M3>(o, (const char*)a.c.v + cur_head * 64 * D * (E4M3 ? 1 : 2), cur_base, lane, sees, most);
+            if (more) load_v(head, base);
+            cur_base = base, cur_head = head;
+        }
+
+        // the unit's wavefronts meet
+        l_run += __shfl_xor(l_run, 32);
+        __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(float4*)&so[wave][row][dt * 32 + 8 * j + 4 * hf] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+        if (hf == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
+        __syncthreads();
+        for (int i = tid; i < a.row_tiles * 32 * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4, tile = r >> 5, rr = r & 31, rw = en.rows0 + r;
+            if (rw >= en.rows1) continue;
+            float m = -INFINITY, l = 0.0f;
+            for (int k = 0; k < n_ks; ++k) m = fmaxf(m, sml[k * a.row_tiles + tile][rr][0]);
+            const float ref = m == -INFINITY ? 0.0f : m;
+            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < n_ks; ++k) {
+                const int w = k * a.row_tiles + tile;
+                const float f = __builtin_amdgcn_exp2f(sml[w][rr][0] - ref);
+                const float4 y = *(const float4*)&so[w][rr][d];
+                l += sml[w][rr][1] * f;
+                x[0] += y.x * f, x[1] += y.y * f, x[2] += y.z * f, x[3] += y.w * f;
+            }
+            if (whole) {
+                finish_row<D>(a, en.b, en.r0, en.n, rw / G, h * G + rw % G, d, m, l, x);
+            } else {
+                const size_t at_row = (size_t)slot * 32 * a.row_tiles + r;
+                *(float4*)(a.part_o + at_row * D + d) = float4{x[0], x[1], x[2], x[3]};
+                if (d == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m, l};
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The parts of units that several workgroups have: a.slices workgroups per unit, each taking every a.slices-th 1024 / D of its rows.
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
+    constexpr int STEP = E4M3 ? 64 : 32, TPR = D / 4, ROWS = 256 / TPR;
+    __shared__ long long lds[4];
+    const int heads = a.c.n_kv_heads, G = a.group_heads;
+    const int slice = blockIdx.x % a.slices, h = blockIdx.x / a.slices % heads, e = blockIdx.x / a.slices / heads;
+    const Entry en = entry_of<STEP>(a, e, nullptr);
+    if (en.rows0 + slice * ROWS >= en.rows1) return;
+    long long before, total, live;
+    sum_entries<STEP>(a, e, lds, &before, &total, &live, nullptr);
+    total *= heads;
+    const long long u0 = before * heads + (long long)h * en.steps;
+    if (u0 + en.steps > total) return;   // not unless the lengths change meanwhile
+    const Share sh = share_of(total, live * heads, a.grid, a.least_steps);
+    const int w0 = sh.of(u0), w1 = sh.of(u0 + en.steps - 1), n = w1 - w0 + 1;
+    if (n == 1) return;
+    const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (u0 > sh.begin(w0) ? 1 : 0);
+    for (int r = slice * ROWS + threadIdx.x / TPR; en.rows0 + r < en.rows1; r += a.slices * ROWS) {
+        auto place = [&](int i) { return (size_t)(i == 0 ? first : 2 * (w0 + i)) * 32 * a.row_tiles + r; };
+        float m = -INFINITY;
+        for (int i = threadIdx.x % TPR; i < n; i += TPR) m = fmaxf(m, a.part_ml[place(i) * 2]);
+        for (int k = TPR / 2; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float l = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const size_t at = place(i);
+            const float2 ml = *(const float2*)(a.part_ml + at * 2);
+            const float4 y = *(const float4*)(a.part_o + at * D + d);
+            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+            l += ml.y * f;
+            x[0] += y.x * f, x[1] += y.y * f, x[2] += y.z * f, x[3] += y.w * f;
+        }
+        const int rw = en.rows0 + r;
+        finish_row<D>(a, en.b, en.r0, en.n, rw / G, h * G + rw % G, d, m, l, x);
+    }
+}
+
+// ---------------------------------------------------------------- selection of pages
+// Scores in whole numbers: a query row is rounded to 8 bits by its largest magnitude over 127, the bounds of a page are 8-bit
+// too, and sum over the dims of max(qi * least, qi * largest), which no key of the page exceeds but for the rounding of q, is one matrix product of
+// [min(qi, 0), max(qi, 0)] with [least, largest].  Its 32-bit result is exact below 2^24, so which pages win does not hang on any order
+// of summation.  A workgroup takes a group's rows of one KV head (through LDS, as 8-bit operands) and 512 pages.
+struct Group {
+    int r0, n, P, t0, t1;   // tokens [t0, t1) of the sequence's
+    int p0;                 // first page of its own: that of its first token's position
+    int end;                // past the last page that it sees
+};
+__device__ __forceinline__ Group group_of(const PagesSelectArgs& a, int b, int grp, uint32_t* status) {
+    Group g;
+    const SeqRows sr = seq_rows(a.ch, b, status);
+    g.r0 = sr.r0, g.n = sr.n;
+    g.P = seq_length(a.c, b, sr.n ? status : nullptr);
+    g.t0 = min(grp * a.group, g.n), g.t1 = min(g.t0 + a.group, g.n);
+    g.p0 = g.end = 0;
+    if (g.t1 > g.t0) {
+        const int cap = a.c.max_pages, sees = a.draft && g.t1 > a.bidir_from ? g.n : g.t1;
+        if (status && g.P + sees > cap * 64) flag(status, ST_CAPACITY);
+        g.p0 = min((g.P + g.t0) / 64, cap);
+        g.end = min((g.P + sees + 63) / 64, cap);
+    }
+    return g;
+}
+
+constexpr int SCORE_PAGES = 512;   // pages per workgroup: 4 wavefronts of 32 at a time
+
+template <int D>
+__global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
+    constexpr int PITCH = 2 * D + 16, KS = 2 * D / 32;
+    __shared__ __align__(16) int8_t qi[PAGES_GROUP_ROWS][PITCH];
+    __shared__ float qs[PAGES_GROUP_ROWS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5, col = lane & 31;
+    const int chunk = blockIdx.x % a.chunks, unit = blockIdx.x / a.chunks, heads = a.c.n_kv_heads, G = a.group_heads;
+    const int h = unit % heads, grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
+    const Group g = group_of(a, b, grp, nullptr);
+    const int lo = max(a.n_first, chunk * SCORE_PAGES), hi = min(g.p0, chunk * SCORE_PAGES + SCORE_PAGES);
+    if (lo >= hi || g.p0 - a.n_first <= a.n_top) return;   // none, or all of them are taken
+
+    // rows of the group: 8 dims per thread, a row's threads adjacent
+    constexpr int C = D / 8, ROWS = 256 / C;
+    const int n = (g.t1 - g.t0) * G, n32 = (n + 31) / 32 * 32;
+    for (int r = tid / C; r < n32; r += ROWS) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+        const int d = tid % C * 8;
+        if (r < n) load8(a.q, g.r0 + g.t0 + r / G, h * G + r % G, d, x);
+        float amax = 0.0f;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i])), odd |= !finite(x[i]);
+#pragma unroll
+        for (int m = 1; m < C; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m)), odd |= __shfl_xor((int)odd, m) != 0;
+        const float sc = amax / 127.0f, by = sc > 0.0f ? sc : 1.0f;
+        uint32_t neg[2] = {0u, 0u}, pos[2] = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int v = odd ? 0 : (int)fmaxf(-127.0f, fminf(127.0f, rintf(x[i] / by)));
+            neg[i / 4] |= (uint32_t)(uint8_t)min(v, 0) << (8 * (i & 3));
+            pos[i / 4] |= (uint32_t)max(v, 0) << (8 * (i & 3));
+        }
+        *(uint2*)&qi[r][d] = uint2{neg[0], neg[1]};
+        *(uint2*)&qi[r][D + d] = uint2{pos[0], pos[1]};
+        if (tid % C == 0) qs[r] = r < n && !odd ? sc : -1.0f;   // -1: a row without a part
+    }
+    __syncthreads();
+
+    for (int p32 = chunk * SCORE_PAGES + wave * 32; p32 < hi; p32 += 128) {
+        const int page = p32 + col;
+        const bool there = page >= lo && page < hi;
+        const int id = there ? page_id(a.c, b, page) : -1;
+        if (there && id < 0) flag(a.status, ST_PAGE);
+        const size_t head = (size_t)max(id, 0) * heads + h;
+        i32x4_t w[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) w[s] = *(const i32x4_t*)(a.c.bounds + head * 2 * D + 32 * s + 16 * hf);
+        const float bs = a.c.bound_scale[head];
+        float best = -INFINITY;
+        for (int r0 = 0; r0 < n32; r0 += 32) {
+            i32x16_t acc;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = 0;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*(const i32x4_t*)&qi[r0 + col][32 * s + 16 * hf], w[s], acc, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float f = qs[r0 + 8 * (r >> 2) + 4 * hf + (r & 3)];
+                if (f >= 0.0f) best = fmaxf(best, (float)acc[r] * f);
+            }
+        }
+        best = fmaxf(best, __shfl_xor(best, 32));
+        if (there && hf == 0) {
+            const float f = !finite(bs) ? INFINITY : best == -INFINITY ? -INFINITY : best * bs;
+            a.scores[(size_t)unit * a.c.max_pages + page] = id < 0 ? -INFINITY : f;
+        }
+    }
+}
+
+// order of scores as unsigned numbers; -0 is 0
+__device__ __forceinline__ uint32_t score_key(float v) {
+    uint32_t u = __float_as_uint(v);
+    if ((u & 0x7FFFFFFFu) == 0u) u = 0u;
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// One workgroup per unit: the n_top-th largest score digit by digit (the counts of a digit's 256 values in LDS), then the taken pages in
+// ascending order.
+__global__ void __launch_bounds__(256) pages_pick_kernel(PagesSelectArgs a) {
+    __shared__ uint32_t hist[256];
+    __shared__ int wsum[4][2];
+    __shared__ uint32_t s_key;
+    __shared__ int s_left;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, unit = blockIdx.x, heads = a.c.n_kv_heads;
+    const int grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
+    const Group g = group_of(a, b, grp, unit % heads == 0 && tid == 0 ? a.status : nullptr);
+    int32_t* out = a.list + (size_t)unit * a.n_list;
+    const float* score = a.scores + (size_t)unit * a.c.max_pages;
+    const int lo = min(a.n_first, g.p0), n = g.p0 - lo;   // candidates
+    uint32_t key = a.n_top > 0 ? 0u : 0xFFFFFFFFu;   // taken: above key, and `left` of those equal to it
+    int left = a.n_top;
+    if (n > a.n_top && a.n_top > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            hist[tid] = 0u;
+            __syncthreads();
+            for (int i = tid; i < n; i += 256) {
+                const uint32_t k = score_key(score[lo + i]);
+                if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            }
+            __syncthreads();
+            // counts of larger digits; the digit where they reach `left`
+            uint32_t up = hist[tid];
+            for (int m = 1; m < 64; m <<= 1) {
+                const uint32_t o = __shfl_down(up, m);
+                if (lane + m < 64) up += o;
+            }
+            if (lane == 0) wsum[wave][0] = (int)up;
+            __syncthreads();
+            for (int w = wave + 1; w < 4; ++w) up += (uint32_t)wsum[w][0];
+            const uint32_t above = up - hist[tid];
+            if ((int)above < left && (int)up >= left) s_key = key | (uint32_t)tid << shift, s_left = left - (int)above;
+            __syncthreads();
+            key = s_key, left = s_left;
+        }
+    }
+    int put = 0;
+    for (int i0 = 0; i0 < g.end; i0 += 256) {
+        const int i = i0 + tid;
+        bool sure = false, tie = false;
+        if (i < g.end) {
+            if (i < lo || i >= g.p0 || n <= a.n_top) sure = true;
+            else {
+                const uint32_t k = score_key(score[i]);
+                sure = k > key, tie = k == key;
+            }
+        }
+        const unsigned long long ties = __ballot(tie), below = (1ull << lane) - 1;
+        if (lane == 0) wsum[wave][0] = __popcll(ties);
+        __syncthreads();
+        int before = __popcll(ties & below), all = 0;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) before += wsum[w][0];
+            all += wsum[w][0];
+        }
+        const bool taken = sure || (tie && before < left);
+        left -= min(left, all);
+        const unsigned long long takes = __ballot(taken);
+        if (lane == 0) wsum[wave][1] = __popcll(takes);
+        __syncthreads();
+        int at = put + __popcll(takes & below);
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) at += wsum[w][1];
+            put += wsum[w][1];
+        }
+        if (taken && at < a.n_list) out[at] = i;
+    }
+    for (int i = put + tid; i < a.n_list; i += 256) out[i] = -1;
+}
+
+HeadRows with_vec(HeadRows r) {
+    const uintptr_t m = r.f32 ? 3 : 7;
+    r.vec = ((uintptr_t)r.data & 15) == 0 && (r.row_stride & m) == 0 && (r.head_stride & m) == 0;
+    return r;
+}
+
+template <typename F>
+hipError_t by_type(const PageCache& c, F f) {
+    if (c.head_dim == 64) return c.e4m3 ? f(std::integral_constant<int, 64>(), std::true_type()) : f(std::integral_constant<int, 64>(), std::false_type());
+    return c.e4m3 ? f(std::integral_constant<int, 128>(), std::true_type()) : f(std::integral_constant<int, 128>(), std::false_type());
+}
+
+}  // namespace
+
+// pages that n adjacent positions touch at most
+static int pages_touched(int n) { return (n + 62) / 64 + 1; }
+
+hipError_t launch_pages_write(const PageCache& c, const HeadRows& k, const HeadRows& v, const uint16_t* blk_k, const uint16_t* blk_v,
+                              const PageChunk& ch, uint32_t* status, hipStream_t s) {
+    const KvSource src{with_vec(k), with_vec(v), blk_k, blk_v};
+    const int touched = pages_touched(ch.max_rows);
+    return by_type(c, [&](auto d, auto e) {
+        pages_write_kernel<decltype(d)::value, decltype(e)::value><<<c.batch * touched * c.n_kv_heads, 256, 0, s>>>(c, src, ch, touched, status);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_pages_read(const PageCache& c, const HeadRows& k, const HeadRows& v, const PageChunk& ch, const int32_t* first, uint32_t* status,
+                             hipStream_t s) {
+    const int touched = pages_touched(ch.max_rows);
+    return by_type(c, [&](auto d, auto e) {
+        pages_read_kernel<decltype(d)::value, decltype(e)::value>
+            <<<c.batch * touched * c.n_kv_heads, 256, 0, s>>>(c, with_vec(k), with_vec(v), ch, first, touched, status);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
+    PagesAttnArgs a = args;
+    a.q = with_vec(a.q), a.out = with_vec(a.out);
+    return by_type(a.c, [&](auto d, auto e) {
+        constexpr int D = decltype(d)::value;
+        constexpr bool E = decltype(e)::value;
+        if (a.q_split) pages_attend_kernel<D, E, 2><<<a.grid, 256, 0, s>>>(a);
+        else if (a.q.f32) pages_attend_kernel<D, E, 3><<<a.grid, 256, 0, s>>>(a);
+        else pages_attend_kernel<D, E, 1><<<a.grid, 256, 0, s>>>(a);
+        const hipError_t st = hipGetLastError();
+        if (st != hipSuccess) return st;
+        pages_combine_kernel<D, E><<<a.n_entries * a.c.n_kv_heads * a.slices, 256, 0, s>>>(a);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_pages_select(const PagesSelectArgs& args, hipStream_t s) {
+    PagesSelectArgs a = args;
+    a.q = with_vec(a.q);
+    a.chunks = cdiv(a.c.max_pages, SCORE_PAGES);
+    const int units = a.c.batch * a.n_groups * a.c.n_kv_heads;
+    if (a.n_top > 0) {
+        if (a.c.head_dim == 64) pages_score_kernel<64><<<units * a.chunks, 256, 0, s>>>(a);
+        else pages_score_kernel<128><<<units * a.chunks, 256, 0, s>>>(a);
+        const hipError_t st = hipGetLastError();
+        if (st != hipSuccess) return st;
+    }
+    pages_pick_kernel<<<units, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace nld

@@ -17,7 +17,8 @@ from . import _lib as C
 __all__ = ["DeviceModel", "DeviceCache", "Workspace", "block_forward", "draft", "verify_accept",
            "accept_from_logits", "verify_accept_noalloc", "denoise_step", "refresh_block", "commit_from_logits", "read_device_status",
            "stream_handle", "VERIFY", "DRAFT", "LogitsWorkspace", "top_logits", "distill_from_logits",
-           "policy_from_logits", "drafter_loss"]
+           "policy_from_logits", "drafter_loss", "PagedCache", "PagesWorkspace", "write_pages", "read_pages", "attend_pages",
+           "select_pages"]
 
 VERIFY = C.NLD_MODE_VERIFY
 DRAFT = C.NLD_MODE_DRAFT
@@ -620,6 +621,176 @@ def drafter_loss(model, cache, ws, logits_ws: LogitsWorkspace, anchor: torch.Ten
                             temperature=temperature, kl_share=kl_share, eta=eta, weight=weight,
                             last_row=out["accept_len"], want_grad=want_grad)
     out.update(o, drafts=drafts, draft_logits=draft_logits)
+    return out
+
+
+PAGE = C.NLD_PAGE
+
+
+class PagedCache:
+    """A paged KV cache (nld_pages in include/nld.h): a pool of n_pages pages of 64 positions per layer, in bfloat16 or
+    float8_e4m3fn (8 bits, a power of two per position and head as scale), ``table`` int32 [batch][max_len / 64] and ``lengths`` int32
+    [batch].  n_pages None: max_len positions for every sequence, each with pages of its own; else the table is
+    the caller's to fill (it starts at -1: no page).  bounds: keep what select_pages reads."""
+
+    def __init__(self, kv_heads: int, head_dim: int, batch: int, max_len: int, n_layers: int = 1, n_pages=None,
+                 dtype=torch.bfloat16, bounds: bool = False, device="cuda"):
+        if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError("dtype must be torch.bfloat16 or torch.float8_e4m3fn")
+        if max_len < 1 or max_len % PAGE:
+            raise ValueError("max_len must be a positive multiple of %d" % PAGE)
+        dev = torch.device(device)
+        width = max_len // PAGE
+        whole = n_pages is None
+        n_pages = batch * width if whole else n_pages
+        if min(kv_heads, batch, n_layers, n_pages) < 1 or max(kv_heads, batch, n_layers, n_pages, width) > _INT32_MAX:
+            raise ValueError("sizes must be positive int32")
+        e4m3 = dtype == torch.float8_e4m3fn
+        heads = (n_layers, n_pages, kv_heads)
+        self.n_layers, self.n_pages, self.kv_heads, self.head_dim = n_layers, n_pages, kv_heads, head_dim
+        self.batch, self.max_len, self.dtype = batch, max_len, dtype
+        self.k = torch.zeros(heads + (PAGE * head_dim,), dtype=dtype, device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.scale = torch.zeros(heads + (2, PAGE), dtype=torch.uint8, device=dev) if e4m3 else None
+        self.bounds = torch.zeros(heads + (2, head_dim), dtype=torch.int8, device=dev) if bounds else None
+        self.bound_scale = torch.zeros(heads, dtype=torch.float32, device=dev) if bounds else None
+        self.table = torch.arange(batch * width, dtype=torch.int32, device=dev).view(batch, width) if whole else \
+            torch.full((batch, width), -1, dtype=torch.int32, device=dev)
+        self.lengths = torch.zeros(batch, dtype=torch.int32, device=dev)
+        self.device = self.k.device
+        self.struct = C.Pages(_ptr(self.k), _ptr(self.v), _ptr(self.scale), _ptr(self.bounds), _ptr(self.bound_scale),
+                              C.NLD_E4M3 if e4m3 else C.NLD_BF16, n_layers, n_pages, kv_heads, head_dim, _ptr(self.table),
+                              _ptr(self.lengths), batch, width)
+
+
+class PagesWorkspace:
+    """Workspace of the calls on a paged cache for n_q_heads query heads, chunks of up to max_rows rows per sequence and selections
+    of groups of at least ``group`` tokens (0: none)."""
+
+    def __init__(self, cache: PagedCache, n_q_heads: int, max_rows: int, group: int = 0):
+        lib = C.load()
+        if max(n_q_heads, max_rows, group) > _INT32_MAX:
+            raise ValueError("sizes must be int32")
+        with torch.cuda.device(cache.device):
+            self.nbytes = lib.nld_pages_workspace_bytes(ctypes.byref(cache.struct), n_q_heads, max_rows, group)
+            if self.nbytes == 0:
+                raise ValueError("no workspace for n_q_heads %d, max_rows %d, group %d over these pages: %s"
+                                 % (n_q_heads, max_rows, group, lib.nld_last_error().decode()))
+            self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.device)
+            C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
+        self.ptr = _ptr(self.buf)
+
+
+def _heads(t: torch.Tensor, name: str, rows, heads: int, cache: PagedCache) -> C.Heads:
+    """Descriptor of rows [rows][heads][head_dim], f32 or bf16, head_dim adjacent, other strides free."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None or t.dim() != 3 or t.device != cache.device:
+        raise ValueError("%s must be a float32 or bfloat16 tensor [rows][heads][head_dim] on %s" % (name, cache.device))
+    if t.shape[1] != heads or t.shape[2] != cache.head_dim or (rows is not None and t.shape[0] != rows):
+        raise ValueError("%s has shape %s, this call needs [%s][%d][%d]" % (name, list(t.shape), rows, heads, cache.head_dim))
+    row, head, dim = t.stride()
+    if dim != 1:
+        raise ValueError("%s: the dims of a head must be adjacent" % name)
+    return C.Heads(t.data_ptr(), dtype, row, head)
+
+
+def _chunk(cache: PagedCache, rows: int, row_start, max_rows) -> C.Chunk:
+    if not 0 < rows <= _INT32_MAX:
+        raise ValueError("a chunk has at least one row")
+    if row_start is None:
+        if rows % cache.batch or (max_rows is not None and max_rows * cache.batch != rows):
+            raise ValueError("without row_start every sequence has the same number of rows")
+        return C.Chunk(rows, rows // cache.batch, 0)
+    start = _rows_of(row_start, "row_start", (cache.batch + 1,), torch.int32, cache.device)
+    max_rows = rows if max_rows is None else max_rows
+    if not 0 < max_rows <= rows:
+        raise ValueError("max_rows must be in [1, rows]")
+    return C.Chunk(rows, max_rows, start)
+
+
+def write_pages(cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor, ws: PagesWorkspace, row_start=None, max_rows=None):
+    """Writes keys and values [rows][kv_heads][head_dim] of new rows into the pages, row i of sequence b at position
+    lengths[b] + i.  row_start (int32 [batch + 1]): the sequences' rows, packed, at most max_rows each (default: any number); None: the
+    same number each.  lengths stay as they are: a caller that keeps the rows adds their number."""
+    ch = _chunk(cache, k.shape[0], row_start, max_rows)
+    _call(C.load().nld_pages_write, cache.device, ws, cache.struct, layer, ch, _heads(k, "k", None, cache.kv_heads, cache),
+          _heads(v, "v", k.shape[0], cache.kv_heads, cache))
+    increment_version([t for t in (cache.k, cache.v, cache.scale, cache.bounds, cache.bound_scale) if t is not None])
+
+
+def read_pages(cache: PagedCache, layer: int, rows: int, ws: PagesWorkspace, dtype=torch.float32, first=None, row_start=None,
+               max_rows=None, outs=None):
+    """Keys and values [rows][kv_heads][head_dim] of positions first[b] + i (int32 [batch]; None: from 0), f32 or bf16, both exact.
+    row_start and max_rows as write_pages.  outs: (k, v) to write into, of any strides."""
+    ch = _chunk(cache, rows, row_start, max_rows)
+    at = _rows_of(first, "first", (cache.batch,), torch.int32, cache.device)
+    if outs is None:
+        k = torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
+        v = torch.empty_like(k)
+    else:
+        k, v = outs
+    _call(C.load().nld_pages_read, cache.device, ws, cache.struct, layer, ch, at, _heads(k, "k", rows, cache.kv_heads, cache),
+          _heads(v, "v", rows, cache.kv_heads, cache))
+    if outs is not None:
+        increment_version([k, v])
+    return k, v
+
+
+def _group_list(cache: PagedCache, ch, group: int):
+    if not 0 < group <= _INT32_MAX:
+        raise ValueError("group must be at least 1")
+    return (cache.batch, -(-ch.max_rows // group), cache.kv_heads)
+
+
+def attend_pages(cache: PagedCache, layer: int, q: torch.Tensor, ws: PagesWorkspace, mode: int = VERIFY, bidir_from: int = 0,
+                 scale=None, pages=None, group: int = 1, row_start=None, max_rows=None, out=None, want_lse: bool = False, lse=None):
+    """Attention of the new rows' queries [rows][q_heads][head_dim] (bf16 or f32) over the pages, after write_pages of their keys and values: causal
+    (VERIFY), or from row bidir_from on over the whole chunk (DRAFT).  scale: 1 / sqrt(head_dim) by default.  pages (int32
+    [batch][groups][kv_heads][n], from select_pages): only those, for each group of ``group`` tokens.  row_start and max_rows as write_pages.
+    Returns (out, lse): out like q, lse f32 [rows][q_heads] with ``want_lse`` or where the caller gives it, else None.  No gradient flows through them."""
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][q_heads][head_dim]")
+    rows, heads = q.shape[0], q.shape[1]
+    qd = _heads(q, "q", None, heads, cache)
+    ch = _chunk(cache, rows, row_start, max_rows)
+    n = 0
+    if pages is not None:
+        n = pages.shape[-1] if pages.dim() == 4 else 0
+        _rows_of(pages, "pages", _group_list(cache, ch, group) + (n,), torch.int32, cache.device)
+    given = [t for t in (out, lse) if t is not None]
+    if out is None:
+        out = q.new_empty(q.shape)
+    if lse is None:
+        lse = q.new_empty((rows, heads), dtype=torch.float32) if want_lse else None
+    to = _rows_of(lse, "lse", (rows, heads), torch.float32, cache.device)
+    _call(C.load().nld_pages_attend, cache.device, ws, cache.struct, layer, ch, qd, heads,
+          cache.head_dim ** -0.5 if scale is None else scale, mode, bidir_from, _ptr(pages), n, group, _heads(out, "out", rows, heads, cache), to)
+    if given:
+        increment_version(given)
+    return out, lse
+
+
+def select_pages(cache: PagedCache, layer: int, q: torch.Tensor, ws: PagesWorkspace, n_top: int, group: int = 1, n_first: int = 1,
+                 mode: int = VERIFY, bidir_from: int = 0, row_start=None, max_rows=None, out=None):
+    """The pages that each group of ``group`` tokens attends to, by KV head: the n_first first ones, its own, and the n_top
+    others with the largest scores (see nld_pages_select in include/nld.h).  The cache keeps bounds.  Returns int32
+    [batch][groups][kv_heads][n], ascending, -1 behind the last, as attend_pages takes it."""
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][q_heads][head_dim]")
+    qd = _heads(q, "q", None, q.shape[1], cache)
+    ch = _chunk(cache, q.shape[0], row_start, max_rows)
+    shape = _group_list(cache, ch, group)
+    if not (0 <= n_top <= _INT32_MAX and 0 <= n_first <= _INT32_MAX):
+        raise ValueError("n_top and n_first must not be negative")
+    lib = C.load()
+    n = lib.nld_pages_list_len(ch.max_rows, group, n_top, n_first, mode) if out is None or out.dim() != 4 else out.shape[3]
+    given = out
+    if out is None:
+        out = torch.empty(shape + (max(n, 1),), dtype=torch.int32, device=cache.device)
+    _rows_of(out, "out", shape + (max(n, 1),), torch.int32, cache.device)
+    _call(lib.nld_pages_select, cache.device, ws, cache.struct, layer, ch, qd, q.shape[1], n_top, n_first, group, mode, bidir_from, _ptr(out), max(n, 1))
+    if given is not None:
+        increment_version(given)
     return out
 
 
