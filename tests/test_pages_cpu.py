@@ -129,7 +129,7 @@ def test_attention_scale_and_list():
 def test_selection_arguments():
     assert select(p=pages()) == INVALID and "bounds" in C.load().nld_last_error().decode()
     for kw, status in ((dict(lst=None), INVALID), (dict(n_top=-1), INVALID), (dict(n_first=-1), INVALID), (dict(n_top=(1 << 24) + 1), SHAPE),
-                       (dict(n_top=47, n_first=2), INVALID), (dict(ws_bytes=256 + 4 * 3 * 2 * 2 * 4 - 1), CAPACITY)):
+                       (dict(n_top=48, n_first=2), INVALID), (dict(ws_bytes=256 + 4 * 3 * 2 * 2 * 4 - 1), CAPACITY)):
         assert select(**kw) == status, kw
 
 
