@@ -891,7 +891,7 @@ PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows
 // Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
 // registers) and are what hides the loads' latency.
 struct PagesPlan {
-    int row_tiles, n_blk, grid, slices;
+    int block_rows, row_tiles, n_blk, grid, slices;
     size_t part_ml, total;
 };
 
@@ -899,14 +899,15 @@ bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int ma
     PagesPlan p{};
     const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
     p.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    const long long blocks = group ? cdiv(max_rows, group) : (rows + 32 * p.row_tiles - 1) / (32 * p.row_tiles);
+    p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;
+    const long long blocks = group ? cdiv(max_rows, group) : (rows + p.block_rows - 1) / p.block_rows;
     if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
     p.n_blk = (int)blocks;
     p.grid = 2 * device_cus();
     // the second launch: a few thousand workgroups at most, and one where units are that many
-    const int turns = cdiv((int)std::min<long long>(rows, 32 * p.row_tiles), 1024 / head_dim);
+    const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
     p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
-    const size_t part_rows = (size_t)2 * p.grid * 32 * p.row_tiles;
+    const size_t part_rows = (size_t)2 * p.grid * p.block_rows;
     p.part_ml = 256 + part_rows * head_dim * 4;
     p.total = align256(p.part_ml + part_rows * 8);
     *out = p;
@@ -946,6 +947,7 @@ PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_head
     a.draft = mode == NLD_MODE_DRAFT;
     a.bidir_from = bidir_from;
     a.scale_log2 = (float)(LOG2E * (double)scale);
+    a.block_rows = p.block_rows;
     a.row_tiles = p.row_tiles;
     a.n_blk = p.n_blk;
     a.n_entries = c.batch * p.n_blk;

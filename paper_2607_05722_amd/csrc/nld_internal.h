@@ -404,10 +404,11 @@ struct PagesAttnArgs {
     const int32_t* list;        // optional [batch][n_blk][kv head][n_list]: the pages of each group of tokens
     int n_list, group;
     float* lse;                 // optional [rows][query head]
-    int row_tiles, n_blk, n_entries;   // 32-row tiles of a workgroup (1, 2, 4); blocks of rows per sequence, of all
+    int block_rows, row_tiles;  // rows of a workgroup: 16 (one tile), or 1, 2 or 4 tiles of 32
+    int n_blk, n_entries;       // blocks of rows per sequence, of all
     int grid, least_steps, slices;
-    float* part_o;              // [2 * grid][32 * row_tiles][head_dim]
-    float* part_ml;             // [2 * grid][32 * row_tiles][2]
+    float* part_o;              // [2 * grid][block_rows][head_dim]
+    float* part_ml;             // [2 * grid][block_rows][2]
     uint32_t* status;
 };
 

@@ -2,10 +2,10 @@
 // of pages by a cheap score.
 //
 // A page holds 64 positions of one layer: per KV head the keys, then (another array) the values, in the order in which the
-// matrix instruction takes them, so that a wavefront's operand is one contiguous load of 16 bytes per lane and nothing is
-// shuffled on the way.  Keys are the A operand of S^T = K Q^T (32 keys x 16 dims a step), values that of
-// O^T = V^T P^T (32 dims x 16 keys a step).  The result of the first product leaves a lane with one row and the keys
-// 8j + 4 hf + i of 32 (hf = lane / 32; i, j = 0..3), so the values' steps take their keys in that order and the weights P
+// matrix instructions take them, so that a wavefront's operand is whole cache lines, 16 bytes per lane, and nothing is
+// shuffled on the way.  Keys are the A operand of S^T = K Q^T, values that of O^T = V^T P^T.  The first product leaves a lane with
+// one row and the keys 16 s + 8 j + 4 hf + i of 32 (i = 0..3, j = 0, 1; with rows in tiles of 32 hf = lane / 32 and both s, with
+// tiles of 16 s = lane / 32, hf = lane / 16 % 2); the values' blocks hold 8 keys of a dim in that order, so the weights P
 // need no exchange between lanes.
 #include <type_traits>
 
@@ -25,21 +25,21 @@ constexpr uint32_t ST_CAPACITY = 2u, ST_LENGTH = 4u, ST_PAGE = 16u, ST_ROWS = 32
 __device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) { atomicOr(status, bit); }
 
 // ---------------------------------------------------------------- places in a page
-// Element offset of (key, dim) in a head's keys, and of the 8 elements that a lane takes of them in one step.  Both
-// types: blocks of 64 lanes (32 keys x 2), a lane's elements adjacent, 8 for bf16 and 16 (two steps) for e4m3.
+// Element offset of (key, dim) in a head's keys.  Blocks of 64 lanes x 16 bytes: 16 keys (of a group of 32 those with
+// key / 8 even, then the others) x 4 pieces of 8 dims (bf16) or 16 (e4m3).
 template <int D, bool E4M3>
 __device__ __forceinline__ int key_at(int key, int d) {
-    const int blk = (key >> 5) * (D / 32) + (d >> 5), lane = ((d >> 4) & 1) * 32 + (key & 31), f = (d >> 3) & 1, e = d & 7;
-    return E4M3 ? blk * 1024 + lane * 16 + f * 8 + e : (blk * 2 + f) * 512 + lane * 8 + e;
+    const int tile = (key >> 5) * 2 + ((key >> 3) & 1), m = ((key >> 4) & 1) * 8 + (key & 7);
+    return E4M3 ? ((tile * (D / 64) + (d >> 6)) * 64 + ((d >> 4) & 3) * 16 + m) * 16 + (d & 15)
+                : ((tile * (D / 32) + (d >> 5)) * 64 + ((d >> 3) & 3) * 16 + m) * 8 + (d & 7);
 }
-// of (key, dim) in a head's values
+// of (key, dim) in a head's values: blocks of 16 dims x 4 pieces of 8 keys, of one group of 32 (bf16) or of both (e4m3)
 template <int D, bool E4M3>
 __device__ __forceinline__ int value_at(int key, int d) {
-    const int k = key & 31, j = k >> 3, hf = (k >> 2) & 1, s = j >> 1, e = (j & 1) * 4 + (k & 3);
-    const int blk = (key >> 5) * (D / 32) + (d >> 5), lane = hf * 32 + (d & 31);
-    return E4M3 ? blk * 1024 + lane * 16 + s * 8 + e : (blk * 2 + s) * 512 + lane * 8 + e;
+    const int piece = ((key >> 4) & 1) * 2 + ((key >> 2) & 1), e = ((key >> 3) & 1) * 4 + (key & 3), at = piece * 16 + (d & 15);
+    return E4M3 ? ((d >> 4) * 64 + at) * 16 + (key >> 5) * 8 + e : (((key >> 5) * (D / 16) + (d >> 4)) * 64 + at) * 8 + e;
 }
-// key of element e of a lane's values in step s of 32 keys
+// key, of a group of 32, of element e of the piece (s, hf) of values
 __device__ __forceinline__ int value_key(int s, int hf, int e) { return 16 * s + 4 * hf + (e & 3) + ((e & 4) << 1); }
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -273,14 +273,14 @@ __global__ void __launch_bounds__(256) pages_write_kernel(PageCache c, KvSource 
 
     // values: a lane's 8 keys of one dim, whole where all of them are new
     for (int at = tid; at < 64 * D / 8; at += 256) {
-        const int lane = at & 63, s = (at >> 6) & 1, blk = at >> 7, kt = blk / (D / 32), d = (blk % (D / 32)) * 32 + (lane & 31);
-        const int k0 = kt * 32 + value_key(s, lane >> 5, 0), k1 = kt * 32 + value_key(s, lane >> 5, 7);
+        const int blk = at >> 6, kt = blk / (D / 16), d = blk % (D / 16) * 16 + (at & 15), s = (at >> 5) & 1, hf = (at >> 4) & 1;
+        const int k0 = kt * 32 + value_key(s, hf, 0), k1 = kt * 32 + value_key(s, hf, 7);
         if (k1 < begin || k0 >= end) continue;
         Elem* to = vp + value_at<D, E4M3>(k0, d);
         if (k0 >= begin && k1 < end) {
             Elem g[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = vt[kt * 32 + value_key(s, lane >> 5, e)][d];
+            for (int e = 0; e < 8; ++e) g[e] = vt[kt * 32 + value_key(s, hf, e)][d];
             if constexpr (E4M3)
                 *(uint2*)to = uint2{(uint32_t)g[0] | (uint32_t)g[1] << 8 | (uint32_t)g[2] << 16 | (uint32_t)g[3] << 24,
                                     (uint32_t)g[4] | (uint32_t)g[5] << 8 | (uint32_t)g[6] << 16 | (uint32_t)g[7] << 24};
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256) pages_write_kernel(PageCache c, KvSource 
                                     (uint32_t)g[4] | (uint32_t)g[5] << 16, (uint32_t)g[6] | (uint32_t)g[7] << 16};
         } else {
             for (int e = 0; e < 8; ++e) {
-                const int k = kt * 32 + value_key(s, lane >> 5, e);
+                const int k = kt * 32 + value_key(s, hf, e);
                 if (k >= begin && k < end) to[e] = vt[k][d];
             }
         }
@@ -369,8 +369,8 @@ __global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k
     const long long row0 = sr.r0 + (page * 64 - P);   // row of the page's first position
 
     for (int at = tid; at < 64 * D / 8; at += 256) {
-        const int lane = at & 63, s = (at >> 6) & 1, blk = at >> 7, kt = blk / (D / 32), d = (blk % (D / 32)) * 32 + (lane & 31);
-        const int k0 = kt * 32 + value_key(s, lane >> 5, 0);
+        const int blk = at >> 6, kt = blk / (D / 16), d = blk % (D / 16) * 16 + (at & 15), s = (at >> 5) & 1, hf = (at >> 4) & 1;
+        const int k0 = kt * 32 + value_key(s, hf, 0);
         if constexpr (E4M3) {
             const uint2 q = *(const uint2*)(vp + value_at<D, true>(k0, d));
             const uint8_t* sc = c.scale + (head * 2 + 1) * 64 + k0;
@@ -378,13 +378,13 @@ __global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k
             for (int e = 0; e < 8; ++e) {
                 const uint32_t w = ((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 0xFFu;
                 const uint32_t x = pair_bf16<false>(w, scale_of(sc[(e & 3) + ((e & 4) << 1)]));
-                vt[kt * 32 + value_key(s, lane >> 5, e)][d] = (uint16_t)x;
+                vt[kt * 32 + value_key(s, hf, e)][d] = (uint16_t)x;
             }
         } else {
             const uint4 q = *(const uint4*)(vp + value_at<D, false>(k0, d));
             const uint32_t u[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) vt[kt * 32 + value_key(s, lane >> 5, e)][d] = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+            for (int e = 0; e < 8; ++e) vt[kt * 32 + value_key(s, hf, e)][d] = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
         }
     }
     for (int t = begin + tid / C; t < end; t += TOK) {
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k
 }
 
 // ---------------------------------------------------------------- work of the attention
-// An entry is a block of a sequence's rows: 32 * row_tiles rows (token, query head of the group) of a KV head, or the
+// An entry is a block of a sequence's rows: block_rows rows (token, query head of the group) of a KV head, or the
 // rows of a group of tokens that share a list of pages.  A unit is an entry and a KV head; its work is counted in steps of
 // 8 KB of keys and 8 KB of values at 128 dims (32 bf16 positions, 64 in 8 bits).  All units' steps, one behind the other, are cut into
 // equal shares, one per workgroup, whatever the lengths are: the committed lengths live on the device, so the kernels work
@@ -441,7 +441,7 @@ __device__ __forceinline__ Entry entry_of(const PagesAttnArgs& a, int e, uint32_
         x.t0 = min(x.blk * a.group, x.n), x.t1 = min(x.t0 + a.group, x.n);
         x.rows0 = x.t0 * G, x.rows1 = x.t1 * G;
     } else {
-        x.rows0 = min(x.blk * 32 * a.row_tiles, x.n * G), x.rows1 = min(x.rows0 + 32 * a.row_tiles, x.n * G);
+        x.rows0 = min(x.blk * a.block_rows, x.n * G), x.rows1 = min(x.rows0 + a.block_rows, x.n * G);
         x.t0 = x.rows0 / G, x.t1 = (x.rows1 + G - 1) / G;
     }
     x.steps = 0;
@@ -555,52 +555,72 @@ __device__ __forceinline__ void finish_row(const PagesAttnArgs& a, int b, int r0
 }
 
 // ---------------------------------------------------------------- attention
-// A workgroup of 4 wavefronts walks its share unit by unit: row_tiles x (4 / row_tiles) wavefronts, one 32-row tile and
+// A workgroup of 4 wavefronts walks its share unit by unit: row_tiles x (4 / row_tiles) wavefronts, one tile of RW rows and
 // every (4 / row_tiles)-th step each.  A step's keys and values go straight from memory to the registers of the wavefront, in operand
-// order; while a step is worked on, the next one's are under way, so that two workgroups per CU keep about 128 KB in flight.  Running
+// order; while a step is worked on, the next one's are under way.  Running
 // maximum and sum per row in base-2 exponents; the weights are carried in two bf16 pieces (three for f32 queries, which are
 // split likewise), so that P V is as exact as the f32 sums.  A unit's wavefronts meet in LDS at its end.
 // Positions that a row does not see have weight 0; a value there that is not finite must not reach the row, and 0 times it
 // would: in steps that some row of the tile does not see whole, values behind every row's last position count as 0, and any
 // other that is not finite is left out of the product and added to the rows that see it.
-template <int D, bool E4M3>
-__device__ __forceinline__ void add_not_finite(f32x16_t* o, const void* values, int base, int lane, int sees, int most) {
+template <int RW>
+struct Tile;
+template <>
+struct Tile<32> {
+    typedef f32x16_t Acc;
+    static constexpr int REGS = 16, DIMS = 16;   // accumulators of a tile, dims of one step of the first product
+    static __device__ __forceinline__ Acc mfma(uint4 a, uint4 b, Acc c) { return mfma_32x32x16(a, b, c); }
+    static __device__ __forceinline__ int piece_s(int lane, int f) { return f & 1; }   // of the f-th eight weights
+    static __device__ __forceinline__ int piece_hf(int lane) { return lane >> 5; }
+    static __device__ __forceinline__ int out_dim(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+};
+template <>
+struct Tile<16> {
+    typedef f32x4_t Acc;
+    static constexpr int REGS = 4, DIMS = 32;
+    static __device__ __forceinline__ Acc mfma(uint4 a, uint4 b, Acc c) { return mfma_16x16x32(a, b, c); }
+    static __device__ __forceinline__ int piece_s(int lane, int f) { return lane >> 5; }
+    static __device__ __forceinline__ int piece_hf(int lane) { return (lane >> 4) & 1; }
+    static __device__ __forceinline__ int out_dim(int lane, int r) { return 4 * (lane >> 4) + r; }
+};
+
+template <int D, bool E4M3, int RW>
+__device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const void* values, int base, int lane, int sees, int most) {
     using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
     const Elem* v = (const Elem*)values;
-    const int hf = lane >> 5;
     for (int key = 0; key < (E4M3 ? 64 : 32); ++key) {
         const int pos = base + key;
         if (pos >= most) break;
         const int slot = pos & 63;
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
+        for (int dt = 0; dt < D / RW; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t w = v[value_at<D, E4M3>(slot, dt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3))];
+            for (int r = 0; r < Tile<RW>::REGS; ++r) {
+                const uint32_t w = v[value_at<D, E4M3>(slot, dt * RW + Tile<RW>::out_dim(lane, r))];
                 const float f = E4M3 ? ((w & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : 0.0f) : bf16_to_f32(w);
                 if (!finite(f) && pos < sees) o[dt][r] += f;
             }
     }
 }
 
-__device__ __forceinline__ bool four_not_finite(uint32_t w) {   // of four e4m3 numbers
-    bool r = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r |= ((w >> (8 * i)) & 0x7Fu) == 0x7Fu;
-    return r;
-}
-
-template <int D, bool E4M3, int NQ>   // NQ: bf16 pieces of a query (1: bf16, 2: split, 3: f32)
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 && !(E4M3 && D == 128) ? 2 : 1))) pages_attend_kernel(PagesAttnArgs a) {
-    constexpr int STEP = E4M3 ? 64 : 32, KT = STEP / 32, KS = D / 16, DT = D / 32, NP = NQ == 3 ? 3 : 2;
-    constexpr int NL = E4M3 ? KT * DT : KS;   // 16-byte loads per lane of a step's keys, and of its values
+template <int D, bool E4M3, int NQ, int RW>   // NQ: bf16 pieces of a query (1: bf16, 2: split, 3: f32); RW: rows of a tile
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RW == 16 || NQ == 1 && !(E4M3 && D == 128) ? 2 : 1)))
+pages_attend_kernel(PagesAttnArgs a) {
+    using T = Tile<RW>;
+    constexpr int STEP = E4M3 ? 64 : 32, KT = STEP / 32, NP = NQ == 3 ? 3 : 2;
+    constexpr int NL = D / 16;                   // 16-byte loads per lane of a step's keys, and of its values
+    constexpr int QS = D / T::DIMS;              // steps of the first product
+    constexpr int SR = STEP * RW / 64;           // scores per lane
+    constexpr int NF = SR / 8;                   // eights of weights: one operand each
+    constexpr int DT = D / RW;
     constexpr int PITCH = D + 4;
-    __shared__ __align__(16) float so[4][32][PITCH];
-    __shared__ float sml[4][32][2];
+    __shared__ __align__(16) float so[4][RW][PITCH];
+    __shared__ float sml[4][RW][2];
     __shared__ long long lds[4];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, row = lane & 31;
-    const int rt = wave % a.row_tiles, ks = wave / a.row_tiles, n_ks = 4 / a.row_tiles;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane % RW, part = lane / RW;
+    const int row_tiles = RW == 16 ? 1 : a.row_tiles;
+    const int rt = wave % row_tiles, ks = wave / row_tiles, n_ks = 4 / row_tiles;
     const int heads = a.c.n_kv_heads, G = a.group_heads;
 
     long long total, live;
@@ -615,6 +635,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
     find_entry<STEP>(a, first, lds, &e, &before);
     if (e >= a.n_entries) return;   // not unless the lengths change meanwhile
     Entry en = entry_of<STEP>(a, e, nullptr);
+
+    // places of a lane's 16 bytes in the blocks of keys and of values
+    const int m32 = 8 * ((row >> 4) & 1) + (row & 7), k_lane = RW == 16 ? lane : ((row >> 3) & 1) * (D / (E4M3 ? 64 : 32)) * 64 + part * 16 + m32;
+    const int v_lane = RW == 16 ? lane : (row >> 4) * 64 + part * 16 + (row & 15);
+    const int key_of_row = RW == 16 ? 16 * (row >> 3) + (row & 7) : row;   // of a tile's first keys
 
     for (long long at = first; at < last;) {
         while (at >= before + (long long)en.steps * heads) {   // entries without rows have no steps
@@ -631,21 +656,21 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
         at = unit0 + s1;
 
         // this wavefront's rows
-        const int myrow = en.rows0 + rt * 32 + row;
+        const int myrow = en.rows0 + rt * RW + row;
         const bool have = myrow < en.rows1;
         const int t = have ? myrow / G : 0, g = have ? myrow % G : 0;
         const int sees = have ? sees_of(a, en.P, en.n, t) : 0;
         int least = have ? sees : 0x7FFFFFFF, most = sees;
-        for (int m = 16; m; m >>= 1) least = min(least, __shfl_xor(least, m)), most = max(most, __shfl_xor(most, m));
+        for (int m = RW / 2; m; m >>= 1) least = min(least, __shfl_xor(least, m)), most = max(most, __shfl_xor(most, m));
         least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
 
-        uint4 q[NQ][KS];
+        uint4 q[NQ][QS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int d = 32 * (s >> 1) + 16 * hf + 8 * (s & 1);
+        for (int s = 0; s < QS; ++s) {
+            // 8 dims: the keys' blocks have a lane's bytes in pieces of 8 (bf16) or of 16, two steps
+            const int d = E4M3 ? 2 * T::DIMS * (s >> 1) + 16 * part + 8 * (s & 1) : T::DIMS * s + 8 * part;
             if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
-                uint4 z{0u, 0u, 0u, 0u};
-                q[0][s] = q[1][s] = z;
+                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
                 if (have) {
                     const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
                     q[0][s] = *(const uint4*)p;
@@ -669,11 +694,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
             }
         }
 
-        f32x16_t o[DT];
+        typename T::Acc o[DT];
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
+            for (int r = 0; r < T::REGS; ++r) o[dt][r] = 0.0f;
         float m_run = -INFINITY, l_run = 0.0f;
 
         // the unit's pages: lane i of the window holds the place and the id of page win + i
@@ -708,25 +733,32 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
             return false;
         };
         uint4 kf[NL], vf[NL];
-        uint32_t ksc[KT], vsc[KT * 4];
+        uint32_t ksc[STEP / RW], vsc[SR / 4];
+        // load i: RW 16: block i.  RW 32: keys (e4m3: group of 32,) block of dims, which half of its pieces; values: dims 32 (i / 2) .., keys 16 (i % 2) ..
         auto load_k = [&](size_t hd, int bs) {
-            const uint4* p = (const uint4*)((const char*)a.c.k + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + lane;
+            const uint4* p = (const uint4*)((const char*)a.c.k + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + k_lane;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) kf[i] = p[i * 64];
+            for (int i = 0; i < NL; ++i) {
+                constexpr int B = D / (E4M3 ? 64 : 32);   // blocks of a tile of 16 keys
+                kf[i] = p[RW == 16 ? i * 64 : (i / (2 * B)) * 2 * B * 64 + (i % (2 * B) >> 1) * 64 + (i & 1) * 32];
+            }
             if constexpr (E4M3) {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) ksc[kt] = a.c.scale[hd * 128 + kt * 32 + row];
+                for (int i = 0; i < STEP / RW; ++i) ksc[i] = a.c.scale[hd * 128 + (RW == 16 ? (i >> 1) * 32 + (i & 1) * 8 : i * 32) + key_of_row];
             }
         };
         auto load_v = [&](size_t hd, int bs) {
-            const uint4* p = (const uint4*)((const char*)a.c.v + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + lane;
+            const uint4* p = (const uint4*)((const char*)a.c.v + hd * 64 * D * (E4M3 ? 1 : 2) + (E4M3 ? 0 : (bs & 32) * D * 2)) + v_lane;
 #pragma unroll
-            for (int i = 0; i < NL; ++i) vf[i] = p[i * 64];
+            for (int i = 0; i < NL; ++i) vf[i] = p[RW == 16 ? i * 64 : (i >> 1) * 128 + (i & 1) * 32];
             if constexpr (E4M3) {
 #pragma unroll
-                for (int i = 0; i < KT * 4; ++i) vsc[i] = *(const uint32_t*)(a.c.scale + hd * 128 + 64 + i * 8 + 4 * hf);
+                for (int i = 0; i < SR / 4; ++i)
+                    vsc[i] = *(const uint32_t*)(a.c.scale + hd * 128 + 64 + (i / (RW / 8)) * 32 + value_key(T::piece_s(lane, i >> 1), T::piece_hf(lane), 4 * (i & 1)));
             }
         };
+        // position, in the step, of a lane's score i
+        auto key_of = [&](int i) { return (i / (RW / 2)) * 32 + value_key(T::piece_s(lane, i >> 3), T::piece_hf(lane), i & 7); };
 
         bool more = next();
         int cur_base = base;
@@ -736,27 +768,28 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
             load_v(cur_head, cur_base);
         }
         while (more) {
-            f32x16_t sc[KT];
+            float x[SR];
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
+            for (int i = 0; i < STEP / RW; ++i) {   // tiles of RW keys
+                typename T::Acc sc;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sc[kt][r] = 0.0f;
+                for (int r = 0; r < T::REGS; ++r) sc[r] = 0.0f;
                 // the small pieces first
 #pragma unroll
                 for (int p = NQ - 1; p >= 0; --p)
 #pragma unroll
-                    for (int i = 0; i < DT; ++i)
-#pragma unroll
-                        for (int f = 0; f < 2; ++f) {
-                            uint4 k;
-                            if constexpr (E4M3) {
-                                const uint4 w = kf[kt * DT + i];
-                                k = f ? eight_bf16(w.z, w.w, scale_of(ksc[kt])) : eight_bf16(w.x, w.y, scale_of(ksc[kt]));
-                            } else {
-                                k = kf[i * 2 + f];
-                            }
-                            sc[kt] = mfma_32x32x16(k, q[p][i * 2 + f], sc[kt]);
+                    for (int j = 0; j < QS; ++j) {
+                        uint4 k;
+                        if constexpr (E4M3) {
+                            const uint4 w = kf[i * (QS / 2) + j / 2];
+                            k = j & 1 ? eight_bf16(w.z, w.w, scale_of(ksc[i])) : eight_bf16(w.x, w.y, scale_of(ksc[i]));
+                        } else {
+                            k = kf[i * QS + j];
                         }
+                        sc = T::mfma(k, q[p][j], sc);
+                    }
+#pragma unroll
+                for (int r = 0; r < T::REGS; ++r) x[i * T::REGS + r] = sc[r];
             }
             const bool masked = cur_base + STEP > least;
             more = next();
@@ -765,38 +798,34 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
             // scores in base-2 exponents, their maximum
             float top = -INFINITY;
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+            for (int i = 0; i < SR; ++i) {
+                x[i] *= a.scale_log2;
+                if (masked && cur_base + key_of(i) >= sees) x[i] = -INFINITY;
+                top = fmaxf(top, x[i]);
+            }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float x = sc[kt][r] * a.scale_log2;
-                    if (masked && cur_base + kt * 32 + 8 * (r >> 2) + 4 * hf + (r & 3) >= sees) x = -INFINITY;
-                    sc[kt][r] = x;
-                    top = fmaxf(top, x);
-                }
-            top = fmaxf(top, __shfl_xor(top, 32));
+            for (int m = RW; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
             if (__any(top > m_run)) {
                 const float m = fmaxf(m_run, top), f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
                 l_run *= f;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+                    for (int r = 0; r < T::REGS; ++r) o[dt][r] *= f;
                 m_run = m;
             }
             const float ref = m_run == -INFINITY ? 0.0f : m_run;
             float sum = 0.0f;
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float p = __builtin_amdgcn_exp2f(sc[kt][r] - ref);
-                    sum += p;
-                    if constexpr (E4M3) {
-                        const float w = scale_of((vsc[kt * 4 + (r >> 2)] >> (8 * (r & 3))) & 0xFFu);
-                        p = p > 0.0f || p != p ? p * w : 0.0f;   // scales of empty places may be anything
-                    }
-                    sc[kt][r] = p;
+            for (int i = 0; i < SR; ++i) {
+                float p = __builtin_amdgcn_exp2f(x[i] - ref);
+                sum += p;
+                if constexpr (E4M3) {
+                    const float w = scale_of((vsc[i >> 2] >> (8 * (i & 3))) & 0xFFu);
+                    p = p > 0.0f || p != p ? p * w : 0.0f;   // scales of empty places may be anything
                 }
+                x[i] = p;
+            }
             l_run += sum;
 
             bool odd = false;
@@ -804,26 +833,25 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
                     uint32_t w[4] = {vf[i].x, vf[i].y, vf[i].z, vf[i].w};
+                    const int ps = RW == 16 ? T::piece_s(lane, 0) : i & 1, ph = T::piece_hf(lane);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (E4M3) {   // four keys of step j / 2: 8 (j & 1) + 4 hf + 0..3
-                            const int pos = cur_base + (i / DT) * 32 + 16 * (j >> 1) + 8 * (j & 1) + 4 * hf;
+                        if constexpr (E4M3) {   // four keys of the group of 32 j / 2
+                            const int pos = cur_base + (j >> 1) * 32 + value_key(ps, ph, 4 * (j & 1));
 #pragma unroll
                             for (int b = 0; b < 4; ++b)
-                                if (pos + b >= most) w[j] &= ~(0xFFu << (8 * b));
-                            if (four_not_finite(w[j])) {
-                                odd = true;
+                                if (pos + b >= most || ((w[j] >> (8 * b)) & 0x7Fu) == 0x7Fu) {
+                                    odd |= pos + b < most;
+                                    w[j] &= ~(0xFFu << (8 * b));
+                                }
+                        } else {
+                            const int pos = cur_base + value_key(ps, ph, 2 * j);
 #pragma unroll
-                                for (int b = 0; b < 4; ++b)
-                                    if (((w[j] >> (8 * b)) & 0x7Fu) == 0x7Fu) w[j] &= ~(0xFFu << (8 * b));
-                            }
-                        } else {   // i = (dt, step), two keys
-                            const int pos = cur_base + value_key(i & 1, hf, 2 * j);
-#pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                if (pos + b >= most) w[j] &= ~(0xFFFFu << (16 * b));
-                                if (((w[j] >> (16 * b)) & 0x7F80u) == 0x7F80u) odd = true, w[j] &= ~(0xFFFFu << (16 * b));
-                            }
+                            for (int b = 0; b < 2; ++b)
+                                if (pos + b >= most || ((w[j] >> (16 * b)) & 0x7F80u) == 0x7F80u) {
+                                    odd |= pos + b < most;
+                                    w[j] &= ~(0xFFFFu << (16 * b));
+                                }
                         }
                     }
                     vf[i] = uint4{w[0], w[1], w[2], w[3]};
@@ -831,71 +859,68 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 
             }
 
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+            for (int f = 0; f < NF; ++f) {
+                uint4 pf[NP];
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    float x[8];
+                for (int p = 0; p < NP; ++p) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = sc[kt][st * 8 + i];
-                    uint4 pf[NP];
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                            x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                        }
-                        pf[p] = uint4{w[0], w[1], w[2], w[3]};
+                    for (int i = 0; i < 4; ++i) {
+                        float* y = x + f * 8 + 2 * i;
+                        w[i] = pack_bf16x2(y[0], y[1]);
+                        y[0] -= bf16_to_f32(w[i] & 0xFFFFu), y[1] -= __uint_as_float(w[i] & 0xFFFF0000u);
                     }
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        uint4 v;
-                        if constexpr (E4M3) {
-                            const uint4 w = vf[kt * DT + dt];
-                            v = st ? eight_bf16(w.z, w.w, 1.0f) : eight_bf16(w.x, w.y, 1.0f);
-                        } else {
-                            v = vf[dt * 2 + st];
-                        }
-#pragma unroll
-                        for (int p = NP - 1; p >= 0; --p) o[dt] = mfma_32x32x16(v, pf[p], o[dt]);
-                    }
+                    pf[p] = uint4{w[0], w[1], w[2], w[3]};
                 }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    uint4 v;
+                    if constexpr (E4M3) {
+                        const uint4 w = RW == 16 ? vf[dt] : vf[dt * 2 + (f & 1)];
+                        v = (RW == 16 ? f : f >> 1) ? eight_bf16(w.z, w.w, 1.0f) : eight_bf16(w.x, w.y, 1.0f);
+                    } else {
+                        v = RW == 16 ? vf[dt] : vf[dt * 2 + f];
+                    }
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) o[dt] = T::mfma(v, pf[p], o[dt]);
+                }
+            }
             if (masked && __any(odd))
-                add_not_finite<D, E4M3>(o, (const char*)a.c.v + cur_head * 64 * D * (E4M3 ? 1 : 2), cur_base, lane, sees, most);
+                add_not_finite<D, E4M3, RW>(o, (const char*)a.c.v + cur_head * 64 * D * (E4M3 ? 1 : 2), cur_base, lane, sees, most);
             if (more) load_v(head, base);
             cur_base = base, cur_head = head;
         }
 
         // the unit's wavefronts meet
-        l_run += __shfl_xor(l_run, 32);
+#pragma unroll
+        for (int m = RW; m < 64; m <<= 1) l_run += __shfl_xor(l_run, m);
         __syncthreads();
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(float4*)&so[wave][row][dt * 32 + 8 * j + 4 * hf] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
-        if (hf == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
+            for (int j = 0; j < T::REGS / 4; ++j)
+                *(float4*)&so[wave][row][dt * RW + T::out_dim(lane, 4 * j)] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+        if (part == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
         __syncthreads();
-        for (int i = tid; i < a.row_tiles * 32 * (D / 4); i += 256) {
-            const int r = i / (D / 4), d = i % (D / 4) * 4, tile = r >> 5, rr = r & 31, rw = en.rows0 + r;
+        for (int i = tid; i < row_tiles * RW * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4, tile = r / RW, rr = r % RW, rw = en.rows0 + r;
             if (rw >= en.rows1) continue;
             float m = -INFINITY, l = 0.0f;
-            for (int k = 0; k < n_ks; ++k) m = fmaxf(m, sml[k * a.row_tiles + tile][rr][0]);
+            for (int k = 0; k < n_ks; ++k) m = fmaxf(m, sml[k * row_tiles + tile][rr][0]);
             const float ref = m == -INFINITY ? 0.0f : m;
-            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int k = 0; k < n_ks; ++k) {
-                const int w = k * a.row_tiles + tile;
+                const int w = k * row_tiles + tile;
                 const float f = __builtin_amdgcn_exp2f(sml[w][rr][0] - ref);
-                const float4 y = *(const float4*)&so[w][rr][d];
+                const float4 z = *(const float4*)&so[w][rr][d];
                 l += sml[w][rr][1] * f;
-                x[0] += y.x * f, x[1] += y.y * f, x[2] += y.z * f, x[3] += y.w * f;
+                y[0] += z.x * f, y[1] += z.y * f, y[2] += z.z * f, y[3] += z.w * f;
             }
             if (whole) {
-                finish_row<D>(a, en.b, en.r0, en.n, rw / G, h * G + rw % G, d, m, l, x);
+                finish_row<D>(a, en.b, en.r0, en.n, rw / G, h * G + rw % G, d, m, l, y);
             } else {
-                const size_t at_row = (size_t)slot * 32 * a.row_tiles + r;
-                *(float4*)(a.part_o + at_row * D + d) = float4{x[0], x[1], x[2], x[3]};
+                const size_t at_row = (size_t)slot * a.block_rows + r;
+                *(float4*)(a.part_o + at_row * D + d) = float4{y[0], y[1], y[2], y[3]};
                 if (d == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m, l};
             }
         }
@@ -922,7 +947,7 @@ __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
     if (n == 1) return;
     const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (u0 > sh.begin(w0) ? 1 : 0);
     for (int r = slice * ROWS + threadIdx.x / TPR; en.rows0 + r < en.rows1; r += a.slices * ROWS) {
-        auto place = [&](int i) { return (size_t)(i == 0 ? first : 2 * (w0 + i)) * 32 * a.row_tiles + r; };
+        auto place = [&](int i) { return (size_t)(i == 0 ? first : 2 * (w0 + i)) * a.block_rows + r; };
         float m = -INFINITY;
         for (int i = threadIdx.x % TPR; i < n; i += TPR) m = fmaxf(m, a.part_ml[place(i) * 2]);
         for (int k = TPR / 2; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
@@ -1166,9 +1191,14 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
     return by_type(a.c, [&](auto d, auto e) {
         constexpr int D = decltype(d)::value;
         constexpr bool E = decltype(e)::value;
-        if (a.q_split) pages_attend_kernel<D, E, 2><<<a.grid, 256, 0, s>>>(a);
-        else if (a.q.f32) pages_attend_kernel<D, E, 3><<<a.grid, 256, 0, s>>>(a);
-        else pages_attend_kernel<D, E, 1><<<a.grid, 256, 0, s>>>(a);
+        auto run = [&](auto nq) {
+            constexpr int NQ = decltype(nq)::value;
+            if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
+            else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
+        };
+        if (a.q_split) run(std::integral_constant<int, 2>());
+        else if (a.q.f32) run(std::integral_constant<int, 3>());
+        else run(std::integral_constant<int, 1>());
         const hipError_t st = hipGetLastError();
         if (st != hipSuccess) return st;
         pages_combine_kernel<D, E><<<a.n_entries * a.c.n_kv_heads * a.slices, 256, 0, s>>>(a);
