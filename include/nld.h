@@ -552,6 +552,27 @@ nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chu
                             int32_t n_top, int32_t n_first, int32_t group, int32_t mode, int32_t bidir_from, int32_t* list, int32_t n_list,
                             void* workspace, size_t ws_bytes, void* stream);
 
+/* The block-decode passes over a paged cache (batch = pages->batch; the pages' layers, KV heads and head_dim are the model's), with the
+ * arguments and results of nld_block_forward, nld_draft and nld_verify_accept.  What differs:
+ *  - the table has pages for positions P_b .. P_b + k - 1, and every pass writes its block's keys and values there, a draft pass too (the
+ *    verify pass writes them again; as in the other cache they are scratch until a commit advances lengths);
+ *  - a block attends to its own keys and values as the pages hold them, in bf16 or 8 bits;
+ *  - sparse (optional): every group of tokens attends to the pages that nld_pages_select would choose for it, KV head by KV head.
+ * A page that is missing sets NLD_DEV_BAD_PAGE (its positions stay unwritten and unseen; a commit still counts them).
+ * Errors: as nld_block_forward, nld_draft, nld_verify_accept, nld_pages_select, INVALID_ARG for pages of another shape than the model's. */
+typedef struct {
+    int32_t n_top, n_first, group;
+} nld_sparse;
+size_t nld_pages_pass_workspace_bytes(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, int32_t k);
+nld_status nld_pages_block_forward(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* tokens, int32_t k,
+                                   int32_t mode, int32_t bidir_from, float* logits, int32_t* argmax, void* workspace, size_t ws_bytes,
+                                   void* stream);
+nld_status nld_pages_draft(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* anchor, int32_t k,
+                           int32_t bidir_from, int32_t* draft, float* logits, void* workspace, size_t ws_bytes, void* stream);
+nld_status nld_pages_verify_accept(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* anchor,
+                                   const int32_t* draft, int32_t k, int32_t* accept_len, int32_t* committed, int32_t* next_anchor,
+                                   float* logits, void* workspace, size_t ws_bytes, void* stream);
+
 /* ---- tracing aid -------------------------------------------------------------
  * While enabled, every kernel launch made by the block-decode calls records a
  * pair of HIP events on its own dispatch (hipExtLaunchKernel), so the times are

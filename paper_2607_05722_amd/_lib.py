@@ -39,7 +39,8 @@ EXPORTED = [
     "nld_read_device_status", "nld_trace_enable", "nld_trace_read", "nld_verify_accept_noalloc",
     "nld_hbm_read_probe", "nld_logits_workspace_bytes", "nld_top_logits", "nld_distill_from_logits",
     "nld_policy_from_logits", "nld_pages_list_len", "nld_pages_workspace_bytes", "nld_pages_write", "nld_pages_read",
-    "nld_pages_attend", "nld_pages_select",
+    "nld_pages_attend", "nld_pages_select", "nld_pages_pass_workspace_bytes", "nld_pages_block_forward", "nld_pages_draft",
+    "nld_pages_verify_accept",
 ]
 
 NLD_F32 = 0
@@ -89,6 +90,10 @@ class Pages(ctypes.Structure):
     _fields_ = [("k", c_vp), ("v", c_vp), ("scale", c_vp), ("bounds", c_vp), ("bound_scale", c_vp), ("dtype", c_i32),
                 ("n_layers", c_i32), ("n_pages", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32), ("table", c_vp),
                 ("lengths", c_vp), ("batch", c_i32), ("max_pages", c_i32)]
+
+
+class Sparse(ctypes.Structure):
+    _fields_ = [("n_top", c_i32), ("n_first", c_i32), ("group", c_i32)]
 
 
 class Chunk(ctypes.Structure):
@@ -211,6 +216,14 @@ def load(path: str = None):
     L.nld_pages_select.restype = c_i32
     L.nld_pages_select.argtypes = [P(Pages), c_i32, P(Chunk), P(Heads), c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp,
                                    c_sz, c_vp]
+    L.nld_pages_pass_workspace_bytes.restype = c_sz
+    L.nld_pages_pass_workspace_bytes.argtypes = [c_vp, P(Pages), P(Sparse), c_i32]
+    L.nld_pages_block_forward.restype = c_i32
+    L.nld_pages_block_forward.argtypes = [c_vp, P(Pages), P(Sparse), c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.nld_pages_draft.restype = c_i32
+    L.nld_pages_draft.argtypes = [c_vp, P(Pages), P(Sparse), c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.nld_pages_verify_accept.restype = c_i32
+    L.nld_pages_verify_accept.argtypes = [c_vp, P(Pages), P(Sparse), c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
     _lib = L
     return L
 

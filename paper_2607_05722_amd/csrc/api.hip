@@ -254,6 +254,154 @@ int device_cus() {
     return cached[dev];
 }
 
+constexpr double LOG2E = 1.44269504088896340736;
+
+// ---------------------------------------------------------------- paged cache
+constexpr int MAX_PAGE_WGS = 1 << 23;    // workgroups of 256 threads in one launch
+constexpr int MAX_SEQ_PAGES = 1 << 24;   // 2^30 positions
+constexpr int MAX_CHUNK_ROWS = 1 << 24;
+
+nld_status check_pages(const nld_pages* c, int layer) {
+    if (!c || !c->k || !c->v || !c->table || !c->lengths) return fail(NLD_ERR_INVALID_ARG, "pages or one of its pointers is NULL");
+    if (c->dtype != NLD_BF16 && c->dtype != NLD_E4M3) return fail(NLD_ERR_INVALID_ARG, "pages: dtype must be NLD_BF16 or NLD_E4M3");
+    if (c->dtype == NLD_E4M3 && !c->scale) return fail(NLD_ERR_INVALID_ARG, "pages: 8-bit pages need their scales");
+    if (!c->bounds != !c->bound_scale) return fail(NLD_ERR_INVALID_ARG, "pages: bounds and bound_scale go together");
+    if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1)
+        return fail(NLD_ERR_INVALID_ARG, "pages: sizes must be positive");
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(NLD_ERR_SHAPE, "pages: head_dim must be 64 or 128");
+    if (c->max_pages > MAX_SEQ_PAGES) return fail(NLD_ERR_SHAPE, "pages: max_pages (%d) exceeds %d", c->max_pages, MAX_SEQ_PAGES);
+    if (layer < 0 || layer >= c->n_layers) return fail(NLD_ERR_INVALID_ARG, "layer must be in [0, %d) (got %d)", c->n_layers, layer);
+    if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->scale | (uintptr_t)c->bounds) % 16 || (uintptr_t)c->bound_scale % 4)
+        return fail(NLD_ERR_INVALID_ARG, "pages: arrays must be 16-byte aligned");
+    return NLD_OK;
+}
+
+PageCache page_layer(const nld_pages* c, int layer) {
+    const size_t heads = (size_t)layer * c->n_pages * c->n_kv_heads, page = (size_t)64 * c->head_dim * (c->dtype == NLD_BF16 ? 2 : 1);
+    PageCache p{};
+    p.k = (char*)c->k + heads * page;
+    p.v = (char*)c->v + heads * page;
+    p.scale = c->dtype == NLD_E4M3 ? (uint8_t*)c->scale + heads * 128 : nullptr;
+    p.bounds = c->bounds ? (int8_t*)c->bounds + heads * 2 * c->head_dim : nullptr;
+    p.bound_scale = c->bounds ? c->bound_scale + heads : nullptr;
+    p.e4m3 = c->dtype == NLD_E4M3;
+    p.n_pages = c->n_pages;
+    p.n_kv_heads = c->n_kv_heads;
+    p.head_dim = c->head_dim;
+    p.table = c->table;
+    p.lengths = c->lengths;
+    p.batch = c->batch;
+    p.max_pages = c->max_pages;
+    return p;
+}
+
+nld_status check_chunk(const nld_pages* c, const nld_chunk* ch) {
+    if (!ch) return fail(NLD_ERR_INVALID_ARG, "chunk is NULL");
+    if (ch->rows < 1 || ch->max_rows < 1 || ch->max_rows > ch->rows)
+        return fail(NLD_ERR_INVALID_ARG, "chunk: max_rows must be in [1, rows] (got %d of %d)", ch->max_rows, ch->rows);
+    if (!ch->row_start && (long long)ch->max_rows * c->batch != ch->rows)
+        return fail(NLD_ERR_INVALID_ARG, "chunk: without row_start, rows (%d) must be batch * max_rows (%d * %d)", ch->rows, c->batch, ch->max_rows);
+    if (ch->rows > MAX_CHUNK_ROWS) return fail(NLD_ERR_SHAPE, "chunk: %d rows exceed %d", ch->rows, MAX_CHUNK_ROWS);
+    return NLD_OK;
+}
+
+// elements from the first one to past the last one
+long long heads_extent(const nld_heads* x, int rows, int heads, int dim) {
+    return (rows - 1) * x->row_stride + (heads - 1) * x->head_stride + dim;
+}
+
+// out: rows and heads must be apart from each other
+nld_status check_heads(const nld_heads* x, const char* what, int rows, int heads, int dim, bool out) {
+    if (!x || !x->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
+    if (x->dtype != NLD_F32 && x->dtype != NLD_BF16) return fail(NLD_ERR_INVALID_ARG, "%s: dtype must be NLD_F32 or NLD_BF16", what);
+    if (x->row_stride < 0 || x->head_stride < 0 || x->row_stride >> 38 || x->head_stride >> 38)
+        return fail(NLD_ERR_INVALID_ARG, "%s: strides must be in [0, 2^38)", what);
+    if ((uintptr_t)x->data % (x->dtype == NLD_BF16 ? 2 : 4)) return fail(NLD_ERR_INVALID_ARG, "%s: data is not aligned to its type", what);
+    if (out) {
+        const long long rs = rows > 1 ? x->row_stride : LLONG_MAX, hs = heads > 1 ? x->head_stride : LLONG_MAX;
+        const long long inner = std::min(rs, hs), outer = std::max(rs, hs), n_inner = rs <= hs ? rows : heads;
+        if (inner < dim || (outer != LLONG_MAX && outer < (n_inner - 1) * inner + dim))
+            return fail(NLD_ERR_INVALID_ARG, "%s: its rows overlap each other", what);
+    }
+    return NLD_OK;
+}
+
+HeadRows head_rows(const nld_heads* x) { return HeadRows{x->data, x->dtype == NLD_F32, 0, x->row_stride, x->head_stride}; }
+PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows, c->row_start}; }
+
+// The attention's plan and workspace: the status word, then the parts of units that workgroups share, or a selection's scores.
+// Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
+// registers) and are what hides the loads' latency.
+struct PagesPlan {
+    int block_rows, row_tiles, n_blk, grid, slices;
+    size_t part_ml, total;
+};
+
+bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, PagesPlan* out) {
+    PagesPlan p{};
+    const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
+    p.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;
+    const long long blocks = group ? cdiv(max_rows, group) : (rows + p.block_rows - 1) / p.block_rows;
+    if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
+    p.n_blk = (int)blocks;
+    p.grid = 2 * device_cus();
+    // the second launch: a few thousand workgroups at most, and one where units are that many
+    const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
+    p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
+    const size_t part_rows = (size_t)2 * p.grid * p.block_rows;
+    p.part_ml = 256 + part_rows * head_dim * 4;
+    p.total = align256(p.part_ml + part_rows * 8);
+    *out = p;
+    return true;
+}
+
+size_t score_bytes(const nld_pages* c, int max_rows, int group) {
+    return (size_t)c->batch * cdiv(max_rows, group) * c->n_kv_heads * c->max_pages * 4;
+}
+
+nld_status check_mode(int mode, int bidir_from, int max_rows) {
+    if (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT) return fail(NLD_ERR_INVALID_ARG, "mode must be 0 or 1");
+    if (bidir_from < 0 || bidir_from > max_rows) return fail(NLD_ERR_INVALID_ARG, "bidir_from must be in [0, max_rows]");
+    return NLD_OK;
+}
+
+nld_status check_group(const nld_pages* c, int n_q_heads, int group) {
+    if (group < 1) return fail(NLD_ERR_INVALID_ARG, "group must be >= 1 (got %d)", group);
+    if ((long long)group * (n_q_heads / c->n_kv_heads) > PAGES_GROUP_ROWS)
+        return fail(NLD_ERR_SHAPE, "group * (n_q_heads / n_kv_heads) = %lld exceeds %d", (long long)group * (n_q_heads / c->n_kv_heads), PAGES_GROUP_ROWS);
+    return NLD_OK;
+}
+
+nld_status check_q_heads(const nld_pages* c, int n_q_heads) {
+    if (n_q_heads < 1 || n_q_heads % c->n_kv_heads)
+        return fail(NLD_ERR_SHAPE, "n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", n_q_heads, c->n_kv_heads);
+    return NLD_OK;
+}
+
+// the launch of an attention: what does not hang on where queries come from and outputs go
+PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_heads, int mode, int bidir_from, float scale, const PagesPlan& p, void* ws,
+                         size_t off) {
+    PagesAttnArgs a{};
+    a.c = c;
+    a.ch = ch;
+    a.group_heads = group_heads;
+    a.draft = mode == NLD_MODE_DRAFT;
+    a.bidir_from = bidir_from;
+    a.scale_log2 = (float)(LOG2E * (double)scale);
+    a.block_rows = p.block_rows;
+    a.row_tiles = p.row_tiles;
+    a.n_blk = p.n_blk;
+    a.n_entries = c.batch * p.n_blk;
+    a.grid = p.grid;
+    a.slices = p.slices;
+    a.least_steps = 4 / p.row_tiles;
+    a.part_o = at<float>(ws, off + 256);
+    a.part_ml = at<float>(ws, off + p.part_ml);
+    a.status = at<uint32_t>(ws, 0);
+    return a;
+}
+
 enum Source { SRC_TOKENS = 0, SRC_DRAFT = 1, SRC_VERIFY = 2, SRC_QUAD = 3 };
 
 struct PassIO {
@@ -280,6 +428,16 @@ struct PassIO {
     // quadratic self-speculation (mode NLD_MODE_QUAD_INTERNAL): chain length and the verifier's mixture
     int quad_k;
     float lambda;
+    const struct PagedPass* paged;   // the cache is a paged one
+};
+
+// A pass over a paged cache: the attention's plan, the selection (n_top, n_first, group; group 0: every page is read), and where in the
+// workspace, behind the pass's own part, the attention's and the lists start.
+struct PagedPass {
+    const nld_pages* pages;
+    PagesPlan plan;
+    int n_top, n_first, group, n_groups, n_list;
+    size_t attn, lists, total;
 };
 
 // Attention mode of a quadratic pass (never a caller's mode value).
@@ -300,6 +458,48 @@ nld_status validate_call(const nld_model* m, const nld_kv_cache* kv, int batch, 
     *out = make_layout(c, batch, k, kv->max_len, quad_k);
     if (ws_bytes < out->total)
         return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, out->total);
+    return NLD_OK;
+}
+
+// What a pass over a paged cache needs of its arguments; kv: the lengths and sizes that the pass takes of a cache.
+nld_status validate_paged(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, int k, int mode, void* ws, size_t ws_bytes, nld_kv_cache* kv,
+                          Layout* out, PagedPass* pp) {
+    if (!m) return fail(NLD_ERR_INVALID_ARG, "model is NULL");
+    nld_status st = check_pages(pages, 0);
+    if (st != NLD_OK) return st;
+    const nld_config& c = m->cfg;
+    if (pages->n_layers != c.n_layers || pages->n_kv_heads != c.n_kv_heads || pages->head_dim != c.head_dim)
+        return fail(NLD_ERR_INVALID_ARG, "pages have %d layers, %d KV heads of %d dims, the model %d, %d of %d", pages->n_layers, pages->n_kv_heads,
+                    pages->head_dim, c.n_layers, c.n_kv_heads, c.head_dim);
+    *kv = nld_kv_cache{pages->k, pages->v, pages->lengths, pages->batch, 64};
+    Layout L;
+    st = validate_call(m, kv, pages->batch, k, ws, ~(size_t)0, &L);   // the pass's own part has none of the other attention's partials worth mention
+    if (st != NLD_OK) return st;
+    kv->max_len = pages->max_pages * 64;
+    PagedPass p{};
+    p.pages = pages;
+    const int G = c.n_q_heads / c.n_kv_heads;
+    if (sparse) {
+        if (!pages->bounds) return fail(NLD_ERR_INVALID_ARG, "a selection needs the pages' bounds");
+        st = check_group(pages, c.n_q_heads, sparse->group);
+        if (st != NLD_OK) return st;
+        p.n_top = sparse->n_top;
+        p.n_first = sparse->n_first;
+        p.group = sparse->group;
+        p.n_groups = cdiv(k, p.group);
+        p.n_list = nld_pages_list_len(k, p.group, p.n_top, p.n_first, mode);
+        if (p.n_list < 1) return fail(NLD_ERR_INVALID_ARG, "n_top and n_first must be in [0, %d]", MAX_SEQ_PAGES);
+        if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
+            return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
+    }
+    if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, &p.plan))
+        return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
+    p.attn = align256(L.total);
+    p.lists = p.attn + std::max(p.plan.total, p.group ? align256(256 + score_bytes(pages, k, p.group)) : 0);
+    p.total = align256(p.lists + (size_t)4 * pages->batch * p.n_groups * pages->n_kv_heads * p.n_list);
+    if (ws_bytes < p.total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, p.total);
+    *out = L;
+    *pp = p;
     return NLD_OK;
 }
 
@@ -432,6 +632,49 @@ hipError_t normed_gemm(int kind, int epi, const PanelPlan* plans, GemmArgs g, vo
     return panel_gemm(epi, plans[kind], g, ws, L, s, nullptr);
 }
 
+// A layer's attention over a paged cache, in place of the other one: the block's keys and values go to their pages (positions P_b + j,
+// in draft passes too: they are scratch until a commit), which the block's queries then read along with the prefix.
+hipError_t paged_attention(const nld_model* mdl, const PagedPass& pp, int mode, int bidir_from, int layer, int k, uint32_t plain, void* ws, const Layout& L,
+                           hipStream_t s) {
+    const nld_config& c = mdl->cfg;
+    const PageCache cache = page_layer(pp.pages, layer);
+    const PageChunk ch{L.M, k, nullptr};
+    uint32_t* status = at<uint32_t>(ws, L.status);
+    hipError_t e = launch_pages_write(cache, HeadRows{}, HeadRows{}, at<uint16_t>(ws, L.blk_k), at<uint16_t>(ws, L.blk_v), ch, status, s);
+    if (e != hipSuccess) return e;
+    PagesAttnArgs a = pages_args(cache, ch, c.n_q_heads / c.n_kv_heads, mode, bidir_from, (float)(1.0 / sqrt((double)c.head_dim)), pp.plan, ws, pp.attn);
+    if (pp.group) {
+        PagesSelectArgs sel{};
+        sel.c = cache;
+        sel.ch = ch;
+        sel.q_split = at<uint16_t>(ws, L.q);
+        sel.q_row_tiles = L.row_tiles;
+        sel.group_heads = a.group_heads;
+        sel.draft = a.draft;
+        sel.bidir_from = bidir_from;
+        sel.n_top = pp.n_top;
+        sel.n_first = pp.n_first;
+        sel.group = pp.group;
+        sel.n_groups = pp.n_groups;
+        sel.n_list = pp.n_list;
+        sel.scores = at<float>(ws, pp.attn + 256);
+        sel.list = at<int32_t>(ws, pp.lists);
+        sel.status = status;
+        e = launch_pages_select(sel, s);
+        if (e != hipSuccess) return e;
+        a.list = sel.list;
+        a.n_list = pp.n_list;
+        a.group = pp.group;
+    }
+    a.q_split = at<uint16_t>(ws, L.q);
+    a.q_row_tiles = L.row_tiles;
+    a.o_split = at<uint16_t>(ws, L.o);
+    a.o_ksteps = cdiv(c.n_q_heads * c.head_dim, 32);
+    a.plain_o = (plain & SITE_O) != 0;
+    a.status = status;
+    return launch_pages_attend(a, s);
+}
+
 nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int k, const PassIO& io, void* ws,
                     const Layout& L, hipStream_t s) {
     const nld_config& c = mdl->cfg;
@@ -505,7 +748,7 @@ nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int
         g.q_row_tiles = L.row_tiles;
         g.kc = kc;
         g.vc = vc;
-        g.write_cache = io.mode == NLD_MODE_VERIFY || io.mode == NLD_MODE_QUAD_INTERNAL;   // quad: chain rows
+        g.write_cache = !io.paged && (io.mode == NLD_MODE_VERIFY || io.mode == NLD_MODE_QUAD_INTERNAL);   // quad: chain rows
         g.quad_k = io.quad_k;
         g.blk_k = at<uint16_t>(ws, L.blk_k);
         g.blk_v = at<uint16_t>(ws, L.blk_v);
@@ -524,6 +767,10 @@ nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int
         }
         if (io.kv_only && l == c.n_layers - 1) break;   // every layer's K/V rows are written
 
+        if (io.paged) {
+            TraceScope ts(NLD_TRACE_ATTENTION, s);
+            HIP_TRY(paged_attention(mdl, *io.paged, io.mode, io.bidir_from, l, k, plain, ws, L, s));
+        }
         AttnArgs at_{};
         at_.q = at<uint16_t>(ws, L.q);
         at_.kc = kc;
@@ -550,7 +797,7 @@ nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int
         at_.n_seq = batch;
         at_.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
         at_.plain = plain & (SITE_P | SITE_O);
-        {
+        if (!io.paged) {
             TraceScope ts(NLD_TRACE_ATTENTION, s);
             HIP_TRY(launch_attention(D, L.attn_kh, L.attn_waves, L.attn_z, L.units, at_, s));
             HIP_TRY(launch_attention_combine(D, L.units, (nq / nkv) * k, at_, s));
@@ -704,7 +951,6 @@ nld_status run_pass(const nld_model* mdl, const nld_kv_cache* kv, int batch, int
 }
 
 // ---------------------------------------------------------------- rows of logits
-constexpr double LOG2E = 1.44269504088896340736;
 constexpr int MAX_LOGIT_ROWS = 1 << 20;
 static_assert(TOP_MAX == NLD_TOP_MAX, "entries per row");
 
@@ -812,152 +1058,6 @@ nld_status loss_args(const nld_logits* z, const nld_logits* grad, float temperat
     a.saved = at<uint2>(ws, L.entries);
     *out = a;
     return NLD_OK;
-}
-
-// ---------------------------------------------------------------- paged cache
-constexpr int MAX_PAGE_WGS = 1 << 23;    // workgroups of 256 threads in one launch
-constexpr int MAX_SEQ_PAGES = 1 << 24;   // 2^30 positions
-constexpr int MAX_CHUNK_ROWS = 1 << 24;
-
-nld_status check_pages(const nld_pages* c, int layer) {
-    if (!c || !c->k || !c->v || !c->table || !c->lengths) return fail(NLD_ERR_INVALID_ARG, "pages or one of its pointers is NULL");
-    if (c->dtype != NLD_BF16 && c->dtype != NLD_E4M3) return fail(NLD_ERR_INVALID_ARG, "pages: dtype must be NLD_BF16 or NLD_E4M3");
-    if (c->dtype == NLD_E4M3 && !c->scale) return fail(NLD_ERR_INVALID_ARG, "pages: 8-bit pages need their scales");
-    if (!c->bounds != !c->bound_scale) return fail(NLD_ERR_INVALID_ARG, "pages: bounds and bound_scale go together");
-    if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->batch < 1 || c->max_pages < 1)
-        return fail(NLD_ERR_INVALID_ARG, "pages: sizes must be positive");
-    if (c->head_dim != 64 && c->head_dim != 128) return fail(NLD_ERR_SHAPE, "pages: head_dim must be 64 or 128");
-    if (c->max_pages > MAX_SEQ_PAGES) return fail(NLD_ERR_SHAPE, "pages: max_pages (%d) exceeds %d", c->max_pages, MAX_SEQ_PAGES);
-    if (layer < 0 || layer >= c->n_layers) return fail(NLD_ERR_INVALID_ARG, "layer must be in [0, %d) (got %d)", c->n_layers, layer);
-    if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->scale | (uintptr_t)c->bounds) % 16 || (uintptr_t)c->bound_scale % 4)
-        return fail(NLD_ERR_INVALID_ARG, "pages: arrays must be 16-byte aligned");
-    return NLD_OK;
-}
-
-PageCache page_layer(const nld_pages* c, int layer) {
-    const size_t heads = (size_t)layer * c->n_pages * c->n_kv_heads, page = (size_t)64 * c->head_dim * (c->dtype == NLD_BF16 ? 2 : 1);
-    PageCache p{};
-    p.k = (char*)c->k + heads * page;
-    p.v = (char*)c->v + heads * page;
-    p.scale = c->dtype == NLD_E4M3 ? (uint8_t*)c->scale + heads * 128 : nullptr;
-    p.bounds = c->bounds ? (int8_t*)c->bounds + heads * 2 * c->head_dim : nullptr;
-    p.bound_scale = c->bounds ? c->bound_scale + heads : nullptr;
-    p.e4m3 = c->dtype == NLD_E4M3;
-    p.n_pages = c->n_pages;
-    p.n_kv_heads = c->n_kv_heads;
-    p.head_dim = c->head_dim;
-    p.table = c->table;
-    p.lengths = c->lengths;
-    p.batch = c->batch;
-    p.max_pages = c->max_pages;
-    return p;
-}
-
-nld_status check_chunk(const nld_pages* c, const nld_chunk* ch) {
-    if (!ch) return fail(NLD_ERR_INVALID_ARG, "chunk is NULL");
-    if (ch->rows < 1 || ch->max_rows < 1 || ch->max_rows > ch->rows)
-        return fail(NLD_ERR_INVALID_ARG, "chunk: max_rows must be in [1, rows] (got %d of %d)", ch->max_rows, ch->rows);
-    if (!ch->row_start && (long long)ch->max_rows * c->batch != ch->rows)
-        return fail(NLD_ERR_INVALID_ARG, "chunk: without row_start, rows (%d) must be batch * max_rows (%d * %d)", ch->rows, c->batch, ch->max_rows);
-    if (ch->rows > MAX_CHUNK_ROWS) return fail(NLD_ERR_SHAPE, "chunk: %d rows exceed %d", ch->rows, MAX_CHUNK_ROWS);
-    return NLD_OK;
-}
-
-// elements from the first one to past the last one
-long long heads_extent(const nld_heads* x, int rows, int heads, int dim) {
-    return (rows - 1) * x->row_stride + (heads - 1) * x->head_stride + dim;
-}
-
-// out: rows and heads must be apart from each other
-nld_status check_heads(const nld_heads* x, const char* what, int rows, int heads, int dim, bool out) {
-    if (!x || !x->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
-    if (x->dtype != NLD_F32 && x->dtype != NLD_BF16) return fail(NLD_ERR_INVALID_ARG, "%s: dtype must be NLD_F32 or NLD_BF16", what);
-    if (x->row_stride < 0 || x->head_stride < 0 || x->row_stride >> 38 || x->head_stride >> 38)
-        return fail(NLD_ERR_INVALID_ARG, "%s: strides must be in [0, 2^38)", what);
-    if ((uintptr_t)x->data % (x->dtype == NLD_BF16 ? 2 : 4)) return fail(NLD_ERR_INVALID_ARG, "%s: data is not aligned to its type", what);
-    if (out) {
-        const long long rs = rows > 1 ? x->row_stride : LLONG_MAX, hs = heads > 1 ? x->head_stride : LLONG_MAX;
-        const long long inner = std::min(rs, hs), outer = std::max(rs, hs), n_inner = rs <= hs ? rows : heads;
-        if (inner < dim || (outer != LLONG_MAX && outer < (n_inner - 1) * inner + dim))
-            return fail(NLD_ERR_INVALID_ARG, "%s: its rows overlap each other", what);
-    }
-    return NLD_OK;
-}
-
-HeadRows head_rows(const nld_heads* x) { return HeadRows{x->data, x->dtype == NLD_F32, 0, x->row_stride, x->head_stride}; }
-PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows, c->row_start}; }
-
-// The attention's plan and workspace: the status word, then the parts of units that workgroups share, or a selection's scores.
-// Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
-// registers) and are what hides the loads' latency.
-struct PagesPlan {
-    int block_rows, row_tiles, n_blk, grid, slices;
-    size_t part_ml, total;
-};
-
-bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, PagesPlan* out) {
-    PagesPlan p{};
-    const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
-    p.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;
-    const long long blocks = group ? cdiv(max_rows, group) : (rows + p.block_rows - 1) / p.block_rows;
-    if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
-    p.n_blk = (int)blocks;
-    p.grid = 2 * device_cus();
-    // the second launch: a few thousand workgroups at most, and one where units are that many
-    const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
-    p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
-    const size_t part_rows = (size_t)2 * p.grid * p.block_rows;
-    p.part_ml = 256 + part_rows * head_dim * 4;
-    p.total = align256(p.part_ml + part_rows * 8);
-    *out = p;
-    return true;
-}
-
-size_t score_bytes(const nld_pages* c, int max_rows, int group) {
-    return (size_t)c->batch * cdiv(max_rows, group) * c->n_kv_heads * c->max_pages * 4;
-}
-
-nld_status check_mode(int mode, int bidir_from, int max_rows) {
-    if (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT) return fail(NLD_ERR_INVALID_ARG, "mode must be 0 or 1");
-    if (bidir_from < 0 || bidir_from > max_rows) return fail(NLD_ERR_INVALID_ARG, "bidir_from must be in [0, max_rows]");
-    return NLD_OK;
-}
-
-nld_status check_group(const nld_pages* c, int n_q_heads, int group) {
-    if (group < 1) return fail(NLD_ERR_INVALID_ARG, "group must be >= 1 (got %d)", group);
-    if ((long long)group * (n_q_heads / c->n_kv_heads) > PAGES_GROUP_ROWS)
-        return fail(NLD_ERR_SHAPE, "group * (n_q_heads / n_kv_heads) = %lld exceeds %d", (long long)group * (n_q_heads / c->n_kv_heads), PAGES_GROUP_ROWS);
-    return NLD_OK;
-}
-
-nld_status check_q_heads(const nld_pages* c, int n_q_heads) {
-    if (n_q_heads < 1 || n_q_heads % c->n_kv_heads)
-        return fail(NLD_ERR_SHAPE, "n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", n_q_heads, c->n_kv_heads);
-    return NLD_OK;
-}
-
-// the launch of an attention: what does not hang on where queries come from and outputs go
-PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_heads, int mode, int bidir_from, float scale, const PagesPlan& p, void* ws,
-                         size_t off) {
-    PagesAttnArgs a{};
-    a.c = c;
-    a.ch = ch;
-    a.group_heads = group_heads;
-    a.draft = mode == NLD_MODE_DRAFT;
-    a.bidir_from = bidir_from;
-    a.scale_log2 = (float)(LOG2E * (double)scale);
-    a.block_rows = p.block_rows;
-    a.row_tiles = p.row_tiles;
-    a.n_blk = p.n_blk;
-    a.n_entries = c.batch * p.n_blk;
-    a.grid = p.grid;
-    a.slices = p.slices;
-    a.least_steps = 4 / p.row_tiles;
-    a.part_o = at<float>(ws, off + 256);
-    a.part_ml = at<float>(ws, off + p.part_ml);
-    a.status = at<uint32_t>(ws, 0);
-    return a;
 }
 
 }  // namespace
@@ -1542,6 +1642,84 @@ nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chu
     a.status = at<uint32_t>(workspace, 0);
     HIP_TRY(launch_pages_select(a, (hipStream_t)stream));
     return NLD_OK;
+}
+
+size_t nld_pages_pass_workspace_bytes(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, int32_t k) {
+    nld_kv_cache kv;
+    Layout L;
+    PagedPass pp;
+    // a draft pass's lists are the longer ones; any pointer stands for the workspace
+    return validate_paged(m, pages, sparse, k, NLD_MODE_DRAFT, &kv, ~(size_t)0, &kv, &L, &pp) == NLD_OK ? pp.total : 0;
+}
+
+nld_status nld_pages_block_forward(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* tokens, int32_t k, int32_t mode,
+                                   int32_t bidir_from, float* logits, int32_t* argmax, void* workspace, size_t ws_bytes, void* stream) {
+    nld_kv_cache kv;
+    Layout L;
+    PagedPass pp;
+    if (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT) return fail(NLD_ERR_INVALID_ARG, "mode must be 0 or 1");
+    nld_status st = validate_paged(m, pages, sparse, k, mode, workspace, ws_bytes, &kv, &L, &pp);
+    if (st != NLD_OK) return st;
+    if (!tokens) return fail(NLD_ERR_INVALID_ARG, "tokens is NULL");
+    if (bidir_from < 0 || bidir_from > k) return fail(NLD_ERR_INVALID_ARG, "bidir_from must be in [0, k]");
+    PassIO io{};
+    io.source = SRC_TOKENS;
+    io.tokens = tokens;
+    io.mode = mode;
+    io.bidir_from = bidir_from;
+    io.logits = logits;
+    io.argmax_out = argmax;
+    io.finish = FINISH_NONE;
+    io.paged = &pp;
+    return run_pass(m, &kv, pages->batch, k, io, workspace, L, (hipStream_t)stream);
+}
+
+nld_status nld_pages_draft(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* anchor, int32_t k, int32_t bidir_from,
+                           int32_t* draft, float* logits, void* workspace, size_t ws_bytes, void* stream) {
+    nld_kv_cache kv;
+    Layout L;
+    PagedPass pp;
+    nld_status st = validate_paged(m, pages, sparse, k, NLD_MODE_DRAFT, workspace, ws_bytes, &kv, &L, &pp);
+    if (st != NLD_OK) return st;
+    if (k < 2) return fail(NLD_ERR_INVALID_ARG, "a draft needs k >= 2");
+    if (!anchor || !draft) return fail(NLD_ERR_INVALID_ARG, "anchor or draft is NULL");
+    if (bidir_from < 0 || bidir_from > k) return fail(NLD_ERR_INVALID_ARG, "bidir_from must be in [0, k]");
+    PassIO io{};
+    io.source = SRC_DRAFT;
+    io.anchor = anchor;
+    io.mode = NLD_MODE_DRAFT;
+    io.bidir_from = bidir_from;
+    io.logits = logits;
+    io.finish = FINISH_DRAFT;
+    io.draft_out = draft;
+    io.paged = &pp;
+    return run_pass(m, &kv, pages->batch, k, io, workspace, L, (hipStream_t)stream);
+}
+
+nld_status nld_pages_verify_accept(const nld_model* m, const nld_pages* pages, const nld_sparse* sparse, const int32_t* anchor, const int32_t* draft,
+                                   int32_t k, int32_t* accept_len, int32_t* committed, int32_t* next_anchor, float* logits, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+    nld_kv_cache kv;
+    Layout L;
+    PagedPass pp;
+    nld_status st = validate_paged(m, pages, sparse, k, NLD_MODE_VERIFY, workspace, ws_bytes, &kv, &L, &pp);
+    if (st != NLD_OK) return st;
+    if (!anchor || !accept_len || !committed || !next_anchor)
+        return fail(NLD_ERR_INVALID_ARG, "anchor, accept_len, committed or next_anchor is NULL");
+    if (k > 1 && !draft) return fail(NLD_ERR_INVALID_ARG, "draft is NULL");
+    PassIO io{};
+    io.source = SRC_VERIFY;
+    io.anchor = anchor;
+    io.draft_in = draft;
+    io.mode = NLD_MODE_VERIFY;
+    io.logits = logits;
+    io.finish = FINISH_ACCEPT;
+    io.accept_len = accept_len;
+    io.committed = committed;
+    io.next_anchor = next_anchor;
+    io.advance_lengths = true;
+    io.paged = &pp;
+    return run_pass(m, &kv, pages->batch, k, io, workspace, L, (hipStream_t)stream);
 }
 
 nld_status nld_trace_enable(int32_t on) {

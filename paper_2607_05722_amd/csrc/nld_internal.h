@@ -418,6 +418,8 @@ struct PagesSelectArgs {
     PageCache c;
     PageChunk ch;
     HeadRows q;
+    const uint16_t* q_split;    // a pass: split queries (q_index with q_row_tiles)
+    int q_row_tiles;
     int group_heads, draft, bidir_from, n_top, n_first, group, n_groups, n_list, chunks;
     float* scores;              // [batch][n_groups][kv head][max_pages]
     int32_t* list;              // [batch][n_groups][kv head][n_list]

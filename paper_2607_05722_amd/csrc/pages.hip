@@ -1015,7 +1015,15 @@ __global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.0f;
         const int d = tid % C * 8;
-        if (r < n) load8(a.q, g.r0 + g.t0 + r / G, h * G + r % G, d, x);
+        if (r < n) {
+            if (a.q_split) {   // a pass's split queries
+                const uint16_t* p = a.q_split + q_index(b * heads + h, r % G * g.n + g.t0 + r / G, d, a.q_row_tiles, D);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]) + bf16_to_f32(p[SPLIT_LO + i]);
+            } else {
+                load8(a.q, g.r0 + g.t0 + r / G, h * G + r % G, d, x);
+            }
+        }
         float amax = 0.0f;
         bool odd = false;
 #pragma unroll

@@ -17,7 +17,8 @@ from . import _lib as C
 __all__ = ["DeviceModel", "DeviceCache", "Workspace", "block_forward", "draft", "verify_accept",
            "accept_from_logits", "verify_accept_noalloc", "denoise_step", "refresh_block", "commit_from_logits", "read_device_status",
            "stream_handle", "VERIFY", "DRAFT", "LogitsWorkspace", "top_logits", "distill_from_logits",
-           "policy_from_logits", "drafter_loss", "PagedCache", "PagesWorkspace", "write_pages", "read_pages", "attend_pages",
+           "policy_from_logits", "drafter_loss", "PagedCache", "PagesWorkspace",
+           "PagedPassWorkspace", "write_pages", "read_pages", "attend_pages",
            "select_pages"]
 
 VERIFY = C.NLD_MODE_VERIFY
@@ -247,30 +248,44 @@ class QuadWorkspace(Workspace):
         C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
 
 
-def block_forward(model, cache, ws, tokens: torch.Tensor, mode: int, bidir_from: int = 0, want_logits=True):
-    """One block pass.  tokens: int32 [batch][k] on the device.  Returns (logits or None, argmax)."""
+def _pass(name, model, cache, sparse, batch):
+    """The entry point of a pass over this cache with its arguments up to the batch."""
+    lib = C.load()
+    if isinstance(cache, PagedCache):
+        if batch != cache.batch:
+            raise ValueError("the cache has %d sequences, the call %d" % (cache.batch, batch))
+        choice = None if sparse is None else ctypes.byref(C.Sparse(*_sparse(sparse)))
+        return getattr(lib, "nld_pages_" + name), (model.handle, ctypes.byref(cache.struct), choice), ()
+    if sparse is not None:
+        raise ValueError("sparse needs a PagedCache")
+    return getattr(lib, "nld_" + name), (model.handle, ctypes.byref(cache.struct)), (batch,)
+
+
+def block_forward(model, cache, ws, tokens: torch.Tensor, mode: int, bidir_from: int = 0, want_logits=True, sparse=None):
+    """One block pass.  tokens: int32 [batch][k] on the device.  Returns (logits or None, argmax).  The cache may be a PagedCache, with a
+    PagedPassWorkspace; sparse (n_top, n_first, group): attention over the pages that select_pages would choose."""
     batch, k = tokens.shape
     dev = model.device
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
     argmax = torch.empty((batch, k), dtype=torch.int32, device=dev)
-    C.check(C.load().nld_block_forward(model.handle, ctypes.byref(cache.struct), _ptr(tokens), batch, k, mode,
-                                       bidir_from, _ptr(logits), _ptr(argmax), ws.ptr, ws.nbytes, stream_handle()))
+    fn, head, size = _pass("block_forward", model, cache, sparse, batch)
+    C.check(fn(*head, _ptr(tokens), *size, k, mode, bidir_from, _ptr(logits), _ptr(argmax), ws.ptr, ws.nbytes, stream_handle()))
     return logits, argmax
 
 
-def draft(model, cache, ws, anchor: torch.Tensor, k: int, bidir_from: int = 0, want_logits=False, out=None):
-    """Diffusion draft over [anchor, mask x (k-1)].  Returns (drafts int32 [batch][k-1], logits or None)."""
+def draft(model, cache, ws, anchor: torch.Tensor, k: int, bidir_from: int = 0, want_logits=False, out=None, sparse=None):
+    """Diffusion draft over [anchor, mask x (k-1)].  Returns (drafts int32 [batch][k-1], logits or None).  cache and sparse as block_forward."""
     batch = anchor.shape[0]
     dev = model.device
     d = out if out is not None else torch.empty((batch, k - 1), dtype=torch.int32, device=dev)
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
-    C.check(C.load().nld_draft(model.handle, ctypes.byref(cache.struct), _ptr(anchor), batch, k, bidir_from, _ptr(d),
-                               _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
+    fn, head, size = _pass("draft", model, cache, sparse, batch)
+    C.check(fn(*head, _ptr(anchor), *size, k, bidir_from, _ptr(d), _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
     return d, logits
 
 
-def verify_accept(model, cache, ws, anchor: torch.Tensor, drafts, k: int, want_logits=False, outs=None):
-    """AR verify + acceptance.  Returns dict of device tensors (accept_len, committed, next_anchor, logits)."""
+def verify_accept(model, cache, ws, anchor: torch.Tensor, drafts, k: int, want_logits=False, outs=None, sparse=None):
+    """AR verify + acceptance.  Returns dict of device tensors (accept_len, committed, next_anchor, logits).  cache and sparse as block_forward."""
     batch = anchor.shape[0]
     dev = model.device
     if outs is None:
@@ -278,9 +293,9 @@ def verify_accept(model, cache, ws, anchor: torch.Tensor, drafts, k: int, want_l
                 "committed": torch.empty((batch, k), dtype=torch.int32, device=dev),
                 "next_anchor": torch.empty(batch, dtype=torch.int32, device=dev)}
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
-    C.check(C.load().nld_verify_accept(model.handle, ctypes.byref(cache.struct), _ptr(anchor), _ptr(drafts), batch, k,
-                                       _ptr(outs["accept_len"]), _ptr(outs["committed"]), _ptr(outs["next_anchor"]),
-                                       _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
+    fn, head, size = _pass("verify_accept", model, cache, sparse, batch)
+    C.check(fn(*head, _ptr(anchor), _ptr(drafts), *size, k, _ptr(outs["accept_len"]), _ptr(outs["committed"]),
+               _ptr(outs["next_anchor"]), _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
     outs = dict(outs)
     outs["logits"] = logits
     return outs
@@ -678,6 +693,27 @@ class PagesWorkspace:
                                  % (n_q_heads, max_rows, group, lib.nld_last_error().decode()))
             self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.device)
             C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
+        self.ptr = _ptr(self.buf)
+
+
+def _sparse(sparse):
+    n_top, n_first, group = sparse
+    if not (0 <= n_top <= _INT32_MAX and 0 <= n_first <= _INT32_MAX and 0 < group <= _INT32_MAX):
+        raise ValueError("sparse is (n_top, n_first, group): n_top and n_first not negative, group at least 1")
+    return n_top, n_first, group
+
+
+class PagedPassWorkspace:
+    """Workspace of block passes over a paged cache: blocks of k rows; sparse as the passes will have it."""
+
+    def __init__(self, model, cache: PagedCache, k: int, sparse=None):
+        lib = C.load()
+        choice = None if sparse is None else ctypes.byref(C.Sparse(*_sparse(sparse)))
+        self.nbytes = lib.nld_pages_pass_workspace_bytes(model.handle, ctypes.byref(cache.struct), choice, k)
+        if self.nbytes == 0:
+            raise ValueError("no workspace for blocks of %d rows over these pages: %s" % (k, lib.nld_last_error().decode()))
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=model.device)
+        C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
         self.ptr = _ptr(self.buf)
 
 

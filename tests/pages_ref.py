@@ -133,3 +133,45 @@ def select(cache, lens, starts, q, n_top, n_first, group, n_list, draft=False, b
                 have = sorted(set(range(min(n_first, p0))) | set(take) | set(range(p0, end)))
                 got[b, g, h, :len(have)] = torch.tensor(have, dtype=torch.int32, device=q.device)
     return got
+
+
+def _bits(x, device):
+    return torch.from_numpy(x.view("int16").copy()).to(device).view(torch.bfloat16).double()
+
+
+def block_pass(shape, source, caches, lens, tokens, draft=False, bidir_from=0, sparse=None):
+    """A block pass of the decoder in 64 bits over paged caches (one per layer, written here): pre-norm RMSNorm, rotate-half RoPE, GQA over
+    the stored keys and values, SwiGLU, final norm, LM head.  tokens [batch][k].  Returns logits [batch][k][vocab]."""
+    dev = caches[0].k.device
+    B, k = tokens.shape
+    H, Hq, D = shape.n_kv_heads, shape.n_q_heads, shape.head_dim
+    starts = [b * k for b in range(B + 1)]
+    x = _bits(source.embed, dev)[tokens.reshape(-1).long()]
+    pos = (torch.tensor(lens, device=dev)[:, None] + torch.arange(k, device=dev)).reshape(-1).double()
+    angle = pos[:, None] * shape.rope_base ** (-2.0 * torch.arange(D // 2, device=dev).double() / D)
+    cos, sin = torch.cos(angle)[:, None], torch.sin(angle)[:, None]
+
+    def norm(y, gain):
+        return y / torch.sqrt((y * y).mean(-1, keepdim=True) + shape.rms_eps) * _bits(gain, dev)
+
+    def rope(y):
+        a, b = y[..., :D // 2], y[..., D // 2:]
+        return torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+
+    for l in range(shape.n_layers):
+        w = {n: (v if "norm" in n else _bits(v, dev)) for n, v in source.layer(l).items()}
+        y = norm(x, w["attn_norm"])
+        q, kk, v = (y @ w[n].T for n in ("wq", "wk", "wv"))
+        q, kk = rope(q.view(-1, Hq, D)), rope(kk.view(-1, H, D))
+        caches[l].write(lens, starts, kk.float(), v.view(-1, H, D).float())
+        lists, group = None, 1
+        if sparse is not None:
+            n_top, n_first, group = sparse
+            n_list = n_first + n_top + ((k if draft else group) + 62) // PAGE + 1
+            lists = select(caches[l], lens, starts, q.float(), n_top, n_first, group, n_list, draft, bidir_from)
+        o = attend(caches[l], lens, starts, q, D ** -0.5, draft, bidir_from, lists, group)[0]
+        x = x + o.reshape(B * k, -1) @ w["wo"].T
+        y = norm(x, w["ffn_norm"])
+        gate = y @ w["w_gate"].T
+        x = x + (gate * torch.sigmoid(gate) * (y @ w["w_up"].T)) @ w["w_down"].T
+    return (norm(x, source.final_norm) @ _bits(source.lm_head, dev).T).view(B, k, -1)

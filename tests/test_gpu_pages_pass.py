@@ -1,0 +1,217 @@
+"""Block-decode passes over a paged cache, in bf16 and in 8 bits, whole and over selected pages: against a 64-bit decoder over the same stored
+rows (tests/pages_ref.py block_pass), and in bf16 against the passes over the other cache.
+
+Bound: the normwise 2e-2 of every pass test.  Both sides hold keys and values in the pages' type; a projection's f32 sum next to a rounding
+border may fall on the other side, one step of the type for that element."""
+import ctypes
+
+import numpy as np
+import pages_ref as ref
+import pytest
+import torch
+from gpu_common import rel_err
+
+pytestmark = pytest.mark.gpu
+
+from synth.workloads import SHAPE_TINY, LazyWeights, tokens  # noqa: E402
+
+if torch.cuda.is_available():
+    from paper_2607_05722_amd import _lib as C
+    from paper_2607_05722_amd import runtime as R
+
+BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
+TOL = 2e-2
+
+
+@pytest.fixture(scope="module")
+def tiny():
+    src = LazyWeights(SHAPE_TINY, 0)
+    return SHAPE_TINY, src, R.DeviceModel(SHAPE_TINY, src)
+
+
+def ids(shape, name, batch, n):
+    return torch.from_numpy(tokens(shape, 0, name, (batch, n)).astype(np.int32)).cuda()
+
+
+class Both:
+    """A paged cache with a shuffled table, and the plain caches of its layers."""
+
+    def __init__(self, shape, pages, batch, max_len, bounds=False, seed=3):
+        self.cache = R.PagedCache(shape.n_kv_heads, shape.head_dim, batch, max_len, n_layers=shape.n_layers, n_pages=batch * max_len // 64 + 2,
+                                  dtype=pages, bounds=bounds)
+        order = torch.randperm(self.cache.n_pages, generator=torch.Generator().manual_seed(seed))[:batch * max_len // 64]
+        self.cache.table.copy_(order.to(torch.int32).view(batch, -1))
+        self.plain = [ref.Cache(batch, max_len, shape.n_kv_heads, shape.head_dim, pages == E4M3, "cuda") for _ in range(shape.n_layers)]
+
+
+def prefill(tiny, both, lens, name="prefix"):
+    """Rows of random keys and values as committed prefixes, in every layer."""
+    shape, _, _ = tiny
+    both.cache.lengths.zero_()
+    starts = [0] + np.cumsum(lens).tolist()
+    ws = R.PagesWorkspace(both.cache, shape.n_q_heads, max(lens))
+    for l in range(shape.n_layers):
+        g = torch.Generator().manual_seed(100 + l)
+        k, v = (torch.randn((starts[-1], shape.n_kv_heads, shape.head_dim), generator=g).cuda() for _ in range(2))
+        R.write_pages(both.cache, l, k, v, ws, row_start=torch.tensor(starts, dtype=torch.int32, device="cuda"), max_rows=max(lens))
+        both.plain[l].write([0] * len(lens), starts, k, v)
+    both.cache.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("lens,k", [([128], 8), ([100, 1, 190], 16), ([63, 64], 1), ([5], 64)])
+def test_block_passes(tiny, pages, lens, k):
+    shape, src, model = tiny
+    both = Both(shape, pages, len(lens), 320)
+    prefill(tiny, both, lens)
+    ws = R.PagedPassWorkspace(model, both.cache, k)
+    toks = ids(shape, "block", len(lens), k)
+    for mode, bidir in ((R.VERIFY, 0), (R.DRAFT, 0), (R.DRAFT, min(3, k))):
+        logits, argmax = R.block_forward(model, both.cache, ws, toks, mode, bidir)
+        assert R.read_device_status(ws) == 0
+        want = ref.block_pass(shape, src, both.plain, lens, toks, mode == R.DRAFT, bidir).cpu().numpy()
+        got = logits.cpu().numpy()
+        assert rel_err(got, want) <= TOL
+        assert np.array_equal(argmax.cpu().numpy(), got.argmax(-1))
+        assert both.cache.lengths.tolist() == lens
+
+
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("sparse", [(2, 1, 1), (1, 0, 4), (3, 1, 16)])
+def test_block_passes_over_selected_pages(tiny, pages, sparse):
+    shape, src, model = tiny
+    lens, k = [700, 330], 16
+    both = Both(shape, pages, 2, 768, bounds=True)
+    prefill(tiny, both, lens)
+    ws = R.PagedPassWorkspace(model, both.cache, k, sparse)
+    toks = ids(shape, "block", 2, k)
+    for mode in (R.VERIFY, R.DRAFT):
+        logits, _ = R.block_forward(model, both.cache, ws, toks, mode, 0, sparse=sparse)
+        assert R.read_device_status(ws) == 0
+        want = ref.block_pass(shape, src, both.plain, lens, toks, mode == R.DRAFT, 0, sparse).cpu().numpy()
+        err = np.abs(logits.cpu().numpy() - want).max(-1) / np.abs(want).max()
+        # the second layer's queries differ by rounding, so a page next to the border may change for a row: few do
+        assert (err <= TOL).mean() >= 0.9, err
+    whole, _ = R.block_forward(model, both.cache, R.PagedPassWorkspace(model, both.cache, k), toks, R.VERIFY)
+    every, _ = R.block_forward(model, both.cache, R.PagedPassWorkspace(model, both.cache, k, (12, 0, 16)), toks, R.VERIFY, sparse=(12, 0, 16))
+    assert rel_err(every.cpu().numpy(), whole.cpu().numpy()) <= 1e-5     # all pages: the same sums in other parts
+
+
+def test_steps_in_bf16_pages_follow_the_other_cache(tiny):
+    """Draft, verify, accept, commit: from the same prefix, over both caches."""
+    shape, _, model = tiny
+    k, batch = 8, 2
+    flat = R.DeviceCache(shape, batch, 256)
+    both = Both(shape, BF16, batch, 256)
+    prefix = ids(shape, "p", batch, 64)
+    wf, wp = R.Workspace(model, batch, 64, 256), R.PagedPassWorkspace(model, both.cache, 64)
+    R.block_forward(model, flat, wf, prefix, R.VERIFY, want_logits=False)
+    R.block_forward(model, both.cache, wp, prefix, R.VERIFY, want_logits=False)
+    flat.lengths += 64
+    both.cache.lengths += 64
+    wf, wp = R.Workspace(model, batch, k, 256), R.PagedPassWorkspace(model, both.cache, k)
+    anchor = ids(shape, "a", batch, 1)[:, 0].contiguous()
+    for step in range(6):
+        d, dl = R.draft(model, flat, wf, anchor, k, want_logits=True)
+        d2, dl2 = R.draft(model, both.cache, wp, anchor, k, want_logits=True)
+        assert rel_err(dl2.cpu().numpy(), dl.cpu().numpy()) <= TOL
+        v = R.verify_accept(model, flat, wf, anchor, d, k, want_logits=True)
+        v2 = R.verify_accept(model, both.cache, wp, anchor, d, k, want_logits=True)
+        assert rel_err(v2["logits"].cpu().numpy(), v["logits"].cpu().numpy()) <= TOL
+        # acceptance by the pass's own logits
+        own = R.accept_from_logits(v2["logits"], d)
+        for name in ("accept_len", "committed", "next_anchor"):
+            assert torch.equal(v2[name], own[name])
+        anchor = v["next_anchor"]
+        both.cache.lengths.copy_(flat.lengths)
+    assert R.read_device_status(wp) == 0
+
+
+def test_self_speculation_in_8_bits_captured(tiny):
+    """A loop of draft and verify in one graph, in place: every replay equals the eager steps of a second cache."""
+    shape, _, model = tiny
+    k, batch = 4, 2
+    sets = [Both(shape, E4M3, batch, 512, bounds=True) for _ in range(2)]
+    for s in sets:
+        prefill(tiny, s, [200, 75])
+    sparse = (2, 1, 4)
+    state = []
+    for s in sets:
+        st = dict(anchor=ids(shape, "a", batch, 1)[:, 0].contiguous(), d=torch.empty((batch, k - 1), dtype=torch.int32, device="cuda"),
+                  ws=R.PagedPassWorkspace(model, s.cache, k, sparse), cache=s.cache)
+        st["outs"] = {"accept_len": torch.empty(batch, dtype=torch.int32, device="cuda"), "committed": torch.empty((batch, k), dtype=torch.int32, device="cuda"),
+                      "next_anchor": st["anchor"]}
+        state.append(st)
+
+    def step(st):
+        R.draft(model, st["cache"], st["ws"], st["anchor"], k, out=st["d"], sparse=sparse)
+        R.verify_accept(model, st["cache"], st["ws"], st["anchor"], st["d"], k, outs=st["outs"], sparse=sparse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(state[0])
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(state[0])
+    step(state[1])
+    for _ in range(5):
+        graph.replay()
+        step(state[1])
+        torch.cuda.synchronize()
+        a, b = state
+        assert torch.equal(a["d"], b["d"]) and torch.equal(a["cache"].lengths, b["cache"].lengths)
+        for name in a["outs"]:
+            assert torch.equal(a["outs"][name], b["outs"][name])
+    assert R.read_device_status(state[0]["ws"]) == 0 and state[0]["cache"].lengths.tolist()[0] >= 206
+
+
+def test_the_drafters_loss_over_pages(tiny):
+    shape, _, model = tiny
+    both = Both(shape, BF16, 1, 256)
+    prefill(tiny, both, [100])
+    anchor = ids(shape, "a", 1, 1)[:, 0].contiguous()
+    out = R.drafter_loss(model, both.cache, R.PagedPassWorkspace(model, both.cache, 8), R.LogitsWorkspace(1, 7, shape.vocab, 32), anchor, 8, n_top=32)
+    assert bool(torch.isfinite(out["loss"]).all()) and both.cache.lengths.item() == 101 + out["accept_len"].item()
+
+
+def test_missing_pages_and_full_tables(tiny):
+    shape, _, model = tiny
+    both = Both(shape, BF16, 1, 128)
+    prefill(tiny, both, [120])
+    anchor = ids(shape, "a", 1, 1)[:, 0].contiguous()
+    ws = R.PagedPassWorkspace(model, both.cache, 16)
+    R.draft(model, both.cache, ws, anchor, 16)
+    assert R.read_device_status(ws) & C.NLD_DEV_CAPACITY
+    both.cache.table[0, 1] = -1
+    R.draft(model, both.cache, ws, anchor, 4)
+    assert R.read_device_status(ws) == C.NLD_DEV_BAD_PAGE
+
+
+def test_refusals(tiny):
+    shape, _, model = tiny
+    good = R.PagedCache(shape.n_kv_heads, shape.head_dim, 2, 128, n_layers=shape.n_layers)
+    anchor = torch.zeros(2, dtype=torch.int32, device="cuda")
+    ws = R.PagedPassWorkspace(model, good, 8)
+    for kw in (dict(kv_heads=1), dict(head_dim=128), dict(n_layers=1)):
+        sizes = dict(kv_heads=shape.n_kv_heads, head_dim=shape.head_dim, n_layers=shape.n_layers)
+        bad = R.PagedCache(batch=2, max_len=128, **{**sizes, **kw})
+        with pytest.raises(C.NLDError, match="the model"):
+            R.draft(model, bad, ws, anchor, 8)
+        with pytest.raises(ValueError):
+            R.PagedPassWorkspace(model, bad, 8)
+    with pytest.raises(C.NLDError, match="bounds"):
+        R.draft(model, good, ws, anchor, 8, sparse=(1, 1, 1))
+    with pytest.raises(C.NLDError, match="workspace"):
+        R.draft(model, good, ws, anchor, 64)
+    with pytest.raises(C.NLDError):
+        R.draft(model, good, ws, anchor, 1)
+    with pytest.raises(ValueError):
+        R.draft(model, good, ws, anchor[:1], 8)
+    with pytest.raises(ValueError):
+        R.draft(model, good, ws, anchor, 8, sparse=(1, 1, 0))
+    with pytest.raises(ValueError):
+        R.draft(model, R.DeviceCache(shape, 2, 128), R.Workspace(model, 2, 8, 128), anchor, 8, sparse=(1, 1, 1))
+    with pytest.raises(ctypes.ArgumentError):
+        R.decode_steps(model, good, ws, anchor, 4, 1)      # the calls that have no form over pages
