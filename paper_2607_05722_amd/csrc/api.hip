@@ -3,6 +3,7 @@
 #include "../../include/nld.h"
 #include "nld_internal.h"
 
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdarg.h>
@@ -333,19 +334,22 @@ PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows
 // Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
 // registers) and are what hides the loads' latency.
 struct PagesPlan {
-    int block_rows, row_tiles, n_blk, grid, slices;
+    int block_rows, row_tiles, n_blk, grid, slices, shared_waves, key_halves;
     size_t part_ml, total;
 };
 
-bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, PagesPlan* out) {
+bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, bool wide, PagesPlan* out) {
     PagesPlan p{};
     const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
-    p.row_tiles = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    p.row_tiles = (int)std::min<long long>(wide ? 4 : 8, (rows + 31) / 32);
+    if (wide && p.row_tiles == 3) p.row_tiles = 4;
     p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;
+    p.key_halves = p.row_tiles <= (wide ? 2 : 4) ? 2 : 1;
+    p.shared_waves = p.row_tiles > 1 ? p.row_tiles * p.key_halves : 0;
     const long long blocks = group ? cdiv(max_rows, group) : (rows + p.block_rows - 1) / p.block_rows;
     if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
     p.n_blk = (int)blocks;
-    p.grid = 2 * device_cus();
+    p.grid = p.shared_waves > 4 || (p.shared_waves && wide) ? device_cus() : 2 * device_cus();
     // the second launch: a few thousand workgroups at most, and one where units are that many
     const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
     p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
@@ -388,14 +392,17 @@ PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_head
     a.group_heads = group_heads;
     a.draft = mode == NLD_MODE_DRAFT;
     a.bidir_from = bidir_from;
-    a.scale_log2 = (float)(LOG2E * (double)scale);
+    a.scale_log2 = std::max((float)(LOG2E * fabs((double)scale)), FLT_MIN);   // not 0: a position that is not seen scores -inf
+    a.negate = scale < 0.0f;
     a.block_rows = p.block_rows;
     a.row_tiles = p.row_tiles;
     a.n_blk = p.n_blk;
     a.n_entries = c.batch * p.n_blk;
     a.grid = p.grid;
     a.slices = p.slices;
-    a.least_steps = 4 / p.row_tiles;
+    a.least_steps = p.shared_waves ? 2 : 4;
+    a.shared_waves = p.shared_waves;
+    a.key_halves = p.key_halves;
     a.part_o = at<float>(ws, off + 256);
     a.part_ml = at<float>(ws, off + p.part_ml);
     a.status = at<uint32_t>(ws, 0);
@@ -492,7 +499,7 @@ nld_status validate_paged(const nld_model* m, const nld_pages* pages, const nld_
         if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
             return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     }
-    if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, &p.plan))
+    if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, pages_wide(2, pages->dtype == NLD_E4M3), &p.plan))
         return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     p.attn = align256(L.total);
     p.lists = p.attn + std::max(p.plan.total, p.group ? align256(256 + score_bytes(pages, k, p.group)) : 0);
@@ -1518,16 +1525,17 @@ int32_t nld_pages_list_len(int32_t max_rows, int32_t group, int32_t n_top, int32
 size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int32_t max_rows, int32_t group) {
     if (check_pages(pages, 0) != NLD_OK || check_q_heads(pages, n_q_heads) != NLD_OK || max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 0)
         return 0;
+    if (group && check_group(pages, n_q_heads, group) != NLD_OK) return 0;
+    const int G = n_q_heads / pages->n_kv_heads;
     PagesPlan p;
-    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, max_rows, 0, &p)) return 0;
-    size_t n = p.total;
-    if (group) {
-        if (check_group(pages, n_q_heads, group) != NLD_OK ||
-            !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, max_rows, group, &p))
-            return 0;
-        n = std::max(n, align256(256 + score_bytes(pages, max_rows, group)));
-    }
-    return n;
+    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, max_rows, group, false, &p)) return 0;
+    // the most that any number of rows up to these, and any type, needs: by the tiles of a workgroup
+    size_t n = 0;
+    const long long rows = (long long)max_rows * G;
+    for (const bool wide : {false, true})
+        for (long long r = 16; r == 16 || r - 32 < std::min(rows, 256LL); r = r == 16 ? 32 : r + 32)
+            if (plan_pages(1, 1, pages->head_dim, 1, (int)r, 0, wide, &p)) n = std::max(n, p.total);
+    return group ? std::max(n, align256(256 + score_bytes(pages, max_rows, group))) : n;
 }
 
 nld_status nld_pages_write(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* k, const nld_heads* v, void* workspace,
@@ -1589,7 +1597,8 @@ nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chu
     }
     if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     PagesPlan p;
-    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, chunk->max_rows, list ? group : 0, &p))
+    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, chunk->max_rows, list ? group : 0,
+                    pages_wide(q->dtype == NLD_F32 ? 3 : 1, pages->dtype == NLD_E4M3), &p))
         return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
     if (ws_bytes < p.total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, p.total);
     PagesAttnArgs a = pages_args(page_layer(pages, layer), page_chunk(chunk), n_q_heads / pages->n_kv_heads, mode, bidir_from, scale, p, workspace, 0);

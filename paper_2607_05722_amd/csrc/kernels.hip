@@ -1330,23 +1330,6 @@ __device__ __forceinline__ int stage_key(int tau, int rho) {
     return 32 * (tau >> 1) + 8 * (rho >> 2) + 4 * (tau & 1) + (rho & 3);
 }
 
-// 16 bytes per lane from global memory to LDS at byte `dst` + 16 * lane (dst uniform).  Inline assembly: the
-// compiler waits for every such load before any later LDS read, which would take the stages one by one.
-// It has no register result; stage_wait() and a barrier stand between it and the reads.
-// ONCE: nobody reads the bytes again before they leave the caches, which the load passes by.
-template <bool ONCE>
-__device__ __forceinline__ void load_to_lds(const void* src, uint32_t dst) {
-    if constexpr (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(dst), "v"(src) : "memory", "m0");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
-}
-// at most N vector memory operations of this wavefront still under way
-template <int N>
-__device__ __forceinline__ void stage_wait() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
 // max (or sum) over the lanes r, r+16, r+32, r+48, in every lane
 __device__ __forceinline__ float rows_max(float v) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

@@ -51,6 +51,23 @@ __device__ __forceinline__ uint4 load_stream(const uint4* p) {
     return uint4{v[0], v[1], v[2], v[3]};
 }
 
+// 16 bytes per lane from global memory to LDS at byte `dst` + 16 * lane (dst uniform).  Inline assembly: the
+// compiler waits for every such load before any later LDS read, which would take the stages one by one.
+// It has no register result; stage_wait() and a barrier stand between it and the reads.
+// ONCE: nobody reads the bytes again before they leave the caches, which the load passes by.
+template <bool ONCE>
+__device__ __forceinline__ void load_to_lds(const void* src, uint32_t dst) {
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(dst), "v"(src) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+}
+// at most N vector memory operations of this wavefront still under way
+template <int N>
+__device__ __forceinline__ void stage_wait() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // Order-preserving key for a float value at column n: larger value wins, then
 // lower column.  -0.0 is folded onto +0.0 so that equal values tie on index.
 __device__ __forceinline__ unsigned long long argmax_key(float v, uint32_t n) {
@@ -400,18 +417,22 @@ struct PagesAttnArgs {
     int q_row_tiles, o_ksteps, plain_o;
     int group_heads;            // query heads per KV head
     int draft, bidir_from;
-    float scale_log2;
+    float scale_log2;           // > 0; negate: of the scale's magnitude, and the queries take its sign
+    int negate;
     const int32_t* list;        // optional [batch][n_blk][kv head][n_list]: the pages of each group of tokens
     int n_list, group;
     float* lse;                 // optional [rows][query head]
     int block_rows, row_tiles;  // rows of a workgroup: 16 (one tile), or 1, 2 or 4 tiles of 32
     int n_blk, n_entries;       // blocks of rows per sequence, of all
     int grid, least_steps, slices;
+    int shared_waves, key_halves;   // > 0: the kernel whose wavefronts share pages through LDS, with so many; wavefronts per tile
     float* part_o;              // [2 * grid][block_rows][head_dim]
     float* part_ml;             // [2 * grid][block_rows][2]
     uint32_t* status;
 };
 
+// Whether the attention of many rows has one wavefront per SIMD: by the queries' pieces and the pages' type.
+__host__ __device__ constexpr bool pages_wide(int pieces, bool e4m3) { return pieces == 3 || (pieces == 2 && e4m3); }
 constexpr int PAGES_GROUP_ROWS = 128;   // rows (tokens x query heads of a KV head) that share a list of pages
 
 struct PagesSelectArgs {

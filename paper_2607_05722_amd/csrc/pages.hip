@@ -504,16 +504,39 @@ __device__ __forceinline__ void sum_entries(const PagesAttnArgs& a, int upto, lo
     if (before) *before = block_sum(first, lds);
 }
 
-// The entry that holds step `s` (per KV head: s / heads) and the steps before it.
+// A workgroup's way through its share.  Steps are numbered KV head by KV head, in each entry by entry: with the shares of one
+// XCD side by side (workgroup w runs on XCD w % 8) the workgroups that read the same keys mostly share an L2.  What hangs on lengths and
+// row_start is looked up by one thread and handed to the others, so that all go the same way whatever is written to these meanwhile.
+struct Walk {
+    Entry en;
+    int e, h, share;
+    long long at, last;   // the share's steps left: [at, last)
+    long long before;     // steps of the entries before e
+    long long per_head;
+    bool first_unit;
+};
+
+// false: nothing to do
 template <int STEP>
-__device__ __forceinline__ void find_entry(const PagesAttnArgs& a, long long s, long long* lds, int* entry, long long* before) {
-    __shared__ long long found_before;
-    __shared__ int found;
+__device__ __forceinline__ bool walk_start(const PagesAttnArgs& a, Walk* w, long long* lds) {
+    const int heads = a.c.n_kv_heads;
+    long long per_head, live;
+    sum_entries<STEP>(a, 0, lds, nullptr, &per_head, &live, blockIdx.x == 0 ? a.status : nullptr);
+    if (per_head == 0) return false;
+    const Share sh = share_of(per_head * heads, live * heads, gridDim.x, a.least_steps);
+    // the shares in use, dealt to the XCDs in eight runs of adjacent ones
+    const int run = sh.wgs / 8, x = blockIdx.x & 7, i = blockIdx.x >> 3;
+    const int share = i < run ? x * run + i : 8 * run + (int)blockIdx.x - 8 * run;
+    if (share >= sh.wgs) return false;
+    const long long first = sh.begin(share);
+    const int h = (int)(first / per_head);
+    const long long s = first - h * per_head;
+    // the entry that holds step s of its KV head
+    if (threadIdx.x == 0) w->e = a.n_entries;
     long long base = 0;
-    if (threadIdx.x == 0) found = a.n_entries;
     for (int e0 = 0;; e0 += blockDim.x) {
         const int e = e0 + threadIdx.x;
-        const long long own = e < a.n_entries ? (long long)entry_of<STEP>(a, e, nullptr).steps * a.c.n_kv_heads : 0;
+        const long long own = e < a.n_entries ? (long long)entry_of<STEP>(a, e, nullptr).steps : 0;
         long long up = own;
         for (int m = 1; m < 64; m <<= 1) {
             const long long o = __shfl_up(up, m);
@@ -523,18 +546,49 @@ __device__ __forceinline__ void find_entry(const PagesAttnArgs& a, long long s, 
         if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = up;
         __syncthreads();
         long long ahead = base, sum = 0;
-        for (int i = 0; i < (int)blockDim.x / 64; ++i) {
-            if (i < (int)threadIdx.x / 64) ahead += lds[i];
-            sum += lds[i];
+        for (int i2 = 0; i2 < (int)blockDim.x / 64; ++i2) {
+            if (i2 < (int)threadIdx.x / 64) ahead += lds[i2];
+            sum += lds[i2];
         }
         const long long lo = ahead + up - own;
-        if (own && lo <= s && s < lo + own) found = e, found_before = lo;
+        if (own && lo <= s && s < lo + own) {
+            w->en = entry_of<STEP>(a, e, nullptr);
+            w->e = e, w->before = lo;
+        }
         base += sum;
         __syncthreads();
-        if (found < a.n_entries || e0 + (int)blockDim.x >= a.n_entries) break;
+        if (w->e < a.n_entries || e0 + (int)blockDim.x >= a.n_entries) break;
     }
-    *entry = found;
-    *before = found_before;
+    if (w->e >= a.n_entries) return false;   // not unless the lengths change meanwhile
+    if (threadIdx.x == 0) {
+        w->h = h, w->share = share, w->at = first, w->last = sh.begin(share + 1), w->per_head = per_head, w->first_unit = true;
+    }
+    __syncthreads();
+    return true;
+}
+
+// On to the next unit; false behind the last.  Called by every thread after it has read what it needs of the present one.
+template <int STEP>
+__device__ __forceinline__ bool walk_next(const PagesAttnArgs& a, Walk* w) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        w->at = w->h * w->per_head + w->before + w->en.steps;
+        w->first_unit = false;
+        w->before += w->en.steps;
+        while (w->at < w->last) {
+            if (++w->e >= a.n_entries) {
+                ++w->h, w->e = 0, w->before = 0;
+                if (w->h >= a.c.n_kv_heads) {   // not unless the lengths change meanwhile
+                    w->at = w->last;
+                    break;
+                }
+            }
+            w->en = entry_of<STEP>(a, w->e, nullptr);
+            if (w->en.steps > 0) break;
+        }
+    }
+    __syncthreads();
+    return w->at < w->last;
 }
 
 // four dims of a finished row (token t of sequence b, query head), and its log-sum-exp: a row that sees nothing is 0
@@ -573,6 +627,12 @@ struct Tile<32> {
     static __device__ __forceinline__ int piece_s(int lane, int f) { return f & 1; }   // of the f-th eight weights
     static __device__ __forceinline__ int piece_hf(int lane) { return lane >> 5; }
     static __device__ __forceinline__ int out_dim(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+    // over the lanes of a row, in every one of them
+    template <typename F>
+    static __device__ __forceinline__ float across(float v, F f) {
+        const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    }
 };
 template <>
 struct Tile<16> {
@@ -582,7 +642,26 @@ struct Tile<16> {
     static __device__ __forceinline__ int piece_s(int lane, int f) { return lane >> 5; }
     static __device__ __forceinline__ int piece_hf(int lane) { return (lane >> 4) & 1; }
     static __device__ __forceinline__ int out_dim(int lane, int r) { return 4 * (lane >> 4) + r; }
+    template <typename F>
+    static __device__ __forceinline__ float across(float v, F f) {
+        v = Tile<32>::across(v, f);
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    }
 };
+
+// A row's maximum follows its scores (in base-2 exponents) once they are 2^8 above it: until then the weights are up to 2^8, which costs
+// sums in f32 and weights in bf16 nothing, and the sums so far need no new scale.
+template <typename Acc, int N>
+__device__ __forceinline__ void rescale(float top, float* m, float* l, Acc (&o)[N]) {
+    if (!__any(top > *m + 8.0f)) return;
+    const float to = fmaxf(*m, top), f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(*m - to);
+    *l *= f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] *= f;
+    *m = to;
+}
+__device__ __forceinline__ float weight(float score, float scale_log2, float ref) { return __builtin_amdgcn_exp2f(__builtin_fmaf(score, scale_log2, -ref)); }
 
 template <int D, bool E4M3, int RW>
 __device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const void* values, int base, int lane, int sees, int most) {
@@ -617,43 +696,28 @@ pages_attend_kernel(PagesAttnArgs a) {
     __shared__ __align__(16) float so[4][RW][PITCH];
     __shared__ float sml[4][RW][2];
     __shared__ long long lds[4];
+    __shared__ Walk walk;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane % RW, part = lane / RW;
     const int row_tiles = RW == 16 ? 1 : a.row_tiles;
     const int rt = wave % row_tiles, ks = wave / row_tiles, n_ks = 4 / row_tiles;
     const int heads = a.c.n_kv_heads, G = a.group_heads;
 
-    long long total, live;
-    sum_entries<STEP>(a, 0, lds, nullptr, &total, &live, blockIdx.x == 0 ? a.status : nullptr);
-    total *= heads;
-    if (total == 0) return;
-    const Share sh = share_of(total, live * heads, gridDim.x, a.least_steps);
-    if ((int)blockIdx.x >= sh.wgs) return;
-    const long long first = sh.begin(blockIdx.x), last = sh.begin(blockIdx.x + 1);
-    int e;
-    long long before;
-    find_entry<STEP>(a, first, lds, &e, &before);
-    if (e >= a.n_entries) return;   // not unless the lengths change meanwhile
-    Entry en = entry_of<STEP>(a, e, nullptr);
+    if (!walk_start<STEP>(a, &walk, lds)) return;
 
     // places of a lane's 16 bytes in the blocks of keys and of values
     const int m32 = 8 * ((row >> 4) & 1) + (row & 7), k_lane = RW == 16 ? lane : ((row >> 3) & 1) * (D / (E4M3 ? 64 : 32)) * 64 + part * 16 + m32;
     const int v_lane = RW == 16 ? lane : (row >> 4) * 64 + part * 16 + (row & 15);
     const int key_of_row = RW == 16 ? 16 * (row >> 3) + (row & 7) : row;   // of a tile's first keys
 
-    for (long long at = first; at < last;) {
-        while (at >= before + (long long)en.steps * heads) {   // entries without rows have no steps
-            before += (long long)en.steps * heads;
-            if (++e >= a.n_entries) return;
-            en = entry_of<STEP>(a, e, nullptr);
-        }
-        const int h = (int)((at - before) / en.steps);
-        const long long unit0 = before + (long long)h * en.steps;
-        const int s0 = __builtin_amdgcn_readfirstlane((int)(at - unit0));
-        const int s1 = __builtin_amdgcn_readfirstlane((int)min(last - unit0, (long long)en.steps));
+    do {
+        const Entry en = walk.en;
+        const int h = walk.h;
+        const long long unit0 = walk.h * walk.per_head + walk.before;
+        const int s0 = __builtin_amdgcn_readfirstlane((int)(walk.at - unit0));
+        const int s1 = __builtin_amdgcn_readfirstlane((int)min(walk.last - unit0, (long long)en.steps));
         const bool whole = s0 == 0 && s1 == en.steps;
-        const int slot = 2 * blockIdx.x + (at > first ? 1 : 0);
-        at = unit0 + s1;
+        const int slot = 2 * walk.share + (walk.first_unit ? 0 : 1);
 
         // this wavefront's rows
         const int myrow = en.rows0 + rt * RW + row;
@@ -681,6 +745,9 @@ pages_attend_kernel(PagesAttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = 0.0f;
                 if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
+                if (a.negate)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
 #pragma unroll
                 for (int p = 0; p < NQ; ++p) {
                     uint32_t w[4];
@@ -795,30 +862,18 @@ pages_attend_kernel(PagesAttnArgs a) {
             more = next();
             if (more) load_k(head, base);
 
-            // scores in base-2 exponents, their maximum
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < SR; ++i) {
-                x[i] *= a.scale_log2;
                 if (masked && cur_base + key_of(i) >= sees) x[i] = -INFINITY;
                 top = fmaxf(top, x[i]);
             }
-#pragma unroll
-            for (int m = RW; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-            if (__any(top > m_run)) {
-                const float m = fmaxf(m_run, top), f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
-                l_run *= f;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < T::REGS; ++r) o[dt][r] *= f;
-                m_run = m;
-            }
+            rescale(T::across(top, [](float u, float w) { return fmaxf(u, w); }) * a.scale_log2, &m_run, &l_run, o);
             const float ref = m_run == -INFINITY ? 0.0f : m_run;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < SR; ++i) {
-                float p = __builtin_amdgcn_exp2f(x[i] - ref);
+                float p = weight(x[i], a.scale_log2, ref);
                 sum += p;
                 if constexpr (E4M3) {
                     const float w = scale_of((vsc[i >> 2] >> (8 * (i & 3))) & 0xFFu);
@@ -924,25 +979,341 @@ pages_attend_kernel(PagesAttnArgs a) {
                 if (d == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m, l};
             }
         }
-        __syncthreads();
-    }
+    } while (walk_next<STEP>(a, &walk));
 }
 
+// ---------------------------------------------------------------- attention of many rows
+// More than one tile of 32 rows: a workgroup has `tiles` of them (up to 8), key_halves wavefronts each (two where there are up to 4
+// tiles: each takes 32 of a page's 64 keys, and they meet at the unit's end).  The wavefronts share each page through LDS, double-buffered:
+// bf16 pages go there straight from memory, in the order in which a wavefront's operands are read; 8-bit pages through registers, where
+// they become bf16 numbers with their scales in, which is exact.  So a page is read, and converted, once for up to 256 rows.
+// bf16 queries: the weights are rounded to one bf16 piece here (2^-8 of each at most, at random, next to the output's own rounding):
+// this kernel is bound by the matrix units, and a second piece is half as many products again in the second product.
+// Queries of two and three pieces take 64 and 96 registers, so that a SIMD holds one wavefront (pages_wide): such a workgroup has four
+// wavefronts and, where loads go straight to LDS, four buffers with three stages under way instead.
+template <int D, bool E4M3, int NQ>
+__global__ void __launch_bounds__(pages_wide(NQ, E4M3) ? 256 : 512) __attribute__((amdgpu_waves_per_eu(pages_wide(NQ, E4M3) ? 1 : 2)))
+pages_attend_shared_kernel(PagesAttnArgs a) {
+    using T = Tile<32>;
+    constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
+    constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
+    constexpr int NB = pages_wide(NQ, E4M3) && !E4M3 ? 4 : 2;
+    __shared__ __align__(16) uint4 stage[NB][2][HALF];   // [buffer][keys, values]
+    __shared__ long long lds[8];
+    __shared__ Walk walk;
+    __shared__ int pg_base[64], pg_id[64], pg_n, pg_odd;   // pg_odd: the page that has values that are not finite
+    __shared__ __align__(8) float2 lds_ml[4 * 64];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, row = lane & 31;
+    const int waves = blockDim.x / 64, tiles = waves / a.key_halves, rt = wave % tiles, kh = wave / tiles;
+    const int heads = a.c.n_kv_heads, G = a.group_heads;
+    const int kt0 = a.key_halves == 2 ? kh : 0, kt1 = a.key_halves == 2 ? kh + 1 : 2;
+    if (!walk_start<STEP>(a, &walk, lds)) return;
+
+    do {
+        const Entry en = walk.en;
+        const int h = walk.h;
+        const long long unit0 = walk.h * walk.per_head + walk.before;
+        const int s0 = __builtin_amdgcn_readfirstlane((int)(walk.at - unit0));
+        const int s1 = __builtin_amdgcn_readfirstlane((int)min(walk.last - unit0, (long long)en.steps));
+        const bool whole = s0 == 0 && s1 == en.steps;
+        const int slot = 2 * walk.share + (walk.first_unit ? 0 : 1);
+
+        const int r = rt * 32 + row, myrow = en.rows0 + r;
+        const bool have = myrow < en.rows1;
+        const int t = have ? myrow / G : 0, g = have ? myrow % G : 0;
+        const int sees = have ? sees_of(a, en.P, en.n, t) : 0;
+        int least = have ? sees : 0x7FFFFFFF, most = sees;
+        for (int m = 16; m; m >>= 1) least = min(least, __shfl_xor(least, m)), most = max(most, __shfl_xor(most, m));
+        least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
+        const int begins = sees_of(a, en.P, en.n, en.t0), ends = sees_of(a, en.P, en.n, en.t1 - 1);   // what each row sees, and what any does
+
+        uint4 q[NQ][QS];
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            const int d = 16 * s + 8 * hf;
+            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
+                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
+                if (have) {
+                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                    q[0][s] = *(const uint4*)p;
+                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
+                }
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
+                if (a.negate)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
+#pragma unroll
+                for (int p = 0; p < NQ; ++p) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                    }
+                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
+                }
+            }
+        }
+        f32x16_t o[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+        float m_run = -INFINITY, l_run = 0.0f;
+        const int32_t* list = a.list ? a.list + ((size_t)(en.b * a.n_blk + en.blk) * heads + h) * a.n_list : nullptr;
+
+        for (int win = s0; win < s1; win += 64) {
+            // the window's pages, those that there are, one behind the other
+            if (wave == 0) {
+                const int i = win + lane, page = i < s1 ? (list ? list[i] : i) : -1;
+                const int id = page >= 0 && page < a.c.max_pages ? a.c.table[(size_t)en.b * a.c.max_pages + page] : -1;
+                const bool seen = page < -1 || (page >= 0 && page * 64LL < ends);
+                const bool good = seen && (unsigned)id < (unsigned)a.c.n_pages;
+                if (seen && !good) flag(a.status, ST_PAGE);
+                const unsigned long long who = __ballot(good);
+                if (good) {
+                    const int at = __popcll(who & ((1ull << lane) - 1));
+                    pg_base[at] = page * 64, pg_id[at] = id;
+                }
+                if (lane == 0) pg_n = __popcll(who), pg_odd = -1;
+            }
+            __syncthreads();
+            const int n = __builtin_amdgcn_readfirstlane(pg_n);
+
+            // bf16: a wavefront's loads of a stage, each one operand (64 lanes x 16 bytes) from where its lanes' pieces lie in the page
+            const int m32 = 8 * (row >> 4) + (row & 7);
+            const int k_lane = ((row >> 3) & 1) * (D / 32) * 64 + hf * 16 + m32, v_lane = (row >> 4) * 64 + hf * 16 + (row & 15);
+            auto fetch = [&](int j, int buf) {
+                const size_t head = ((size_t)__builtin_amdgcn_readfirstlane(pg_id[j]) * heads + h) * 64 * D;
+                const uint4* kp = (const uint4*)((const uint16_t*)a.c.k + head) + k_lane;
+                const uint4* vp = (const uint4*)((const uint16_t*)a.c.v + head) + v_lane;
+                const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&stage[buf][0][0];
+                for (int i = wave; i < 4 * QS; i += NB == 4 ? 4 : waves) {
+                    const bool value = i >= 2 * QS;
+                    const int o2 = value ? i - 2 * QS : i, kt = o2 / QS, s = o2 % QS;   // values: s = (dims of 32, step)
+                    const uint4* p = value ? vp + (kt * (D / 16) + (s >> 1) * 2) * 64 + (s & 1) * 32 : kp + (kt * 2 * (D / 32) + (s >> 1)) * 64 + (s & 1) * 32;
+                    load_to_lds<false>(p, __builtin_amdgcn_readfirstlane(to + (uint32_t)i * 1024u));
+                }
+            };
+            // 8 bits: a thread's 16-byte pieces of a stage (at most two of the keys and two of the values: there are at least 4 wavefronts)
+            constexpr int NI = D / 64;
+            uint4 rk[NI], rv[NI];
+            uint32_t rks[NI], rvs[4];   // of the values: the same for both pieces, which are whole blocks apart
+            auto fetch8 = [&](int j) {
+                const size_t hd = (size_t)__builtin_amdgcn_readfirstlane(pg_id[j]) * heads + h;
+                const uint4* kp = (const uint4*)((const uint8_t*)a.c.k + hd * 64 * D);
+                const uint4* vp = (const uint4*)((const uint8_t*)a.c.v + hd * 64 * D);
+                const uint8_t* sc = a.c.scale + hd * 128;
+#pragma unroll
+                for (int u = 0; u < NI; ++u) {
+                    const int i = tid + u * (int)blockDim.x;
+                    if (i < 4 * D) {
+                        rk[u] = kp[i];
+                        const int m = i & 15, tile = i / (D / 64 * 64);
+                        rks[u] = sc[(tile >> 1) * 32 + (tile & 1) * 8 + 16 * (m >> 3) + (m & 7)];
+                        rv[u] = vp[i];
+                    }
+                }
+                const int pc = (tid >> 4) & 3;
+                const uint32_t* vs = (const uint32_t*)(sc + 64 + 16 * (pc >> 1) + 4 * (pc & 1));
+#pragma unroll
+                for (int x = 0; x < 4; ++x) rvs[x] = vs[(x >> 1) * 8 + (x & 1) * 2];
+            };
+            auto put8 = [&](int buf) {
+#pragma unroll
+                for (int u = 0; u < NI; ++u) {
+                    const int i = tid + u * (int)blockDim.x;
+                    if (i < 4 * D) {
+                        const int m = i & 15, pc = (i >> 4) & 3, blk = i >> 6;
+                        {   // 16 dims of a key: two lanes' pieces of one step
+                            const int tile = blk / (D / 64), kt = tile >> 1, rho = (tile & 1) * 8 + 16 * (m >> 3) + (m & 7), s = (blk % (D / 64)) * 4 + pc;
+                            uint4* to = &stage[buf][0][(kt * QS + s) * 64 + rho];
+                            const float f = scale_of(rks[u]);
+                            to[0] = eight_bf16(rk[u].x, rk[u].y, f);
+                            to[32] = eight_bf16(rk[u].z, rk[u].w, f);
+                        }
+                        // 8 keys of a dim, of both groups of 32
+                        const int d = blk * 16 + m;
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const uint32_t b = kt ? (x < 2 ? rv[u].z : rv[u].w) : (x < 2 ? rv[u].x : rv[u].y), sb = rvs[kt * 2 + (x >> 1)] >> (16 * (x & 1));
+                                const float f0 = scale_of(sb & 0xFFu), f1 = scale_of((sb >> 8) & 0xFFu);
+                                const uint32_t lo = x & 1 ? pair_bf16<true>(b, f0) : pair_bf16<false>(b, f0), hi = x & 1 ? pair_bf16<true>(b, f1) : pair_bf16<false>(b, f1);
+                                w[x] = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+                            }
+                            stage[buf][1][(kt * QS + (d >> 5) * 2 + (pc >> 1)) * 64 + (pc & 1) * 32 + (d & 31)] = uint4{w[0], w[1], w[2], w[3]};
+                        }
+                    }
+                }
+            };
+
+            if (n > 0) {
+                if constexpr (E4M3) {
+                    fetch8(0);
+                    put8(0);
+                } else {
+                    for (int i = 0; i < min(n, NB - 1); ++i) fetch(i, i);
+                }
+            }
+            for (int j = 0; j < n; ++j) {
+                const int buf = j % NB;
+                if constexpr (NB == 4) {   // QS loads per wavefront and stage; stages j + 1 and j + 2 may still be under way
+                    if (n - j > 2) stage_wait<2 * QS>();
+                    else if (n - j == 2) stage_wait<QS>();
+                    else stage_wait<0>();
+                } else if constexpr (!E4M3) {
+                    stage_wait<0>();
+                }
+                __syncthreads();   // the stage is there, and nobody reads the one before any more
+                if constexpr (E4M3) {
+                    if (j + 1 < n) fetch8(j + 1);
+                } else {
+                    if (j + NB - 1 < n) fetch(j + NB - 1, (j + NB - 1) % NB);
+                }
+                const int page0 = __builtin_amdgcn_readfirstlane(pg_base[j]);
+                bool odd = false;
+                if (page0 + 64 > begins) {   // some row does not see the whole page: its values, for all wavefronts
+                    for (int i = tid; i < HALF; i += blockDim.x) {
+                        const int pos = page0 + i / (QS * 64) * 32;
+                        const uint4 v = stage[buf][1][i];
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                        bool change = false;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool behind = pos + value_key((i >> 6) & 1, (i >> 5) & 1, e) >= ends, not_finite = ((w[e / 2] >> (16 * (e & 1))) & 0x7F80u) == 0x7F80u;
+                            if (behind || not_finite) w[e / 2] &= ~(0xFFFFu << (16 * (e & 1))), change = true;
+                            if (!behind && not_finite) pg_odd = j;
+                        }
+                        if (change) stage[buf][1][i] = uint4{w[0], w[1], w[2], w[3]};
+                    }
+                    __syncthreads();
+                    odd = pg_odd == j;
+                }
+#pragma unroll 1
+                for (int kt = kt0; kt < kt1; ++kt) {   // 32 keys against the wavefront's rows
+                    const int base = page0 + kt * 32;
+                    if (base >= most) break;
+                    const uint4* ks = &stage[buf][0][kt * QS * 64 + lane];
+                    const uint4* vs = &stage[buf][1][kt * QS * 64 + lane];
+                    f32x16_t x;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < QS; ++s) {
+                        const uint4 k = ks[s * 64];
+#pragma unroll
+                        for (int p = NQ - 1; p >= 0; --p) x = T::mfma(k, q[p][s], x);
+                    }
+                    if (base + 32 > least)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (base + value_key(i >> 3, hf, i & 7) >= sees) x[i] = -INFINITY;
+                    float top = x[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+                    rescale(T::across(top, [](float u, float w) { return fmaxf(u, w); }) * a.scale_log2, &m_run, &l_run, o);
+                    const float ref = m_run == -INFINITY ? 0.0f : m_run;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        x[i] = weight(x[i], a.scale_log2, ref);
+                        sum += x[i];
+                    }
+                    l_run += sum;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        float y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = x[s * 8 + i];
+                        uint4 pf[NP];
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                w[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+                                y[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), y[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                            }
+                            pf[p] = uint4{w[0], w[1], w[2], w[3]};
+                        }
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            uint4 v = vs[(dt * 2 + s) * 64];
+#pragma unroll
+                            for (int p = NP - 1; p >= 0; --p) o[dt] = T::mfma(v, pf[p], o[dt]);
+                        }
+                    }
+                    if (odd)
+                        add_not_finite<D, E4M3, 32>(o, (const char*)a.c.v + ((size_t)pg_id[j] * heads + h) * 64 * D * (E4M3 ? 1 : 2), base, lane, sees, min(most, base + 32));
+                }
+                if constexpr (E4M3)
+                    if (j + 1 < n) put8(buf ^ 1);
+            }
+            __syncthreads();   // the window, and the last stage, have been read
+        }
+
+        l_run += __shfl_xor(l_run, 32);
+        if (a.key_halves == 2) {   // the second half's sums go to the first's wavefront, through the stages' place
+            float4* to = (float4*)&stage[0][0][0] + rt * (DT * 4) * 64 + lane;
+            float2* ml = lds_ml + rt * 64 + lane;
+            if (kh == 1) {
+#pragma unroll
+                for (int i = 0; i < DT * 4; ++i) to[i * 64] = float4{o[i >> 2][(i & 3) * 4], o[i >> 2][(i & 3) * 4 + 1], o[i >> 2][(i & 3) * 4 + 2], o[i >> 2][(i & 3) * 4 + 3]};
+                *ml = float2{m_run, l_run};
+            }
+            __syncthreads();
+            if (kh == 0) {
+                const float2 z = *ml;
+                const float m = fmaxf(m_run, z.x), ref = m == -INFINITY ? 0.0f : m;
+                const float f0 = __builtin_amdgcn_exp2f(m_run - ref), f1 = __builtin_amdgcn_exp2f(z.x - ref);
+                l_run = l_run * f0 + z.y * f1;
+                m_run = m;
+#pragma unroll
+                for (int i = 0; i < DT * 4; ++i) {
+                    const float4 y = to[i * 64];
+                    const float w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i >> 2][(i & 3) * 4 + e] = o[i >> 2][(i & 3) * 4 + e] * f0 + w[e] * f1;
+                }
+            }
+        }
+        if (kh == 0 && have) {
+            const size_t at_row = (size_t)slot * a.block_rows + r;
+#pragma unroll
+            for (int i = 0; i < DT * 4; ++i) {
+                const int d = (i >> 2) * 32 + T::out_dim(lane, (i & 3) * 4);
+                const float y[4] = {o[i >> 2][(i & 3) * 4], o[i >> 2][(i & 3) * 4 + 1], o[i >> 2][(i & 3) * 4 + 2], o[i >> 2][(i & 3) * 4 + 3]};
+                if (whole) finish_row<D>(a, en.b, en.r0, en.n, t, h * G + g, d, m_run, l_run, y);
+                else *(float4*)(a.part_o + at_row * D + d) = float4{y[0], y[1], y[2], y[3]};
+            }
+            if (!whole && hf == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m_run, l_run};
+        }
+    } while (walk_next<STEP>(a, &walk));
+}
+
+
 // The parts of units that several workgroups have: a.slices workgroups per unit, each taking every a.slices-th 1024 / D of its rows.
-template <int D, bool E4M3>
+template <int D, int STEP>
 __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
-    constexpr int STEP = E4M3 ? 64 : 32, TPR = D / 4, ROWS = 256 / TPR;
+    constexpr int TPR = D / 4, ROWS = 256 / TPR;
     __shared__ long long lds[4];
     const int heads = a.c.n_kv_heads, G = a.group_heads;
     const int slice = blockIdx.x % a.slices, h = blockIdx.x / a.slices % heads, e = blockIdx.x / a.slices / heads;
     const Entry en = entry_of<STEP>(a, e, nullptr);
     if (en.rows0 + slice * ROWS >= en.rows1) return;
-    long long before, total, live;
-    sum_entries<STEP>(a, e, lds, &before, &total, &live, nullptr);
-    total *= heads;
-    const long long u0 = before * heads + (long long)h * en.steps;
-    if (u0 + en.steps > total) return;   // not unless the lengths change meanwhile
-    const Share sh = share_of(total, live * heads, a.grid, a.least_steps);
+    long long before, per_head, live;
+    sum_entries<STEP>(a, e, lds, &before, &per_head, &live, nullptr);
+    const long long u0 = h * per_head + before;
+    if (before + en.steps > per_head) return;   // not unless the lengths change meanwhile
+    const Share sh = share_of(per_head * heads, live * heads, a.grid, a.least_steps);
     const int w0 = sh.of(u0), w1 = sh.of(u0 + en.steps - 1), n = w1 - w0 + 1;
     if (n == 1) return;
     const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (u0 > sh.begin(w0) ? 1 : 0);
@@ -1201,7 +1572,8 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         constexpr bool E = decltype(e)::value;
         auto run = [&](auto nq) {
             constexpr int NQ = decltype(nq)::value;
-            if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
+            if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
+            else if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
             else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
         };
         if (a.q_split) run(std::integral_constant<int, 2>());
@@ -1209,7 +1581,9 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         else run(std::integral_constant<int, 1>());
         const hipError_t st = hipGetLastError();
         if (st != hipSuccess) return st;
-        pages_combine_kernel<D, E><<<a.n_entries * a.c.n_kv_heads * a.slices, 256, 0, s>>>(a);
+        const int wgs = a.n_entries * a.c.n_kv_heads * a.slices;
+        if (a.shared_waves || E) pages_combine_kernel<D, 64><<<wgs, 256, 0, s>>>(a);
+        else pages_combine_kernel<D, 32><<<wgs, 256, 0, s>>>(a);
         return hipGetLastError();
     });
 }

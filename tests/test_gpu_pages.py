@@ -3,8 +3,8 @@
 Bounds.  Writing, reading and selecting are exact: every stored value, bound and list is compared bit for bit.
 Attention: a score is an f32 sum of D exact products (bf16 times bf16; three pieces of an f32 query leave 2^-24 of it), so with
 S = the largest sum of |q_d k_d scale| of a row it is off by at most (D + 4) * 2^-24 * S, and its exponent, a product, a difference and one
-exp2, by (|s| + |max|) * 2^-23 more; the weights are off by e = twice that (their sum takes the same terms).  The weights are rounded to
-two bf16 pieces (2^-16) for bf16 queries and to three (2^-24) for f32 ones.  Sums of n terms in steps of 32: (n / 32 + 64) * 2^-24.
+exp2, by (|s| + |max|) * 2^-23 more; the weights are off by e = twice that (their sum takes the same terms).  The weights are rounded, for
+bf16 queries to two bf16 pieces (2^-16), or to one (2^-8) where more than 32 rows share a KV head's keys, for f32 ones to three (2^-24).  Sums of n terms in steps of 32: (n / 32 + 64) * 2^-24.
 Hence, with A = sum of weights times |v|:
     out   (e + pieces + (n / 32 + 64) * 2^-24) * A, and half a step of its type: 2^-8 (bf16) or 2^-23 (f32: two roundings) of |out|
     lse   e / 2 + (n / 32 + 64) * 2^-24 + 2^-23 |lse|
@@ -106,7 +106,8 @@ class Setup:
         n = self.max_len
         e = 2 * ((self.D + 4) * 2.0 ** -24 * s + 2 * s * 2.0 ** -23 + 2.0 ** -23)
         sums = (n / 32 + 64) * 2.0 ** -24
-        half, piece = (2.0 ** -8, 2.0 ** -16) if out.dtype == BF16 else (2.0 ** -23, 2.0 ** -24)
+        many = min(group if lists is not None else self.most, self.most) * q.shape[1] // self.H > 32
+        half, piece = (2.0 ** -8, 2.0 ** -8 if many else 2.0 ** -16) if out.dtype == BF16 else (2.0 ** -23, 2.0 ** -24)
         off = (out.double() - o).abs()
         most = half * o.abs() + (e[..., None] + piece + sums) * a
         assert bool((off <= most).all()), float((off - most).max())
