@@ -338,18 +338,17 @@ struct PagesPlan {
     size_t part_ml, total;
 };
 
-bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, bool wide, PagesPlan* out) {
+bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, bool raw, PagesPlan* out) {
     PagesPlan p{};
     const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
-    p.row_tiles = (int)std::min<long long>(wide ? 4 : 8, (rows + 31) / 32);
-    if (wide && p.row_tiles == 3) p.row_tiles = 4;
+    p.row_tiles = (int)std::min<long long>(8, (rows + 31) / 32);
     p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;
-    p.key_halves = p.row_tiles <= (wide ? 2 : 4) ? 2 : 1;
+    p.key_halves = p.row_tiles <= 4 ? 2 : 1;
     p.shared_waves = p.row_tiles > 1 ? p.row_tiles * p.key_halves : 0;
     const long long blocks = group ? cdiv(max_rows, group) : (rows + p.block_rows - 1) / p.block_rows;
     if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
     p.n_blk = (int)blocks;
-    p.grid = p.shared_waves > 4 || (p.shared_waves && wide) ? device_cus() : 2 * device_cus();
+    p.grid = p.shared_waves > 4 || (p.shared_waves && raw) ? device_cus() : 2 * device_cus();
     // the second launch: a few thousand workgroups at most, and one where units are that many
     const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
     p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
@@ -499,7 +498,7 @@ nld_status validate_paged(const nld_model* m, const nld_pages* pages, const nld_
         if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
             return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     }
-    if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, pages_wide(2, pages->dtype == NLD_E4M3), &p.plan))
+    if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, pages_raw(2, pages->dtype == NLD_E4M3), &p.plan))
         return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     p.attn = align256(L.total);
     p.lists = p.attn + std::max(p.plan.total, p.group ? align256(256 + score_bytes(pages, k, p.group)) : 0);
@@ -1532,9 +1531,9 @@ size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int3
     // the most that any number of rows up to these, and any type, needs: by the tiles of a workgroup
     size_t n = 0;
     const long long rows = (long long)max_rows * G;
-    for (const bool wide : {false, true})
+    for (const bool raw : {false, true})
         for (long long r = 16; r == 16 || r - 32 < std::min(rows, 256LL); r = r == 16 ? 32 : r + 32)
-            if (plan_pages(1, 1, pages->head_dim, 1, (int)r, 0, wide, &p)) n = std::max(n, p.total);
+            if (plan_pages(1, 1, pages->head_dim, 1, (int)r, 0, raw, &p)) n = std::max(n, p.total);
     return group ? std::max(n, align256(256 + score_bytes(pages, max_rows, group))) : n;
 }
 
@@ -1598,7 +1597,7 @@ nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chu
     if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     PagesPlan p;
     if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, n_q_heads / pages->n_kv_heads, chunk->max_rows, list ? group : 0,
-                    pages_wide(q->dtype == NLD_F32 ? 3 : 1, pages->dtype == NLD_E4M3), &p))
+                    pages_raw(q->dtype == NLD_F32 ? 3 : 1, pages->dtype == NLD_E4M3), &p))
         return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
     if (ws_bytes < p.total) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs %zu", ws_bytes, p.total);
     PagesAttnArgs a = pages_args(page_layer(pages, layer), page_chunk(chunk), n_q_heads / pages->n_kv_heads, mode, bidir_from, scale, p, workspace, 0);

@@ -62,6 +62,10 @@ __device__ __forceinline__ void load_to_lds(const void* src, uint32_t dst) {
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
 }
+// the same from `base` (uniform) plus a lane's `off` bytes
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory", "m0");
+}
 // at most N vector memory operations of this wavefront still under way
 template <int N>
 __device__ __forceinline__ void stage_wait() {
@@ -431,8 +435,9 @@ struct PagesAttnArgs {
     uint32_t* status;
 };
 
-// Whether the attention of many rows has one wavefront per SIMD: by the queries' pieces and the pages' type.
-__host__ __device__ constexpr bool pages_wide(int pieces, bool e4m3) { return pieces == 3 || (pieces == 2 && e4m3); }
+// Whether the attention of many rows keeps pages in LDS as they are on their way (it then has the CU to itself): by the queries' pieces and the
+// pages' type.
+__host__ __device__ constexpr bool pages_raw(int pieces, bool e4m3) { return pieces > 1 && e4m3; }
 constexpr int PAGES_GROUP_ROWS = 128;   // rows (tokens x query heads of a KV head) that share a list of pages
 
 struct PagesSelectArgs {

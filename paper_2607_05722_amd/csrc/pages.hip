@@ -567,6 +567,26 @@ __device__ __forceinline__ bool walk_start(const PagesAttnArgs& a, Walk* w, long
     return true;
 }
 
+// The present unit, in scalar registers.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+struct Unit {
+    Entry en;
+    int h, s0, s1, slot;   // KV head; steps [s0, s1) are this workgroup's; place of its part
+    bool whole;
+};
+__device__ __forceinline__ Unit walk_unit(const Walk& w) {
+    Unit u;
+    const Entry& e = w.en;
+    u.en = Entry{scalar(e.b), scalar(e.blk), scalar(e.r0), scalar(e.n), scalar(e.P), scalar(e.t0), scalar(e.t1), scalar(e.rows0), scalar(e.rows1), scalar(e.steps)};
+    u.h = scalar(w.h);
+    const long long unit0 = w.h * w.per_head + w.before;
+    u.s0 = scalar((int)(w.at - unit0));
+    u.s1 = scalar((int)min(w.last - unit0, (long long)e.steps));
+    u.slot = 2 * scalar(w.share) + (scalar(w.first_unit) ? 0 : 1);
+    u.whole = u.s0 == 0 && u.s1 == u.en.steps;
+    return u;
+}
+
 // On to the next unit; false behind the last.  Called by every thread after it has read what it needs of the present one.
 template <int STEP>
 __device__ __forceinline__ bool walk_next(const PagesAttnArgs& a, Walk* w) {
@@ -711,13 +731,10 @@ pages_attend_kernel(PagesAttnArgs a) {
     const int key_of_row = RW == 16 ? 16 * (row >> 3) + (row & 7) : row;   // of a tile's first keys
 
     do {
-        const Entry en = walk.en;
-        const int h = walk.h;
-        const long long unit0 = walk.h * walk.per_head + walk.before;
-        const int s0 = __builtin_amdgcn_readfirstlane((int)(walk.at - unit0));
-        const int s1 = __builtin_amdgcn_readfirstlane((int)min(walk.last - unit0, (long long)en.steps));
-        const bool whole = s0 == 0 && s1 == en.steps;
-        const int slot = 2 * walk.share + (walk.first_unit ? 0 : 1);
+        const Unit unit = walk_unit(walk);
+        const Entry& en = unit.en;
+        const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
+        const bool whole = unit.whole;
 
         // this wavefront's rows
         const int myrow = en.rows0 + rt * RW + row;
@@ -982,6 +999,26 @@ pages_attend_kernel(PagesAttnArgs a) {
     } while (walk_next<STEP>(a, &walk));
 }
 
+// at most n of this wavefront's loads still under way (n: of a wavefront, at most 17)
+__device__ __forceinline__ void wait_loads(int n) {
+    switch (n) {
+        case 0: stage_wait<0>(); break;
+        case 1: stage_wait<1>(); break;
+        case 2: stage_wait<2>(); break;
+        case 3: stage_wait<3>(); break;
+        case 4: stage_wait<4>(); break;
+        case 5: stage_wait<5>(); break;
+        case 6: stage_wait<6>(); break;
+        case 7: stage_wait<7>(); break;
+        case 8: stage_wait<8>(); break;
+        case 10: stage_wait<10>(); break;
+        case 12: stage_wait<12>(); break;
+        case 14: stage_wait<14>(); break;
+        case 16: stage_wait<16>(); break;
+        default: stage_wait<0>(); break;   // fewer than n are as good
+    }
+}
+
 // ---------------------------------------------------------------- attention of many rows
 // More than one tile of 32 rows: a workgroup has `tiles` of them (up to 8), key_halves wavefronts each (two where there are up to 4
 // tiles: each takes 32 of a page's 64 keys, and they meet at the unit's end).  The wavefronts share each page through LDS, double-buffered:
@@ -989,16 +1026,19 @@ pages_attend_kernel(PagesAttnArgs a) {
 // they become bf16 numbers with their scales in, which is exact.  So a page is read, and converted, once for up to 256 rows.
 // bf16 queries: the weights are rounded to one bf16 piece here (2^-8 of each at most, at random, next to the output's own rounding):
 // this kernel is bound by the matrix units, and a second piece is half as many products again in the second product.
-// Queries of two and three pieces take 64 and 96 registers, so that a SIMD holds one wavefront (pages_wide): such a workgroup has four
-// wavefronts and, where loads go straight to LDS, four buffers with three stages under way instead.
+// Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (pages_raw) go to LDS as they
+// are, two stages ahead, and become bf16 a stage ahead of their use.
 template <int D, bool E4M3, int NQ>
-__global__ void __launch_bounds__(pages_wide(NQ, E4M3) ? 256 : 512) __attribute__((amdgpu_waves_per_eu(pages_wide(NQ, E4M3) ? 1 : 2)))
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 pages_attend_shared_kernel(PagesAttnArgs a) {
     using T = Tile<32>;
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
-    constexpr int NB = pages_wide(NQ, E4M3) && !E4M3 ? 4 : 2;
-    __shared__ __align__(16) uint4 stage[NB][2][HALF];   // [buffer][keys, values]
+    constexpr bool DEEP = pages_raw(NQ, E4M3);
+    constexpr int RAW = DEEP ? 3 : 0;
+    constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
+    __shared__ __align__(16) uint4 stage[2][2][HALF];   // [buffer][keys, values]
+    __shared__ __align__(16) uint4 raw[RAW ? RAW : 1][RAW ? HALF + 8 : 1];   // [buffer]: keys, values, scales in 8 bits
     __shared__ long long lds[8];
     __shared__ Walk walk;
     __shared__ int pg_base[64], pg_id[64], pg_n, pg_odd;   // pg_odd: the page that has values that are not finite
@@ -1011,13 +1051,10 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
     if (!walk_start<STEP>(a, &walk, lds)) return;
 
     do {
-        const Entry en = walk.en;
-        const int h = walk.h;
-        const long long unit0 = walk.h * walk.per_head + walk.before;
-        const int s0 = __builtin_amdgcn_readfirstlane((int)(walk.at - unit0));
-        const int s1 = __builtin_amdgcn_readfirstlane((int)min(walk.last - unit0, (long long)en.steps));
-        const bool whole = s0 == 0 && s1 == en.steps;
-        const int slot = 2 * walk.share + (walk.first_unit ? 0 : 1);
+        const Unit unit = walk_unit(walk);
+        const Entry& en = unit.en;
+        const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
+        const bool whole = unit.whole;
 
         const int r = rt * 32 + row, myrow = en.rows0 + r;
         const bool have = myrow < en.rows1;
@@ -1070,36 +1107,47 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
         for (int win = s0; win < s1; win += 64) {
             // the window's pages, those that there are, one behind the other
             if (wave == 0) {
-                const int i = win + lane, page = i < s1 ? (list ? list[i] : i) : -1;
+                int ln = lane;
+                asm("" : "+v"(ln));
+                const int i = win + ln, page = i < s1 ? (list ? list[i] : i) : -1;
                 const int id = page >= 0 && page < a.c.max_pages ? a.c.table[(size_t)en.b * a.c.max_pages + page] : -1;
                 const bool seen = page < -1 || (page >= 0 && page * 64LL < ends);
                 const bool good = seen && (unsigned)id < (unsigned)a.c.n_pages;
                 if (seen && !good) flag(a.status, ST_PAGE);
                 const unsigned long long who = __ballot(good);
                 if (good) {
-                    const int at = __popcll(who & ((1ull << lane) - 1));
+                    const int at = __popcll(who & ((1ull << ln) - 1));
                     pg_base[at] = page * 64, pg_id[at] = id;
                 }
-                if (lane == 0) pg_n = __popcll(who), pg_odd = -1;
+                if (ln == 0) pg_n = __popcll(who), pg_odd = -1;
             }
             __syncthreads();
             const int n = __builtin_amdgcn_readfirstlane(pg_n);
 
             // bf16: a wavefront's loads of a stage, each one operand (64 lanes x 16 bytes) from where its lanes' pieces lie in the page
-            const int m32 = 8 * (row >> 4) + (row & 7);
-            const int k_lane = ((row >> 3) & 1) * (D / 32) * 64 + hf * 16 + m32, v_lane = (row >> 4) * 64 + hf * 16 + (row & 15);
+            int ln = lane;
+            asm("" : "+v"(ln));
+            const int m32 = 8 * ((ln >> 4) & 1) + (ln & 7), h16 = (ln >> 5) * 16;
+            const uint32_t k_lane = (((ln >> 3) & 1) * (D / 32) * 64 + h16 + m32) * 16, v_lane = (((ln >> 4) & 1) * 64 + h16 + (ln & 15)) * 16;   // bytes
             auto fetch = [&](int j, int buf) {
-                const size_t head = ((size_t)__builtin_amdgcn_readfirstlane(pg_id[j]) * heads + h) * 64 * D;
-                const uint4* kp = (const uint4*)((const uint16_t*)a.c.k + head) + k_lane;
-                const uint4* vp = (const uint4*)((const uint16_t*)a.c.v + head) + v_lane;
-                const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&stage[buf][0][0];
-                for (int i = wave; i < 4 * QS; i += NB == 4 ? 4 : waves) {
-                    const bool value = i >= 2 * QS;
-                    const int o2 = value ? i - 2 * QS : i, kt = o2 / QS, s = o2 % QS;   // values: s = (dims of 32, step)
-                    const uint4* p = value ? vp + (kt * (D / 16) + (s >> 1) * 2) * 64 + (s & 1) * 32 : kp + (kt * 2 * (D / 32) + (s >> 1)) * 64 + (s & 1) * 32;
-                    load_to_lds<false>(p, __builtin_amdgcn_readfirstlane(to + (uint32_t)i * 1024u));
+                const size_t hd = (size_t)scalar(pg_id[j]) * heads + h;
+                const char* kp = (const char*)a.c.k + hd * 64 * D * (E4M3 ? 1 : 2);
+                const char* vp = (const char*)a.c.v + hd * 64 * D * (E4M3 ? 1 : 2);
+                const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)(E4M3 ? &raw[RAW ? buf : 0][0] : &stage[buf][0][0]);
+                for (int i = wave; i < LOADS; i += waves) {
+                    const uint32_t dst = scalar(to + (uint32_t)i * 1024u);
+                    if constexpr (E4M3) {
+                        if (i < LOADS - 1) load_to_lds(i < LOADS / 2 ? kp + i * 1024 : vp + (i - LOADS / 2) * 1024, (uint32_t)ln * 16u, dst);
+                        else if (ln < 8) load_to_lds(a.c.scale + hd * 128, (uint32_t)ln * 16u, dst);
+                    } else {
+                        const bool value = i >= 2 * QS;
+                        const int o2 = value ? i - 2 * QS : i, kt = o2 / QS, s = o2 % QS;   // values: s = (dims of 32, step)
+                        if (value) load_to_lds(vp + ((kt * (D / 16) + (s >> 1) * 2) * 64 + (s & 1) * 32) * 16, v_lane, dst);
+                        else load_to_lds(kp + ((kt * 2 * (D / 32) + (s >> 1)) * 64 + (s & 1) * 32) * 16, k_lane, dst);
+                    }
                 }
             };
+            const int mine = (LOADS - wave + waves - 1) / waves;   // loads of this wavefront per stage
             // 8 bits: a thread's 16-byte pieces of a stage (at most two of the keys and two of the values: there are at least 4 wavefronts)
             constexpr int NI = D / 64;
             uint4 rk[NI], rv[NI];
@@ -1124,63 +1172,73 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) rvs[x] = vs[(x >> 1) * 8 + (x & 1) * 2];
             };
+            // one piece of the keys (16 dims of a key) and one of the values (8 keys of a dim, of both groups of 32) as bf16 numbers
+            auto put_piece = [&](int buf, int i, const uint4& kq, uint32_t kscale, const uint4& vq, const uint32_t* vscale) {
+                const int m = i & 15, pc = (i >> 4) & 3, blk = i >> 6;
+                const int tile = blk / (D / 64), rho = (tile & 1) * 8 + 16 * (m >> 3) + (m & 7), s = (blk % (D / 64)) * 4 + pc, d = blk * 16 + m;
+                uint4* to = &stage[buf][0][((tile >> 1) * QS + s) * 64 + rho];   // two lanes' pieces of one step
+                const float f = scale_of(kscale);
+                to[0] = eight_bf16(kq.x, kq.y, f);
+                to[32] = eight_bf16(kq.z, kq.w, f);
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t b = kt ? (x < 2 ? vq.z : vq.w) : (x < 2 ? vq.x : vq.y), sb = vscale[kt * 2 + (x >> 1)] >> (16 * (x & 1));
+                        const float f0 = scale_of(sb & 0xFFu), f1 = scale_of((sb >> 8) & 0xFFu);
+                        const uint32_t lo = x & 1 ? pair_bf16<true>(b, f0) : pair_bf16<false>(b, f0), hi = x & 1 ? pair_bf16<true>(b, f1) : pair_bf16<false>(b, f1);
+                        w[x] = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+                    }
+                    stage[buf][1][(kt * QS + (d >> 5) * 2 + (pc >> 1)) * 64 + (pc & 1) * 32 + (d & 31)] = uint4{w[0], w[1], w[2], w[3]};
+                }
+            };
             auto put8 = [&](int buf) {
 #pragma unroll
                 for (int u = 0; u < NI; ++u) {
                     const int i = tid + u * (int)blockDim.x;
-                    if (i < 4 * D) {
-                        const int m = i & 15, pc = (i >> 4) & 3, blk = i >> 6;
-                        {   // 16 dims of a key: two lanes' pieces of one step
-                            const int tile = blk / (D / 64), kt = tile >> 1, rho = (tile & 1) * 8 + 16 * (m >> 3) + (m & 7), s = (blk % (D / 64)) * 4 + pc;
-                            uint4* to = &stage[buf][0][(kt * QS + s) * 64 + rho];
-                            const float f = scale_of(rks[u]);
-                            to[0] = eight_bf16(rk[u].x, rk[u].y, f);
-                            to[32] = eight_bf16(rk[u].z, rk[u].w, f);
-                        }
-                        // 8 keys of a dim, of both groups of 32
-                        const int d = blk * 16 + m;
-#pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const uint32_t b = kt ? (x < 2 ? rv[u].z : rv[u].w) : (x < 2 ? rv[u].x : rv[u].y), sb = rvs[kt * 2 + (x >> 1)] >> (16 * (x & 1));
-                                const float f0 = scale_of(sb & 0xFFu), f1 = scale_of((sb >> 8) & 0xFFu);
-                                const uint32_t lo = x & 1 ? pair_bf16<true>(b, f0) : pair_bf16<false>(b, f0), hi = x & 1 ? pair_bf16<true>(b, f1) : pair_bf16<false>(b, f1);
-                                w[x] = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
-                            }
-                            stage[buf][1][(kt * QS + (d >> 5) * 2 + (pc >> 1)) * 64 + (pc & 1) * 32 + (d & 31)] = uint4{w[0], w[1], w[2], w[3]};
-                        }
-                    }
+                    if (i < 4 * D) put_piece(buf, i, rk[u], rks[u], rv[u], rvs);
+                }
+            };
+            auto put_raw = [&](int from, int buf) {
+                const uint8_t* sc = (const uint8_t*)&raw[RAW ? from : 0][RAW ? HALF : 0];
+#pragma unroll 1
+                for (int i = tid; i < 4 * D; i += blockDim.x) {
+                    const int m = i & 15, pc = (i >> 4) & 3, tile = i / D;
+                    const uint32_t* vs = (const uint32_t*)(sc + 64 + 16 * (pc >> 1) + 4 * (pc & 1));
+                    const uint32_t vscale[4] = {vs[0], vs[2], vs[8], vs[10]};
+                    put_piece(buf, i, raw[RAW ? from : 0][RAW ? i : 0], sc[(tile >> 1) * 32 + (tile & 1) * 8 + 16 * (m >> 3) + (m & 7)], raw[RAW ? from : 0][RAW ? HALF / 2 + i : 0], vscale);
                 }
             };
 
             if (n > 0) {
-                if constexpr (E4M3) {
+                if constexpr (DEEP) {
+                    for (int i = 0; i < min(n, 3); ++i) fetch(i, i);
+                    wait_loads(mine * (min(n, 3) - 1));
+                    __syncthreads();
+                    put_raw(0, 0);
+                } else if constexpr (E4M3) {
                     fetch8(0);
                     put8(0);
                 } else {
-                    for (int i = 0; i < min(n, NB - 1); ++i) fetch(i, i);
+                    fetch(0, 0);
                 }
             }
             for (int j = 0; j < n; ++j) {
-                const int buf = j % NB;
-                if constexpr (NB == 4) {   // QS loads per wavefront and stage; stages j + 1 and j + 2 may still be under way
-                    if (n - j > 2) stage_wait<2 * QS>();
-                    else if (n - j == 2) stage_wait<QS>();
-                    else stage_wait<0>();
-                } else if constexpr (!E4M3) {
-                    stage_wait<0>();
-                }
+                const int buf = j & 1;
+                if constexpr (DEEP) wait_loads(mine * max(min(n - 2 - j, 1), 0));   // stage j + 2 may still be under way
+                else if constexpr (!E4M3) stage_wait<0>();
                 __syncthreads();   // the stage is there, and nobody reads the one before any more
-                if constexpr (E4M3) {
-                    if (j + 1 < n) fetch8(j + 1);
-                } else {
-                    if (j + NB - 1 < n) fetch(j + NB - 1, (j + NB - 1) % NB);
+                if constexpr (DEEP) {
+                    if (j + 3 < n) fetch(j + 3, j % 3);
+                } else if (j + 1 < n) {
+                    if constexpr (E4M3) fetch8(j + 1);
+                    else fetch(j + 1, buf ^ 1);
                 }
                 const int page0 = __builtin_amdgcn_readfirstlane(pg_base[j]);
                 bool odd = false;
                 if (page0 + 64 > begins) {   // some row does not see the whole page: its values, for all wavefronts
+#pragma unroll 1
                     for (int i = tid; i < HALF; i += blockDim.x) {
                         const int pos = page0 + i / (QS * 64) * 32;
                         const uint4 v = stage[buf][1][i];
@@ -1197,15 +1255,16 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     __syncthreads();
                     odd = pg_odd == j;
                 }
-                // A tile's keys and values are requested from LDS well before they are multiplied, all at once: one by one each product would wait
-                // out the latency of its own (drafts over 8 bits 174 us, 164 so).
-                constexpr bool AHEAD = pages_wide(NQ, E4M3) || (NQ == 1 && !E4M3);   // registers for the next tile's keys too
-                uint4 kf[QS], vf[QS];
-                auto load_keys = [&](int kt) {
+                // A tile's keys and values are requested from LDS several at once, well before they are multiplied: one by one each product would wait
+                // out the latency of its own.  Queries of one piece over bf16 pages leave registers for all of a tile's, and the next tile's keys.
+                constexpr bool AHEAD = NQ == 1 && !E4M3;
+                constexpr int CH = AHEAD ? QS : NQ == 3 ? 2 : 4;
+                uint4 kf[CH], vf[AHEAD ? QS : DT];
+                auto load_keys = [&](int kt, int s0) {
 #pragma unroll
-                    for (int s = 0; s < QS; ++s) kf[s] = stage[buf][0][(kt * QS + s) * 64 + lane];
+                    for (int s = 0; s < CH; ++s) kf[s] = stage[buf][0][(kt * QS + s0 + s) * 64 + lane];
                 };
-                if (AHEAD && page0 + kt0 * 32 < most) load_keys(kt0);
+                if (AHEAD && page0 + kt0 * 32 < most) load_keys(kt0, 0);
 #pragma unroll 1
                 for (int kt = kt0; kt < kt1; ++kt) {   // 32 keys against the wavefront's rows
                     const int base = page0 + kt * 32;
@@ -1213,15 +1272,22 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     f32x16_t x;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-                    if (!AHEAD) load_keys(kt);
-                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int s = 0; s < QS; ++s)
+                    for (int s0 = 0; s0 < QS; s0 += CH) {
+                        if (!AHEAD) load_keys(kt, s0);
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int p = NQ - 1; p >= 0; --p) x = T::mfma(kf[s], q[p][s], x);
+                        for (int s = 0; s < CH; ++s)
 #pragma unroll
-                    for (int s = 0; s < QS; ++s) vf[s] = stage[buf][1][(kt * QS + s) * 64 + lane];
-                    if (AHEAD && kt + 1 < kt1) load_keys(kt + 1);
+                            for (int p = NQ - 1; p >= 0; --p) x = T::mfma(kf[s], q[p][s0 + s], x);
+                    }
+                    // values: step s of dims dt at 2 dt + s; all at once, or a step's
+                    auto load_values = [&](int s) {
+#pragma unroll
+                        for (int i = 0; i < (AHEAD ? QS : DT); ++i) vf[i] = stage[buf][1][(kt * QS + (AHEAD ? i : 2 * i + s)) * 64 + lane];
+                    };
+                    load_values(0);
+                    if (AHEAD && kt + 1 < kt1) load_keys(kt + 1, 0);
                     __builtin_amdgcn_sched_barrier(0);
                     if (base + 32 > least)
 #pragma unroll
@@ -1244,28 +1310,29 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                         float y[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) y[i] = x[s * 8 + i];
-                        uint4 pf[NP];
 #pragma unroll
-                        for (int p = 0; p < NP; ++p) {
+                        for (int p = 0; p < NP; ++p) {   // a piece of the weights at a time
                             uint32_t w[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 w[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
                                 y[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), y[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
                             }
-                            pf[p] = uint4{w[0], w[1], w[2], w[3]};
-                        }
+                            const uint4 pf{w[0], w[1], w[2], w[3]};
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-                            for (int p = NP - 1; p >= 0; --p) o[dt] = T::mfma(vf[dt * 2 + s], pf[p], o[dt]);
+                            for (int dt = 0; dt < DT; ++dt) o[dt] = T::mfma(vf[AHEAD ? dt * 2 + s : dt], pf, o[dt]);
+                            if (NQ == 3) __builtin_amdgcn_sched_barrier(0);
                         }
+                        if (!AHEAD && s == 0) load_values(1);
                     }
                     if (odd)
                         add_not_finite<D, E4M3, 32>(o, (const char*)a.c.v + ((size_t)pg_id[j] * heads + h) * 64 * D * (E4M3 ? 1 : 2), base, lane, sees, min(most, base + 32));
                 }
                 if constexpr (E4M3)
-                    if (j + 1 < n) put8(buf ^ 1);
+                    if (j + 1 < n) {
+                        if constexpr (DEEP) put_raw((j + 1) % 3, buf ^ 1);
+                        else put8(buf ^ 1);
+                    }
             }
             __syncthreads();   // the window, and the last stage, have been read
         }
@@ -1295,13 +1362,16 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                 }
             }
         }
-        if (kh == 0 && have) {
-            const size_t at_row = (size_t)slot * a.block_rows + r;
+        int r_out = r;
+        asm("" : "+v"(r_out));   // worked out again: the row's place would take registers all the way
+        const int row_out = en.rows0 + r_out, t_out = row_out / G, g_out = row_out % G;
+        if (kh == 0 && row_out < en.rows1) {
+            const size_t at_row = (size_t)slot * a.block_rows + r_out;
 #pragma unroll
             for (int i = 0; i < DT * 4; ++i) {
                 const int d = (i >> 2) * 32 + T::out_dim(lane, (i & 3) * 4);
                 const float y[4] = {o[i >> 2][(i & 3) * 4], o[i >> 2][(i & 3) * 4 + 1], o[i >> 2][(i & 3) * 4 + 2], o[i >> 2][(i & 3) * 4 + 3]};
-                if (whole) finish_row<D>(a, en.b, en.r0, en.n, t, h * G + g, d, m_run, l_run, y);
+                if (whole) finish_row<D>(a, en.b, en.r0, en.n, t_out, h * G + g_out, d, m_run, l_run, y);
                 else *(float4*)(a.part_o + at_row * D + d) = float4{y[0], y[1], y[2], y[3]};
             }
             if (!whole && hf == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m_run, l_run};
