@@ -435,8 +435,8 @@ struct PagesAttnArgs {
     uint32_t* status;
 };
 
-// Whether the attention of many rows keeps pages in LDS as they are on their way (it then has the CU to itself): by the queries' pieces and the
-// pages' type.
+// Whether the attention of many rows keeps 8-bit pages in LDS as they are on their way, and then has the CU to itself also with four
+// wavefronts: by the queries' pieces.
 __host__ __device__ constexpr bool pages_raw(int pieces, bool e4m3) { return pieces > 1 && e4m3; }
 constexpr int PAGES_GROUP_ROWS = 128;   // rows (tokens x query heads of a KV head) that share a list of pages
 

@@ -1026,18 +1026,21 @@ __device__ __forceinline__ void wait_loads(int n) {
 // they become bf16 numbers with their scales in, which is exact.  So a page is read, and converted, once for up to 256 rows.
 // bf16 queries: the weights are rounded to one bf16 piece here (2^-8 of each at most, at random, next to the output's own rounding):
 // this kernel is bound by the matrix units, and a second piece is half as many products again in the second product.
-// Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (pages_raw) go to LDS as they
+// Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (DEEP) go to LDS as they
 // are, two stages ahead, and become bf16 a stage ahead of their use.
-template <int D, bool E4M3, int NQ>
+// PIPE (five tiles and more, one piece): the workgroup has the CU to itself, three buffers, and a wavefront computes the next tile's scores while it
+// takes the present one's exponentials, product by product: left to themselves the two wavefronts of a SIMD, which every page's barrier
+// sets off together, use the matrix unit together and then wait for it together.
+template <int D, bool E4M3, int NQ, bool PIPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 pages_attend_shared_kernel(PagesAttnArgs a) {
     using T = Tile<32>;
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
-    constexpr bool DEEP = pages_raw(NQ, E4M3);
+    constexpr bool DEEP = E4M3 && (NQ > 1 || PIPE);
     constexpr int RAW = DEEP ? 3 : 0;
     constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
-    __shared__ __align__(16) uint4 stage[2][2][HALF];   // [buffer][keys, values]
+    __shared__ __align__(16) uint4 stage[PIPE ? 3 : 2][2][HALF];   // [buffer][keys, values]
     __shared__ __align__(16) uint4 raw[RAW ? RAW : 1][RAW ? HALF + 8 : 1];   // [buffer]: keys, values, scales in 8 bits
     __shared__ long long lds[8];
     __shared__ Walk walk;
@@ -1211,6 +1214,138 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                 }
             };
 
+            // Values of page j that some row of the block does not see, for all wavefronts: 0 behind what any row sees, and where they are not finite.
+            // Whether there were any of these.
+            auto clean = [&](int j, int buf) -> bool {
+                const int page0 = scalar(pg_base[j]);
+                if (page0 + 64 <= begins) return false;
+#pragma unroll 1
+                for (int i = tid; i < HALF; i += blockDim.x) {
+                    const int pos = page0 + i / (QS * 64) * 32;
+                    const uint4 v = stage[buf][1][i];
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    bool change = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool behind = pos + value_key((i >> 6) & 1, (i >> 5) & 1, e) >= ends, not_finite = ((w[e / 2] >> (16 * (e & 1))) & 0x7F80u) == 0x7F80u;
+                        if (behind || not_finite) w[e / 2] &= ~(0xFFFFu << (16 * (e & 1))), change = true;
+                        if (!behind && not_finite) pg_odd = j;
+                    }
+                    if (change) stage[buf][1][i] = uint4{w[0], w[1], w[2], w[3]};
+                }
+                __syncthreads();
+                return pg_odd == j;
+            };
+            auto add_odd = [&](int j, int base) {
+                add_not_finite<D, E4M3, 32>(o, (const char*)a.c.v + ((size_t)pg_id[j] * heads + h) * 64 * D * (E4M3 ? 1 : 2), base, lane, sees, min(most, base + 32));
+            };
+
+            if constexpr (PIPE) {
+                uint4 kf[QS], vf[QS];
+                f32x16_t x;
+                auto load_keys = [&](int buf, int kt) {
+#pragma unroll
+                    for (int s = 0; s < QS; ++s) kf[s] = stage[buf][0][(kt * QS + s) * 64 + lane];
+                };
+                auto mask = [&](int base) {
+                    if (base + 32 > least)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (base + value_key(i >> 3, hf, i & 7) >= sees) x[i] = -INFINITY;
+                };
+                // A tile whose scores are in x, and the scores of the next one, whose keys are in (nbuf, nkt), into x.
+                auto body = [&](int buf, int kt, int nbuf, int nkt) {
+                    load_keys(nbuf, nkt);
+                    float top = x[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+                    rescale(T::across(top, [](float u, float w) { return fmaxf(u, w); }) * a.scale_log2, &m_run, &l_run, o);
+                    const float ref = m_run == -INFINITY ? 0.0f : m_run;
+#pragma unroll
+                    for (int s = 0; s < QS; ++s) vf[s] = stage[buf][1][(kt * QS + s) * 64 + lane];
+                    __builtin_amdgcn_sched_barrier(0);
+                    f32x16_t y;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < QS; ++s) y = T::mfma(kf[s], q[0][s], y);
+                    float sum = 0.0f;
+                    uint4 pf[2];
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float u = weight(x[s * 8 + 2 * i], a.scale_log2, ref), v = weight(x[s * 8 + 2 * i + 1], a.scale_log2, ref);
+                            sum += u;
+                            sum += v;
+                            w[i] = pack_bf16x2(u, v);
+                        }
+                        pf[s] = uint4{w[0], w[1], w[2], w[3]};
+                    }
+                    l_run += sum;
+#pragma unroll
+                    for (int i = 0; i < QS; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // one product,
+                        __builtin_amdgcn_sched_group_barrier(0x002, 40 / QS, 0);   // its share of the other instructions
+                        __builtin_amdgcn_sched_group_barrier(0x400, 16 / QS, 0);   // and of the exponentials
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[dt] = T::mfma(vf[dt * 2 + s], pf[s], o[dt]);
+                    x = y;
+                };
+                if (n > 0) {
+                    if constexpr (E4M3) {
+                        for (int i = 0; i < min(n, 3); ++i) fetch(i, i);
+                        wait_loads(n > 2 ? mine : 0);   // the first two are there
+                        __syncthreads();
+                        put_raw(0, 0);
+                    } else {
+                        fetch(0, 0);
+                        stage_wait<0>();
+                    }
+                    __syncthreads();
+                    bool odd = clean(0, 0);
+                    if (!E4M3 && n > 1) fetch(1, 1);
+                    int buf = 0, page0 = scalar(pg_base[0]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+                    load_keys(0, 0);
+#pragma unroll
+                    for (int s = 0; s < QS; ++s) x = T::mfma(kf[s], q[0][s], x);
+                    mask(page0);
+#pragma unroll 1
+                    for (int j = 0; j < n; ++j) {
+                        body(buf, 0, buf, 1);
+                        mask(page0 + 32);
+                        if (odd) add_odd(j, page0);
+                        bool odd_next = false;
+                        const int nbuf = buf == 2 ? 0 : buf + 1;
+                        if (j + 1 < n) {   // the next page is there, for all, and the one before this is not read any more
+                            if constexpr (E4M3) put_raw(nbuf, nbuf);   // page j + 1 is in place (j + 1) % 3 of both
+                            stage_wait<0>();
+                            __syncthreads();
+                            odd_next = clean(j + 1, nbuf);
+                            if constexpr (E4M3) {
+                                if (j + 3 < n) fetch(j + 3, buf);
+                            } else {
+                                if (j + 2 < n) fetch(j + 2, nbuf == 2 ? 0 : nbuf + 1);
+                            }
+                        }
+                        body(buf, 1, j + 1 < n ? nbuf : buf, 0);   // behind the last page: scores that nobody takes
+                        if (odd) add_odd(j, page0 + 32);
+                        odd = odd_next, buf = nbuf;
+                        if (j + 1 < n) page0 = scalar(pg_base[j + 1]);
+                        mask(page0);
+                    }
+                }
+                __syncthreads();
+                continue;
+            }
+
             if (n > 0) {
                 if constexpr (DEEP) {
                     for (int i = 0; i < min(n, 3); ++i) fetch(i, i);
@@ -1236,25 +1371,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     else fetch(j + 1, buf ^ 1);
                 }
                 const int page0 = __builtin_amdgcn_readfirstlane(pg_base[j]);
-                bool odd = false;
-                if (page0 + 64 > begins) {   // some row does not see the whole page: its values, for all wavefronts
-#pragma unroll 1
-                    for (int i = tid; i < HALF; i += blockDim.x) {
-                        const int pos = page0 + i / (QS * 64) * 32;
-                        const uint4 v = stage[buf][1][i];
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                        bool change = false;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool behind = pos + value_key((i >> 6) & 1, (i >> 5) & 1, e) >= ends, not_finite = ((w[e / 2] >> (16 * (e & 1))) & 0x7F80u) == 0x7F80u;
-                            if (behind || not_finite) w[e / 2] &= ~(0xFFFFu << (16 * (e & 1))), change = true;
-                            if (!behind && not_finite) pg_odd = j;
-                        }
-                        if (change) stage[buf][1][i] = uint4{w[0], w[1], w[2], w[3]};
-                    }
-                    __syncthreads();
-                    odd = pg_odd == j;
-                }
+                const bool odd = clean(j, buf);
                 // A tile's keys and values are requested from LDS several at once, well before they are multiplied: one by one each product would wait
                 // out the latency of its own.  Queries of one piece over bf16 pages leave registers for all of a tile's, and the next tile's keys.
                 constexpr bool AHEAD = NQ == 1 && !E4M3;
@@ -1325,8 +1442,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                         }
                         if (!AHEAD && s == 0) load_values(1);
                     }
-                    if (odd)
-                        add_not_finite<D, E4M3, 32>(o, (const char*)a.c.v + ((size_t)pg_id[j] * heads + h) * 64 * D * (E4M3 ? 1 : 2), base, lane, sees, min(most, base + 32));
+                    if (odd) add_odd(j, base);
                 }
                 if constexpr (E4M3)
                     if (j + 1 < n) {
@@ -1652,7 +1768,8 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         constexpr bool E = decltype(e)::value;
         auto run = [&](auto nq) {
             constexpr int NQ = decltype(nq)::value;
-            if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
+            if (a.shared_waves && a.row_tiles > 4 && NQ == 1) pages_attend_shared_kernel<D, E, NQ, NQ == 1><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
+            else if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ, false><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
             else if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
             else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
         };
