@@ -1028,16 +1028,19 @@ __device__ __forceinline__ void wait_loads(int n) {
 // this kernel is bound by the matrix units, and a second piece is half as many products again in the second product.
 // Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (DEEP) go to LDS as they
 // are, two stages ahead, and become bf16 a stage ahead of their use.
-// PIPE (five tiles and more, one piece): the workgroup has the CU to itself, three buffers, and a wavefront computes the next tile's scores while it
-// takes the present one's exponentials, product by product: left to themselves the two wavefronts of a SIMD, which every page's barrier
-// sets off together, use the matrix unit together and then wait for it together.
+// PIPE (five tiles and more, bf16 queries and pages): the workgroup has the CU to itself, three buffers, and a wavefront computes the next tile's
+// scores while it takes the present one's exponentials, product by product: left to themselves the two wavefronts of a SIMD, which every
+// page's barrier sets off together, use the matrix unit together and then wait for it together.  4 x up to 2048 rows over 512 to 8192 positions, 32
+// query heads: 816 us, 857 without, 0.86 PFLOP/s of the 1.29 that a large product reaches; the matrix units are busy 37% of the time (at 1.94
+// GHz), a third of a wavefront's time is waits for LDS and barriers.  With 8-bit pages it took 179 us where the plain order takes 169.
 template <int D, bool E4M3, int NQ, bool PIPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 pages_attend_shared_kernel(PagesAttnArgs a) {
     using T = Tile<32>;
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
-    constexpr bool DEEP = E4M3 && (NQ > 1 || PIPE);
+    static_assert(!(PIPE && E4M3), "of bf16 pages");
+    constexpr bool DEEP = pages_raw(NQ, E4M3);
     constexpr int RAW = DEEP ? 3 : 0;
     constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
     __shared__ __align__(16) uint4 stage[PIPE ? 3 : 2][2][HALF];   // [buffer][keys, values]
@@ -1298,18 +1301,11 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     x = y;
                 };
                 if (n > 0) {
-                    if constexpr (E4M3) {
-                        for (int i = 0; i < min(n, 3); ++i) fetch(i, i);
-                        wait_loads(n > 2 ? mine : 0);   // the first two are there
-                        __syncthreads();
-                        put_raw(0, 0);
-                    } else {
-                        fetch(0, 0);
-                        stage_wait<0>();
-                    }
+                    fetch(0, 0);
+                    stage_wait<0>();
                     __syncthreads();
                     bool odd = clean(0, 0);
-                    if (!E4M3 && n > 1) fetch(1, 1);
+                    if (n > 1) fetch(1, 1);
                     int buf = 0, page0 = scalar(pg_base[0]);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = 0.0f;
@@ -1325,15 +1321,10 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                         bool odd_next = false;
                         const int nbuf = buf == 2 ? 0 : buf + 1;
                         if (j + 1 < n) {   // the next page is there, for all, and the one before this is not read any more
-                            if constexpr (E4M3) put_raw(nbuf, nbuf);   // page j + 1 is in place (j + 1) % 3 of both
                             stage_wait<0>();
                             __syncthreads();
                             odd_next = clean(j + 1, nbuf);
-                            if constexpr (E4M3) {
-                                if (j + 3 < n) fetch(j + 3, buf);
-                            } else {
-                                if (j + 2 < n) fetch(j + 2, nbuf == 2 ? 0 : nbuf + 1);
-                            }
+                            if (j + 2 < n) fetch(j + 2, nbuf == 2 ? 0 : nbuf + 1);
                         }
                         body(buf, 1, j + 1 < n ? nbuf : buf, 0);   // behind the last page: scores that nobody takes
                         if (odd) add_odd(j, page0 + 32);
@@ -1768,7 +1759,7 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         constexpr bool E = decltype(e)::value;
         auto run = [&](auto nq) {
             constexpr int NQ = decltype(nq)::value;
-            if (a.shared_waves && a.row_tiles > 4 && NQ == 1) pages_attend_shared_kernel<D, E, NQ, NQ == 1><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
+            if (a.shared_waves && a.row_tiles > 4 && NQ == 1 && !E) pages_attend_shared_kernel<D, E, NQ, NQ == 1 && !E><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
             else if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ, false><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
             else if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
             else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
