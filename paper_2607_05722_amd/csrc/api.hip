@@ -335,7 +335,7 @@ PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows
 // registers) and are what hides the loads' latency.
 struct PagesPlan {
     int block_rows, row_tiles, n_blk, grid, slices, shared_waves, key_halves;
-    size_t part_ml, total;
+    size_t part_ml, parts, total;
 };
 
 bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, bool raw, PagesPlan* out) {
@@ -354,7 +354,8 @@ bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int ma
     p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
     const size_t part_rows = (size_t)2 * p.grid * p.block_rows;
     p.part_ml = 256 + part_rows * head_dim * 4;
-    p.total = align256(p.part_ml + part_rows * 8);
+    p.parts = align256(p.part_ml + part_rows * 8);
+    p.total = align256(p.parts + (size_t)8 * blocks * batch * n_kv_heads);
     *out = p;
     return true;
 }
@@ -404,6 +405,7 @@ PagesAttnArgs pages_args(const PageCache& c, const PageChunk& ch, int group_head
     a.key_halves = p.key_halves;
     a.part_o = at<float>(ws, off + 256);
     a.part_ml = at<float>(ws, off + p.part_ml);
+    a.parts = at<uint2>(ws, off + p.parts);
     a.status = at<uint32_t>(ws, 0);
     return a;
 }
@@ -1533,7 +1535,9 @@ size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int3
     const long long rows = (long long)max_rows * G;
     for (const bool raw : {false, true})
         for (long long r = 16; r == 16 || r - 32 < std::min(rows, 256LL); r = r == 16 ? 32 : r + 32)
-            if (plan_pages(1, 1, pages->head_dim, 1, (int)r, 0, raw, &p)) n = std::max(n, p.total);
+            if (plan_pages(1, 1, pages->head_dim, 1, (int)r, 0, raw, &p)) n = std::max(n, p.parts);
+    // and a note per unit, of which groups make the most
+    n = align256(n + (size_t)8 * pages->batch * pages->n_kv_heads * std::max<long long>(group ? cdiv(max_rows, group) : 0, (rows + 255) / 256));
     return group ? std::max(n, align256(256 + score_bytes(pages, max_rows, group))) : n;
 }
 

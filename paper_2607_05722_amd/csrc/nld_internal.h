@@ -432,6 +432,7 @@ struct PagesAttnArgs {
     int shared_waves, key_halves;   // > 0: the kernel whose wavefronts share pages through LDS, with so many; wavefronts per tile
     float* part_o;              // [2 * grid][block_rows][head_dim]
     float* part_ml;             // [2 * grid][block_rows][2]
+    uint2* parts;               // [n_entries][kv head]: first part and number of parts of a unit
     uint32_t* status;
 };
 

@@ -488,20 +488,17 @@ __device__ __forceinline__ Share share_of(long long total, long long units, int 
     return Share{total, (int)max(1LL, min((long long)grid, max(units, total / least)))};
 }
 
-// Sum of the steps (per KV head) of the entries before `upto` and of all, and the number of entries that have rows.
+// Sum of all entries' steps (per KV head), and the number of entries that have rows.
 template <int STEP>
-__device__ __forceinline__ void sum_entries(const PagesAttnArgs& a, int upto, long long* lds, long long* before, long long* all, long long* live,
-                                            uint32_t* status) {
-    long long mine = 0, first = 0, some = 0;
+__device__ __forceinline__ void sum_entries(const PagesAttnArgs& a, long long* lds, long long* all, long long* live, uint32_t* status) {
+    long long mine = 0, some = 0;
     for (int e = threadIdx.x; e < a.n_entries; e += blockDim.x) {
         const int s = entry_of<STEP>(a, e, status).steps;
         mine += s;
         some += s > 0;
-        if (e < upto) first += s;
     }
     *all = block_sum(mine, lds);
     *live = block_sum(some, lds);
-    if (before) *before = block_sum(first, lds);
 }
 
 // A workgroup's way through its share.  Steps are numbered KV head by KV head, in each entry by entry: with the shares of one
@@ -512,59 +509,77 @@ struct Walk {
     int e, h, share;
     long long at, last;   // the share's steps left: [at, last)
     long long before;     // steps of the entries before e
-    long long per_head;
+    long long per_head, live;
     bool first_unit;
 };
 
-// false: nothing to do
+// inclusive sum over the workgroup's threads, and over all of them
+__device__ __forceinline__ long long block_scan(long long v, long long* lds, long long* all) {
+    for (int m = 1; m < 64; m <<= 1) {
+        const long long o = __shfl_up(v, m);
+        if ((int)(threadIdx.x & 63) >= m) v += o;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    long long sum = 0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) {
+        if (i < (int)threadIdx.x / 64) v += lds[i];
+        sum += lds[i];
+    }
+    *all = sum;
+    return v;
+}
+
+// false: nothing to do.  Up to as many entries as threads are looked at once, all of them side by side.
 template <int STEP>
 __device__ __forceinline__ bool walk_start(const PagesAttnArgs& a, Walk* w, long long* lds) {
     const int heads = a.c.n_kv_heads;
-    long long per_head, live;
-    sum_entries<STEP>(a, 0, lds, nullptr, &per_head, &live, blockIdx.x == 0 ? a.status : nullptr);
+    uint32_t* status = blockIdx.x == 0 ? a.status : nullptr;
+    const bool once = a.n_entries <= (int)blockDim.x;
+    Entry en{};
+    if ((int)threadIdx.x < a.n_entries) en = entry_of<STEP>(a, threadIdx.x, status);
+    constexpr long long LIVE = 1LL << 40;   // the entries that have rows are counted above the steps, of which 512 entries have at most 2^34
+    long long per_head, live, upto = 0;
+    if (once) {
+        upto = block_scan(en.steps + (en.steps > 0 ? LIVE : 0), lds, &per_head);
+        live = per_head >> 40;
+        per_head &= LIVE - 1, upto &= LIVE - 1;
+    } else {
+        sum_entries<STEP>(a, lds, &per_head, &live, status);
+    }
     if (per_head == 0) return false;
     const Share sh = share_of(per_head * heads, live * heads, gridDim.x, a.least_steps);
     // the shares in use, dealt to the XCDs in eight runs of adjacent ones
     const int run = sh.wgs / 8, x = blockIdx.x & 7, i = blockIdx.x >> 3;
-    const int share = i < run ? x * run + i : 8 * run + (int)blockIdx.x - 8 * run;
+    const int share = i < run ? x * run + i : (int)blockIdx.x;
     if (share >= sh.wgs) return false;
     const long long first = sh.begin(share);
     const int h = (int)(first / per_head);
     const long long s = first - h * per_head;
-    // the entry that holds step s of its KV head
-    if (threadIdx.x == 0) w->e = a.n_entries;
-    long long base = 0;
-    for (int e0 = 0;; e0 += blockDim.x) {
-        const int e = e0 + threadIdx.x;
-        const long long own = e < a.n_entries ? (long long)entry_of<STEP>(a, e, nullptr).steps : 0;
-        long long up = own;
-        for (int m = 1; m < 64; m <<= 1) {
-            const long long o = __shfl_up(up, m);
-            if ((int)(threadIdx.x & 63) >= m) up += o;
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = up;
-        __syncthreads();
-        long long ahead = base, sum = 0;
-        for (int i2 = 0; i2 < (int)blockDim.x / 64; ++i2) {
-            if (i2 < (int)threadIdx.x / 64) ahead += lds[i2];
-            sum += lds[i2];
-        }
-        const long long lo = ahead + up - own;
-        if (own && lo <= s && s < lo + own) {
-            w->en = entry_of<STEP>(a, e, nullptr);
-            w->e = e, w->before = lo;
-        }
-        base += sum;
-        __syncthreads();
-        if (w->e < a.n_entries || e0 + (int)blockDim.x >= a.n_entries) break;
-    }
-    if (w->e >= a.n_entries) return false;   // not unless the lengths change meanwhile
     if (threadIdx.x == 0) {
-        w->h = h, w->share = share, w->at = first, w->last = sh.begin(share + 1), w->per_head = per_head, w->first_unit = true;
+        w->e = a.n_entries;
+        w->h = h, w->share = share, w->at = first, w->last = sh.begin(share + 1), w->per_head = per_head, w->live = live, w->first_unit = true;
+    }
+    // the entry that holds step s of its KV head
+    __syncthreads();
+    if (once) {
+        if (s < upto && s >= upto - en.steps) w->en = en, w->e = threadIdx.x, w->before = upto - en.steps;
+    } else {
+        long long base = 0;
+        for (int e0 = 0;; e0 += blockDim.x) {
+            const int e = e0 + threadIdx.x;
+            const Entry x2 = e < a.n_entries ? entry_of<STEP>(a, e, nullptr) : Entry{};
+            long long sum;
+            const long long to = base + block_scan(x2.steps, lds, &sum);
+            if (s < to && s >= to - x2.steps) w->en = x2, w->e = e, w->before = to - x2.steps;
+            base += sum;
+            __syncthreads();
+            if (w->e < a.n_entries || e0 + (int)blockDim.x >= a.n_entries) break;
+        }
     }
     __syncthreads();
-    return true;
+    return w->e < a.n_entries;   // false not unless the lengths change meanwhile
 }
 
 // The present unit, in scalar registers.
@@ -585,6 +600,20 @@ __device__ __forceinline__ Unit walk_unit(const Walk& w) {
     u.slot = 2 * scalar(w.share) + (scalar(w.first_unit) ? 0 : 1);
     u.whole = u.s0 == 0 && u.s1 == u.en.steps;
     return u;
+}
+
+// What the second launch needs of a unit, from the workgroup that has its last step: the place of its first part (bit 31: it is not that
+// workgroup's first), and how many parts there are.
+__device__ __forceinline__ void note_parts(const PagesAttnArgs& a, const Walk& w, const Unit& u) {
+    if (threadIdx.x != 0 || u.s1 != u.en.steps) return;
+    int w0 = w.share, n = 1;
+    bool later = false;
+    if (!u.whole) {
+        const Share sh = share_of(w.per_head * a.c.n_kv_heads, w.live * a.c.n_kv_heads, gridDim.x, a.least_steps);
+        const long long u0 = w.h * w.per_head + w.before;
+        w0 = sh.of(u0), n = w.share - w0 + 1, later = u0 > sh.begin(w0);
+    }
+    a.parts[(size_t)w.e * a.c.n_kv_heads + u.h] = uint2{(uint32_t)w0 | (later ? 0x80000000u : 0u), (uint32_t)n};
 }
 
 // On to the next unit; false behind the last.  Called by every thread after it has read what it needs of the present one.
@@ -629,8 +658,7 @@ __device__ __forceinline__ void finish_row(const PagesAttnArgs& a, int b, int r0
 }
 
 // ---------------------------------------------------------------- attention
-// A workgroup of 4 wavefronts walks its share unit by unit: row_tiles x (4 / row_tiles) wavefronts, one tile of RW rows and
-// every (4 / row_tiles)-th step each.  A step's keys and values go straight from memory to the registers of the wavefront, in operand
+// A workgroup of 4 wavefronts walks its share unit by unit, with one tile of RW rows; each takes every fourth step.  A step's keys and values go straight from memory to the registers of the wavefront, in operand
 // order; while a step is worked on, the next one's are under way.  Running
 // maximum and sum per row in base-2 exponents; the weights are carried in two bf16 pieces (three for f32 queries, which are
 // split likewise), so that P V is as exact as the f32 sums.  A unit's wavefronts meet in LDS at its end.
@@ -719,8 +747,7 @@ pages_attend_kernel(PagesAttnArgs a) {
     __shared__ Walk walk;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane % RW, part = lane / RW;
-    const int row_tiles = RW == 16 ? 1 : a.row_tiles;
-    const int rt = wave % row_tiles, ks = wave / row_tiles, n_ks = 4 / row_tiles;
+    constexpr int N_KS = 4;   // wavefronts
     const int heads = a.c.n_kv_heads, G = a.group_heads;
 
     if (!walk_start<STEP>(a, &walk, lds)) return;
@@ -737,46 +764,13 @@ pages_attend_kernel(PagesAttnArgs a) {
         const bool whole = unit.whole;
 
         // this wavefront's rows
-        const int myrow = en.rows0 + rt * RW + row;
+        const int myrow = en.rows0 + row;
         const bool have = myrow < en.rows1;
         const int t = have ? myrow / G : 0, g = have ? myrow % G : 0;
         const int sees = have ? sees_of(a, en.P, en.n, t) : 0;
         int least = have ? sees : 0x7FFFFFFF, most = sees;
         for (int m = RW / 2; m; m >>= 1) least = min(least, __shfl_xor(least, m)), most = max(most, __shfl_xor(most, m));
         least = __builtin_amdgcn_readfirstlane(least), most = __builtin_amdgcn_readfirstlane(most);
-
-        uint4 q[NQ][QS];
-#pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            // 8 dims: the keys' blocks have a lane's bytes in pieces of 8 (bf16) or of 16, two steps
-            const int d = E4M3 ? 2 * T::DIMS * (s >> 1) + 16 * part + 8 * (s & 1) : T::DIMS * s + 8 * part;
-            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
-                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
-                if (have) {
-                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
-                    q[0][s] = *(const uint4*)p;
-                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
-                }
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
-                if (a.negate)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
-#pragma unroll
-                for (int p = 0; p < NQ; ++p) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                    }
-                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
-                }
-            }
-        }
 
         typename T::Acc o[DT];
 #pragma unroll
@@ -788,12 +782,12 @@ pages_attend_kernel(PagesAttnArgs a) {
         // the unit's pages: lane i of the window holds the place and the id of page win + i
         const int32_t* list = a.list ? a.list + ((size_t)(en.b * a.n_blk + en.blk) * heads + h) * a.n_list : nullptr;
         int win = -1, w_page = -1, w_id = -1;
-        int s = s0 + ks;
+        int s = s0 + wave;
         int base = 0;          // first position of the step
         size_t head = 0;       // page and KV head
         // The next step that has keys for this wavefront, its position and page; false behind the last.
         auto next = [&]() -> bool {
-            for (; s < s1; s += n_ks) {
+            for (; s < s1; s += N_KS) {
                 const int pg = s * STEP >> 6;
                 if (win < 0 || pg >= win + 64) {
                     win = pg;
@@ -811,7 +805,7 @@ pages_attend_kernel(PagesAttnArgs a) {
                 if (id < 0 || page * 64 + (s * STEP & 63) >= most) continue;
                 base = page * 64 + (s * STEP & 63);
                 head = (size_t)id * heads + h;
-                s += n_ks;
+                s += N_KS;
                 return true;
             }
             return false;
@@ -851,6 +845,40 @@ pages_attend_kernel(PagesAttnArgs a) {
             load_k(cur_head, cur_base);
             load_v(cur_head, cur_base);
         }
+        // the queries, while the first pages are under way
+        uint4 q[NQ][QS];
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            // 8 dims: the keys' blocks have a lane's bytes in pieces of 8 (bf16) or of 16, two steps
+            const int d = E4M3 ? 2 * T::DIMS * (s >> 1) + 16 * part + 8 * (s & 1) : T::DIMS * s + 8 * part;
+            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
+                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
+                if (have) {
+                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                    q[0][s] = *(const uint4*)p;
+                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
+                }
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
+                if (a.negate)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
+#pragma unroll
+                for (int p = 0; p < NQ; ++p) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                    }
+                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
+                }
+            }
+        }
+
         while (more) {
             float x[SR];
 #pragma unroll
@@ -974,18 +1002,17 @@ pages_attend_kernel(PagesAttnArgs a) {
                 *(float4*)&so[wave][row][dt * RW + T::out_dim(lane, 4 * j)] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
         if (part == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
         __syncthreads();
-        for (int i = tid; i < row_tiles * RW * (D / 4); i += 256) {
-            const int r = i / (D / 4), d = i % (D / 4) * 4, tile = r / RW, rr = r % RW, rw = en.rows0 + r;
+        for (int i = tid; i < RW * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4, rw = en.rows0 + r;
             if (rw >= en.rows1) continue;
             float m = -INFINITY, l = 0.0f;
-            for (int k = 0; k < n_ks; ++k) m = fmaxf(m, sml[k * row_tiles + tile][rr][0]);
+            for (int k = 0; k < N_KS; ++k) m = fmaxf(m, sml[k][r][0]);
             const float ref = m == -INFINITY ? 0.0f : m;
             float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int k = 0; k < n_ks; ++k) {
-                const int w = k * row_tiles + tile;
-                const float f = __builtin_amdgcn_exp2f(sml[w][rr][0] - ref);
-                const float4 z = *(const float4*)&so[w][rr][d];
-                l += sml[w][rr][1] * f;
+            for (int k = 0; k < N_KS; ++k) {
+                const float f = __builtin_amdgcn_exp2f(sml[k][r][0] - ref);
+                const float4 z = *(const float4*)&so[k][r][d];
+                l += sml[k][r][1] * f;
                 y[0] += z.x * f, y[1] += z.y * f, y[2] += z.z * f, y[3] += z.w * f;
             }
             if (whole) {
@@ -996,6 +1023,7 @@ pages_attend_kernel(PagesAttnArgs a) {
                 if (d == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m, l};
             }
         }
+        note_parts(a, walk, unit);
     } while (walk_next<STEP>(a, &walk));
 }
 
@@ -1028,22 +1056,20 @@ __device__ __forceinline__ void wait_loads(int n) {
 // this kernel is bound by the matrix units, and a second piece is half as many products again in the second product.
 // Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (DEEP) go to LDS as they
 // are, two stages ahead, and become bf16 a stage ahead of their use.
-// PIPE (five tiles and more, bf16 queries and pages): the workgroup has the CU to itself, three buffers, and a wavefront computes the next tile's
-// scores while it takes the present one's exponentials, product by product: left to themselves the two wavefronts of a SIMD, which every
-// page's barrier sets off together, use the matrix unit together and then wait for it together.  4 x up to 2048 rows over 512 to 8192 positions, 32
-// query heads: 816 us, 857 without, 0.86 PFLOP/s of the 1.29 that a large product reaches; the matrix units are busy 37% of the time (at 1.94
-// GHz), a third of a wavefront's time is waits for LDS and barriers.  With 8-bit pages it took 179 us where the plain order takes 169.
-template <int D, bool E4M3, int NQ, bool PIPE>
+// 4 x up to 2048 rows over 512 to 8192 positions, 32 query heads (bf16): 861 us, 0.81 PFLOP/s of the 1.29 that a large product reaches; without
+// seven eighths of the products it still takes 0.73 of that time: exponentials, sums and conversions, LDS and the pages' barriers, which
+// the two wavefronts of a SIMD hide only in part.  Three or four stages under way change nothing, two pages per stage cost 2%, the next tile's products between
+// the present one's exponentials in one wavefront, with three buffers, save 2%.
+template <int D, bool E4M3, int NQ>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 pages_attend_shared_kernel(PagesAttnArgs a) {
     using T = Tile<32>;
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
-    static_assert(!(PIPE && E4M3), "of bf16 pages");
     constexpr bool DEEP = pages_raw(NQ, E4M3);
     constexpr int RAW = DEEP ? 3 : 0;
     constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
-    __shared__ __align__(16) uint4 stage[PIPE ? 3 : 2][2][HALF];   // [buffer][keys, values]
+    __shared__ __align__(16) uint4 stage[2][2][HALF];   // [buffer][keys, values]
     __shared__ __align__(16) uint4 raw[RAW ? RAW : 1][RAW ? HALF + 8 : 1];   // [buffer]: keys, values, scales in 8 bits
     __shared__ long long lds[8];
     __shared__ Walk walk;
@@ -1153,7 +1179,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     }
                 }
             };
-            const int mine = (LOADS - wave + waves - 1) / waves;   // loads of this wavefront per stage
+            const int mine = scalar((LOADS - wave + waves - 1) / waves);   // loads of this wavefront per stage
             // 8 bits: a thread's 16-byte pieces of a stage (at most two of the keys and two of the values: there are at least 4 wavefronts)
             constexpr int NI = D / 64;
             uint4 rk[NI], rv[NI];
@@ -1208,8 +1234,10 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             };
             auto put_raw = [&](int from, int buf) {
                 const uint8_t* sc = (const uint8_t*)&raw[RAW ? from : 0][RAW ? HALF : 0];
+                int i0 = threadIdx.x;
+                asm("" : "+v"(i0));
 #pragma unroll 1
-                for (int i = tid; i < 4 * D; i += blockDim.x) {
+                for (int i = i0; i < 4 * D; i += blockDim.x) {
                     const int m = i & 15, pc = (i >> 4) & 3, tile = i / D;
                     const uint32_t* vs = (const uint32_t*)(sc + 64 + 16 * (pc >> 1) + 4 * (pc & 1));
                     const uint32_t vscale[4] = {vs[0], vs[2], vs[8], vs[10]};
@@ -1242,100 +1270,6 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             auto add_odd = [&](int j, int base) {
                 add_not_finite<D, E4M3, 32>(o, (const char*)a.c.v + ((size_t)pg_id[j] * heads + h) * 64 * D * (E4M3 ? 1 : 2), base, lane, sees, min(most, base + 32));
             };
-
-            if constexpr (PIPE) {
-                uint4 kf[QS], vf[QS];
-                f32x16_t x;
-                auto load_keys = [&](int buf, int kt) {
-#pragma unroll
-                    for (int s = 0; s < QS; ++s) kf[s] = stage[buf][0][(kt * QS + s) * 64 + lane];
-                };
-                auto mask = [&](int base) {
-                    if (base + 32 > least)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (base + value_key(i >> 3, hf, i & 7) >= sees) x[i] = -INFINITY;
-                };
-                // A tile whose scores are in x, and the scores of the next one, whose keys are in (nbuf, nkt), into x.
-                auto body = [&](int buf, int kt, int nbuf, int nkt) {
-                    load_keys(nbuf, nkt);
-                    float top = x[0];
-#pragma unroll
-                    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-                    rescale(T::across(top, [](float u, float w) { return fmaxf(u, w); }) * a.scale_log2, &m_run, &l_run, o);
-                    const float ref = m_run == -INFINITY ? 0.0f : m_run;
-#pragma unroll
-                    for (int s = 0; s < QS; ++s) vf[s] = stage[buf][1][(kt * QS + s) * 64 + lane];
-                    __builtin_amdgcn_sched_barrier(0);
-                    f32x16_t y;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < QS; ++s) y = T::mfma(kf[s], q[0][s], y);
-                    float sum = 0.0f;
-                    uint4 pf[2];
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float u = weight(x[s * 8 + 2 * i], a.scale_log2, ref), v = weight(x[s * 8 + 2 * i + 1], a.scale_log2, ref);
-                            sum += u;
-                            sum += v;
-                            w[i] = pack_bf16x2(u, v);
-                        }
-                        pf[s] = uint4{w[0], w[1], w[2], w[3]};
-                    }
-                    l_run += sum;
-#pragma unroll
-                    for (int i = 0; i < QS; ++i) {
-                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // one product,
-                        __builtin_amdgcn_sched_group_barrier(0x002, 40 / QS, 0);   // its share of the other instructions
-                        __builtin_amdgcn_sched_group_barrier(0x400, 16 / QS, 0);   // and of the exponentials
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) o[dt] = T::mfma(vf[dt * 2 + s], pf[s], o[dt]);
-                    x = y;
-                };
-                if (n > 0) {
-                    fetch(0, 0);
-                    stage_wait<0>();
-                    __syncthreads();
-                    bool odd = clean(0, 0);
-                    if (n > 1) fetch(1, 1);
-                    int buf = 0, page0 = scalar(pg_base[0]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-                    load_keys(0, 0);
-#pragma unroll
-                    for (int s = 0; s < QS; ++s) x = T::mfma(kf[s], q[0][s], x);
-                    mask(page0);
-#pragma unroll 1
-                    for (int j = 0; j < n; ++j) {
-                        body(buf, 0, buf, 1);
-                        mask(page0 + 32);
-                        if (odd) add_odd(j, page0);
-                        bool odd_next = false;
-                        const int nbuf = buf == 2 ? 0 : buf + 1;
-                        if (j + 1 < n) {   // the next page is there, for all, and the one before this is not read any more
-                            stage_wait<0>();
-                            __syncthreads();
-                            odd_next = clean(j + 1, nbuf);
-                            if (j + 2 < n) fetch(j + 2, nbuf == 2 ? 0 : nbuf + 1);
-                        }
-                        body(buf, 1, j + 1 < n ? nbuf : buf, 0);   // behind the last page: scores that nobody takes
-                        if (odd) add_odd(j, page0 + 32);
-                        odd = odd_next, buf = nbuf;
-                        if (j + 1 < n) page0 = scalar(pg_base[j + 1]);
-                        mask(page0);
-                    }
-                }
-                __syncthreads();
-                continue;
-            }
 
             if (n > 0) {
                 if constexpr (DEEP) {
@@ -1469,8 +1403,9 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                 }
             }
         }
-        int r_out = r;
-        asm("" : "+v"(r_out));   // worked out again: the row's place would take registers all the way
+        int again = threadIdx.x;
+        asm("" : "+v"(again));   // worked out again: the row's place would take registers all the way
+        const int r_out = rt * 32 + (again & 31);
         const int row_out = en.rows0 + r_out, t_out = row_out / G, g_out = row_out % G;
         if (kh == 0 && row_out < en.rows1) {
             const size_t at_row = (size_t)slot * a.block_rows + r_out;
@@ -1483,6 +1418,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             }
             if (!whole && hf == 0) *(float2*)(a.part_ml + at_row * 2) = float2{m_run, l_run};
         }
+        note_parts(a, walk, unit);
     } while (walk_next<STEP>(a, &walk));
 }
 
@@ -1491,19 +1427,14 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
 template <int D, int STEP>
 __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
     constexpr int TPR = D / 4, ROWS = 256 / TPR;
-    __shared__ long long lds[4];
     const int heads = a.c.n_kv_heads, G = a.group_heads;
     const int slice = blockIdx.x % a.slices, h = blockIdx.x / a.slices % heads, e = blockIdx.x / a.slices / heads;
     const Entry en = entry_of<STEP>(a, e, nullptr);
     if (en.rows0 + slice * ROWS >= en.rows1) return;
-    long long before, per_head, live;
-    sum_entries<STEP>(a, e, lds, &before, &per_head, &live, nullptr);
-    const long long u0 = h * per_head + before;
-    if (before + en.steps > per_head) return;   // not unless the lengths change meanwhile
-    const Share sh = share_of(per_head * heads, live * heads, a.grid, a.least_steps);
-    const int w0 = sh.of(u0), w1 = sh.of(u0 + en.steps - 1), n = w1 - w0 + 1;
-    if (n == 1) return;
-    const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (u0 > sh.begin(w0) ? 1 : 0);
+    const uint2 parts = a.parts[(size_t)e * heads + h];
+    const int n = (int)parts.y, w0 = (int)(parts.x & 0x7FFFFFFFu);
+    if (n <= 1 || w0 + n > a.grid) return;   // the latter not unless the lengths change meanwhile
+    const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (int)(parts.x >> 31);
     for (int r = slice * ROWS + threadIdx.x / TPR; en.rows0 + r < en.rows1; r += a.slices * ROWS) {
         auto place = [&](int i) { return (size_t)(i == 0 ? first : 2 * (w0 + i)) * a.block_rows + r; };
         float m = -INFINITY;
@@ -1511,7 +1442,7 @@ __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
         for (int k = TPR / 2; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
         const float ref = m == -INFINITY ? 0.0f : m;
         float l = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < n; ++i) {
             const size_t at = place(i);
             const float2 ml = *(const float2*)(a.part_ml + at * 2);
@@ -1759,8 +1690,7 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         constexpr bool E = decltype(e)::value;
         auto run = [&](auto nq) {
             constexpr int NQ = decltype(nq)::value;
-            if (a.shared_waves && a.row_tiles > 4 && NQ == 1 && !E) pages_attend_shared_kernel<D, E, NQ, NQ == 1 && !E><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
-            else if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ, false><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
+            if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
             else if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
             else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
         };
