@@ -497,7 +497,7 @@ nld_status validate_paged(const nld_model* m, const nld_pages* pages, const nld_
         p.n_groups = cdiv(k, p.group);
         p.n_list = nld_pages_list_len(k, p.group, p.n_top, p.n_first, mode);
         if (p.n_list < 1) return fail(NLD_ERR_INVALID_ARG, "n_top and n_first must be in [0, %d]", MAX_SEQ_PAGES);
-        if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
+        if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 128) > MAX_PAGE_WGS)
             return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     }
     if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, pages_raw(2, pages->dtype == NLD_E4M3), &p.plan))
@@ -1632,7 +1632,7 @@ nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chu
     if (need < 1) return fail(NLD_ERR_SHAPE, "n_top (%d) or n_first (%d) exceeds %d", n_top, n_first, MAX_SEQ_PAGES);
     if (n_list < need) return fail(NLD_ERR_INVALID_ARG, "n_list is %d, this call needs %d", n_list, need);
     const int n_groups = cdiv(chunk->max_rows, group);
-    if ((long long)pages->batch * n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 512) > MAX_PAGE_WGS)
+    if ((long long)pages->batch * n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 128) > MAX_PAGE_WGS)
         return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
     if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     const size_t bytes = align256(256 + (n_top ? score_bytes(pages, chunk->max_rows, group) : 0));

@@ -128,6 +128,19 @@ __device__ __forceinline__ void store4(const HeadRows& r, long long row, int hea
     }
 }
 
+__device__ __forceinline__ void store8(const HeadRows& r, long long row, int head, int d, uint4 s) {   // eight bf16 numbers
+    const uint32_t w[4] = {s.x, s.y, s.z, s.w};
+    if (!r.f32 && r.vec) {
+        *(uint4*)((uint16_t*)r.data + (size_t)(row * r.row_stride + head * r.head_stride + d)) = s;
+        return;
+    }
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    store4(r, row, head, d, x);
+    store4(r, row, head, d + 4, x + 4);
+}
+
 // ---------------------------------------------------------------- writing rows
 // One workgroup per page that a sequence's new rows touch, and KV head.  A thread takes 8 dims of a row: the keys go to
 // their place at once, the values through LDS, where a lane's 8 keys of one dim meet.  e4m3: the row's power of two is the
@@ -208,23 +221,32 @@ __global__ void __launch_bounds__(256) pages_write_kernel(PageCache c, KvSource 
     for (int e = 0; e < 8; ++e) lo[e] = INFINITY, hi[e] = -INFINITY;
     bool odd = false;   // a stored key that is not finite
 
-    for (int t = begin + tid / C;; t += TOK) {
-        const bool there = t < end;
-        if (__all(!there)) break;
-        float x[2][8];
-        float amax[2] = {0.0f, 0.0f};
+    // every row of this thread is requested before any is worked on
+    constexpr int TURNS = 64 / TOK;
+    float rows[TURNS][2][8];
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u)
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
+            const int t = u * TOK + tid / C;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[w][e] = 0.0f;
-            if (there) load_kv8<D>(src, w == 1, sr.r0 + (page * 64 + t - P), page * 64 + t - P, b, h, c.n_kv_heads, d0, x[w]);
-            if constexpr (E4M3) {
+            for (int e = 0; e < 8; ++e) rows[u][w][e] = 0.0f;
+            if (t >= begin && t < end) load_kv8<D>(src, w == 1, sr.r0 + (page * 64 + t - P), page * 64 + t - P, b, h, c.n_kv_heads, d0, rows[u][w]);
+        }
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) {
+        const int t = u * TOK + tid / C;
+        const bool there = t >= begin && t < end;
+        float (&x)[2][8] = rows[u];
+        float amax[2] = {0.0f, 0.0f};
+        if constexpr (E4M3)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) amax[w] = fmaxf(amax[w], finite(x[w][e]) ? fabsf(x[w][e]) : 0.0f);
 #pragma unroll
                 for (int m = 1; m < C; m <<= 1) amax[w] = fmaxf(amax[w], __shfl_xor(amax[w], m));
             }
-        }
         if (!there) continue;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
@@ -368,49 +390,58 @@ __global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k
     const Elem* vp = (const Elem*)c.v + head * 64 * D;
     const long long row0 = sr.r0 + (page * 64 - P);   // row of the page's first position
 
-    for (int at = tid; at < 64 * D / 8; at += 256) {
-        const int blk = at >> 6, kt = blk / (D / 16), d = blk % (D / 16) * 16 + (at & 15), s = (at >> 5) & 1, hf = (at >> 4) & 1;
+    // everything is requested before any of it is worked on
+    constexpr int PIECES = 64 * D / 8 / 256, TURNS = 64 / TOK;
+    uint4 vq[PIECES], kq[TURNS];
+    uint32_t vs[PIECES][2], ks[TURNS];
+#pragma unroll
+    for (int u = 0; u < PIECES; ++u) {
+        const int at = tid + u * 256, blk = at >> 6, kt = blk / (D / 16), d = blk % (D / 16) * 16 + (at & 15), s = (at >> 5) & 1, hf = (at >> 4) & 1;
         const int k0 = kt * 32 + value_key(s, hf, 0);
         if constexpr (E4M3) {
             const uint2 q = *(const uint2*)(vp + value_at<D, true>(k0, d));
-            const uint8_t* sc = c.scale + (head * 2 + 1) * 64 + k0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t w = ((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 0xFFu;
-                const uint32_t x = pair_bf16<false>(w, scale_of(sc[(e & 3) + ((e & 4) << 1)]));
-                vt[kt * 32 + value_key(s, hf, e)][d] = (uint16_t)x;
-            }
+            vq[u] = uint4{q.x, q.y, 0u, 0u};
+            const uint32_t* sc = (const uint32_t*)(c.scale + (head * 2 + 1) * 64 + k0);
+            vs[u][0] = sc[0], vs[u][1] = sc[2];
         } else {
-            const uint4 q = *(const uint4*)(vp + value_at<D, false>(k0, d));
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vt[kt * 32 + value_key(s, hf, e)][d] = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+            vq[u] = *(const uint4*)(vp + value_at<D, false>(k0, d));
         }
     }
-    for (int t = begin + tid / C; t < end; t += TOK) {
-        uint4 s;
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) {
+        const int t = u * TOK + tid / C;
+        if (t < begin || t >= end) continue;
         if constexpr (E4M3) {
             const uint2 q = *(const uint2*)(kp + key_at<D, true>(t, d0));
-            s = eight_bf16(q.x, q.y, scale_of(c.scale[head * 2 * 64 + t]));
+            kq[u] = uint4{q.x, q.y, 0u, 0u};
+            ks[u] = c.scale[head * 2 * 64 + t];
         } else {
-            s = *(const uint4*)(kp + key_at<D, false>(t, d0));
+            kq[u] = *(const uint4*)(kp + key_at<D, false>(t, d0));
         }
-        const uint32_t u[4] = {s.x, s.y, s.z, s.w};
-        float x[8];
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
-        store4(k, row0 + t, h, d0, x);
-        store4(k, row0 + t, h, d0 + 4, x + 4);
+    for (int u = 0; u < PIECES; ++u) {
+        const int at = tid + u * 256, blk = at >> 6, kt = blk / (D / 16), d = blk % (D / 16) * 16 + (at & 15), s = (at >> 5) & 1, hf = (at >> 4) & 1;
+        const uint32_t w[4] = {vq[u].x, vq[u].y, vq[u].z, vq[u].w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint32_t x;
+            if constexpr (E4M3) x = pair_bf16<false>((w[e / 4] >> (8 * (e & 3))) & 0xFFu, scale_of((vs[u][e / 4] >> (8 * (e & 3))) & 0xFFu));
+            else x = w[e / 2] >> (16 * (e & 1));
+            vt[kt * 32 + value_key(s, hf, e)][d] = (uint16_t)x;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) {
+        const int t = u * TOK + tid / C;
+        if (t < begin || t >= end) continue;
+        uint4 s = kq[u];
+        if constexpr (E4M3) s = eight_bf16(s.x, s.y, scale_of(ks[u]));
+        store8(k, row0 + t, h, d0, s);
     }
     __syncthreads();
     for (int t = begin + tid / C; t < end; t += TOK) {
-        const uint4 s = *(const uint4*)&vt[t][d0];
-        const uint32_t u[4] = {s.x, s.y, s.z, s.w};
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
-        store4(v, row0 + t, h, d0, x);
-        store4(v, row0 + t, h, d0 + 4, x + 4);
+        store8(v, row0 + t, h, d0, *(const uint4*)&vt[t][d0]);
     }
 }
 
@@ -1460,7 +1491,7 @@ __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
 // Scores in whole numbers: a query row is rounded to 8 bits by its largest magnitude over 127, the bounds of a page are 8-bit
 // too, and sum over the dims of max(qi * least, qi * largest), which no key of the page exceeds but for the rounding of q, is one matrix product of
 // [min(qi, 0), max(qi, 0)] with [least, largest].  Its 32-bit result is exact below 2^24, so which pages win does not hang on any order
-// of summation.  A workgroup takes a group's rows of one KV head (through LDS, as 8-bit operands) and 512 pages.
+// of summation.
 struct Group {
     int r0, n, P, t0, t1;   // tokens [t0, t1) of the sequence's
     int p0;                 // first page of its own: that of its first token's position
@@ -1482,31 +1513,28 @@ __device__ __forceinline__ Group group_of(const PagesSelectArgs& a, int b, int g
     return g;
 }
 
-constexpr int SCORE_PAGES = 512;   // pages per workgroup: 4 wavefronts of 32 at a time
+constexpr int SCORE_PAGES = 128;    // pages per workgroup of the scores alone: 4 wavefronts of 32
+constexpr int SELECT_PAGES = 4096;  // pages that one workgroup scores and picks from, with their scores in LDS
 
+// A group's rows of one KV head as 8-bit operands: 8 dims per thread, a row's threads adjacent.  Rows up to a multiple of 32.
 template <int D>
-__global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
-    constexpr int PITCH = 2 * D + 16, KS = 2 * D / 32;
-    __shared__ __align__(16) int8_t qi[PAGES_GROUP_ROWS][PITCH];
-    __shared__ float qs[PAGES_GROUP_ROWS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5, col = lane & 31;
-    const int chunk = blockIdx.x % a.chunks, unit = blockIdx.x / a.chunks, heads = a.c.n_kv_heads, G = a.group_heads;
-    const int h = unit % heads, grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
-    const Group g = group_of(a, b, grp, nullptr);
-    const int lo = max(a.n_first, chunk * SCORE_PAGES), hi = min(g.p0, chunk * SCORE_PAGES + SCORE_PAGES);
-    if (lo >= hi || g.p0 - a.n_first <= a.n_top) return;   // none, or all of them are taken
-
-    // rows of the group: 8 dims per thread, a row's threads adjacent
-    constexpr int C = D / 8, ROWS = 256 / C;
-    const int n = (g.t1 - g.t0) * G, n32 = (n + 31) / 32 * 32;
-    for (int r = tid / C; r < n32; r += ROWS) {
+struct GroupRows {
+    static constexpr int PITCH = 2 * D + 16;
+    int8_t qi[PAGES_GROUP_ROWS][PITCH];   // [min(q, 0), max(q, 0)]
+    float qs[PAGES_GROUP_ROWS];           // -1: a row without a part
+};
+template <int D>
+__device__ __forceinline__ int load_group(const PagesSelectArgs& a, const Group& g, int b, int h, GroupRows<D>* out) {
+    constexpr int C = D / 8;
+    const int G = a.group_heads, n = (g.t1 - g.t0) * G, n32 = (n + 31) / 32 * 32;
+    for (int r = threadIdx.x / C; r < n32; r += blockDim.x / C) {
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-        const int d = tid % C * 8;
+        const int d = threadIdx.x % C * 8;
         if (r < n) {
             if (a.q_split) {   // a pass's split queries
-                const uint16_t* p = a.q_split + q_index(b * heads + h, r % G * g.n + g.t0 + r / G, d, a.q_row_tiles, D);
+                const uint16_t* p = a.q_split + q_index(b * a.c.n_kv_heads + h, r % G * g.n + g.t0 + r / G, d, a.q_row_tiles, D);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]) + bf16_to_f32(p[SPLIT_LO + i]);
             } else {
@@ -1527,42 +1555,52 @@ __global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
             neg[i / 4] |= (uint32_t)(uint8_t)min(v, 0) << (8 * (i & 3));
             pos[i / 4] |= (uint32_t)max(v, 0) << (8 * (i & 3));
         }
-        *(uint2*)&qi[r][d] = uint2{neg[0], neg[1]};
-        *(uint2*)&qi[r][D + d] = uint2{pos[0], pos[1]};
-        if (tid % C == 0) qs[r] = r < n && !odd ? sc : -1.0f;   // -1: a row without a part
+        *(uint2*)&out->qi[r][d] = uint2{neg[0], neg[1]};
+        *(uint2*)&out->qi[r][D + d] = uint2{pos[0], pos[1]};
+        if (threadIdx.x % C == 0) out->qs[r] = r < n && !odd ? sc : -1.0f;
     }
-    __syncthreads();
+    return n32;
+}
 
-    for (int p32 = chunk * SCORE_PAGES + wave * 32; p32 < hi; p32 += 128) {
-        const int page = p32 + col;
-        const bool there = page >= lo && page < hi;
-        const int id = there ? page_id(a.c, b, page) : -1;
-        if (there && id < 0) flag(a.status, ST_PAGE);
-        const size_t head = (size_t)max(id, 0) * heads + h;
-        i32x4_t w[KS];
+// bounds of a page as an operand: lanes col and col + 32 have its halves
+template <int D>
+struct PageBounds {
+    i32x4_t w[2 * D / 32];
+    float scale;
+    int id;
+};
+template <int D>
+__device__ __forceinline__ PageBounds<D> load_bounds(const PagesSelectArgs& a, int b, int h, int page, bool there, int hf) {
+    PageBounds<D> p;
+    p.id = there ? page_id(a.c, b, page) : -1;
+    if (there && p.id < 0) flag(a.status, ST_PAGE);
+    const size_t head = (size_t)max(p.id, 0) * a.c.n_kv_heads + h;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) w[s] = *(const i32x4_t*)(a.c.bounds + head * 2 * D + 32 * s + 16 * hf);
-        const float bs = a.c.bound_scale[head];
-        float best = -INFINITY;
-        for (int r0 = 0; r0 < n32; r0 += 32) {
-            i32x16_t acc;
+    for (int s = 0; s < 2 * D / 32; ++s) p.w[s] = *(const i32x4_t*)(a.c.bounds + head * 2 * D + 32 * s + 16 * hf);
+    p.scale = a.c.bound_scale[head];
+    return p;
+}
+// score of a lane's page
+template <int D>
+__device__ __forceinline__ float page_score(const PageBounds<D>& p, const GroupRows<D>& rows, int n32, int lane) {
+    const int hf = lane >> 5, col = lane & 31;
+    float best = -INFINITY;
+    for (int r0 = 0; r0 < n32; r0 += 32) {
+        i32x16_t acc;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = 0;
+        for (int r = 0; r < 16; ++r) acc[r] = 0;
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
-                acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*(const i32x4_t*)&qi[r0 + col][32 * s + 16 * hf], w[s], acc, 0, 0, 0);
+        for (int s = 0; s < 2 * D / 32; ++s)
+            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*(const i32x4_t*)&rows.qi[r0 + col][32 * s + 16 * hf], p.w[s], acc, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float f = qs[r0 + 8 * (r >> 2) + 4 * hf + (r & 3)];
-                if (f >= 0.0f) best = fmaxf(best, (float)acc[r] * f);
-            }
-        }
-        best = fmaxf(best, __shfl_xor(best, 32));
-        if (there && hf == 0) {
-            const float f = !finite(bs) ? INFINITY : best == -INFINITY ? -INFINITY : best * bs;
-            a.scores[(size_t)unit * a.c.max_pages + page] = id < 0 ? -INFINITY : f;
+        for (int r = 0; r < 16; ++r) {
+            const float f = rows.qs[r0 + 8 * (r >> 2) + 4 * hf + (r & 3)];
+            if (f >= 0.0f) best = fmaxf(best, (float)acc[r] * f);
         }
     }
+    best = fmaxf(best, __shfl_xor(best, 32));
+    const float f = !finite(p.scale) ? INFINITY : best == -INFINITY ? -INFINITY : best * p.scale;
+    return p.id < 0 ? -INFINITY : f;
 }
 
 // order of scores as unsigned numbers; -0 is 0
@@ -1572,53 +1610,53 @@ __device__ __forceinline__ uint32_t score_key(float v) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One workgroup per unit: the n_top-th largest score digit by digit (the counts of a digit's 256 values in LDS), then the taken pages in
-// ascending order.
-__global__ void __launch_bounds__(256) pages_pick_kernel(PagesSelectArgs a) {
+// The taken pages of a unit, in ascending order: the n_top-th largest of n > n_top keys (key_of(i): of page lo + i) digit by digit, with the
+// counts of a digit's 256 values in LDS, then page by page.
+template <int THREADS, typename F>
+__device__ __forceinline__ void pick_pages(const PagesSelectArgs& a, const Group& g, int unit, int lo, int n, F key_of) {
+    constexpr int W = THREADS / 64;
     __shared__ uint32_t hist[256];
-    __shared__ int wsum[4][2];
+    __shared__ int wsum[W][2];
     __shared__ uint32_t s_key;
     __shared__ int s_left;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, unit = blockIdx.x, heads = a.c.n_kv_heads;
-    const int grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
-    const Group g = group_of(a, b, grp, unit % heads == 0 && tid == 0 ? a.status : nullptr);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int32_t* out = a.list + (size_t)unit * a.n_list;
-    const float* score = a.scores + (size_t)unit * a.c.max_pages;
-    const int lo = min(a.n_first, g.p0), n = g.p0 - lo;   // candidates
     uint32_t key = a.n_top > 0 ? 0u : 0xFFFFFFFFu;   // taken: above key, and `left` of those equal to it
     int left = a.n_top;
     if (n > a.n_top && a.n_top > 0) {
         for (int shift = 24; shift >= 0; shift -= 8) {
-            hist[tid] = 0u;
+            if (tid < 256) hist[tid] = 0u;
             __syncthreads();
-            for (int i = tid; i < n; i += 256) {
-                const uint32_t k = score_key(score[lo + i]);
+            for (int i = tid; i < n; i += THREADS) {
+                const uint32_t k = key_of(i);
                 if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
             }
             __syncthreads();
             // counts of larger digits; the digit where they reach `left`
-            uint32_t up = hist[tid];
+            uint32_t up = tid < 256 ? hist[tid] : 0u;
             for (int m = 1; m < 64; m <<= 1) {
                 const uint32_t o = __shfl_down(up, m);
                 if (lane + m < 64) up += o;
             }
             if (lane == 0) wsum[wave][0] = (int)up;
             __syncthreads();
-            for (int w = wave + 1; w < 4; ++w) up += (uint32_t)wsum[w][0];
-            const uint32_t above = up - hist[tid];
-            if ((int)above < left && (int)up >= left) s_key = key | (uint32_t)tid << shift, s_left = left - (int)above;
+            if (tid < 256) {
+                for (int w = wave + 1; w < 4; ++w) up += (uint32_t)wsum[w][0];
+                const uint32_t above = up - hist[tid];
+                if ((int)above < left && (int)up >= left) s_key = key | (uint32_t)tid << shift, s_left = left - (int)above;
+            }
             __syncthreads();
             key = s_key, left = s_left;
         }
     }
     int put = 0;
-    for (int i0 = 0; i0 < g.end; i0 += 256) {
+    for (int i0 = 0; i0 < g.end; i0 += THREADS) {
         const int i = i0 + tid;
         bool sure = false, tie = false;
         if (i < g.end) {
             if (i < lo || i >= g.p0 || n <= a.n_top) sure = true;
             else {
-                const uint32_t k = score_key(score[i]);
+                const uint32_t k = key_of(i - lo);
                 sure = k > key, tie = k == key;
             }
         }
@@ -1626,7 +1664,7 @@ __global__ void __launch_bounds__(256) pages_pick_kernel(PagesSelectArgs a) {
         if (lane == 0) wsum[wave][0] = __popcll(ties);
         __syncthreads();
         int before = __popcll(ties & below), all = 0;
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             if (w < wave) before += wsum[w][0];
             all += wsum[w][0];
         }
@@ -1636,13 +1674,74 @@ __global__ void __launch_bounds__(256) pages_pick_kernel(PagesSelectArgs a) {
         if (lane == 0) wsum[wave][1] = __popcll(takes);
         __syncthreads();
         int at = put + __popcll(takes & below);
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             if (w < wave) at += wsum[w][1];
             put += wsum[w][1];
         }
         if (taken && at < a.n_list) out[at] = i;
     }
-    for (int i = put + tid; i < a.n_list; i += 256) out[i] = -1;
+    for (int i = put + tid; i < a.n_list; i += THREADS) out[i] = -1;
+}
+
+// Scores and choice of a unit in one workgroup of 8 wavefronts.
+template <int D>
+__global__ void __launch_bounds__(512) pages_select_kernel(PagesSelectArgs a) {
+    __shared__ __align__(16) GroupRows<D> rows;
+    __shared__ uint32_t keys[SELECT_PAGES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = blockIdx.x, heads = a.c.n_kv_heads;
+    const int h = unit % heads, grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
+    const Group g = group_of(a, b, grp, h == 0 && threadIdx.x == 0 ? a.status : nullptr);
+    const int lo = min(a.n_first, g.p0), n = g.p0 - lo;   // candidates
+    if (n > a.n_top && a.n_top > 0) {
+        int i = wave * 32 + (lane & 31);
+        PageBounds<D> p = load_bounds<D>(a, b, h, lo + i, i < n, lane >> 5);   // under way with the queries
+        const int n32 = load_group<D>(a, g, b, h, &rows);
+        __syncthreads();
+        for (int i0 = 0; i0 < n; i0 += 256) {
+            const PageBounds<D> now = p;
+            const int next = i + 256;
+            if (i0 + 256 < n) p = load_bounds<D>(a, b, h, lo + next, next < n, lane >> 5);
+            const float f = page_score<D>(now, rows, n32, lane);
+            if (i < n && lane < 32) keys[i] = score_key(f);
+            i = next;
+        }
+        __syncthreads();
+    }
+    pick_pages<512>(a, g, unit, lo, n, [&](int i) { return keys[i]; });
+}
+
+// The same in two launches, for more pages than that, or for few units: a workgroup per unit and 128 pages, then one per unit.
+template <int D>
+__global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
+    __shared__ __align__(16) GroupRows<D> rows;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int chunk = blockIdx.x % a.chunks, unit = blockIdx.x / a.chunks, heads = a.c.n_kv_heads;
+    const int h = unit % heads, grp = unit / heads % a.n_groups, b = unit / heads / a.n_groups;
+    const Group g = group_of(a, b, grp, nullptr);
+    const int lo = max(a.n_first, chunk * SCORE_PAGES), hi = min(g.p0, chunk * SCORE_PAGES + SCORE_PAGES);
+    if (lo >= hi || g.p0 - a.n_first <= a.n_top) return;   // none, or all of them are taken
+    const int page = chunk * SCORE_PAGES + wave * 32 + (lane & 31);
+    const bool there = page >= lo && page < hi;
+    const PageBounds<D> p = load_bounds<D>(a, b, h, page, there, lane >> 5);   // under way with the queries
+    const int n32 = load_group<D>(a, g, b, h, &rows);
+    __syncthreads();
+    const float f = page_score<D>(p, rows, n32, lane);
+    if (there && lane < 32) a.scores[(size_t)unit * a.c.max_pages + page] = f;
+}
+
+__global__ void __launch_bounds__(512) pages_pick_kernel(PagesSelectArgs a) {
+    __shared__ uint32_t keys[SELECT_PAGES];
+    const int unit = blockIdx.x, heads = a.c.n_kv_heads;
+    const Group g = group_of(a, unit / heads / a.n_groups, unit / heads % a.n_groups, unit % heads == 0 && threadIdx.x == 0 ? a.status : nullptr);
+    const int lo = min(a.n_first, g.p0), n = g.p0 - lo;
+    const float* score = a.scores + (size_t)unit * a.c.max_pages + lo;
+    if (n > SELECT_PAGES || n <= a.n_top || a.n_top == 0) {
+        pick_pages<512>(a, g, unit, lo, n, [&](int i) { return score_key(score[i]); });
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += 512) keys[i] = score_key(score[i]);
+    __syncthreads();
+    pick_pages<512>(a, g, unit, lo, n, [&](int i) { return keys[i]; });
 }
 
 HeadRows with_vec(HeadRows r) {
@@ -1711,13 +1810,23 @@ hipError_t launch_pages_select(const PagesSelectArgs& args, hipStream_t s) {
     a.q = with_vec(a.q);
     a.chunks = cdiv(a.c.max_pages, SCORE_PAGES);
     const int units = a.c.batch * a.n_groups * a.c.n_kv_heads;
+    // One launch where its workgroups fill the card, or have few pages each.  One against two launches: 2048 units of 136 pages 50 against 65
+    // us, 256 units of 257 pages 9.8 against 13.1; but 8 units of 1025 pages 17.2 against 13.5, and selection and attention of 64 units of 1025
+    // pages 58.3 against 55.1, of 32 units of 2049 75 against 63: there one workgroup reads the bounds of all of a unit's pages.
+    // NLD_SELECT_ONE overrides.
+    const bool one = a.c.max_pages <= SELECT_PAGES && env_int("NLD_SELECT_ONE", a.c.max_pages <= 256 || units >= 256);
+    if (one) {
+        if (a.c.head_dim == 64) pages_select_kernel<64><<<units, 512, 0, s>>>(a);
+        else pages_select_kernel<128><<<units, 512, 0, s>>>(a);
+        return hipGetLastError();
+    }
     if (a.n_top > 0) {
         if (a.c.head_dim == 64) pages_score_kernel<64><<<units * a.chunks, 256, 0, s>>>(a);
         else pages_score_kernel<128><<<units * a.chunks, 256, 0, s>>>(a);
         const hipError_t st = hipGetLastError();
         if (st != hipSuccess) return st;
     }
-    pages_pick_kernel<<<units, 256, 0, s>>>(a);
+    pages_pick_kernel<<<units, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 

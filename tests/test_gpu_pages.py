@@ -490,9 +490,11 @@ SELECT = [([900], [1], 1, 4, 1, 0), ([64, 0, 700], [1, 1, 1], 1, 3, 0, 0), ([450
           ([640], [16], 16, 6, 4, 1), ([300, 5], [33, 20], 8, 0, 1, 1), ([400], [3], 1, 100, 0, 0)]
 
 
+@pytest.mark.parametrize("launches", ["one", "two"])
 @pytest.mark.parametrize("pages", [BF16, E4M3])
 @pytest.mark.parametrize("lens,news,group,n_top,n_first,mode", SELECT)
-def test_selection(pages, lens, news, group, n_top, n_first, mode):
+def test_selection(monkeypatch, launches, pages, lens, news, group, n_top, n_first, mode):
+    monkeypatch.setenv("NLD_SELECT_ONE", "1" if launches == "one" else "0")
     for dim, dtype in ((64, F32), (128, BF16)):
         s = Setup(pages, 2, dim, lens, news).fill()
         q = randn((s.rows, 8, dim), 5, dtype)
@@ -506,8 +508,10 @@ def test_selection(pages, lens, news, group, n_top, n_first, mode):
         s.check(q, mode=mode, bidir_from=min(2, s.most), lists=got, group=group)
 
 
-def test_selection_takes_the_lower_page_among_equal_scores():
+@pytest.mark.parametrize("launches", ["one", "two"])
+def test_selection_takes_the_lower_page_among_equal_scores(monkeypatch, launches):
     """Pages with one and the same keys, scores of zero of both signs, and more of them than the block of one count."""
+    monkeypatch.setenv("NLD_SELECT_ONE", "1" if launches == "one" else "0")
     s = Setup(BF16, 1, 64, [64 * 40], [1])
     k = torch.zeros((64 * 40, 1, 64), dtype=BF16, device=DEV)
     k[64 * 5:64 * 6], k[64 * 31:64 * 32], k[64 * 33:64 * 35] = 1.0, 1.0, -1.0
@@ -519,7 +523,9 @@ def test_selection_takes_the_lower_page_among_equal_scores():
     assert R.select_pages(s.cache, 0, -q, ws, 4, n_first=0)[0, 0, 0].tolist()[:5] == [0, 1, 33, 34, 40]
 
 
-def test_selection_of_what_is_not_finite():
+@pytest.mark.parametrize("launches", ["one", "two"])
+def test_selection_of_what_is_not_finite(monkeypatch, launches):
+    monkeypatch.setenv("NLD_SELECT_ONE", "1" if launches == "one" else "0")
     s = Setup(BF16, 1, 64, [640], [2])
     k = randn((642, 1, 64), 1)
     k[64 * 7 + 3, 0, 9] = NAN
@@ -535,8 +541,10 @@ def test_selection_of_what_is_not_finite():
     assert R.select_pages(s.cache, 0, q, ws, 2, n_first=1, group=2)[0, 0, 0].tolist()[:4] == [0, 1, 7, 10]
 
 
-def test_selection_over_a_long_sequence():
-    """More pages than one workgroup scores, and than fit one round of the pick."""
+@pytest.mark.parametrize("launches", ["one", "two"])
+def test_selection_over_a_long_sequence(monkeypatch, launches):
+    """More pages than one workgroup scores at a time, and than fit one round of the pick."""
+    monkeypatch.setenv("NLD_SELECT_ONE", "1" if launches == "one" else "0")
     s = Setup(E4M3, 2, 64, [64 * 1100 + 7], [2]).fill()
     q = randn((2, 4, 64), 5)
     ws = s.workspace(4, group=2)
