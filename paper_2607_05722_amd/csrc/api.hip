@@ -331,8 +331,13 @@ HeadRows head_rows(const nld_heads* x) { return HeadRows{x->data, x->dtype == NL
 PageChunk page_chunk(const nld_chunk* c) { return PageChunk{c->rows, c->max_rows, c->row_start}; }
 
 // The attention's plan and workspace: the status word, then the parts of units that workgroups share, or a selection's scores.
-// Row tiles: as few as the rows of a sequence and KV head need, at most four to a workgroup.  Two workgroups per CU have room (LDS,
-// registers) and are what hides the loads' latency.
+// Rows of a KV head (tokens x query heads of its group), or of a group of tokens with a list:
+//  - up to 16: one 16-row tile per workgroup, 17 to 32: one 32-row tile; keys and values go straight to registers, four wavefronts to a
+//    workgroup, two of these to a CU (a token of 32 ragged sequences over 8 bits: 79 us, 113 with 32-row tiles);
+//  - more: up to eight 32-row tiles that share each page through LDS, two wavefronts per tile where there are up to four of them.  Against
+//    single tiles, two or four to a workgroup: draft blocks of 160 rows over 8 bits 174 against 352 us, prompts 882 against 1383, verify
+//    blocks of 64 f32 rows 164 against 222.
+// Two workgroups of four wavefronts fit a CU by LDS and registers, else one.
 struct PagesPlan {
     int block_rows, row_tiles, n_blk, grid, slices, shared_waves, key_halves;
     size_t part_ml, parts, total;
@@ -349,9 +354,9 @@ bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int ma
     if (blocks * batch * n_kv_heads > MAX_PAGE_WGS) return false;
     p.n_blk = (int)blocks;
     p.grid = p.shared_waves > 4 || (p.shared_waves && raw) ? device_cus() : 2 * device_cus();
-    // the second launch: a few thousand workgroups at most, and one where units are that many
+    // the second launch: a few thousand workgroups, and one per unit where units are that many
     const int turns = cdiv((int)std::min<long long>(rows, p.block_rows), 1024 / head_dim);
-    p.slices = (int)std::max(1LL, std::min<long long>(turns, 2048 / (blocks * batch * n_kv_heads)));
+    p.slices = (int)std::max(1LL, std::min<long long>(turns, 8192 / (blocks * batch * n_kv_heads)));
     const size_t part_rows = (size_t)2 * p.grid * p.block_rows;
     p.part_ml = 256 + part_rows * head_dim * 4;
     p.parts = align256(p.part_ml + part_rows * 8);
