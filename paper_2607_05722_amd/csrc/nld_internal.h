@@ -426,7 +426,7 @@ struct PagesAttnArgs {
     const int32_t* list;        // optional [batch][n_blk][kv head][n_list]: the pages of each group of tokens
     int n_list, group;
     float* lse;                 // optional [rows][query head]
-    int block_rows, row_tiles;  // rows of a workgroup: 16 (one tile), or 1, 2 or 4 tiles of 32
+    int block_rows, row_tiles;  // rows of a workgroup: 16 (one tile), or 1 to 8 tiles of 32
     int n_blk, n_entries;       // blocks of rows per sequence, of all
     int grid, least_steps, slices;
     int shared_waves, key_halves;   // > 0: the kernel whose wavefronts share pages through LDS, with so many; wavefronts per tile
