@@ -248,12 +248,14 @@ class QuadWorkspace(Workspace):
         C.check(lib.nld_workspace_init(_ptr(self.buf), self.nbytes, stream_handle()))
 
 
-def _pass(name, model, cache, sparse, batch):
+def _pass(name, model, cache, ws, sparse, batch):
     """The entry point of a pass over this cache with its arguments up to the batch."""
     lib = C.load()
     if isinstance(cache, PagedCache):
         if batch != cache.batch:
             raise ValueError("the cache has %d sequences, the call %d" % (cache.batch, batch))
+        if ws.buf.device != cache.device:
+            raise ValueError("the workspace is on %s, the cache on %s" % (ws.buf.device, cache.device))
         choice = None if sparse is None else ctypes.byref(C.Sparse(*_sparse(sparse)))
         return getattr(lib, "nld_pages_" + name), (model.handle, ctypes.byref(cache.struct), choice), ()
     if sparse is not None:
@@ -268,7 +270,7 @@ def block_forward(model, cache, ws, tokens: torch.Tensor, mode: int, bidir_from:
     dev = model.device
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
     argmax = torch.empty((batch, k), dtype=torch.int32, device=dev)
-    fn, head, size = _pass("block_forward", model, cache, sparse, batch)
+    fn, head, size = _pass("block_forward", model, cache, ws, sparse, batch)
     C.check(fn(*head, _ptr(tokens), *size, k, mode, bidir_from, _ptr(logits), _ptr(argmax), ws.ptr, ws.nbytes, stream_handle()))
     return logits, argmax
 
@@ -279,7 +281,7 @@ def draft(model, cache, ws, anchor: torch.Tensor, k: int, bidir_from: int = 0, w
     dev = model.device
     d = out if out is not None else torch.empty((batch, k - 1), dtype=torch.int32, device=dev)
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
-    fn, head, size = _pass("draft", model, cache, sparse, batch)
+    fn, head, size = _pass("draft", model, cache, ws, sparse, batch)
     C.check(fn(*head, _ptr(anchor), *size, k, bidir_from, _ptr(d), _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
     return d, logits
 
@@ -293,7 +295,7 @@ def verify_accept(model, cache, ws, anchor: torch.Tensor, drafts, k: int, want_l
                 "committed": torch.empty((batch, k), dtype=torch.int32, device=dev),
                 "next_anchor": torch.empty(batch, dtype=torch.int32, device=dev)}
     logits = torch.empty((batch, k, model.shape.vocab), dtype=torch.float32, device=dev) if want_logits else None
-    fn, head, size = _pass("verify_accept", model, cache, sparse, batch)
+    fn, head, size = _pass("verify_accept", model, cache, ws, sparse, batch)
     C.check(fn(*head, _ptr(anchor), _ptr(drafts), *size, k, _ptr(outs["accept_len"]), _ptr(outs["committed"]),
                _ptr(outs["next_anchor"]), _ptr(logits), ws.ptr, ws.nbytes, stream_handle()))
     outs = dict(outs)

@@ -1,5 +1,6 @@
 """The calls on a paged cache: argument checks (nothing is enqueued), and the plain versions that the GPU tests compare with. No GPU needed."""
 import ctypes
+from types import SimpleNamespace
 
 import pages_ref as ref
 import pytest
@@ -240,3 +241,14 @@ def test_plain_bounds_hold():
         lo, hi = bd[0].double() * scale, bd[1].double() * scale
         assert bool((lo <= k[:50].double().amin(0) + near).all()) and bool((hi >= k[:50].double().amax(0) - near).all())
         assert int(bd.abs().max()) <= 127
+
+
+@pytest.mark.parametrize("call", ["block_forward", "draft", "verify_accept"])
+def test_passes_refuse_a_cache_on_another_device(call):
+    cache = R.PagedCache(2, 64, 1, 64, device="cpu")
+    model = SimpleNamespace(device=torch.device("cpu"), shape=SimpleNamespace(vocab=8), handle=None)
+    ws = SimpleNamespace(buf=torch.empty(256, dtype=torch.uint8, device="meta"), ptr=0, nbytes=256)
+    one = torch.zeros(1, dtype=torch.int32)
+    args = {"block_forward": (one.view(1, 1), R.VERIFY), "draft": (one, 2), "verify_accept": (one, one.view(1, 1), 2)}[call]
+    with pytest.raises(ValueError, match="workspace is on meta, the cache on cpu"):
+        getattr(R, call)(model, cache, ws, *args)
