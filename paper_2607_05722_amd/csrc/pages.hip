@@ -767,7 +767,7 @@ __device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const 
 // Few rows, up to one tile of 16 or 32 of a KV head: one pass over a share's pages with each row's running maximum and sum, the steps dealt to
 // four wavefronts that meet at the unit's end through LDS.  Bound by memory: every page is read once, straight to registers, where its
 // layout makes it an operand, and a wavefront asks for its next step's keys and values before it works on this one's.
-// bf16 queries: two pieces of the weights, at most 2^-16 of each, since the matrix units are idle here; f32 queries: three pieces of both.
+// bf16 queries: two pieces of the weights, at most 2^-16 of each, since memory and not the products bounds this kernel; f32 queries: three pieces of both.
 // One token of 32 sequences of up to 8192 positions, 32 query heads, e4m3 (297 MB): 61 us, 4.9 TB/s of the 6.5 that plain reads reach, and 72
 // with the second launch and the gap between the two; one token over 4096 positions, bf16 (17 MB): 14 us of latency, 21.5 with the second.
 template <int D, bool E4M3, int NQ, int RW>   // NQ: bf16 pieces of a query (1: bf16, 2: split, 3: f32); RW: rows of a tile
