@@ -64,7 +64,7 @@ struct SeqRows {
 __device__ __forceinline__ SeqRows seq_rows(const PageChunk& c, int b, uint32_t* status) {
     if (!c.row_start) return SeqRows{b * c.max_rows, c.max_rows};
     const int s = c.row_start[b], e = c.row_start[b + 1];
-    const int r0 = min(max(s, 0), c.rows), n = max(0, min(min(e, c.rows) - r0, c.max_rows));
+    const int r0 = min(max(s, 0), c.rows), n = min(min(max(e, r0), c.rows) - r0, c.max_rows);   // e before the difference: it may be any number
     if (status && (r0 != s || r0 + n != e)) flag(status, ST_ROWS);
     return SeqRows{r0, n};
 }

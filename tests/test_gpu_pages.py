@@ -456,6 +456,49 @@ def test_bad_row_starts():
         assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS, start
 
 
+STARTS = [([4, -2 ** 31, 8], [], [0, 1, 2, 3]), ([4, 3 - 2 ** 31, -2 ** 31], [], []), ([-2 ** 31, 4, -2 ** 31], [0, 1, 2, 3], []),
+          ([0, 2 ** 31 - 1, -2 ** 31], [0, 1, 2, 3], []), ([-1, -1, 2 ** 31 - 1], [], [0, 1, 2, 3]), ([8, 8, -5], [], []), ([6, 9, 2], [6, 7], []),
+          ([7, -2 ** 31 + 6, 3], [], [0, 1, 2])]
+
+
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("start,first,second", STARTS)
+def test_bad_row_starts_reach_no_other_rows(pages, start, first, second):
+    """8 rows, at most 4 each: the rows that either sequence has, and no others, are read and written, whatever the starts are.  The rows lie
+    inside larger arrays."""
+    s = Setup(pages, 1, 64, [20, 30], [4, 4]).fill()
+    ws = s.workspace(2, 8, 4)
+    has = torch.zeros(24, dtype=torch.bool, device=DEV)
+    has[[8 + r for r in first + second]] = True
+    inner = slice(8, 16)
+    row_start = on_device(start)
+    q, out, lse = randn((24, 2, 64), 3), torch.full((24, 2, 64), 5.0, dtype=BF16, device=DEV), torch.full((24, 2), 5.0, device=DEV)
+    R.attend_pages(s.cache, 0, q[inner], ws, row_start=row_start, max_rows=4, out=out[inner], lse=lse[inner])
+    assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS
+    assert torch.equal((out != 5.0).flatten(1).any(1), has) and torch.equal((lse != 5.0).any(1), has)
+    k, v = (torch.full((24, 1, 64), 5.0, device=DEV) for _ in range(2))
+    R.read_pages(s.cache, 0, 8, ws, row_start=row_start, max_rows=4, outs=(k[inner], v[inner]))
+    assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS
+    for x, plain in ((k, s.plain.k), (v, s.plain.v)):
+        for b, rows in enumerate((first, second)):
+            for i, r in enumerate(rows):
+                assert torch.equal(x[8 + r].double(), plain[b, i])
+        assert bool((x[~has] == 5.0).all())
+    lists = R.select_pages(s.cache, 0, q[inner], ws, 1, group=4, row_start=row_start, max_rows=4)
+    assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS
+    assert [bool((lists[b] == -1).all()) for b in range(2)] == [not first, not second]
+    rows = randn((24, 1, 64), 9)
+    R.write_pages(s.cache, 0, rows[inner], rows[inner], ws, row_start=row_start, max_rows=4)
+    assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS
+    for b, mine in enumerate((first, second)):
+        new = ref.stored(rows[[8 + r for r in mine]], pages == E4M3)
+        p = s.lens[b]
+        s.plain.k[b, p:p + len(mine)] = s.plain.v[b, p:p + len(mine)] = new
+    k, v = R.read_pages(s.cache, 0, 58, ws, row_start=on_device([0, 24, 58]), max_rows=34)
+    assert torch.equal(k[:24].double(), s.plain.k[0, :24]) and torch.equal(k[24:].double(), s.plain.k[1, :34])
+    assert torch.equal(v[:24].double(), s.plain.v[0, :24]) and torch.equal(v[24:].double(), s.plain.v[1, :34])
+
+
 # ------------------------------------------------------------------------------------------ lists and selection
 @pytest.mark.parametrize("group", [1, 3, 8])
 def test_lists(group):
