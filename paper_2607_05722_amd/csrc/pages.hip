@@ -1669,7 +1669,7 @@ __device__ __forceinline__ void pick_pages(const PagesSelectArgs& a, const Group
         bool sure = false, tie = false;
         if (i < g.end) {
             if (i < lo || i >= g.p0 || n <= a.n_top) sure = true;
-            else {
+            else if (a.n_top > 0) {   // 0: nobody worked out keys, and no candidate is taken
                 const uint32_t k = key_of(i - lo);
                 sure = k > key, tie = k == key;
             }

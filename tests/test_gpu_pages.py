@@ -9,6 +9,8 @@ Hence, with A = sum of weights times |v|:
     out   (e + pieces + (n / 32 + 64) * 2^-24) * A, and half a step of its type: 2^-8 (bf16) or 2^-23 (f32: two roundings) of |out|
     lse   e / 2 + (n / 32 + 64) * 2^-24 + 2^-23 |lse|
 """
+from types import SimpleNamespace
+
 import numpy as np
 import pages_ref as ref
 import pytest
@@ -604,6 +606,26 @@ def test_selection_over_a_long_sequence(monkeypatch, launches):
         best = torch.sort(score, descending=True, stable=True)[1][:20].tolist()
         assert got[0, 0, h].tolist()[:22] == sorted(best + [0, 1100])
     s.check(q, lists=got, group=2)
+
+
+@pytest.mark.parametrize("launches", ["one", "two"])
+@pytest.mark.parametrize("width", [300, 5000])
+def test_selection_of_the_first_and_own_pages_alone(monkeypatch, launches, width):
+    """n_top 0 needs no scores, and a workspace of 256 bytes will do: here the end of an allocation."""
+    monkeypatch.setenv("NLD_SELECT_ONE", "1" if launches == "one" else "0")
+    c = R.PagedCache(2, 64, 2, 64 * width, n_pages=1, bounds=True, device=DEV)
+    c.table.zero_()                       # one page in every place: none is read
+    c.lengths.copy_(on_device([64 * width - 66, 5]))
+    buf = torch.zeros(1024, dtype=torch.uint8, device=DEV)[768:]
+    ws = SimpleNamespace(buf=buf, ptr=buf.data_ptr(), nbytes=256)
+    for group, n_first in ((1, 0), (4, 3)):
+        got = R.select_pages(c, 0, randn((8, 4, 64), 5), ws, 0, group=group, n_first=n_first)
+        assert R.read_device_status(ws) == 0
+        for b, p in enumerate((64 * width - 66, 5)):
+            for j in range(got.shape[1]):
+                own = range((p + j * group) // 64, (p + min((j + 1) * group, 4) - 1) // 64 + 1)
+                want = sorted(set(range(min(n_first, own[0]))) | set(own))
+                assert got[b, j].tolist() == [want + [-1] * (got.shape[3] - len(want))] * 2
 
 
 # ------------------------------------------------------------------------------------------ together, as they are used
