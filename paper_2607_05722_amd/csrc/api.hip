@@ -1525,7 +1525,8 @@ int32_t nld_pages_list_len(int32_t max_rows, int32_t group, int32_t n_top, int32
     if (max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 1 || group > MAX_CHUNK_ROWS || n_top < 0 || n_first < 0 ||
         n_top > MAX_SEQ_PAGES || n_first > MAX_SEQ_PAGES || (mode != NLD_MODE_VERIFY && mode != NLD_MODE_DRAFT))
         return 0;
-    return n_first + n_top + ((mode == NLD_MODE_DRAFT ? max_rows : group) + 62) / 64 + 1;
+    // a group's own pages: those of its tokens' positions, of which there are no more than rows (a draft's: of all rows)
+    return n_first + n_top + ((mode == NLD_MODE_DRAFT ? max_rows : std::min(group, max_rows)) + 62) / 64 + 1;
 }
 
 size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int32_t max_rows, int32_t group) {
@@ -1665,7 +1666,7 @@ size_t nld_pages_pass_workspace_bytes(const nld_model* m, const nld_pages* pages
     nld_kv_cache kv;
     Layout L;
     PagedPass pp;
-    // a draft pass's lists are the longer ones; any pointer stands for the workspace
+    // a draft pass's lists are the longer ones: its groups see all rows; any pointer stands for the workspace
     return validate_paged(m, pages, sparse, k, NLD_MODE_DRAFT, &kv, ~(size_t)0, &kv, &L, &pp) == NLD_OK ? pp.total : 0;
 }
 

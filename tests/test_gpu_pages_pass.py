@@ -97,6 +97,24 @@ def test_block_passes_over_selected_pages(tiny, pages, sparse):
     assert rel_err(every.cpu().numpy(), whole.cpu().numpy()) <= 1e-5     # all pages: the same sums in other parts
 
 
+@pytest.mark.parametrize("k,group", [(1, 4), (2, 16), (4, 64)])
+def test_selected_pages_of_groups_larger_than_the_block(tiny, k, group):
+    """One workspace for draft and verify passes of a batch large enough that a list's rounding to 256 bytes hides no entry."""
+    shape, _, model = tiny
+    batch, sparse = 64 // shape.n_kv_heads * 2, (3, 1, group)
+    both = Both(shape, BF16, batch, 640, bounds=True)
+    prefill(tiny, both, [(41 * i) % 560 + 1 for i in range(batch)])
+    ws = R.PagedPassWorkspace(model, both.cache, k, sparse)
+    toks = ids(shape, "block", batch, k)
+    for mode in (R.VERIFY, R.DRAFT):
+        logits, _ = R.block_forward(model, both.cache, ws, toks, mode, 0, sparse=sparse)
+        same, _ = R.block_forward(model, both.cache, R.PagedPassWorkspace(model, both.cache, k, (3, 1, k)), toks, mode, 0, sparse=(3, 1, k))
+        assert R.read_device_status(ws) == 0 and torch.equal(logits, same)
+    if k == 1:
+        R.verify_accept(model, both.cache, ws, toks[:, 0].contiguous(), None, 1, sparse=sparse)
+        assert R.read_device_status(ws) == 0
+
+
 def test_steps_in_bf16_pages_follow_the_other_cache(tiny):
     """Draft, verify, accept, commit: from the same prefix, over both caches."""
     shape, _, model = tiny

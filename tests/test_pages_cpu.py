@@ -143,6 +143,15 @@ def test_list_len():
         assert f(*bad) == 0
 
 
+def test_list_len_of_groups_larger_than_the_chunk():
+    """A group has no more tokens than the chunk, and a draft's list is never the shorter one."""
+    f = C.load().nld_pages_list_len
+    assert [f(1, 4, 0, 0, 0), f(1, 1 << 24, 2, 1, 0), f(2, 128, 0, 0, 0), f(65, 128, 0, 0, 0), f(66, 128, 0, 0, 0)] == [1, 4, 2, 2, 3]
+    for rows in (1, 2, 3, 16, 63, 64, 65, 66, 200):
+        for group in (1, 2, 4, 16, 64, 128):
+            assert f(rows, group, 5, 1, 0) <= f(rows, group, 5, 1, 1)
+
+
 def test_workspace_bytes():
     f = lambda p, *a: C.load().nld_pages_workspace_bytes(ref_of(p), *a)
     assert f(None, 4, 2, 0) == 0 and f(pages(head_dim=80), 4, 2, 0) == 0 and f(pages(), 3, 2, 0) == 0
