@@ -1478,7 +1478,7 @@ __global__ void __launch_bounds__(256) pages_combine_kernel(PagesAttnArgs a) {
     if (en.rows0 + slice * ROWS >= en.rows1) return;
     const uint2 parts = a.parts[(size_t)e * heads + h];
     const int n = (int)parts.y, w0 = (int)(parts.x & 0x7FFFFFFFu);
-    if (n <= 1 || w0 + n > a.grid) return;   // the latter not unless the lengths change meanwhile
+    if (n <= 1 || n > a.grid || w0 > a.grid - n) return;   // past the grid: not unless lengths or rows change meanwhile, and then it may be any number
     const int d = threadIdx.x % TPR * 4, first = 2 * w0 + (int)(parts.x >> 31);
     for (int r = slice * ROWS + threadIdx.x / TPR; en.rows0 + r < en.rows1; r += a.slices * ROWS) {
         auto place = [&](int i) { return (size_t)(i == 0 ? first : 2 * (w0 + i)) * a.block_rows + r; };
