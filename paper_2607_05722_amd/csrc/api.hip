@@ -345,6 +345,7 @@ struct PagesPlan {
 
 bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int max_rows, int group, bool raw, PagesPlan* out) {
     PagesPlan p{};
+    if ((long long)max_rows * group_heads > INT_MAX - 256) return false;   // the kernels count a sequence's rows of a KV head in int
     const long long rows = (long long)(group ? std::min(group, max_rows) : max_rows) * group_heads;
     p.row_tiles = (int)std::min<long long>(8, (rows + 31) / 32);
     p.block_rows = rows <= 16 ? 16 : 32 * p.row_tiles;

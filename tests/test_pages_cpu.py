@@ -127,6 +127,14 @@ def test_attention_scale_and_list():
     assert need > 256 and attend(ws_bytes=need // 2) == CAPACITY
 
 
+@pytest.mark.parametrize("group", [0, 1])
+def test_rows_of_a_kv_head_fit_an_int(group):
+    n = 1 << 24
+    kw = dict(p=pages(batch=1, n_kv_heads=1), ch=chunk(n, n, P), n_q=128, q=heads(row=128 * 64), out=heads(1 << 44, row=128 * 64), group=group, n_list=4)
+    assert attend(lst=P if group else None, **kw) == SHAPE and "too many" in C.load().nld_last_error().decode()
+    assert C.load().nld_pages_workspace_bytes(ctypes.byref(kw["p"]), 128, n, group) == 0
+
+
 def test_selection_arguments():
     assert select(p=pages()) == INVALID and "bounds" in C.load().nld_last_error().decode()
     for kw, status in ((dict(lst=None), INVALID), (dict(n_top=-1), INVALID), (dict(n_first=-1), INVALID), (dict(n_top=(1 << 24) + 1), SHAPE),
