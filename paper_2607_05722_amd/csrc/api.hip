@@ -1592,7 +1592,7 @@ nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chu
     if (st == NLD_OK) st = check_heads(out, "out", chunk->rows, n_q_heads, pages->head_dim, true);
     if (st == NLD_OK) st = check_mode(mode, bidir_from, chunk->max_rows);
     if (st != NLD_OK) return st;
-    if (!(fabsf(scale) < INFINITY)) return fail(NLD_ERR_INVALID_ARG, "scale must be finite");
+    if (!(fabsf(scale) <= 0x1p127f)) return fail(NLD_ERR_INVALID_ARG, "scale must be in [-2^127, 2^127]");   // finite in base-2 exponents too
     if (q->dtype != out->dtype) return fail(NLD_ERR_INVALID_ARG, "q and out must have one dtype");
     {
         const size_t es = q->dtype == NLD_BF16 ? 2 : 4;

@@ -127,6 +127,11 @@ def test_attention_scale_and_list():
     assert need > 256 and attend(ws_bytes=need // 2) == CAPACITY
 
 
+def test_attention_scales_that_pass_f32_in_base_2():
+    for bad in (3e38, -3e38, 2.0 ** 127 * 1.0001):
+        assert attend(scale=bad) == INVALID and "scale" in C.load().nld_last_error().decode()
+
+
 @pytest.mark.parametrize("group", [0, 1])
 def test_rows_of_a_kv_head_fit_an_int(group):
     n = 1 << 24
