@@ -686,8 +686,7 @@ class PagesWorkspace:
 
     def __init__(self, cache: PagedCache, n_q_heads: int, max_rows: int, group: int = 0):
         lib = C.load()
-        if max(n_q_heads, max_rows, group) > _INT32_MAX:
-            raise ValueError("sizes must be int32")
+        _int32(n_q_heads=n_q_heads, max_rows=max_rows, group=group)
         with torch.cuda.device(cache.device):
             self.nbytes = lib.nld_pages_workspace_bytes(ctypes.byref(cache.struct), n_q_heads, max_rows, group)
             if self.nbytes == 0:
@@ -719,12 +718,19 @@ class PagedPassWorkspace:
         self.ptr = _ptr(self.buf)
 
 
+def _int32(**numbers):
+    """Refuses what a call's int32 would keep the lower half of."""
+    for name, x in numbers.items():
+        if not -_INT32_MAX <= x <= _INT32_MAX:
+            raise ValueError("%s must be int32 (got %d)" % (name, x))
+
+
 def _heads(t: torch.Tensor, name: str, rows, heads: int, cache: PagedCache) -> C.Heads:
     """Descriptor of rows [rows][heads][head_dim], f32 or bf16, head_dim adjacent, other strides free."""
     dtype = _DTYPES.get(t.dtype)
     if dtype is None or t.dim() != 3 or t.device != cache.device:
         raise ValueError("%s must be a float32 or bfloat16 tensor [rows][heads][head_dim] on %s" % (name, cache.device))
-    if t.shape[1] != heads or t.shape[2] != cache.head_dim or (rows is not None and t.shape[0] != rows):
+    if t.shape[1] != heads or heads > _INT32_MAX or t.shape[2] != cache.head_dim or (rows is not None and t.shape[0] != rows):
         raise ValueError("%s has shape %s, this call needs [%s][%d][%d]" % (name, list(t.shape), rows, heads, cache.head_dim))
     row, head, dim = t.stride()
     if dim != 1:
@@ -750,6 +756,7 @@ def write_pages(cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor,
     """Writes keys and values [rows][kv_heads][head_dim] of new rows into the pages, row i of sequence b at position
     lengths[b] + i.  row_start (int32 [batch + 1]): the sequences' rows, packed, at most max_rows each (default: any number); None: the
     same number each.  lengths stay as they are: a caller that keeps the rows adds their number."""
+    _int32(layer=layer)
     ch = _chunk(cache, k.shape[0], row_start, max_rows)
     _call(C.load().nld_pages_write, cache.device, ws, cache.struct, layer, ch, _heads(k, "k", None, cache.kv_heads, cache),
           _heads(v, "v", k.shape[0], cache.kv_heads, cache))
@@ -760,6 +767,7 @@ def read_pages(cache: PagedCache, layer: int, rows: int, ws: PagesWorkspace, dty
                max_rows=None, outs=None):
     """Keys and values [rows][kv_heads][head_dim] of positions first[b] + i (int32 [batch]; None: from 0), f32 or bf16, both exact.
     row_start and max_rows as write_pages.  outs: (k, v) to write into, of any strides."""
+    _int32(layer=layer)
     ch = _chunk(cache, rows, row_start, max_rows)
     at = _rows_of(first, "first", (cache.batch,), torch.int32, cache.device)
     if outs is None:
@@ -788,6 +796,7 @@ def attend_pages(cache: PagedCache, layer: int, q: torch.Tensor, ws: PagesWorksp
     Returns (out, lse): out like q, lse f32 [rows][q_heads] with ``want_lse`` or where the caller gives it, else None.  No gradient flows through them."""
     if q.dim() != 3:
         raise ValueError("q must be [rows][q_heads][head_dim]")
+    _int32(layer=layer, mode=mode, bidir_from=bidir_from)
     rows, heads = q.shape[0], q.shape[1]
     qd = _heads(q, "q", None, heads, cache)
     ch = _chunk(cache, rows, row_start, max_rows)
@@ -815,6 +824,7 @@ def select_pages(cache: PagedCache, layer: int, q: torch.Tensor, ws: PagesWorksp
     [batch][groups][kv_heads][n], ascending, -1 behind the last, as attend_pages takes it."""
     if q.dim() != 3:
         raise ValueError("q must be [rows][q_heads][head_dim]")
+    _int32(layer=layer, mode=mode, bidir_from=bidir_from)
     qd = _heads(q, "q", None, q.shape[1], cache)
     ch = _chunk(cache, q.shape[0], row_start, max_rows)
     shape = _group_list(cache, ch, group)

@@ -225,6 +225,21 @@ def test_binding_refuses():
             R.select_pages(c, 0, x, None, **kw)
 
 
+@pytest.mark.parametrize("by", [2 ** 32, -2 ** 32, 2 ** 31])
+def test_binding_refuses_numbers_past_int32(by):
+    c, x = cpu_cache(), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    for call in (lambda: R.write_pages(c, by, x, x, None), lambda: R.read_pages(c, by, 2, None), lambda: R.attend_pages(c, by, x, None),
+                 lambda: R.attend_pages(c, 0, x, None, mode=by), lambda: R.attend_pages(c, 0, x, None, bidir_from=by),
+                 lambda: R.select_pages(c, by, x, None, 1), lambda: R.select_pages(c, 0, x, None, 1, mode=by),
+                 lambda: R.select_pages(c, 0, x, None, 1, bidir_from=by), lambda: R.PagesWorkspace(c, 2 + by, 1), lambda: R.PagesWorkspace(c, 2, 1 + by),
+                 lambda: R.PagesWorkspace(c, 2, 1, by)):
+        with pytest.raises(ValueError, match="int32"):
+            call()
+    if by > 2 ** 31:
+        with pytest.raises(ValueError):
+            R.attend_pages(c, 0, torch.zeros(64, dtype=torch.bfloat16).as_strided((2, by + 2, 64), (0, 0, 1)), None)
+
+
 # ------------------------------------------------------------------------------------------ the plain versions
 def test_plain_8_bit_values_are_the_types():
     """Against torch's own type at scale 1, over all of its finite values, halfway between them, and beside."""
