@@ -518,7 +518,7 @@ nld_status nld_pages_write(const nld_pages* pages, int32_t layer, const nld_chun
 
 /* Reads positions first[b] + i back into the chunk's rows (first: int32 [batch]; NULL: from 0), committed or not, in f32 or bf16,
  * both exact.  k and v must not overlap each other.  Device errors: as above (a negative first: BAD_LENGTH); what is not read is left as it was.
- * Errors: as above, INVALID_ARG for rows that overlap each other. */
+ * Errors: as above, INVALID_ARG for rows that overlap each other (k and v may lie in one array if they have the same strides). */
 nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const int32_t* first, const nld_heads* k,
                           const nld_heads* v, void* workspace, size_t ws_bytes, void* stream);
 
@@ -532,7 +532,7 @@ nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk
  * [n_kv_heads][n_list], places in the sequence's table, -1: none; each of them counts as often as it stands there.  Group j holds tokens
  * j * group .. of its sequence.  n_list and group are not looked at without a list.
  * Device errors: as nld_pages_write.  Errors: as nld_pages_write, INVALID_ARG for an unknown mode, bidir_from outside [0, max_rows], a
- * scale outside [-2^127, 2^127], q and out of two dtypes or overlapping, n_list < 1, group < 1, SHAPE for n_q_heads not a multiple of n_kv_heads, or
+ * scale outside [-2^127, 2^127], q and out of two dtypes or overlapping (they may lie in one array if they have the same strides), n_list < 1, group < 1, SHAPE for n_q_heads not a multiple of n_kv_heads, or
  * group * (n_q_heads / n_kv_heads) > 128. */
 nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chunk* chunk, const nld_heads* q, int32_t n_q_heads,
                             float scale, int32_t mode, int32_t bidir_from, const int32_t* list, int32_t n_list, int32_t group,

@@ -306,11 +306,6 @@ nld_status check_chunk(const nld_pages* c, const nld_chunk* ch) {
     return NLD_OK;
 }
 
-// elements from the first one to past the last one
-long long heads_extent(const nld_heads* x, int rows, int heads, int dim) {
-    return (rows - 1) * x->row_stride + (heads - 1) * x->head_stride + dim;
-}
-
 // out: rows and heads must be apart from each other
 nld_status check_heads(const nld_heads* x, const char* what, int rows, int heads, int dim, bool out) {
     if (!x || !x->data) return fail(NLD_ERR_INVALID_ARG, "%s or its data is NULL", what);
@@ -325,6 +320,26 @@ nld_status check_heads(const nld_heads* x, const char* what, int rows, int heads
             return fail(NLD_ERR_INVALID_ARG, "%s: its rows overlap each other", what);
     }
     return NLD_OK;
+}
+
+// Whether two arrays of rows of one type, the second without overlaps of its own, share an element.  Arrays of unlike strides: whether their
+// ranges meet.
+bool heads_overlap(const nld_heads* a, const nld_heads* b, int rows, int heads, int dim) {
+    typedef __int128 wide;   // (rows - 1) * stride alone is up to 2^62 elements
+    const int es = b->dtype == NLD_BF16 ? 2 : 4;
+    auto extent = [&](const nld_heads* x) { return (wide)(rows - 1) * x->row_stride + (wide)(heads - 1) * x->head_stride + dim; };
+    const wide apart = (wide)(uintptr_t)b->data - (wide)(uintptr_t)a->data;
+    if (apart >= extent(a) * es || -apart >= extent(b) * es) return false;
+    if ((rows > 1 && a->row_stride != b->row_stride) || (heads > 1 && a->head_stride != b->head_stride) || apart % es) return true;
+    const wide d = apart / es;
+    const long long rs = rows > 1 ? b->row_stride : 0, hs = heads > 1 ? b->head_stride : 0;
+    // an element of both: d = i * rs + j * hs + less than dim, with i rows and j heads between the two
+    for (int j = 1 - heads; j < heads; ++j) {
+        const wide rest = d - (wide)j * hs, i0 = rs ? rest / rs : 0;
+        for (wide i = i0 - 1; i <= i0 + 1; ++i)
+            if (i > -rows && i < rows && rest - i * rs < dim && rest - i * rs > -dim) return true;
+    }
+    return false;
 }
 
 HeadRows head_rows(const nld_heads* x) { return HeadRows{x->data, x->dtype == NLD_F32, 0, x->row_stride, x->head_stride}; }
@@ -1575,6 +1590,7 @@ nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk
     if (k->dtype != v->dtype || k->data == v->data) return fail(NLD_ERR_INVALID_ARG, "k and v must have one dtype and be apart");
     if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     if (ws_bytes < 256) return fail(NLD_ERR_CAPACITY, "workspace holds %zu bytes, this call needs 256", ws_bytes);
+    if (heads_overlap(k, v, chunk->rows, pages->n_kv_heads, pages->head_dim)) return fail(NLD_ERR_INVALID_ARG, "v overlaps k");
     if (((long long)(chunk->max_rows + 62) / 64 + 1) * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS)
         return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
     HIP_TRY(launch_pages_read(page_layer(pages, layer), head_rows(k), head_rows(v), page_chunk(chunk), first, at<uint32_t>(workspace, 0),
@@ -1594,12 +1610,7 @@ nld_status nld_pages_attend(const nld_pages* pages, int32_t layer, const nld_chu
     if (st != NLD_OK) return st;
     if (!(fabsf(scale) <= 0x1p127f)) return fail(NLD_ERR_INVALID_ARG, "scale must be in [-2^127, 2^127]");   // finite in base-2 exponents too
     if (q->dtype != out->dtype) return fail(NLD_ERR_INVALID_ARG, "q and out must have one dtype");
-    {
-        const size_t es = q->dtype == NLD_BF16 ? 2 : 4;
-        const char *q0 = (const char*)q->data, *q1 = q0 + heads_extent(q, chunk->rows, n_q_heads, pages->head_dim) * es;
-        const char *o0 = (const char*)out->data, *o1 = o0 + heads_extent(out, chunk->rows, n_q_heads, pages->head_dim) * es;
-        if (o0 < q1 && q0 < o1) return fail(NLD_ERR_INVALID_ARG, "out overlaps q");
-    }
+    if (heads_overlap(q, out, chunk->rows, n_q_heads, pages->head_dim)) return fail(NLD_ERR_INVALID_ARG, "out overlaps q");
     if (list) {
         st = check_group(pages, n_q_heads, group);
         if (st != NLD_OK) return st;

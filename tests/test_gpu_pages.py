@@ -251,6 +251,23 @@ def test_strides_and_alignment(pages, dtype, row_pad, head_pad, lead, heads_firs
         assert bool((buf == 77.0).all())
 
 
+@pytest.mark.parametrize("heads_apart", [False, True])
+def test_arrays_that_share_a_buffer(heads_apart):
+    """Queries and outputs, and keys and values read back, as the halves of every row, or of every head, of one tensor."""
+    s = Setup(BF16, 2, 64, [70, 3], [5, 66]).fill()
+    both = torch.full((71, 2, 4, 64), 7.0, dtype=BF16, device=DEV) if not heads_apart else torch.full((71, 4, 2, 64), 7.0, dtype=BF16, device=DEV).transpose(1, 2)
+    q, out = both[:, 0], both[:, 1]
+    q.copy_(randn((71, 4, 64), 5))
+    s.check(q.contiguous())
+    s.check(q, out=out)
+    assert torch.equal(q, randn((71, 4, 64), 5))
+    k, v = torch.zeros((71, 2, 2, 64), device=DEV).unbind(2 if heads_apart else 1)
+    R.read_pages(s.cache, 0, 71, s.workspace(2), first=s.cache.lengths, row_start=s.row_start, max_rows=66, outs=(k, v))
+    assert torch.equal(k[5:].double(), s.plain.k[1, 3:69]) and torch.equal(v[:5].double(), s.plain.v[0, 70:75])
+    with pytest.raises(C.NLDError, match="overlaps"):
+        R.read_pages(s.cache, 0, 71, s.workspace(2), row_start=s.row_start, outs=(k, k.as_strided(k.shape, k.stride(), k.storage_offset() + 32)))
+
+
 def test_rows_outside_the_sequences_stay_as_they_are():
     s = Setup(BF16, 2, 64, [10, 20], [3, 2]).fill()
     start = on_device([2, 5, 7])     # rows 0, 1 and 7, 8 belong to nobody

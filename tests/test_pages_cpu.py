@@ -106,6 +106,26 @@ def test_types_and_places_of_rows():
     assert "overlaps" in C.load().nld_last_error().decode()
 
 
+def test_rows_of_one_array():
+    """6 rows of 4 heads of 64: 256 elements of a row of 512, or every second piece of 64.  What passes is refused for its workspace."""
+    for apart, row, head, ok in ((256, 512, 64, True), (255, 512, 64, False), (257, 512, 64, False), (-256, 512, 64, True), (-255, 512, 64, False),
+                                 (512 * 2 + 256, 512, 64, True), (512 * 2 + 255, 512, 64, False), (512 * 5, 512, 64, False), (512 * 6, 512, 64, True),
+                                 (512 * 5 + 256, 512, 64, True), (64, 512, 128, True), (63, 512, 128, False), (65, 512, 128, False), (448, 512, 128, True),
+                                 (-64, 512, 128, True), (64 + 512 * 3, 512, 128, True), (64, 128, 128 * 6, True), (64 + 128 * 6, 128, 128 * 6, True),
+                                 (128 * 6, 128, 128 * 6, False)):
+        got = attend(q=heads(1 << 20, row=row, head=head), out=heads((1 << 20) + 2 * apart, row=row, head=head), ws_bytes=0)
+        assert got == (CAPACITY if ok else INVALID), (apart, row, head)
+    assert attend(q=heads(P), out=heads(P + 2 * 256, row=1024), ws_bytes=0) == INVALID      # other strides
+    assert attend(q=heads(P), out=heads(P + 513), ws_bytes=0) == INVALID                    # between two elements
+    one = chunk(3, 1)                                                                       # strides of a single row or head count for nothing
+    assert attend(p=pages(batch=1), ch=chunk(1, 1), q=heads(row=7), out=heads(P + 2 * 256, row=9), ws_bytes=0) == CAPACITY
+    assert attend(p=pages(n_kv_heads=1), ch=one, n_q=1, q=heads(row=128, head=3), out=heads(P + 128, row=128, head=5), ws_bytes=0) == CAPACITY
+    # (1 << 20) x 16 pages are too many for one launch: the check behind that of the rows
+    many = dict(p=pages(batch=1 << 20, n_kv_heads=16), ch=chunk(1 << 20, 1), k=heads(row=2048))
+    assert read(v=heads(P + 2 * 1024, row=2048), **many) == SHAPE and read(v=heads(P + 2 * 1023, row=2048), **many) == INVALID
+    assert read(v=heads(P + 2 * 2048 * 77, row=2048), **many) == INVALID and "overlaps" in C.load().nld_last_error().decode()
+
+
 @pytest.mark.parametrize("call", [attend, select])
 def test_attention_arguments(call):
     for kw, status in ((dict(n_q=0), SHAPE), (dict(n_q=3), SHAPE), (dict(n_q=-2), SHAPE), (dict(mode=2), INVALID), (dict(mode=-1), INVALID),
