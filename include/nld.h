@@ -581,7 +581,8 @@ nld_status nld_pages_verify_accept(const nld_model* m, const nld_pages* pages, c
  * those events and returns, per kernel class, the summed milliseconds and the
  * number of class instances since the last read (host arrays of length n >=
  * NLD_TRACE_CLASSES), then clears the record.  An instance is one step of the
- * pass: the attention class holds the attention and merge kernels, the O
+ * pass: the attention class holds the attention and merge kernels (over pages
+ * also the writing of the block's rows and the selection), the O
  * projection class also the LoRA down-projection when an adapter runs. */
 #define NLD_TRACE_EMBED 0
 #define NLD_TRACE_QKV 1

@@ -42,8 +42,6 @@
 
 #include "nld_internal.h"
 
-#include <hip/hip_ext.h>
-
 #include <math.h>
 
 namespace nld {
@@ -63,16 +61,6 @@ __device__ unsigned long long g_timeline[8][8192][8];
 #define NLD_TS(cls, ph) do { } while (0)
 #endif
 enum TimelineClass { TL_QKV = 0, TL_ATTENTION = 1, TL_COMBINE = 2, TL_GATE_UP = 3, TL_O = 4, TL_DOWN = 5, TL_LM = 6 };
-
-// Every kernel launch goes through here: a plain launch, or, while launch tracing is on,
-// a launch whose start and stop events are recorded on the dispatch itself.
-template <typename... KArgs, typename... Args>
-static void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t s, Args... args) {
-    hipEvent_t e0, e1;
-    if (trace_launch_events(&e0, &e1)) hipExtLaunchKernelGGL(kernel, grid, block, 0, s, e0, e1, 0, args...);
-    else kernel<<<grid, block, 0, s>>>(args...);
-}
-
 
 static constexpr uint32_t DEV_BAD_TOKEN = 0x1u;
 static constexpr uint32_t DEV_CAPACITY = 0x2u;

@@ -2,6 +2,7 @@
 // gfx950 (CDNA4) only: 64-wide wavefronts, v_mfma_f32_16x16x32_bf16.
 #pragma once
 
+#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -457,6 +458,15 @@ struct PagesSelectArgs {
 // While tracing is on, returns true with a fresh pair of events for the next launch, which
 // then records them on its own dispatch (start and end of the kernel itself).
 bool trace_launch_events(hipEvent_t* start, hipEvent_t* stop);
+
+// Every kernel launch of a pass goes through here: a plain launch, or, while launch tracing is on,
+// a launch whose start and stop events are recorded on the dispatch itself.
+template <typename... KArgs, typename... Args>
+static void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t s, Args... args) {
+    hipEvent_t e0, e1;
+    if (trace_launch_events(&e0, &e1)) hipExtLaunchKernelGGL(kernel, grid, block, 0, s, e0, e1, 0, args...);
+    else kernel<<<grid, block, 0, s>>>(args...);
+}
 
 // ---------------------------------------------------------------- launchers (kernels.hip)
 hipError_t launch_pack(const PackArgs& a, hipStream_t s);

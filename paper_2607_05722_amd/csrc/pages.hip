@@ -1782,7 +1782,7 @@ hipError_t launch_pages_write(const PageCache& c, const HeadRows& k, const HeadR
     const KvSource src{with_vec(k), with_vec(v), blk_k, blk_v};
     const int touched = pages_touched(ch.max_rows);
     return by_type(c, [&](auto d, auto e) {
-        pages_write_kernel<decltype(d)::value, decltype(e)::value><<<c.batch * touched * c.n_kv_heads, 256, 0, s>>>(c, src, ch, touched, status);
+        launch(pages_write_kernel<decltype(d)::value, decltype(e)::value>, dim3(c.batch * touched * c.n_kv_heads), dim3(256), s, c, src, ch, touched, status);
         return hipGetLastError();
     });
 }
@@ -1791,8 +1791,8 @@ hipError_t launch_pages_read(const PageCache& c, const HeadRows& k, const HeadRo
                              hipStream_t s) {
     const int touched = pages_touched(ch.max_rows);
     return by_type(c, [&](auto d, auto e) {
-        pages_read_kernel<decltype(d)::value, decltype(e)::value>
-            <<<c.batch * touched * c.n_kv_heads, 256, 0, s>>>(c, with_vec(k), with_vec(v), ch, first, touched, status);
+        launch(pages_read_kernel<decltype(d)::value, decltype(e)::value>, dim3(c.batch * touched * c.n_kv_heads), dim3(256), s, c, with_vec(k), with_vec(v), ch, first,
+               touched, status);
         return hipGetLastError();
     });
 }
@@ -1805,9 +1805,9 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         constexpr bool E = decltype(e)::value;
         auto run = [&](auto nq) {
             constexpr int NQ = decltype(nq)::value;
-            if (a.shared_waves) pages_attend_shared_kernel<D, E, NQ><<<a.grid, a.shared_waves * 64, 0, s>>>(a);
-            else if (a.block_rows == 16) pages_attend_kernel<D, E, NQ, 16><<<a.grid, 256, 0, s>>>(a);
-            else pages_attend_kernel<D, E, NQ, 32><<<a.grid, 256, 0, s>>>(a);
+            if (a.shared_waves) launch(pages_attend_shared_kernel<D, E, NQ>, dim3(a.grid), dim3(a.shared_waves * 64), s, a);
+            else if (a.block_rows == 16) launch(pages_attend_kernel<D, E, NQ, 16>, dim3(a.grid), dim3(256), s, a);
+            else launch(pages_attend_kernel<D, E, NQ, 32>, dim3(a.grid), dim3(256), s, a);
         };
         if (a.q_split) run(std::integral_constant<int, 2>());
         else if (a.q.f32) run(std::integral_constant<int, 3>());
@@ -1815,8 +1815,8 @@ hipError_t launch_pages_attend(const PagesAttnArgs& args, hipStream_t s) {
         const hipError_t st = hipGetLastError();
         if (st != hipSuccess) return st;
         const int wgs = a.n_entries * a.c.n_kv_heads * a.slices;
-        if (a.shared_waves || E) pages_combine_kernel<D, 64><<<wgs, 256, 0, s>>>(a);
-        else pages_combine_kernel<D, 32><<<wgs, 256, 0, s>>>(a);
+        if (a.shared_waves || E) launch(pages_combine_kernel<D, 64>, dim3(wgs), dim3(256), s, a);
+        else launch(pages_combine_kernel<D, 32>, dim3(wgs), dim3(256), s, a);
         return hipGetLastError();
     });
 }
@@ -1832,17 +1832,17 @@ hipError_t launch_pages_select(const PagesSelectArgs& args, hipStream_t s) {
     // NLD_SELECT_ONE overrides.
     const bool one = a.c.max_pages <= SELECT_PAGES && env_int("NLD_SELECT_ONE", a.c.max_pages <= 256 || units >= 256);
     if (one) {
-        if (a.c.head_dim == 64) pages_select_kernel<64><<<units, 512, 0, s>>>(a);
-        else pages_select_kernel<128><<<units, 512, 0, s>>>(a);
+        if (a.c.head_dim == 64) launch(pages_select_kernel<64>, dim3(units), dim3(512), s, a);
+        else launch(pages_select_kernel<128>, dim3(units), dim3(512), s, a);
         return hipGetLastError();
     }
     if (a.n_top > 0) {
-        if (a.c.head_dim == 64) pages_score_kernel<64><<<units * a.chunks, 256, 0, s>>>(a);
-        else pages_score_kernel<128><<<units * a.chunks, 256, 0, s>>>(a);
+        if (a.c.head_dim == 64) launch(pages_score_kernel<64>, dim3(units * a.chunks), dim3(256), s, a);
+        else launch(pages_score_kernel<128>, dim3(units * a.chunks), dim3(256), s, a);
         const hipError_t st = hipGetLastError();
         if (st != hipSuccess) return st;
     }
-    pages_pick_kernel<<<units, 512, 0, s>>>(a);
+    launch(pages_pick_kernel, dim3(units), dim3(512), s, a);
     return hipGetLastError();
 }
 

@@ -185,6 +185,31 @@ def test_self_speculation_in_8_bits_captured(tiny):
     assert R.read_device_status(state[0]["ws"]) == 0 and state[0]["cache"].lengths.tolist()[0] >= 206
 
 
+@pytest.mark.parametrize("sparse", [None, (2, 1, 4)])
+def test_a_traced_pass_has_its_attention(tiny, sparse):
+    """One instance of the attention class per layer, with the time of its kernels; a pass is the same with tracing on."""
+    shape, _, model = tiny
+    both = Both(shape, BF16, 2, 512, bounds=True)
+    prefill(tiny, both, [400, 75])
+    ws, toks = R.PagedPassWorkspace(model, both.cache, 4, sparse), ids(shape, "block", 2, 4)
+    want, _ = R.block_forward(model, both.cache, ws, toks, R.VERIFY, sparse=sparse)
+    lib, n = C.load(), len(C.TRACE_CLASSES)
+    ms, counts = (ctypes.c_float * n)(), (ctypes.c_int32 * n)()
+    torch.cuda.synchronize()
+    lib.nld_trace_enable(1)
+    try:
+        got, _ = R.block_forward(model, both.cache, ws, toks, R.VERIFY, sparse=sparse)
+        R.write_pages(both.cache, 0, *(torch.zeros((8, shape.n_kv_heads, shape.head_dim), device="cuda") for _ in range(2)),
+                      R.PagesWorkspace(both.cache, shape.n_q_heads, 4))       # not a pass: not recorded
+        torch.cuda.synchronize()
+        C.check(lib.nld_trace_read(ms, counts, n))
+    finally:
+        lib.nld_trace_enable(0)
+    by = {name: (counts[i], ms[i]) for i, name in enumerate(C.TRACE_CLASSES)}
+    assert by["attention"][0] == shape.n_layers and by["attention"][1] > 0.0, by
+    assert by["qkv"][0] == shape.n_layers and torch.equal(got, want)
+
+
 def test_the_drafters_loss_over_pages(tiny):
     shape, _, model = tiny
     both = Both(shape, BF16, 1, 256)
