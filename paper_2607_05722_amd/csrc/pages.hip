@@ -545,6 +545,7 @@ struct Walk {
     long long before;     // steps of the entries before e
     long long per_head, live;
     bool first_unit;
+    bool odd, careful;    // the present unit has sums that are not finite; it is worked on a second time
 };
 
 // inclusive sum over the workgroup's threads, and over all of them
@@ -594,6 +595,7 @@ __device__ __forceinline__ bool walk_start(const PagesAttnArgs& a, Walk* w, long
     if (threadIdx.x == 0) {
         w->e = a.n_entries;
         w->h = h, w->share = share, w->at = first, w->last = sh.begin(share + 1), w->per_head = per_head, w->live = live, w->first_unit = true;
+        w->odd = w->careful = false;
     }
     // the entry that holds step s of its KV head
     __syncthreads();
@@ -621,7 +623,7 @@ __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirst
 struct Unit {
     Entry en;
     int h, s0, s1, slot;   // KV head; steps [s0, s1) are this workgroup's; place of its part
-    bool whole;
+    bool whole, careful;
 };
 __device__ __forceinline__ Unit walk_unit(const Walk& w) {
     Unit u;
@@ -633,6 +635,7 @@ __device__ __forceinline__ Unit walk_unit(const Walk& w) {
     u.s1 = scalar((int)min(w.last - unit0, (long long)e.steps));
     u.slot = 2 * scalar(w.share) + (scalar(w.first_unit) ? 0 : 1);
     u.whole = u.s0 == 0 && u.s1 == u.en.steps;
+    u.careful = scalar(w.careful) != 0;
     return u;
 }
 
@@ -650,11 +653,14 @@ __device__ __forceinline__ void note_parts(const PagesAttnArgs& a, const Walk& w
     a.parts[(size_t)w.e * a.c.n_kv_heads + u.h] = uint2{(uint32_t)w0 | (later ? 0x80000000u : 0u), (uint32_t)n};
 }
 
-// On to the next unit; false behind the last.  Called by every thread after it has read what it needs of the present one.
+// On to the next unit, or to a second pass over this one; false behind the last.  Called by every thread after it has read what it needs of the present one.
 template <int STEP>
 __device__ __forceinline__ bool walk_next(const PagesAttnArgs& a, Walk* w) {
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && w->odd && !w->careful) {
+        w->careful = true;
+    } else if (threadIdx.x == 0) {
+        w->odd = w->careful = false;
         w->at = w->h * w->per_head + w->before + w->en.steps;
         w->first_unit = false;
         w->before += w->en.steps;
@@ -698,7 +704,11 @@ __device__ __forceinline__ void finish_row(const PagesAttnArgs& a, int b, int r0
 // split likewise), so that P V is as exact as the f32 sums.  A unit's wavefronts meet in LDS at its end.
 // Positions that a row does not see have weight 0; a value there that is not finite must not reach the row, and 0 times it
 // would: in steps that some row of the tile does not see whole, values behind every row's last position count as 0, and any
-// other that is not finite is left out of the product and added to the rows that see it.
+// other that is not finite is left out of the product and added to the rows that see it.  In the other steps nobody looks: such a value
+// leaves the sums not finite, infinite ones as NaN, since a weight's smaller pieces may be 0 or negative.  Sums that are not finite
+// at the end are worked out once more (`careful`), with all values looked at as above, and infinite keys kept from the queries' smaller
+// pieces likewise.  So an infinite value comes out as what it is wherever it stands, and a score of -inf has weight 0.  8-bit pages hold no
+// infinity, and their NaN comes out as NaN at once.
 template <int RW>
 struct Tile;
 template <>
@@ -745,6 +755,54 @@ __device__ __forceinline__ void rescale(float top, float* m, float* l, Acc (&o)[
 }
 __device__ __forceinline__ float weight(float score, float scale_log2, float ref) { return __builtin_amdgcn_exp2f(__builtin_fmaf(score, scale_log2, -ref)); }
 
+// Puts 0 in the place of those of eight bf16 numbers that are not finite; whether there were any.
+__device__ __forceinline__ bool only_finite(uint4* x) {
+    uint32_t w[4] = {x->x, x->y, x->z, x->w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
+        if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
+    }
+    const bool some = ((w[0] ^ x->x) | (w[1] ^ x->y) | (w[2] ^ x->z) | (w[3] ^ x->w)) != 0u;
+    *x = uint4{w[0], w[1], w[2], w[3]};
+    return some;
+}
+template <typename Acc, int N>
+__device__ __forceinline__ bool any_not_finite(const Acc (&o)[N]) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < (int)(sizeof(Acc) / 4); ++r) t = __builtin_fmaf(o[i][r], 0.0f, t);   // NaN, once one is not finite
+    return __any(t != t);
+}
+
+// Adds to a lane's scores x what bf16 keys that are not finite give them, with whole queries.
+template <int D, int NQ, int N, typename F>
+__device__ __forceinline__ void add_not_finite_keys(const PagesAttnArgs& a, float (&x)[N], F key_of, const uint16_t* keys, int first, const Entry& en, int h, int t,
+                                                    int g, bool have) {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d) {
+            const float k = bf16_to_f32(keys[key_at<D, false>(first + key_of(i), d)]);
+            if (finite(k) || !have) continue;
+            float q;
+            if constexpr (NQ == 2) {
+                const uint16_t* p = a.q_split + q_index(en.b * a.c.n_kv_heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                q = bf16_to_f32(p[0]) + bf16_to_f32(p[SPLIT_LO]);
+            } else {
+                q = ((const float*)a.q.data)[(en.r0 + t) * a.q.row_stride + (h * a.group_heads + g) * a.q.head_stride + d];
+                if (a.negate) q = -q;
+            }
+            sum += q * k;
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] += j == i ? sum : 0.0f;
+    }
+}
+
 template <int D, bool E4M3, int RW>
 __device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const void* values, int base, int lane, int sees, int most) {
     using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
@@ -781,6 +839,7 @@ pages_attend_kernel(PagesAttnArgs a) {
     constexpr int NF = SR / 8;                   // eights of weights: one operand each
     constexpr int DT = D / RW;
     constexpr int PITCH = D + 4;
+    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // infinite keys are worked on apart
     __shared__ __align__(16) float so[4][RW][PITCH];
     __shared__ float sml[4][RW][2];
     __shared__ long long lds[4];
@@ -801,7 +860,7 @@ pages_attend_kernel(PagesAttnArgs a) {
         const Unit unit = walk_unit(walk);
         const Entry& en = unit.en;
         const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
-        const bool whole = unit.whole;
+        const bool whole = unit.whole, careful = !E4M3 && unit.careful;
 
         // this wavefront's rows
         const int myrow = en.rows0 + row;
@@ -921,6 +980,10 @@ pages_attend_kernel(PagesAttnArgs a) {
 
         while (more) {
             float x[SR];
+            bool odd_keys = false;
+            if (PIECES_OF_KEYS && careful)
+#pragma unroll
+                for (int i = 0; i < NL; ++i) odd_keys |= only_finite(&kf[i]);
 #pragma unroll
             for (int i = 0; i < STEP / RW; ++i) {   // tiles of RW keys
                 typename T::Acc sc;
@@ -943,7 +1006,8 @@ pages_attend_kernel(PagesAttnArgs a) {
 #pragma unroll
                 for (int r = 0; r < T::REGS; ++r) x[i * T::REGS + r] = sc[r];
             }
-            const bool masked = cur_base + STEP > least;
+            if (PIECES_OF_KEYS && __any(odd_keys)) add_not_finite_keys<D, NQ>(a, x, key_of, (const uint16_t*)a.c.k + cur_head * 64 * D, cur_base & 63, en, h, t, g, have);
+            const bool masked = careful || cur_base + STEP > least;
             more = next();
             if (more) load_k(head, base);
 
@@ -1041,6 +1105,7 @@ pages_attend_kernel(PagesAttnArgs a) {
             for (int j = 0; j < T::REGS / 4; ++j)
                 *(float4*)&so[wave][row][dt * RW + T::out_dim(lane, 4 * j)] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
         if (part == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
+        if (!E4M3 && any_not_finite(o) && lane == 0) walk.odd = true;
         __syncthreads();
         for (int i = tid; i < RW * (D / 4); i += 256) {
             const int r = i / (D / 4), d = i % (D / 4) * 4, rw = en.rows0 + r;
@@ -1110,6 +1175,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
     constexpr bool DEEP = pages_raw(NQ, E4M3);
+    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // infinite keys are worked on apart
     constexpr int RAW = DEEP ? 3 : 0;
     constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
     __shared__ __align__(16) uint4 stage[2][2][HALF];   // [buffer][keys, values]
@@ -1129,7 +1195,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
         const Unit unit = walk_unit(walk);
         const Entry& en = unit.en;
         const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
-        const bool whole = unit.whole;
+        const bool whole = unit.whole, careful = !E4M3 && unit.careful;
 
         const int r = rt * 32 + row, myrow = en.rows0 + r;
         const bool have = myrow < en.rows1;
@@ -1292,7 +1358,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             // Whether there were any of these.
             auto clean = [&](int j, int buf) -> bool {
                 const int page0 = scalar(pg_base[j]);
-                if (page0 + 64 <= begins) return false;
+                if (!careful && page0 + 64 <= begins) return false;
 #pragma unroll 1
                 for (int i = tid; i < HALF; i += blockDim.x) {
                     const int pos = page0 + i / (QS * 64) * 32;
@@ -1355,16 +1421,29 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                     const int base = page0 + kt * 32;
                     if (base >= most) break;
                     f32x16_t x;
+                    bool odd_keys = false;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = 0.0f;
 #pragma unroll
                     for (int s0 = 0; s0 < QS; s0 += CH) {
                         if (!AHEAD) load_keys(kt, s0);
                         __builtin_amdgcn_sched_barrier(0);
+                        if (PIECES_OF_KEYS && careful)
+#pragma unroll
+                            for (int s = 0; s < CH; ++s) odd_keys |= only_finite(&kf[s]);
 #pragma unroll
                         for (int s = 0; s < CH; ++s)
 #pragma unroll
                             for (int p = NQ - 1; p >= 0; --p) x = T::mfma(kf[s], q[p][s0 + s], x);
+                    }
+                    if (PIECES_OF_KEYS && __any(odd_keys)) {
+                        float y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[i] = x[i];
+                        add_not_finite_keys<D, NQ>(a, y, [&](int i) { return value_key(i >> 3, hf, i & 7); },
+                                                   (const uint16_t*)a.c.k + ((size_t)pg_id[j] * heads + h) * 64 * D, kt * 32, en, h, t, g, have);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = y[i];
                     }
                     // values: step s of dims dt at 2 dt + s; all at once, or a step's
                     auto load_values = [&](int s) {
@@ -1420,6 +1499,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             }
             __syncthreads();   // the window, and the last stage, have been read
         }
+        if (!E4M3 && any_not_finite(o) && lane == 0) walk.odd = true;
 
         l_run += __shfl_xor(l_run, 32);
         if (a.key_halves == 2) {   // the second half's sums go to the first's wavefront, through the stages' place

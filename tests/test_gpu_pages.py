@@ -400,6 +400,67 @@ def test_values_not_finite_of_both_signs():
     assert bool(torch.isfinite(out[:, 0, :5]).all())
 
 
+TILES = [(1, 4, 1), (8, 8, 2), (40, 4, 2), (80, 8, 2)]     # rows, query heads, KV heads: a tile of 16, one of 32, several with two halves, eight
+
+
+@pytest.mark.parametrize("n,q_heads,kv_heads", TILES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinite_values_wherever_they_stand(n, q_heads, kv_heads, dim, dtype):
+    """Values among the first, middle and last committed rows and the new ones: each row that sees one has it in that dim, both signs
+    make NaN, and all other numbers are those of the same call without them, bit for bit."""
+    lens, news = [300, 1900], [n, n]
+    k, v, kn, vn = (randn((m, kv_heads, dim), i, BF16) for i, m in ((1, 2200), (2, 2200), (3, 2 * n), (4, 2 * n)))
+    q = randn((2 * n, q_heads, dim), 5, dtype)
+    got = []
+    at = [(0, INF, 3), (130, -INF, 4), (299, INF, 5), (17, INF, 6), (250, -INF, 6), (300, NAN, 8), (1500, INF, 9), (2199, -INF, 10)]   # row, value, dim
+    G, H = q_heads // kv_heads, kv_heads - 1
+    for odd in (True, False):
+        v2, vn2 = v.clone(), vn.clone()
+        if odd:
+            for row, bad, d in at:
+                v2[row, H, d] = bad
+            vn2[0, H, 12] = INF
+        s = Setup(BF16, kv_heads, dim, lens, news)
+        s.write([0, 0], lens, k, v2)
+        s.write(lens, news, kn, vn2)
+        got.append(R.attend_pages(s.cache, 0, q, s.workspace(q_heads), row_start=s.row_start, max_rows=n, want_lse=True))
+    (out, lse), (clean, lse2) = got
+    want = clean.clone()
+    hs = slice(H * G, (H + 1) * G)
+    for d, bad in ((3, INF), (4, -INF), (5, INF), (6, NAN), (12, INF)):
+        want[:n, hs, d] = bad
+    for d, bad in ((8, NAN), (9, INF), (10, -INF)):
+        want[n:, hs, d] = bad
+    same = (out == want) | (torch.isnan(out) & torch.isnan(want))
+    assert bool(same.all()), (~same).nonzero()[:5].tolist()
+    assert torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("n,q_heads,kv_heads", TILES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinite_keys(n, q_heads, kv_heads, dim, dtype):
+    """A score of -inf has weight 0: the row is that of a key of -1e30 there, bit for bit; one of +inf makes it NaN."""
+    lens, news = [300, 1900], [n, n]
+    k, v, kn, vn = (randn((m, kv_heads, dim), i, BF16) for i, m in ((1, 2200), (2, 2200), (3, 2 * n), (4, 2 * n)))
+    q = randn((2 * n, q_heads, dim), 5, dtype)
+    q[..., 7] += torch.where(q[..., 7] >= 0, 0.5, -0.5).to(dtype)
+    G, got = q_heads // kv_heads, []
+    for bad in (INF, 1e30):
+        for row in (70, 900):
+            k[row, :, 7] = -bad
+        s = Setup(BF16, kv_heads, dim, lens, news)
+        s.write([0, 0], lens, k, v)
+        s.write(lens, news, kn, vn)
+        got.append(R.attend_pages(s.cache, 0, q, s.workspace(q_heads), row_start=s.row_start, max_rows=n, want_lse=True))
+    (out, lse), (clean, lse2) = got
+    fine = q[..., 7] > 0
+    assert bool(fine.any()) and bool((~fine).any())
+    assert torch.equal(out[fine], clean[fine]) and torch.equal(lse[fine], lse2[fine])
+    assert bool(torch.isnan(out[~fine]).all()) and bool(torch.isnan(lse[~fine]).all())
+
+
 def test_large_scores_and_queries_not_finite():
     s = Setup(BF16, 1, 64, [100], [4])
     k = randn((100, 1, 64), 1, BF16, 100.0)
