@@ -381,8 +381,17 @@ bool plan_pages(int batch, int n_kv_heads, int head_dim, int group_heads, int ma
     return true;
 }
 
+long long select_units(const nld_pages* c, int max_rows, int group) { return (long long)c->batch * cdiv(max_rows, group) * c->n_kv_heads; }
+
+// Room for the scores of two launches.  So many units that one launch takes them have scores of their own in LDS; fewer of them may take two.
 size_t score_bytes(const nld_pages* c, int max_rows, int group) {
-    return (size_t)c->batch * cdiv(max_rows, group) * c->n_kv_heads * c->max_pages * 4;
+    const long long units = select_units(c, max_rows, group);
+    return (size_t)(select_in_one(c->max_pages, units) ? std::min<long long>(units, SELECT_UNITS - 1) : units) * c->max_pages * 4;
+}
+
+bool select_fits(const nld_pages* c, int max_rows, int group) {
+    const long long units = select_units(c, max_rows, group);
+    return units * (select_in_one(c->max_pages, units) ? 1 : cdiv(c->max_pages, SCORE_PAGES)) <= MAX_PAGE_WGS;
 }
 
 nld_status check_mode(int mode, int bidir_from, int max_rows) {
@@ -518,7 +527,7 @@ nld_status validate_paged(const nld_model* m, const nld_pages* pages, const nld_
         p.n_groups = cdiv(k, p.group);
         p.n_list = nld_pages_list_len(k, p.group, p.n_top, p.n_first, mode);
         if (p.n_list < 1) return fail(NLD_ERR_INVALID_ARG, "n_top and n_first must be in [0, %d]", MAX_SEQ_PAGES);
-        if ((long long)pages->batch * p.n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 128) > MAX_PAGE_WGS)
+        if (!select_fits(pages, k, p.group))
             return fail(NLD_ERR_SHAPE, "%d sequences are too many for one call", pages->batch);
     }
     if (2LL * pages->batch * pages->n_kv_heads > MAX_PAGE_WGS || !plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, k, p.group, pages_raw(2, pages->dtype == NLD_E4M3), &p.plan))
@@ -1649,8 +1658,7 @@ nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chu
     const int need = nld_pages_list_len(chunk->max_rows, group, n_top, n_first, mode);
     if (need < 1) return fail(NLD_ERR_SHAPE, "n_top (%d) or n_first (%d) exceeds %d", n_top, n_first, MAX_SEQ_PAGES);
     if (n_list < need) return fail(NLD_ERR_INVALID_ARG, "n_list is %d, this call needs %d", n_list, need);
-    const int n_groups = cdiv(chunk->max_rows, group);
-    if ((long long)pages->batch * n_groups * pages->n_kv_heads * cdiv(pages->max_pages, 128) > MAX_PAGE_WGS)
+    if (!select_fits(pages, chunk->max_rows, group))
         return fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, chunk->max_rows);
     if (!workspace) return fail(NLD_ERR_INVALID_ARG, "workspace is NULL");
     const size_t bytes = align256(256 + (n_top ? score_bytes(pages, chunk->max_rows, group) : 0));
@@ -1665,7 +1673,7 @@ nld_status nld_pages_select(const nld_pages* pages, int32_t layer, const nld_chu
     a.n_top = n_top;
     a.n_first = n_first;
     a.group = group;
-    a.n_groups = n_groups;
+    a.n_groups = cdiv(chunk->max_rows, group);
     a.n_list = n_list;
     a.scores = at<float>(workspace, 256);
     a.list = list;

@@ -442,6 +442,17 @@ struct PagesAttnArgs {
 __host__ __device__ constexpr bool pages_raw(int pieces, bool e4m3) { return pieces > 1 && e4m3; }
 constexpr int PAGES_GROUP_ROWS = 128;   // rows (tokens x query heads of a KV head) that share a list of pages
 
+constexpr int SCORE_PAGES = 128;    // pages per workgroup of the scores alone: 4 wavefronts of 32
+constexpr int SELECT_PAGES = 4096;  // pages that one workgroup scores and picks from, with their scores in LDS
+constexpr int SELECT_UNITS = 256;   // units (groups x KV heads) that fill the card
+// Selection in one launch where its workgroups fill the card, or have few pages each.  One against two launches: 2048 units of 136 pages 50 against 65
+// us, 256 units of 257 pages 9.8 against 13.1; but 8 units of 1025 pages 17.2 against 13.5, and selection and attention of 64 units of 1025
+// pages 58.3 against 55.1, of 32 units of 2049 75 against 63: there one workgroup reads the bounds of all of a unit's pages.
+// NLD_SELECT_ONE overrides.
+inline bool select_in_one(int max_pages, long long units) {
+    return max_pages <= SELECT_PAGES && env_int("NLD_SELECT_ONE", max_pages <= 256 || units >= SELECT_UNITS);
+}
+
 struct PagesSelectArgs {
     PageCache c;
     PageChunk ch;

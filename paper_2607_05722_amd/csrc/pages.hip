@@ -1607,8 +1607,6 @@ __device__ __forceinline__ Group group_of(const PagesSelectArgs& a, int b, int g
     return g;
 }
 
-constexpr int SCORE_PAGES = 128;    // pages per workgroup of the scores alone: 4 wavefronts of 32
-constexpr int SELECT_PAGES = 4096;  // pages that one workgroup scores and picks from, with their scores in LDS
 
 // A group's rows of one KV head as 8-bit operands: 8 dims per thread, a row's threads adjacent.  Rows up to a multiple of 32.
 template <int D>
@@ -1906,12 +1904,7 @@ hipError_t launch_pages_select(const PagesSelectArgs& args, hipStream_t s) {
     a.q = with_vec(a.q);
     a.chunks = cdiv(a.c.max_pages, SCORE_PAGES);
     const int units = a.c.batch * a.n_groups * a.c.n_kv_heads;
-    // One launch where its workgroups fill the card, or have few pages each.  One against two launches: 2048 units of 136 pages 50 against 65
-    // us, 256 units of 257 pages 9.8 against 13.1; but 8 units of 1025 pages 17.2 against 13.5, and selection and attention of 64 units of 1025
-    // pages 58.3 against 55.1, of 32 units of 2049 75 against 63: there one workgroup reads the bounds of all of a unit's pages.
-    // NLD_SELECT_ONE overrides.
-    const bool one = a.c.max_pages <= SELECT_PAGES && env_int("NLD_SELECT_ONE", a.c.max_pages <= 256 || units >= 256);
-    if (one) {
+    if (select_in_one(a.c.max_pages, units)) {
         if (a.c.head_dim == 64) launch(pages_select_kernel<64>, dim3(units), dim3(512), s, a);
         else launch(pages_select_kernel<128>, dim3(units), dim3(512), s, a);
         return hipGetLastError();

@@ -706,6 +706,26 @@ def test_selection_of_the_first_and_own_pages_alone(monkeypatch, launches, width
                 assert got[b, j].tolist() == [want + [-1] * (got.shape[3] - len(want))] * 2
 
 
+def test_a_workspace_serves_selections_in_one_launch_and_in_two():
+    """300 units take one launch and room for 255 units' scores; 255, 254 and 100 of them take two, in the same workspace."""
+    s = Setup(BF16, 1, 64, [64 * 300], [300]).fill()
+    q = randn((300, 2, 64), 5)
+    ws = s.workspace(2, 300, 1)
+    ids = s.cache.table[0, :304].long()
+    bd, bs = s.cache.bounds[0][ids, 0].double(), s.cache.bound_scale[0][ids, 0]
+    qs = ref.over_127(q.float().abs().amax(-1))
+    qi = torch.round(q.float() / qs[..., None]).double()
+    score = torch.cat([torch.clamp(qi, max=0.0), torch.clamp(qi, min=0.0)], -1) @ torch.cat([bd[:, 0], bd[:, 1]], -1).T     # whole numbers
+    score = (score.float() * qs[..., None]).amax(1) * bs
+    for n in (300, 256, 255, 254, 100):
+        got = R.select_pages(s.cache, 0, q[:n], ws, 6)[0, :, 0].tolist()
+        assert R.read_device_status(ws) == 0
+        for i in range(n):
+            own = (64 * 300 + i) // 64
+            best = torch.sort(score[i, 1:own], descending=True, stable=True)[1][:6] + 1
+            assert got[i] == sorted(best.tolist() + [0, own]), (n, i)
+
+
 # ------------------------------------------------------------------------------------------ together, as they are used
 @pytest.mark.parametrize("pages", [BF16, E4M3])
 def test_a_prompt_then_decoding_by_selected_pages(pages):

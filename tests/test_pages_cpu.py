@@ -194,6 +194,22 @@ def test_workspace_bytes():
     assert f(pages(), 4, 100, 0) <= f(pages(), 4, 100, 1)
 
 
+def test_scores_of_a_selection_in_one_launch(monkeypatch):
+    """Where there are 256 units and more of up to 4096 pages the scores need no workspace, and the launch has a workgroup per unit."""
+    monkeypatch.delenv("NLD_SELECT_ONE", raising=False)
+    f = lambda p, *a: C.load().nld_pages_workspace_bytes(ref_of(p), *a)
+    p = full(batch=64, n_kv_heads=8, max_pages=1024)
+    units = 64 * 2048 * 8
+    assert f(p, 32, 2048, 1) <= f(p, 32, 2048, 0) + 255 * 1024 * 4 + 8 * units + 512
+    assert f(p, 32, 1, 1) >= 255 * 1024 * 4 and f(full(batch=64, n_kv_heads=8, max_pages=4097), 32, 2048, 1) >= units * 4097 * 4
+    n = 1 << 14
+    many = dict(ch=chunk(64 * n, n), n_q=8, q=heads(row=512), ws_bytes=0)
+    assert select(p=p, **many) == CAPACITY
+    assert select(p=full(batch=64, n_kv_heads=8, max_pages=4097), **many) == SHAPE
+    monkeypatch.setenv("NLD_SELECT_ONE", "0")
+    assert select(p=p, **many) == SHAPE and f(p, 32, 2048, 1) >= units * 1024 * 4
+
+
 # ------------------------------------------------------------------------------------------ the binding
 def cpu_cache(**kw):
     return R.PagedCache(2, 64, 2, 128, device="cpu", **kw)
