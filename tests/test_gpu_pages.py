@@ -323,6 +323,24 @@ def test_long_sequences_meet_from_many_workgroups(pages, dtype):
     s.check(randn((3, 8, 64), 5, dtype, 2.0))
 
 
+@pytest.mark.parametrize("cus", [1, 3])
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,q_heads,dim", [(1, 4, 64), (2, 8, 128), (7, 8, 64), (8, 8, 128), (20, 8, 64), (20, 8, 128), (70, 8, 64)])
+def test_few_workgroups_with_long_shares(monkeypatch, cus, pages, dtype, n, q_heads, dim):
+    """Shares of more pages than a window has, and of many units: tiles of 16 and of 32 rows, two of these, and eight."""
+    monkeypatch.setenv("NLD_CUS", str(cus))
+    s = Setup(pages, 2, dim, [64 * 150 + 5, 0, 700, 64 * 65], [n, n, 1, max(1, n // 2)], garbage=0xFF).fill()
+    q = randn((s.rows, q_heads, dim), 5, dtype)
+    s.check(q)
+    s.check(q, mode=1, bidir_from=1)
+    group = min(n, 3)
+    width = s.max_len // 64
+    lists = torch.stack([torch.randperm(width, generator=gen(i))[:90] for i in range(4 * -(-n // group) * 2)]).view(4, -1, 2, 90).to(torch.int32)
+    lists[:, :, 1, 40:50] = -1
+    s.check(q, lists=lists.to(DEV), group=group)
+
+
 def test_many_sequences():
     """More blocks of rows than a workgroup has threads, some of them without rows."""
     lens = [(i * 37) % 150 for i in range(300)]
@@ -684,6 +702,25 @@ def test_selection_over_a_long_sequence(monkeypatch, launches):
         best = torch.sort(score, descending=True, stable=True)[1][:20].tolist()
         assert got[0, 0, h].tolist()[:22] == sorted(best + [0, 1100])
     s.check(q, lists=got, group=2)
+
+
+@pytest.mark.parametrize("group", [1, 3])
+def test_selection_over_more_pages_than_one_workgroup_keeps(group):
+    """Over 4096 candidates: their scores stay in memory."""
+    n, rows = 4200, 3
+    s = Setup(E4M3, 1, 64, [64 * n + 7], [rows]).fill()
+    q = randn((rows, 4, 64), 5)
+    got = R.select_pages(s.cache, 0, q, s.workspace(4, group=group), 30, group=group)
+    bd, bs = s.cache.bounds[0].double(), s.cache.bound_scale[0]
+    ids = s.cache.table[0, :n].long()
+    qs = ref.over_127(q.float().abs().amax(-1))
+    qi = torch.round(q.float() / qs[..., None]).double()
+    score = torch.cat([torch.clamp(qi, max=0.0), torch.clamp(qi, min=0.0)], -1) @ torch.cat([bd[ids, 0, 0], bd[ids, 0, 1]], -1).T     # whole numbers
+    score = (score.float() * qs[..., None]).amax(1)
+    for j in range(-(-rows // group)):
+        best = torch.sort((score[j * group:(j + 1) * group].amax(0) * bs[ids, 0])[1:], descending=True, stable=True)[1][:30] + 1
+        assert got[0, j, 0].tolist()[:32] == sorted(best.tolist() + [0, n])
+    s.check(q, lists=got, group=group)
 
 
 @pytest.mark.parametrize("launches", ["one", "two"])

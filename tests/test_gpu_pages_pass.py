@@ -13,7 +13,7 @@ from gpu_common import rel_err
 
 pytestmark = pytest.mark.gpu
 
-from synth.workloads import SHAPE_TINY, LazyWeights, tokens  # noqa: E402
+from synth.workloads import SHAPE_TINY, LazyWeights, ModelShape, tokens  # noqa: E402
 
 if torch.cuda.is_available():
     from paper_2607_05722_amd import _lib as C
@@ -95,6 +95,93 @@ def test_block_passes_over_selected_pages(tiny, pages, sparse):
     whole, _ = R.block_forward(model, both.cache, R.PagedPassWorkspace(model, both.cache, k), toks, R.VERIFY)
     every, _ = R.block_forward(model, both.cache, R.PagedPassWorkspace(model, both.cache, k, (12, 0, 16)), toks, R.VERIFY, sparse=(12, 0, 16))
     assert rel_err(every.cpu().numpy(), whole.cpu().numpy()) <= 1e-5     # all pages: the same sums in other parts
+
+
+# head_dim 128: two query heads to a KV head, and five
+WIDE = {g: ModelShape(n_layers=2, hidden=256, n_q_heads=2 * g, n_kv_heads=2, head_dim=128, ffn=344, vocab=512) for g in (2, 5)}
+
+
+@pytest.fixture(scope="module")
+def wide():
+    src = {g: LazyWeights(shape, 1) for g, shape in WIDE.items()}
+    return {g: (WIDE[g], src[g], R.DeviceModel(WIDE[g], src[g])) for g in WIDE}
+
+
+def by_row(got, want):
+    """Norm of the difference over the norm, of each row."""
+    return np.linalg.norm(got - want, axis=-1) / np.linalg.norm(want, axis=-1)
+
+
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("heads,lens,k", [(2, [300], 1), (2, [100, 1, 190], 8), (2, [63, 400], 16), (2, [64, 250], 33), (5, [130, 700], 3), (5, [300, 9], 32),
+                                          (5, [60], 51)])
+def test_block_passes_of_128_dims(wide, pages, heads, lens, k):
+    """2 to 255 rows of a KV head (256 are the most of a pass): one tile of 16, of 32, several, and eight."""
+    shape, src, model = wide[heads]
+    both = Both(shape, pages, len(lens), 768)
+    prefill(wide[heads], both, lens)
+    ws = R.PagedPassWorkspace(model, both.cache, k)
+    toks = ids(shape, "block", len(lens), k)
+    for mode, bidir in ((R.VERIFY, 0), (R.DRAFT, 0), (R.DRAFT, min(3, k))):
+        logits, argmax = R.block_forward(model, both.cache, ws, toks, mode, bidir)
+        assert R.read_device_status(ws) == 0
+        want = ref.block_pass(shape, src, both.plain, lens, toks, mode == R.DRAFT, bidir).cpu().numpy()
+        got = logits.cpu().numpy()
+        assert float(by_row(got, want).max()) <= TOL
+        assert np.array_equal(argmax.cpu().numpy(), got.argmax(-1))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("k", [12, 24, 40])
+def test_infinite_keys_in_a_pass(dim, k):
+    """Rows whose queries score -inf against a committed key are those of a key of 1e8 there, bit for bit; the others are NaN."""
+    shape = ModelShape(n_layers=1, hidden=256, n_q_heads=2, n_kv_heads=2, head_dim=dim, ffn=344, vocab=512)
+    model = R.DeviceModel(shape, LazyWeights(shape, 2))
+    cache = R.PagedCache(2, dim, 1, 256)
+    g = torch.Generator().manual_seed(7)
+    rows, values = (torch.randn((150, 2, dim), generator=g).cuda() for _ in range(2))
+    toks, got = ids(shape, "block", 1, k), []
+    for big in (float("inf"), 1e8):
+        rows[30, 1, 9] = big
+        cache.lengths.zero_()
+        R.write_pages(cache, 0, rows, values, R.PagesWorkspace(cache, 2, 150))
+        cache.lengths.fill_(150)
+        ws = R.PagedPassWorkspace(model, cache, k)
+        got.append(R.block_forward(model, cache, ws, toks, R.VERIFY)[0][0])
+        assert R.read_device_status(ws) == 0
+    odd = torch.isnan(got[0])
+    lost = odd.any(-1)
+    assert torch.equal(lost, odd.all(-1)) and 0 < int(lost.sum()) < k
+    assert torch.equal(got[0][~lost], got[1][~lost]) and bool(torch.isfinite(got[1]).all())
+
+
+@pytest.mark.parametrize("pages", [BF16, E4M3])
+@pytest.mark.parametrize("heads,k,sparse", [(2, 16, (2, 1, 1)), (2, 16, (1, 0, 4)), (5, 16, (3, 1, 16)), (5, 1, (4, 0, 1))])
+def test_passes_of_128_dims_over_selected_pages(wide, pages, heads, k, sparse):
+    """Every page has the keys of the first, times a power of two of its own: the scores of two pages are apart by a factor of two, so
+    both sides choose the same, and every row is compared."""
+    shape, src, model = wide[heads]
+    lens = [700, 330]
+    both = Both(shape, pages, 2, 768, bounds=True)
+    starts, rows = [0, 700, 1030], torch.cat([torch.arange(n) for n in lens])
+    power = torch.cat([torch.randperm(-(-n // 64), generator=torch.Generator().manual_seed(n))[torch.arange(n) // 64] - 5 for n in lens])
+    ws = R.PagesWorkspace(both.cache, shape.n_q_heads, 700)
+    for l in range(shape.n_layers):
+        g = torch.Generator().manual_seed(200 + l)
+        page = torch.randn((64, shape.n_kv_heads, shape.head_dim), generator=g)
+        k_rows = (page[rows % 64] * 2.0 ** power[:, None, None]).cuda()
+        v_rows = torch.randn((1030, shape.n_kv_heads, shape.head_dim), generator=g).cuda()
+        R.write_pages(both.cache, l, k_rows, v_rows, ws, row_start=torch.tensor(starts, dtype=torch.int32, device="cuda"), max_rows=700)
+        both.plain[l].write([0, 0], starts, k_rows, v_rows)
+    both.cache.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
+    ws = R.PagedPassWorkspace(model, both.cache, k, sparse)
+    toks = ids(shape, "block", 2, k)
+    for mode in (R.VERIFY, R.DRAFT):
+        logits, _ = R.block_forward(model, both.cache, ws, toks, mode, 0, sparse=sparse)
+        assert R.read_device_status(ws) == 0
+        want = ref.block_pass(shape, src, both.plain, lens, toks, mode == R.DRAFT, 0, sparse).cpu().numpy()
+        err = by_row(logits.cpu().numpy(), want)
+        assert float(err.max()) <= TOL, err
 
 
 @pytest.mark.parametrize("k,group", [(1, 4), (2, 16), (4, 64)])
