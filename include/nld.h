@@ -526,7 +526,10 @@ nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk
  * Row i of sequence b sees the positions below P_b + i + 1 (NLD_MODE_VERIFY), or in NLD_MODE_DRAFT, from row bidir_from on, all
  * below P_b + n_b; query head h reads KV head h / (n_q_heads / n_kv_heads):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse (optional) f32 [rows][n_q_heads] = log sum_j exp(scale * q . k_j).
- * q and out are both bf16 or both f32 (f32 queries and weights are carried in three bf16 pieces, sums are f32 throughout).
+ * q and out are both bf16 or both f32; sums are f32 throughout.  f32 queries and weights are carried in three bf16 pieces (2^-24).  With bf16
+ * queries the weights are carried in two (2^-16), or, where more than 32 rows (new rows, or those of a group with a list, times the
+ * query heads of a KV head) share the pages, in one: each weight is then off by up to 2^-8 of itself, the output by about as much as its own
+ * rounding, and the last bits of a row hang on how many rows max_rows and group say there may be.  Ask with f32 queries where that matters.
  * A row that sees nothing, or only scores of -inf, gets 0 and -inf.  What a row does not see does not reach it, whatever it is.
  * What it sees and is not finite counts as in the formula, wherever it stands: a score of -inf has weight 0, one of +inf or NaN makes the
  * row and its lse NaN (a finite one over 2^29 in magnitude may, too), an infinite value makes its dim of the output infinite (infinities of both signs, or NaN: NaN).  Weights are divided by their sum at the

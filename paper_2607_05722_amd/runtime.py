@@ -526,7 +526,7 @@ def _written(outs, names, grad=None):
 def _call(fn, device, ws, *args):
     """fn(*args, workspace, its size, stream) on `device` and its current stream."""
     if ws.buf.device != device:
-        raise ValueError("the workspace is on %s, the logits on %s" % (ws.buf.device, device))
+        raise ValueError("the workspace is on %s, the call's tensors on %s" % (ws.buf.device, device))
     if device.index != torch.cuda.current_device():
         with torch.cuda.device(device):
             C.check(fn(*args, ws.ptr, ws.nbytes, stream_handle()))
@@ -793,6 +793,7 @@ def attend_pages(cache: PagedCache, layer: int, q: torch.Tensor, ws: PagesWorksp
     """Attention of the new rows' queries [rows][q_heads][head_dim] (bf16 or f32) over the pages, after write_pages of their keys and values: causal
     (VERIFY), or from row bidir_from on over the whole chunk (DRAFT).  scale: 1 / sqrt(head_dim) by default.  pages (int32
     [batch][groups][kv_heads][n], from select_pages): only those, for each group of ``group`` tokens.  row_start and max_rows as write_pages.
+    With bf16 queries the softmax weights are rounded to bf16 where more than 32 rows (times query heads per KV head) share the pages; not with f32.
     Returns (out, lse): out like q, lse f32 [rows][q_heads] with ``want_lse`` or where the caller gives it, else None.  No gradient flows through them."""
     if q.dim() != 3:
         raise ValueError("q must be [rows][q_heads][head_dim]")
