@@ -149,7 +149,7 @@ __device__ __forceinline__ void store8(const HeadRows& r, long long row, int hea
 // Bounds: the least and largest stored key of each dim among the page's positions up to the last one written, rounded
 // outwards to 8 bits; earlier positions are read back.  The bound scale of a page with a key that is not finite is +inf.
 // A page per workgroup because its bounds are of all its positions: nobody else writes them.  8 x up to 512 rows, 8 heads, bf16 to e4m3
-// (11 MB read, 6 MB written): 12.5 us, latency: three dependent turns, loads, LDS and the bounds' sums.  One token: 4.4 us.
+// (11 MB read, 6 MB written): 12.4 us, latency: three dependent turns, loads, LDS and the bounds' sums.  One token: 4.4 us.
 struct KvSource {        // the rows to write: strided tensors, or the split block K/V of a pass
     HeadRows k, v;
     const uint16_t* blk_k;   // [unit][hi, lo][64][D]
@@ -826,8 +826,8 @@ __device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const 
 // four wavefronts that meet at the unit's end through LDS.  Bound by memory: every page is read once, straight to registers, where its
 // layout makes it an operand, and a wavefront asks for its next step's keys and values before it works on this one's.
 // bf16 queries: two pieces of the weights, at most 2^-16 of each, since memory and not the products bounds this kernel; f32 queries: three pieces of both.
-// One token of 32 sequences of up to 8192 positions, 32 query heads, e4m3 (297 MB): 61 us, 4.9 TB/s of the 6.5 that plain reads reach, and 72
-// with the second launch and the gap between the two; one token over 4096 positions, bf16 (17 MB): 14 us of latency, 21.5 with the second.
+// One token of 32 sequences of up to 8192 positions, 32 query heads, e4m3 (297 MB): 59 us, 5.1 TB/s of the 6.5 that plain reads reach, and 73
+// with the second launch and the gap between the two; one token over 4096 positions, bf16 (17 MB): 15 us of latency, 21.7 with the second.
 template <int D, bool E4M3, int NQ, int RW>   // NQ: bf16 pieces of a query (1: bf16, 2: split, 3: f32); RW: rows of a tile
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RW == 16 || NQ == 1 && !(E4M3 && D == 128) ? 2 : 1)))
 pages_attend_kernel(PagesAttnArgs a) {
@@ -1164,10 +1164,10 @@ __device__ __forceinline__ void wait_loads(int n) {
 // No unit is full: in that prompt the matrix units are busy 34% of the time and the vector units as much, wavefronts wait 37% of theirs.
 // Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (DEEP) go to LDS as they
 // are, two stages ahead, and become bf16 a stage ahead of their use.
-// 4 x up to 2048 rows over 512 to 8192 positions, 32 query heads (bf16): 857 us, 0.81 PFLOP/s of the 1.29 that a large product reaches; without
+// 4 x up to 2048 rows over 512 to 8192 positions, 32 query heads (bf16): 851 us, 0.82 PFLOP/s of the 1.29 that a large product reaches; without
 // seven eighths of the products it still takes 0.73 of that time: exponentials, sums and conversions, LDS and the pages' barriers, which
 // the two wavefronts of a SIMD hide only in part.  Three or four stages under way change nothing, two pages per stage cost 2%, the next tile's products between
-// the present one's exponentials in one wavefront, with three buffers, save 2%.
+// the present one's exponentials in one wavefront, with three buffers, save 2% (884 against 900 us, in turn).
 template <int D, bool E4M3, int NQ>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 pages_attend_shared_kernel(PagesAttnArgs a) {
@@ -1804,7 +1804,7 @@ __global__ void __launch_bounds__(512) pages_select_kernel(PagesSelectArgs a) {
 }
 
 // The same in two launches, for more pages than that, or for few units: a workgroup per unit and 128 pages, then one per unit.
-// 64 units of up to 1024 pages (11 MB of bounds): scores 8.7 us, choice 8.1, both latency.
+// 64 units of up to 1024 pages (11 MB of bounds): scores 9.1 us, choice 8.7, both latency.
 template <int D>
 __global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
     __shared__ __align__(16) GroupRows<D> rows;
