@@ -480,12 +480,9 @@ __device__ __forceinline__ Entry entry_of(const PagesAttnArgs& a, int e, uint32_
     }
     x.steps = 0;
     if (x.rows1 > x.rows0) {
-        if (a.list) x.steps = a.n_list * (64 / STEP);
-        else {
-            const int sees = a.draft && x.t1 > a.bidir_from ? x.n : x.t1;
-            if (status && x.P + sees > a.c.max_pages * 64) flag(status, ST_CAPACITY);
-            x.steps = (min(x.P + sees, a.c.max_pages * 64) + STEP - 1) / STEP;
-        }
+        const int sees = a.draft && x.t1 > a.bidir_from ? x.n : x.t1;
+        if (status && x.P + sees > a.c.max_pages * 64) flag(status, ST_CAPACITY);
+        x.steps = a.list ? a.n_list * (64 / STEP) : (min(x.P + sees, a.c.max_pages * 64) + STEP - 1) / STEP;
     }
     return x;
 }

@@ -554,6 +554,20 @@ def test_bad_row_starts():
         assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS, start
 
 
+@pytest.mark.parametrize("group", [1, 20])
+def test_rows_past_the_table_with_a_list(group):
+    s = Setup(BF16, 1, 64, [120], [8], slack=0).fill()     # 128 positions: the table is full
+    ws = s.workspace(4, 20, 1)
+    q = randn((20, 4, 64), 3)
+    lists = on_device([0, 1]).repeat(1, 20 // group, 1, 1)
+    R.attend_pages(s.cache, 0, q[:8], ws, pages=lists[:, :-(-8 // group)].contiguous(), group=group)
+    assert R.read_device_status(ws) == 0
+    out, lse = R.attend_pages(s.cache, 0, q, ws, pages=lists, group=group, want_lse=True)
+    assert R.read_device_status(ws) == C.NLD_DEV_CAPACITY
+    s.lens, s.start, s.news, s.most = [120], [0, 20], [20], 20
+    s.compare(out, lse, q, lists=lists, group=group)       # rows past the table see all of it
+
+
 STARTS = [([4, -2 ** 31, 8], [], [0, 1, 2, 3]), ([4, 3 - 2 ** 31, -2 ** 31], [], []), ([-2 ** 31, 4, -2 ** 31], [0, 1, 2, 3], []),
           ([0, 2 ** 31 - 1, -2 ** 31], [0, 1, 2, 3], []), ([-1, -1, 2 ** 31 - 1], [], [0, 1, 2, 3]), ([8, 8, -5], [], []), ([6, 9, 2], [6, 7], []),
           ([7, -2 ** 31 + 6, 3], [], [0, 1, 2])]
