@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(256) pages_read_kernel(PageCache c, HeadRows k
     const SeqRows sr = seq_rows(ch, b, tell ? status : nullptr);
     int P = first ? first[b] : 0;
     if (P < 0) {
-        if (tell) flag(status, ST_LENGTH);
+        if (tell && sr.n) flag(status, ST_LENGTH);
         return;
     }
     P = min(P, c.max_pages * 64);

@@ -349,6 +349,14 @@ def test_many_sequences():
     s.check(randn((s.rows, 2, 64), 5))
 
 
+def test_many_sequences_of_many_rows():
+    """More blocks than threads where several tiles share the pages: 520 sequences, half of them without rows."""
+    lens = [(i * 37) % 150 for i in range(520)]
+    news = [33 + i % 3 if i % 8 == 1 else i % 2 for i in range(520)]
+    s = Setup(BF16, 1, 64, lens, news).fill()
+    s.check(randn((s.rows, 1, 64), 5))
+
+
 def test_one_number_of_rows_for_all_needs_no_row_start():
     s = Setup(BF16, 2, 64, [10, 70], [4, 4])
     rows = [randn((80, 2, 64), i) for i in (1, 2)]
@@ -552,6 +560,25 @@ def test_bad_row_starts():
         rows = randn((8, 1, 64), 9)
         R.write_pages(s.cache, 0, rows, rows, ws, row_start=on_device(start), max_rows=4)
         assert R.read_device_status(ws) == C.NLD_DEV_BAD_ROWS, start
+
+
+def test_sequences_without_rows_report_nothing():
+    """A padded batch: what stands in the places of a sequence that has no rows is not looked at."""
+    s = Setup(BF16, 1, 64, [20, 30, 40], [4, 0, 4]).fill()
+    ws = s.workspace(2, 8, 4)
+    s.cache.table[1] = -7
+    q, rows = randn((8, 2, 64), 3), randn((8, 1, 64), 4)
+    for bad in (-1, -2 ** 31, 2 ** 31 - 1):
+        s.cache.lengths[1] = bad
+        first = on_device([20, bad, 40])
+        R.write_pages(s.cache, 0, rows, rows, ws, row_start=s.row_start, max_rows=4)
+        k, _ = R.read_pages(s.cache, 0, 8, ws, first=first, row_start=s.row_start, max_rows=4)
+        assert torch.equal(k, rows.float())
+        R.attend_pages(s.cache, 0, q, ws, row_start=s.row_start, max_rows=4)
+        lists = R.select_pages(s.cache, 0, q, ws, 1, group=4, row_start=s.row_start, max_rows=4)
+        assert bool((lists[1] == -1).all())
+        R.attend_pages(s.cache, 0, q, ws, pages=lists, group=4, row_start=s.row_start, max_rows=4)
+        assert R.read_device_status(ws) == 0, bad
 
 
 @pytest.mark.parametrize("group", [1, 20])
