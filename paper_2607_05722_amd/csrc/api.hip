@@ -1555,12 +1555,18 @@ int32_t nld_pages_list_len(int32_t max_rows, int32_t group, int32_t n_top, int32
 }
 
 size_t nld_pages_workspace_bytes(const nld_pages* pages, int32_t n_q_heads, int32_t max_rows, int32_t group) {
-    if (check_pages(pages, 0) != NLD_OK || check_q_heads(pages, n_q_heads) != NLD_OK || max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 0)
+    if (check_pages(pages, 0) != NLD_OK || check_q_heads(pages, n_q_heads) != NLD_OK) return 0;
+    if (max_rows < 1 || max_rows > MAX_CHUNK_ROWS || group < 0) {
+        fail(NLD_ERR_INVALID_ARG, "max_rows must be in [1, %d] and group >= 0 (got %d and %d)", MAX_CHUNK_ROWS, max_rows, group);
         return 0;
+    }
     if (group && check_group(pages, n_q_heads, group) != NLD_OK) return 0;
     const int G = n_q_heads / pages->n_kv_heads;
     PagesPlan p;
-    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, max_rows, group, false, &p)) return 0;
+    if (!plan_pages(pages->batch, pages->n_kv_heads, pages->head_dim, G, max_rows, group, false, &p)) {
+        fail(NLD_ERR_SHAPE, "%d sequences of up to %d rows are too many for one call", pages->batch, max_rows);
+        return 0;
+    }
     // the most that any number of rows up to these, and any type, needs: by the tiles of a workgroup
     size_t n = 0;
     const long long rows = (long long)max_rows * G;

@@ -194,6 +194,14 @@ def test_workspace_bytes():
     assert f(pages(), 4, 100, 0) <= f(pages(), 4, 100, 1)
 
 
+def test_workspace_bytes_says_what_it_refuses():
+    f, error = lambda p, *a: C.load().nld_pages_workspace_bytes(ref_of(p), *a), lambda: C.load().nld_last_error().decode()
+    big = pages(batch=1 << 20, n_kv_heads=16)
+    for args, text in (((pages(), 4, 0, 0), "max_rows"), ((pages(), 4, 2, -1), "group"), ((pages(), 4, (1 << 24) + 1, 0), "max_rows"), ((big, 16, 1, 0), "too many"),
+                       ((pages(), 4, 2, 65), "group"), ((pages(), 3, 2, 0), "n_q_heads"), ((pages(head_dim=80), 4, 2, 0), "head_dim")):
+        assert write(p=pages(n_layers=0)) == INVALID and f(*args) == 0 and text in error(), (args[1:], error())
+
+
 def test_scores_of_a_selection_in_one_launch(monkeypatch):
     """Where there are 256 units and more of up to 4096 pages the scores need no workspace, and the launch has a workgroup per unit."""
     monkeypatch.delenv("NLD_SELECT_ONE", raising=False)
