@@ -532,8 +532,9 @@ nld_status nld_pages_read(const nld_pages* pages, int32_t layer, const nld_chunk
  * rounding, and the last bits of a row hang on how many rows max_rows and group say there may be.  Ask with f32 queries where that matters.
  * A row that sees nothing, or only scores of -inf, gets 0 and -inf.  What a row does not see does not reach it, whatever it is.
  * What it sees and is not finite counts as in the formula, wherever it stands: a score of -inf has weight 0, one of +inf or NaN makes the
- * row and its lse NaN (a finite one over 2^29 in magnitude may, too), an infinite value makes its dim of the output infinite (infinities of both signs, or NaN: NaN).  Weights are divided by their sum at the
- * end and are up to 2^8 till then, so the sums in f32 hold values up to 2^119 / (number of positions) for certain.
+ * row and its lse NaN (a finite one over 2^29 in magnitude may, too), an infinite value makes its dim of the output infinite (NaN beside the other
+ * sign's, or where f32 holds no weight for it), NaN makes it NaN.  Weights are divided by their sum at the end and are up to 2^8 till
+ * then, so the sums in f32 hold values up to 2^119 / (number of positions) for certain.
  * list (optional): only positions of the pages in the list of the row's group are seen: int32 [batch][ceil(max_rows / group)]
  * [n_kv_heads][n_list], places in the sequence's table, -1: none; each of them counts as often as it stands there.  Group j holds tokens
  * j * group .. of its sequence.  n_list and group are not looked at without a list.

@@ -703,9 +703,9 @@ __device__ __forceinline__ void finish_row(const PagesAttnArgs& a, int b, int r0
 // would: in steps that some row of the tile does not see whole, values behind every row's last position count as 0, and any
 // other that is not finite is left out of the product and added to the rows that see it.  In the other steps nobody looks: such a value
 // leaves the sums not finite, infinite ones as NaN, since a weight's smaller pieces may be 0 or negative.  Sums that are not finite
-// at the end are worked out once more (`careful`), with all values looked at as above, and infinite keys kept from the queries' smaller
-// pieces likewise.  So an infinite value comes out as what it is wherever it stands, and a score of -inf has weight 0.  8-bit pages hold no
-// infinity, and their NaN comes out as NaN at once.
+// at the end are worked out once more (`careful`), with all values looked at as above, and infinite keys taken out of the products and
+// added likewise where queries are in pieces.  So an infinite value comes out as what it is wherever it stands, and a score of -inf has
+// weight 0.  Nothing is worked out twice where weights are one piece, or over 8-bit pages, which hold no infinity: NaN comes out as NaN at once.
 template <int RW>
 struct Tile;
 template <>
@@ -752,13 +752,13 @@ __device__ __forceinline__ void rescale(float top, float* m, float* l, Acc (&o)[
 }
 __device__ __forceinline__ float weight(float score, float scale_log2, float ref) { return __builtin_amdgcn_exp2f(__builtin_fmaf(score, scale_log2, -ref)); }
 
-// Puts 0 in the place of those of eight bf16 numbers that are not finite; whether there were any.
-__device__ __forceinline__ bool only_finite(uint4* x) {
+// Puts 0 in the place of the infinities among eight bf16 numbers; whether there were any.
+__device__ __forceinline__ bool no_infinity(uint4* x) {
     uint32_t w[4] = {x->x, x->y, x->z, x->w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
-        if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
+        if ((w[i] & 0x7FFFu) == 0x7F80u) w[i] &= 0xFFFF0000u;
+        if ((w[i] & 0x7FFF0000u) == 0x7F800000u) w[i] &= 0xFFFFu;
     }
     const bool some = ((w[0] ^ x->x) | (w[1] ^ x->y) | (w[2] ^ x->z) | (w[3] ^ x->w)) != 0u;
     *x = uint4{w[0], w[1], w[2], w[3]};
@@ -774,26 +774,30 @@ __device__ __forceinline__ bool any_not_finite(const Acc (&o)[N]) {
     return __any(t != t);
 }
 
-// Adds to a lane's scores x what bf16 keys that are not finite give them, with whole queries.
+// Adds to a lane's scores x what infinite bf16 keys give them, with whole queries.
 template <int D, int NQ, int N, typename F>
-__device__ __forceinline__ void add_not_finite_keys(const PagesAttnArgs& a, float (&x)[N], F key_of, const uint16_t* keys, int first, const Entry& en, int h, int t,
+__device__ __forceinline__ void add_infinite_keys(const PagesAttnArgs& a, float (&x)[N], F key_of, const uint16_t* keys, int first, const Entry& en, int h, int t,
                                                     int g, bool have) {
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
         float sum = 0.0f;
+        for (int d0 = 0; d0 < D; d0 += 8) {
+            uint4 eight = *(const uint4*)(keys + key_at<D, false>(first + key_of(i), d0));
+            if (!no_infinity(&eight) || !have) continue;
 #pragma unroll 1
-        for (int d = 0; d < D; ++d) {
-            const float k = bf16_to_f32(keys[key_at<D, false>(first + key_of(i), d)]);
-            if (finite(k) || !have) continue;
-            float q;
-            if constexpr (NQ == 2) {
-                const uint16_t* p = a.q_split + q_index(en.b * a.c.n_kv_heads + h, g * en.n + t, d, a.q_row_tiles, D);
-                q = bf16_to_f32(p[0]) + bf16_to_f32(p[SPLIT_LO]);
-            } else {
-                q = ((const float*)a.q.data)[(en.r0 + t) * a.q.row_stride + (h * a.group_heads + g) * a.q.head_stride + d];
-                if (a.negate) q = -q;
+            for (int d = d0; d < d0 + 8; ++d) {
+                const float k = bf16_to_f32(keys[key_at<D, false>(first + key_of(i), d)]);
+                if (fabsf(k) != INFINITY) continue;
+                float q;
+                if constexpr (NQ == 2) {
+                    const uint16_t* p = a.q_split + q_index(en.b * a.c.n_kv_heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                    q = bf16_to_f32(p[0]) + bf16_to_f32(p[SPLIT_LO]);
+                } else {
+                    q = ((const float*)a.q.data)[(en.r0 + t) * a.q.row_stride + (h * a.group_heads + g) * a.q.head_stride + d];
+                    if (a.negate) q = -q;
+                }
+                sum += q * k;
             }
-            sum += q * k;
         }
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] += j == i ? sum : 0.0f;
@@ -836,7 +840,8 @@ pages_attend_kernel(PagesAttnArgs a) {
     constexpr int NF = SR / 8;                   // eights of weights: one operand each
     constexpr int DT = D / RW;
     constexpr int PITCH = D + 4;
-    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // infinite keys are worked on apart
+    constexpr bool TWICE = !E4M3 && NP > 1;            // sums that are not finite are worked out once more
+    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // and infinite keys by themselves
     __shared__ __align__(16) float so[4][RW][PITCH];
     __shared__ float sml[4][RW][2];
     __shared__ long long lds[4];
@@ -857,7 +862,7 @@ pages_attend_kernel(PagesAttnArgs a) {
         const Unit unit = walk_unit(walk);
         const Entry& en = unit.en;
         const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
-        const bool whole = unit.whole, careful = !E4M3 && unit.careful;
+        const bool whole = unit.whole, careful = TWICE && unit.careful;
 
         // this wavefront's rows
         const int myrow = en.rows0 + row;
@@ -980,7 +985,7 @@ pages_attend_kernel(PagesAttnArgs a) {
             bool odd_keys = false;
             if (PIECES_OF_KEYS && careful)
 #pragma unroll
-                for (int i = 0; i < NL; ++i) odd_keys |= only_finite(&kf[i]);
+                for (int i = 0; i < NL; ++i) odd_keys |= no_infinity(&kf[i]);
 #pragma unroll
             for (int i = 0; i < STEP / RW; ++i) {   // tiles of RW keys
                 typename T::Acc sc;
@@ -1003,7 +1008,7 @@ pages_attend_kernel(PagesAttnArgs a) {
 #pragma unroll
                 for (int r = 0; r < T::REGS; ++r) x[i * T::REGS + r] = sc[r];
             }
-            if (PIECES_OF_KEYS && __any(odd_keys)) add_not_finite_keys<D, NQ>(a, x, key_of, (const uint16_t*)a.c.k + cur_head * 64 * D, cur_base & 63, en, h, t, g, have);
+            if (PIECES_OF_KEYS && __any(odd_keys)) add_infinite_keys<D, NQ>(a, x, key_of, (const uint16_t*)a.c.k + cur_head * 64 * D, cur_base & 63, en, h, t, g, have);
             const bool masked = careful || cur_base + STEP > least;
             more = next();
             if (more) load_k(head, base);
@@ -1102,7 +1107,7 @@ pages_attend_kernel(PagesAttnArgs a) {
             for (int j = 0; j < T::REGS / 4; ++j)
                 *(float4*)&so[wave][row][dt * RW + T::out_dim(lane, 4 * j)] = float4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
         if (part == 0) sml[wave][row][0] = m_run, sml[wave][row][1] = l_run;
-        if (!E4M3 && any_not_finite(o) && lane == 0) walk.odd = true;
+        if (TWICE && any_not_finite(o) && lane == 0) walk.odd = true;
         __syncthreads();
         for (int i = tid; i < RW * (D / 4); i += 256) {
             const int r = i / (D / 4), d = i % (D / 4) * 4, rw = en.rows0 + r;
@@ -1172,7 +1177,8 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
     constexpr int STEP = 64, QS = D / 16, DT = D / 32, NP = NQ;
     constexpr int HALF = 2 * QS * 64;               // 16-byte pieces of a stage's keys, and of its values: [32 keys][step] x 64 lanes
     constexpr bool DEEP = pages_raw(NQ, E4M3);
-    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // infinite keys are worked on apart
+    constexpr bool TWICE = !E4M3 && NP > 1;            // sums that are not finite are worked out once more
+    constexpr bool PIECES_OF_KEYS = NQ > 1 && !E4M3;   // and infinite keys by themselves
     constexpr int RAW = DEEP ? 3 : 0;
     constexpr int LOADS = E4M3 ? D / 4 / 2 + 1 : 4 * QS;   // 1 KiB loads of a stage (8 bits: and one of the scales)
     __shared__ __align__(16) uint4 stage[2][2][HALF];   // [buffer][keys, values]
@@ -1192,7 +1198,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
         const Unit unit = walk_unit(walk);
         const Entry& en = unit.en;
         const int h = unit.h, s0 = unit.s0, s1 = unit.s1, slot = unit.slot;
-        const bool whole = unit.whole, careful = !E4M3 && unit.careful;
+        const bool whole = unit.whole, careful = TWICE && unit.careful;
 
         const int r = rt * 32 + row, myrow = en.rows0 + r;
         const bool have = myrow < en.rows1;
@@ -1427,7 +1433,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                         __builtin_amdgcn_sched_barrier(0);
                         if (PIECES_OF_KEYS && careful)
 #pragma unroll
-                            for (int s = 0; s < CH; ++s) odd_keys |= only_finite(&kf[s]);
+                            for (int s = 0; s < CH; ++s) odd_keys |= no_infinity(&kf[s]);
 #pragma unroll
                         for (int s = 0; s < CH; ++s)
 #pragma unroll
@@ -1437,7 +1443,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
                         float y[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) y[i] = x[i];
-                        add_not_finite_keys<D, NQ>(a, y, [&](int i) { return value_key(i >> 3, hf, i & 7); },
+                        add_infinite_keys<D, NQ>(a, y, [&](int i) { return value_key(i >> 3, hf, i & 7); },
                                                    (const uint16_t*)a.c.k + ((size_t)pg_id[j] * heads + h) * 64 * D, kt * 32, en, h, t, g, have);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) x[i] = y[i];
@@ -1496,7 +1502,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
             }
             __syncthreads();   // the window, and the last stage, have been read
         }
-        if (!E4M3 && any_not_finite(o) && lane == 0) walk.odd = true;
+        if (TWICE && any_not_finite(o) && lane == 0) walk.odd = true;
 
         l_run += __shfl_xor(l_run, 32);
         if (a.key_halves == 2) {   // the second half's sums go to the first's wavefront, through the stages' place
