@@ -804,6 +804,41 @@ __device__ __forceinline__ void add_infinite_keys(const PagesAttnArgs& a, float 
     }
 }
 
+// A lane's queries as operands, eight dims from dim_of(step) on: a row's bf16 pieces (one, a pass's two, three of f32), 0 for a row that there is not.
+template <int D, int NQ, int QS, typename F>
+__device__ __forceinline__ void load_queries(const PagesAttnArgs& a, const Entry& en, int h, int t, int g, bool have, uint4 (&q)[NQ][QS], F dim_of) {
+#pragma unroll
+    for (int s = 0; s < QS; ++s) {
+        const int d = dim_of(s);
+        if constexpr (NQ == 2) {   // rows (query head, block row)
+            q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
+            if (have) {
+                const uint16_t* p = a.q_split + q_index(en.b * a.c.n_kv_heads + h, g * en.n + t, d, a.q_row_tiles, D);
+                q[0][s] = *(const uint4*)p;
+                q[1][s] = *(const uint4*)(p + SPLIT_LO);
+            }
+        } else {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+            if (have) load8(a.q, en.r0 + t, h * a.group_heads + g, d, x);
+            if (a.negate)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = -x[i];
+#pragma unroll
+            for (int p = 0; p < NQ; ++p) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                    x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                }
+                q[p][s] = uint4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+}
+
 template <int D, bool E4M3, int RW>
 __device__ __forceinline__ void add_not_finite(typename Tile<RW>::Acc* o, const void* values, int base, int lane, int sees, int most) {
     using Elem = typename std::conditional<E4M3, uint8_t, uint16_t>::type;
@@ -946,39 +981,9 @@ pages_attend_kernel(PagesAttnArgs a) {
             load_k(cur_head, cur_base);
             load_v(cur_head, cur_base);
         }
-        // the queries, while the first pages are under way
+        // the queries, while the first pages are under way: the keys' blocks have a lane's bytes in pieces of 8 dims (bf16) or of 16, two steps
         uint4 q[NQ][QS];
-#pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            // 8 dims: the keys' blocks have a lane's bytes in pieces of 8 (bf16) or of 16, two steps
-            const int d = E4M3 ? 2 * T::DIMS * (s >> 1) + 16 * part + 8 * (s & 1) : T::DIMS * s + 8 * part;
-            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
-                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
-                if (have) {
-                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
-                    q[0][s] = *(const uint4*)p;
-                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
-                }
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
-                if (a.negate)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
-#pragma unroll
-                for (int p = 0; p < NQ; ++p) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                    }
-                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
-                }
-            }
-        }
+        load_queries<D, NQ>(a, en, h, t, g, have, q, [&](int s) { return E4M3 ? 2 * T::DIMS * (s >> 1) + 16 * part + 8 * (s & 1) : T::DIMS * s + 8 * part; });
 
         while (more) {
             float x[SR];
@@ -1210,36 +1215,7 @@ pages_attend_shared_kernel(PagesAttnArgs a) {
         const int begins = sees_of(a, en.P, en.n, en.t0), ends = sees_of(a, en.P, en.n, en.t1 - 1);   // what each row sees, and what any does
 
         uint4 q[NQ][QS];
-#pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            const int d = 16 * s + 8 * hf;
-            if constexpr (NQ == 2) {   // a pass's split queries, rows (query head, block row)
-                q[0][s] = q[1][s] = uint4{0u, 0u, 0u, 0u};
-                if (have) {
-                    const uint16_t* p = a.q_split + q_index(en.b * heads + h, g * en.n + t, d, a.q_row_tiles, D);
-                    q[0][s] = *(const uint4*)p;
-                    q[1][s] = *(const uint4*)(p + SPLIT_LO);
-                }
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (have) load8(a.q, en.r0 + t, h * G + g, d, x);
-                if (a.negate)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = -x[i];
-#pragma unroll
-                for (int p = 0; p < NQ; ++p) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                        x[2 * i] -= bf16_to_f32(w[i] & 0xFFFFu), x[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
-                    }
-                    q[p][s] = uint4{w[0], w[1], w[2], w[3]};
-                }
-            }
-        }
+        load_queries<D, NQ>(a, en, h, t, g, have, q, [&](int s) { return 16 * s + 8 * hf; });
         f32x16_t o[DT];
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
