@@ -1168,10 +1168,10 @@ __device__ __forceinline__ void wait_loads(int n) {
 // a second piece is as many products again in the second product, and the subtractions and conversions that make it.  One against two:
 // prompts 843 against 1065 us, draft blocks of 160 rows over 8 bits 164 against 192, selected blocks 63 against 65; error of the
 // output against 64 bits 0.0022 against the 0.0017 of its own rounding.
-// No unit is full: in that prompt the matrix units are busy 34% of the time and the vector units as much, wavefronts wait 37% of theirs.
+// No unit is full: in that prompt the matrix units are busy 35% of the time and the vector units as much, wavefronts wait 37% of theirs.
 // Queries of two and three pieces take 64 and 96 registers and leave none for 8-bit pages on their way: these (DEEP) go to LDS as they
 // are, two stages ahead, and become bf16 a stage ahead of their use.
-// 4 x up to 2048 rows over 512 to 8192 positions, 32 query heads (bf16): 851 us, 0.82 PFLOP/s of the 1.29 that a large product reaches; without
+// 4 x up to 2048 rows over 512 to 8192 positions, 32 query heads (bf16): 850 us, 0.82 PFLOP/s of the 1.29 that a large product reaches; without
 // seven eighths of the products it still takes 0.73 of that time: exponentials, sums and conversions, LDS and the pages' barriers, which
 // the two wavefronts of a SIMD hide only in part.  Three or four stages under way change nothing, two pages per stage cost 2%, the next tile's products between
 // the present one's exponentials in one wavefront, with three buffers, save 2% (884 against 900 us, in turn).
@@ -1783,7 +1783,7 @@ __global__ void __launch_bounds__(512) pages_select_kernel(PagesSelectArgs a) {
 }
 
 // The same in two launches, for more pages than that, or for few units: a workgroup per unit and 128 pages, then one per unit.
-// 64 units of up to 1024 pages (11 MB of bounds): scores 9.1 us, choice 8.7, both latency.
+// 64 units of up to 1024 pages (11 MB of bounds): scores 8.5 us, choice 8.0, both latency.
 template <int D>
 __global__ void __launch_bounds__(256) pages_score_kernel(PagesSelectArgs a) {
     __shared__ __align__(16) GroupRows<D> rows;
